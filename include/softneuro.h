@@ -484,6 +484,64 @@ int sn_dp_stats(const sn_graph* g, int32_t layer, int64_t* n_states, int64_t* n_
 void sn_graph_destroy(sn_graph* g);
 const char* sn_last_error(void);
 
+/* ------------------------------------------------------------------------
+ * Sequence operators: what a net of gated sequence blocks runs per layer
+ * besides the layers of a graph -- products with 4-bit weights, a selective
+ * state space scan with its short causal convolution, and the norms around a
+ * block.  Each is a handle (sn_op) made once from host weights and called on
+ * device tensors, on prompts of many rows and on single tokens.
+ *
+ *  - A handle owns its weights and its workspace; a run allocates nothing,
+ *    copies nothing to the host, does not synchronise and may be captured in
+ *    a HIP graph.  A handle is not thread-safe, and as a graph's runs use one
+ *    workspace, calls of one scan handle must follow each other on one stream
+ *    (or be ordered by events); norm and product handles have no workspace.
+ *  - Rows of a tensor are `stride` elements apart (stride >= the row's
+ *    length) and each row is contiguous.  Any alignment of whole elements is
+ *    accepted; 16-byte aligned rows take the wide loads.
+ *  - device = -1 makes a host-only handle: its runs check their arguments
+ *    and then return SN_E_DEVICE.
+ *  - Zero rows (m, rows or tokens of 0) are allowed and write nothing but
+ *    what is said below.
+ *  - Sums, statistics and states are float32; an output is rounded once, to
+ *    nearest-even.                                                         */
+typedef struct sn_op sn_op;
+void sn_op_destroy(sn_op* op);
+
+/* Norms before and after a block, with the block's gate, residual and scale,
+ * in one pass over the rows:
+ *
+ *   t = x;            gate = SN_GATE_BEFORE:  t = t * silu(g)
+ *   t = norm(t; post_w, post_b) in groups     (if post_w)
+ *                     gate = SN_GATE_AFTER:   t = t * silu(g)
+ *   t = scale * t     (scale_v[dim] if given, else the number `scale`)
+ *   res_out = res + t                         (if res_dtype >= 0)
+ *   y = norm(res + t; pre_w, pre_b)           (if pre_w; norm(t) without residual)
+ *   y = t                                     (if neither pre_w nor residual)
+ *
+ * norm is SN_NORM_RMS: v / sqrt(mean(v^2) + eps) * w + b, or SN_NORM_LAYER:
+ * (v - mean) / sqrt(var + eps) * w + b; the post norm takes each of `groups`
+ * equal parts of a row by itself (1 unless pre_w is null).  All in float32:
+ * the second norm sees the residual sum before it is rounded.  y may be x,
+ * and res_out may be res (same strides).  An absent tensor is null.        */
+typedef enum { SN_NORM_RMS = 0, SN_NORM_LAYER = 1 } sn_norm_kind;
+typedef enum { SN_GATE_NONE = 0, SN_GATE_BEFORE = 1, SN_GATE_AFTER = 2 } sn_gate;
+typedef struct {
+  int32_t dtype;     /* x, gate and y */
+  int32_t res_dtype; /* res and res_out: dtype or SN_F32; -1: no residual */
+  int32_t dim;       /* row length, at most 32768 */
+  int32_t groups;
+  int32_t kind;      /* sn_norm_kind, of both norms */
+  int32_t gate;      /* sn_gate */
+  float eps;         /* > 0 */
+  float scale;
+} sn_norm_desc;
+int sn_norm_create(const sn_norm_desc* desc, const float* post_w, const float* post_b, const float* pre_w,
+                   const float* pre_b, const float* scale_v, int32_t device, sn_op** out);
+int sn_norm_run(sn_op* op, int64_t rows, const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
+                const void* res, int64_t res_stride, void* res_out, int64_t res_out_stride, void* y,
+                int64_t y_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "api_guard.hpp"
 #include "core.hpp"
 
 using namespace sn;
@@ -13,28 +14,6 @@ struct sn_graph {
   Graph g;
 };
 
-static thread_local std::string t_err;
-
-template <class F>
-static int guarded(F&& f) {
-  try {
-    f();
-    return SN_OK;
-  } catch (const Error& e) {
-    t_err = e.what();
-    return e.code;
-  } catch (const std::bad_alloc&) {
-    t_err = "out of host memory";
-    return SN_E_INTERNAL;
-  } catch (const std::exception& e) {
-    t_err = e.what();
-    return SN_E_INTERNAL;
-  } catch (...) {
-    t_err = "unknown error";
-    return SN_E_INTERNAL;
-  }
-}
-
 #define CHECK_G(gp)                                         \
   do {                                                      \
     if (!(gp)) fail(SN_E_INVALID, "null graph pointer");    \
@@ -42,7 +21,7 @@ static int guarded(F&& f) {
 
 extern "C" {
 
-const char* sn_last_error(void) { return t_err.c_str(); }
+const char* sn_last_error(void) { return api_error().c_str(); }
 
 int sn_graph_create(int32_t dtype, int32_t n, int32_t c, int32_t h, int32_t w, int32_t device,
                     sn_graph** out) {

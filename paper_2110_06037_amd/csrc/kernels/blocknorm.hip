@@ -1,0 +1,213 @@
+// Norms before and after a block with its gate, scale and residual, one pass
+// over the rows: t = norm(x * silu(g)) (or norm(x) * silu(g)), r' = r +
+// scale * t, y = norm(r').  Every step is elementwise but the statistics, so
+// a row is read once, held in registers in float32 through both norms, and
+// written once; the layer norm's variance is summed from the centred
+// registers.  Bound by memory: the bytes of x, g, r, r' and y.
+#include "seq.hpp"
+
+namespace sn {
+namespace k {
+
+// WPR: waves per row; NV: chunks of 8 elements per thread.  A row of D
+// elements fits when D <= 512 WPR NV.  VEC: chunks are 8 consecutive elements
+// (16-byte loads); else element j of chunk i is strided over the row's
+// threads, so loads of single elements still coalesce.
+template <typename T, typename R, bool VEC, int WPR, int NV>
+__global__ __launch_bounds__(WPR < 4 ? 256 : 64 * WPR) void block_norm_kernel(NormArgs a) {
+  constexpr int TPR = 64 * WPR;
+  constexpr int ROWS = WPR < 4 ? 4 / WPR : 1;
+  __shared__ float red[4][ROWS][WPR];
+  const int t = threadIdx.x % TPR;
+  const int slot = threadIdx.x / TPR;
+  const int D = a.dim / a.groups;
+  const int64_t units = a.rows * a.groups;
+  const int64_t unit = (int64_t)blockIdx.x * ROWS + slot;
+  const bool on = unit < units;  // threads without a row take part in the barriers
+  const int64_t row = on ? unit / a.groups : 0;
+  const int col = on ? (int)(unit - row * a.groups) * D : 0;
+
+  auto at = [&](int i, int j) { return VEC ? (i * TPR + t) * 8 + j : (i * 8 + j) * TPR + t; };
+  auto load = [&](auto* p, int64_t stride, float (&v)[NV][8]) {
+    typedef std::remove_cv_t<std::remove_pointer_t<decltype(p)>> E;
+    const E* q = p + row * stride + col;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if constexpr (VEC) {
+        const int c = at(i, 0);
+        V8<E> u = on && c < D ? ld8(q + c) : zero8<E>();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = to_f(u.v[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = at(i, j);
+          v[i][j] = on && c < D ? to_f(q[c]) : 0.f;
+        }
+      }
+    }
+  };
+  auto store = [&](auto* p, int64_t stride, const float (&v)[NV][8]) {
+    typedef std::remove_pointer_t<decltype(p)> E;
+    E* q = p + row * stride + col;
+    if (!on) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if constexpr (VEC) {
+        const int c = at(i, 0);
+        V8<E> u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u.v[j] = from_f<E>(v[i][j]);
+        if (c < D) st8(q + c, u);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = at(i, j);
+          if (c < D) q[c] = from_f<E>(v[i][j]);
+        }
+      }
+    }
+  };
+  int phase = 0;
+  auto total = [&](float s) {
+    s = wave_sum(s);
+    if constexpr (WPR > 1) {
+      float* m = red[phase++][slot];
+      if ((t & 63) == 0) m[t >> 6] = s;
+      __syncthreads();
+      s = 0.f;
+#pragma unroll
+      for (int w = 0; w < WPR; ++w) s += m[w];
+    }
+    return s;
+  };
+  // per-channel vectors, read where they are used (cached: all rows share them)
+  auto vec = [&](const float* w, int c0, int i, float (&o)[8]) {
+    if constexpr (VEC) {
+      const int c = at(i, 0);
+      const V8<float> u = c < D ? ld8(w + c0 + c) : zero8<float>();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = u.v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = at(i, j) < D ? w[c0 + at(i, j)] : 0.f;
+    }
+  };
+  const float inv = 1.f / (float)D;
+  auto norm = [&](float (&v)[NV][8], const float* w, const float* b, int c0) {
+    if (a.kind == 1) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += v[i][j];
+      const float mean = total(s) * inv;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = at(i, j) < D ? v[i][j] - mean : 0.f;
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fmaf(v[i][j], v[i][j], s);
+    const float k = rsqrtf(fmaf(total(s), inv, a.eps));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float wv[8];
+      vec(w, c0, i, wv);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= k * wv[j];
+      if (b) {
+        vec(b, c0, i, wv);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] += wv[j];
+      }
+    }
+  };
+
+  float v[NV][8], g[NV][8], r[NV][8];
+  load(static_cast<const T*>(a.x), a.xs, v);
+  if (a.gate) load(static_cast<const T*>(a.g), a.gs, g);
+  if (a.rdtype >= 0) load(static_cast<const R*>(a.r), a.rs, r);
+  if (a.gate == 1) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= silu_f(g[i][j]);
+  }
+  if (a.post_w) norm(v, a.post_w, a.post_b, col);
+  if (a.gate == 2) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= silu_f(g[i][j]);
+  }
+  if (a.scale_v) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float sv[8];
+      vec(a.scale_v, col, i, sv);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= sv[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= a.scale;
+  }
+  if (a.rdtype >= 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] += r[i][j];
+    store(static_cast<R*>(a.ro), a.ros, v);
+  }
+  if (a.pre_w) norm(v, a.pre_w, a.pre_b, col);
+  if (a.y) store(static_cast<T*>(a.y), a.ys, v);
+}
+
+template <typename T, typename R, bool VEC>
+static void launch_norm(const NormArgs& a, hipStream_t st) {
+  const int D = a.dim / a.groups;
+  const int64_t units = a.rows * a.groups;
+  const auto grid = [&](int rows_per_block) { return dim3((unsigned)((units + rows_per_block - 1) / rows_per_block)); };
+#define SN_NORM(WPR, NV)                                                                               \
+  SN_LAUNCH((block_norm_kernel<T, R, VEC, WPR, NV>), grid(WPR < 4 ? 4 / WPR : 1), \
+            dim3(WPR < 4 ? 256 : 64 * WPR), 0, st, a)
+  if (D <= 512) SN_NORM(1, 1);
+  else if (D <= 2048) SN_NORM(4, 1);
+  else if (D <= 4096) SN_NORM(4, 2);
+  else if (D <= 8192) SN_NORM(16, 1);
+  else if (D <= 16384) SN_NORM(16, 2);
+  else SN_NORM(16, 4);
+#undef SN_NORM
+}
+
+template <typename T, typename R>
+static void launch_norm_v(const NormArgs& a, hipStream_t st) {
+  // wide loads: every row of every tensor starts at a multiple of 16 bytes
+  // (32-byte chunks of float32 go as two loads)
+  const int D = a.dim / a.groups;
+  const int e = sizeof(T), er = sizeof(R);
+  bool vec = D % 8 == 0 && al16(a.x) && al16(a.xs * e);
+  if (a.gate) vec = vec && al16(a.g) && al16(a.gs * e);
+  if (a.rdtype >= 0) vec = vec && al16(a.r) && al16(a.rs * er) && al16(a.ro) && al16(a.ros * er);
+  if (a.y) vec = vec && al16(a.y) && al16(a.ys * e);
+  if (vec) launch_norm<T, R, true>(a, st);
+  else launch_norm<T, R, false>(a, st);
+}
+
+void block_norm(const NormArgs& a, hipStream_t st) {
+  check(a.dim >= 1 && a.groups >= 1 && a.dim % a.groups == 0 && a.dim <= kNormMaxDim && a.rows >= 1 &&
+            a.rows * a.groups < (int64_t(1) << 31) && (a.rdtype == -1 || a.rdtype == a.dtype || a.rdtype == 0),
+        "norm shapes");
+  if (a.dtype == 0) launch_norm_v<float, float>(a, st);
+  else if (a.dtype == 1) a.rdtype == 0 ? launch_norm_v<f16, float>(a, st) : launch_norm_v<f16, f16>(a, st);
+  else a.rdtype == 0 ? launch_norm_v<bf16, float>(a, st) : launch_norm_v<bf16, bf16>(a, st);
+}
+
+}  // namespace k
+}  // namespace sn

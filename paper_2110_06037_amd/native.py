@@ -27,6 +27,8 @@ ACT = {"none": 0, "relu": 1, "relu6": 2}
 SELECT_DPRS, SELECT_FIXED = 0, 1
 OPT_LAYOUTS, OPT_ALGOS, OPT_PARAMS, OPT_HIPGRAPH, OPT_SEED, OPT_FLUSH, OPT_KEEP, OPT_DTYPES, OPT_WS_LIMIT = range(9)
 DTYPE_NAME = {v: k for k, v in DTYPE.items()}
+NORM = {"rms": 0, "layer": 1}
+GATE = {"none": 0, "before": 1, "after": 2}
 
 STATUS = {0: "SN_OK", -1: "SN_E_INVALID", -2: "SN_E_SHAPE", -3: "SN_E_STATE",
           -4: "SN_E_UNSUPPORTED", -5: "SN_E_DEVICE", -6: "SN_E_NOMEM", -7: "SN_E_INTERNAL"}
@@ -50,11 +52,19 @@ class RoutineDesc(ctypes.Structure):
                 ("cost_ns", ctypes.c_int64), ("ws_bytes", ctypes.c_int64), ("name", ctypes.c_char * 64)]
 
 
+class NormDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("res_dtype", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("kind", ctypes.c_int32), ("gate", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
 # exported functions: name -> (restype, argtypes)
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _I32P = ctypes.POINTER(ctypes.c_int32)
 _I64P = ctypes.POINTER(ctypes.c_int64)
+_I64 = ctypes.c_int64
+_F32P = ctypes.POINTER(ctypes.c_float)
 SIGNATURES = {
     "sn_graph_create": (ctypes.c_int, [_I32, _I32, _I32, _I32, _I32, _I32, ctypes.POINTER(_P)]),
     "sn_set_option": (ctypes.c_int, [_P, _I32, ctypes.c_int64]),
@@ -89,6 +99,10 @@ SIGNATURES = {
     "sn_layer_shape": (ctypes.c_int, [_P, _I32, _I32P]),
     "sn_dp_stats": (ctypes.c_int, [_P, _I32, _I64P, _I64P]),
     "sn_graph_destroy": (None, [_P]),
+    "sn_op_destroy": (None, [_P]),
+    "sn_norm_create": (ctypes.c_int, [ctypes.POINTER(NormDesc), _F32P, _F32P, _F32P, _F32P, _F32P, _I32,
+                                      ctypes.POINTER(_P)]),
+    "sn_norm_run": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
     "sn_last_error": (ctypes.c_char_p, []),
 }
 

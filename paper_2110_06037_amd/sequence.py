@@ -1,0 +1,150 @@
+"""Python face of the sequence operators (sn_op handles of the C ABI).
+
+Each class makes a handle from host weights (numpy arrays) and runs it on
+device tensors: rows are the first dimension, rows may be strided (a slice of
+a wider projection), elements of a row are contiguous.  A run enqueues on the
+current stream of the handle's device, or on ``stream``, and returns at once.
+"""
+
+from __future__ import annotations
+
+import ctypes
+
+import numpy as np
+
+from . import native as N
+
+
+def _f32(v, shape, name):
+    """A float32 host array of the given shape, or None."""
+    if v is None:
+        return None
+    a = np.ascontiguousarray(v, dtype=np.float32)
+    if a.shape != tuple(shape):
+        raise ValueError(f"{name} has shape {a.shape}, not {tuple(shape)}")
+    return a
+
+
+def _fp(a):
+    return None if a is None else a.ctypes.data_as(ctypes.POINTER(ctypes.c_float))
+
+
+class _Op:
+    """A handle's lifetime, and what every run does with its tensors."""
+
+    def __init__(self, dtype, device):
+        import torch
+        self._op = None
+        self.lib = N.lib()
+        self._torch = torch
+        self._types = {N.F32: torch.float32, N.F16: torch.float16, N.BF16: torch.bfloat16}
+        self.dtype = N.DTYPE[dtype] if isinstance(dtype, str) else dtype
+        if self.dtype not in self._types:
+            raise ValueError(f"unknown dtype {dtype!r}")
+        self.torch_dtype = self._types[self.dtype]
+        self.device = device
+        self._dev = torch.device("cuda", device) if device >= 0 else None
+
+    def close(self):
+        if getattr(self, "_op", None):
+            self.lib.sn_op_destroy(self._op)
+            self._op = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _rows(self, t, name, shape, dtype=None):
+        """The row stride of a device tensor [rows, n] that a kernel may use as it is."""
+        if t.dtype != (dtype or self.torch_dtype):
+            raise TypeError(f"{name} is {t.dtype}, not {dtype or self.torch_dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+        if t.device != self._dev:
+            raise ValueError(f"{name} is on {t.device}, the handle on {self._dev}")
+        s = t.stride()
+        if s[1] != 1 and shape[1] > 1:
+            raise ValueError(f"the elements of a row of {name} are not contiguous")
+        return s[0] if shape[0] > 1 else shape[1]
+
+    def _stream(self, stream, tensors):
+        """The stream's pointer; on another stream than the current one the
+        tensors' memory is kept from reuse until its work is done."""
+        cur = self._torch.cuda.current_stream(self._dev)
+        if stream is None:
+            return cur.cuda_stream
+        if isinstance(stream, int):
+            if stream == cur.cuda_stream:
+                return stream
+            stream = self._torch.cuda.ExternalStream(stream, device=self._dev)
+        if stream.cuda_stream != cur.cuda_stream:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+        return stream.cuda_stream
+
+
+class BlockNorm(_Op):
+    """Norms before and after a block with its gate, scale and residual.
+
+    ``run`` computes, in float32 and in one pass::
+
+        t = x;  t *= silu(gate)                      # gate="before"
+        t = norm(t) * post + post_bias               # in `groups` parts, if post is given
+        t *= silu(gate)                              # gate="after"
+        t *= scale                                   # number or vector
+        res_out = residual + t                       # with a residual type
+        y = norm(res_out or t) * pre + pre_bias      # if pre is given; else t without a residual
+
+    ``kind`` is "rms" or "layer"; ``residual`` names the residual's element
+    type (None: no residual)."""
+
+    def __init__(self, dtype, dim, kind="rms", post=None, post_bias=None, pre=None, pre_bias=None, scale=None,
+                 gate="none", groups=1, eps=1e-5, residual=None, device=0):
+        super().__init__(dtype, device)
+        rd = -1 if residual is None else N.DTYPE[residual] if isinstance(residual, str) else residual
+        self.dim, self.gate = dim, gate
+        self.res_dtype = None if rd < 0 else self._types[rd]
+        self.has_y = pre is not None or rd < 0
+        vector = scale is not None and np.ndim(scale) > 0
+        arrays = [_f32(v, (dim,), n) for v, n in ((post, "post"), (post_bias, "post_bias"), (pre, "pre"),
+                                                  (pre_bias, "pre_bias"), (scale if vector else None, "scale"))]
+        d = N.NormDesc(self.dtype, rd, dim, groups, N.NORM[kind], N.GATE[gate], eps,
+                       1.0 if scale is None or vector else float(scale))
+        p = ctypes.c_void_p()
+        N.check(self.lib.sn_norm_create(ctypes.byref(d), *[_fp(a) for a in arrays], device, ctypes.byref(p)))
+        self._op = p
+
+    def run(self, x, gate=None, residual=None, out=None, res_out=None, stream=None):
+        """Enqueue on x [rows, dim]; returns (y, res_out), None for the one that
+        the handle does not have.  ``out`` may be x and ``res_out`` residual."""
+        shape = x.shape
+        if len(shape) != 2 or shape[1] != self.dim:
+            raise ValueError(f"x has shape {tuple(shape)}, not [rows, {self.dim}]")
+        xs = self._rows(x, "x", shape)
+        gp = gs = rp = rs = op = os = yp = ys = 0
+        if gate is not None:
+            gp, gs = gate.data_ptr(), self._rows(gate, "gate", shape)
+        if residual is not None:
+            if self.res_dtype is None:
+                raise ValueError("a residual given to a handle without one")
+            rp, rs = residual.data_ptr(), self._rows(residual, "residual", shape, self.res_dtype)
+        if self.res_dtype is not None:
+            if res_out is None:
+                res_out = self._torch.empty(shape, dtype=self.res_dtype, device=x.device)
+            op, os = res_out.data_ptr(), self._rows(res_out, "res_out", shape, self.res_dtype)
+        if self.has_y:
+            if out is None:
+                out = self._torch.empty(shape, dtype=self.torch_dtype, device=x.device)
+            yp, ys = out.data_ptr(), self._rows(out, "out", shape)
+        st = self._stream(stream, (x, gate, residual, out, res_out))
+        N.check(self.lib.sn_norm_run(self._op, shape[0], x.data_ptr(), xs, gp, gs, rp, rs, op, os, yp, ys, st))
+        return out, res_out

@@ -542,6 +542,25 @@ int sn_norm_run(sn_op* op, int64_t rows, const void* x, int64_t x_stride, const 
                 const void* res, int64_t res_stride, void* res_out, int64_t res_out_stride, void* y,
                 int64_t y_stride, void* stream);
 
+/* Product with 4-bit weights:
+ *
+ *   y[m][k] = act( sum_c x[m][c] * s[k][c / group] * (q[k][c] - z[k][c / group]) + bias[k] )
+ *
+ * q: [rows][ceil(cols / 2)] bytes, feature 2j in the low half of byte j;
+ * scale: [rows][ceil(cols / group)] binary16 patterns; zero: codes 0 .. 15 of
+ * the same shape, or null for 8; bias: [rows] float32 or null.  group is a
+ * multiple of 32; a last group may be short.                               */
+typedef struct {
+  int32_t dtype; /* x and y */
+  int32_t rows;  /* output features */
+  int32_t cols;  /* input features */
+  int32_t group;
+  int32_t act;   /* sn_act */
+} sn_linear4_desc;
+int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint16_t* scale, const uint8_t* zero,
+                      const float* bias, int32_t device, sn_op** out);
+int sn_linear4_run(sn_op* op, int64_t m, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

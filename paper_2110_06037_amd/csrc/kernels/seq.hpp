@@ -31,6 +31,22 @@ struct NormArgs {
 constexpr int kNormMaxDim = 32768;
 void block_norm(const NormArgs& a, hipStream_t st);
 
+// ------------------------------------------------------------------ products with 4-bit weights
+struct Linear4Args {
+  int dtype, act;
+  int64_t m;
+  int rows, cols, group;
+  const uint8_t* q;   // [rows][ceil(cols / 2)]
+  const f16* scale;   // [rows][groups]
+  const uint8_t* zero;  // [rows][groups] or null
+  const float* bias;    // [rows] or null
+  const void* x;
+  int64_t xs;
+  void* y;
+  int64_t ys;
+};
+void linear4(const Linear4Args& a, hipStream_t st);
+
 // ------------------------------------------------------------------ device helpers
 constexpr float kLog2e = 1.44269504088896340736f;
 

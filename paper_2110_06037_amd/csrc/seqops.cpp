@@ -17,7 +17,7 @@ using namespace sn;
     if (e_ != hipSuccess) fail(SN_E_DEVICE, std::string(#expr) + ": " + hipGetErrorString(e_)); \
   } while (0)
 
-enum OpKind { OP_NORM };
+enum OpKind { OP_NORM, OP_LINEAR4 };
 
 struct sn_op {
   const OpKind kind;
@@ -111,6 +111,12 @@ struct NormOp : sn_op {
   using sn_op::sn_op;
 };
 
+// ------------------------------------------------------------------ 4-bit products
+struct Linear4Op : sn_op {
+  k::Linear4Args a{};
+  using sn_op::sn_op;
+};
+
 }  // namespace
 
 extern "C" {
@@ -185,6 +191,56 @@ int sn_norm_run(sn_op* p, int64_t rows, const void* x, int64_t x_stride, const v
     a.ro = res_out, a.ros = res_out_stride, a.y = y, a.ys = y_stride;
     OnDevice on(op.device);
     k::block_norm(a, static_cast<hipStream_t>(stream));
+    HIPCHK(hipGetLastError());
+  });
+}
+
+int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint16_t* scale, const uint8_t* zero,
+                      const float* bias, int32_t device, sn_op** out) {
+  return guarded([&] {
+    if (!out) fail(SN_E_INVALID, "null output pointer");
+    *out = nullptr;
+    if (!desc || !q || !scale) fail(SN_E_INVALID, "null description, codes or scales");
+    const sn_linear4_desc& d = *desc;
+    check_dtype(d.dtype);
+    if (d.rows < 1 || d.cols < 1) fail(SN_E_SHAPE, "rows and cols must be positive");
+    if (d.rows > (1 << 24) || d.cols > (1 << 20)) fail(SN_E_UNSUPPORTED, "more than 2^24 rows or 2^20 cols");
+    if (d.group < 32 || d.group % 32) fail(SN_E_SHAPE, "group must be a multiple of 32");
+    if (d.act < SN_ACT_NONE || d.act > SN_ACT_RELU6) fail(SN_E_INVALID, "unknown activation");
+    const int64_t groups = (d.cols + (int64_t)d.group - 1) / d.group;
+    const int64_t n = d.rows * groups;
+    for (int64_t i = 0; i < n; ++i)
+      if ((scale[i] & 0x7c00) == 0x7c00) fail(SN_E_INVALID, "a scale is not finite");
+    for (int64_t i = 0; zero && i < n; ++i)
+      if (zero[i] > 15) fail(SN_E_INVALID, "a zero point above 15");
+    check_finite(bias, d.rows, "bias");
+    check_device(device);
+    std::unique_ptr<Linear4Op> op(new Linear4Op(OP_LINEAR4, device));
+    k::Linear4Args& a = op->a;
+    a.dtype = d.dtype, a.act = d.act, a.rows = d.rows, a.cols = d.cols, a.group = d.group;
+    if (device >= 0) {
+      OnDevice on(device);
+      a.q = op->upload(q, (size_t)d.rows * ((d.cols + 1) / 2));
+      a.scale = reinterpret_cast<const k::f16*>(op->upload(scale, n));
+      a.zero = op->upload(zero, n);
+      a.bias = op->upload(bias, d.rows);
+    }
+    *out = op.release();
+  });
+}
+
+int sn_linear4_run(sn_op* p, int64_t m, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream) {
+  return guarded([&] {
+    Linear4Op& op = op_of<Linear4Op>(p, OP_LINEAR4);
+    k::Linear4Args a = op.a;
+    if (m < 0 || m > 65535 * 8) fail(SN_E_SHAPE, "m must be in 0..524280");
+    check_rows(x, x_stride, m, a.cols, a.dtype, "x");
+    check_rows(y, y_stride, m, a.rows, a.dtype, "y");
+    need_device(op);
+    if (!m) return;
+    a.m = m, a.x = x, a.xs = x_stride, a.y = y, a.ys = y_stride;
+    OnDevice on(op.device);
+    k::linear4(a, static_cast<hipStream_t>(stream));
     HIPCHK(hipGetLastError());
   });
 }

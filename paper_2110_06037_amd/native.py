@@ -58,6 +58,11 @@ class NormDesc(ctypes.Structure):
                 ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
 
 
+class Linear4Desc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("group", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
 # exported functions: name -> (restype, argtypes)
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -103,6 +108,8 @@ SIGNATURES = {
     "sn_norm_create": (ctypes.c_int, [ctypes.POINTER(NormDesc), _F32P, _F32P, _F32P, _F32P, _F32P, _I32,
                                       ctypes.POINTER(_P)]),
     "sn_norm_run": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
+    "sn_linear4_create": (ctypes.c_int, [ctypes.POINTER(Linear4Desc), _P, _P, _P, _F32P, _I32, ctypes.POINTER(_P)]),
+    "sn_linear4_run": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _P]),
     "sn_last_error": (ctypes.c_char_p, []),
 }
 

@@ -92,6 +92,80 @@ class _Op:
         return stream.cuda_stream
 
 
+def quantize4(w, group=128, zero=False):
+    """4-bit codes of a weight matrix [rows, cols]: (q, scale, zero points) as
+    ``Linear4`` takes them, each group of ``group`` columns rounded to the
+    nearest of 16 steps: symmetric around code 8, or with ``zero`` from the
+    group's least to its largest value."""
+    w = np.asarray(w, np.float32)
+    rows, cols = w.shape
+    groups = -(-cols // group)
+    g = np.zeros((rows, groups * group), np.float32)
+    g[:, :cols] = w
+    g = g.reshape(rows, groups, group)
+    if zero:
+        lo, hi = np.minimum(g.min(2), 0), np.maximum(g.max(2), 0)
+        scale = ((hi - lo) / 15).astype(np.float16)
+    else:
+        scale = (np.abs(g).max(2) / 7.5).astype(np.float16)
+    scale = np.maximum(scale, np.float16(6.2e-5))  # no group's scale below the normal numbers
+    step = scale.astype(np.float32)
+    z = np.clip(np.rint(-lo / step), 0, 15).astype(np.uint8) if zero else None
+    code = np.clip(np.rint(g / step[..., None]) + (8 if z is None else z[..., None]), 0, 15)
+    code = code.reshape(rows, -1)[:, :cols + cols % 2].astype(np.uint8)
+    if code.shape[1] % 2:
+        code = np.pad(code, ((0, 0), (0, 1)))
+    return code[:, 0::2] | (code[:, 1::2] << 4), scale, z
+
+
+class Linear4(_Op):
+    """Product with 4-bit weights: y[m, k] = act(sum_c x[m, c] * scale[k, c // group]
+    * (q[k, c] - zero[k, c // group]) + bias[k]).
+
+    ``q``: uint8 [rows, ceil(cols / 2)], feature 2j in the low half of byte j;
+    ``scale``: float16 [rows, ceil(cols / group)]; ``zero``: uint8 codes 0 .. 15
+    of the same shape, or None for 8; ``bias``: float32 [rows] or None;
+    ``group``: a multiple of 32."""
+
+    def __init__(self, dtype, q, scale, zero=None, bias=None, cols=None, group=128, act="none", device=0):
+        super().__init__(dtype, device)
+        q = np.ascontiguousarray(q, dtype=np.uint8)
+        self.rows = q.shape[0]
+        self.cols = 2 * q.shape[1] if cols is None else cols
+        if q.shape[1] != (self.cols + 1) // 2:
+            raise ValueError(f"{q.shape[1]} bytes of codes a row do not hold {self.cols} columns")
+        scale = np.ascontiguousarray(scale, dtype=np.float16)
+        shape = (self.rows, -(-self.cols // group))
+        if scale.shape != shape:
+            raise ValueError(f"scale has shape {scale.shape}, not {shape}")
+        if zero is not None:
+            zero = np.ascontiguousarray(zero, dtype=np.uint8)
+            if zero.shape != shape:
+                raise ValueError(f"zero has shape {zero.shape}, not {shape}")
+        bias = _f32(bias, (self.rows,), "bias")
+        d = N.Linear4Desc(self.dtype, self.rows, self.cols, group, N.ACT[act])
+        p = ctypes.c_void_p()
+        N.check(self.lib.sn_linear4_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data,
+                                           None if zero is None else zero.ctypes.data, _fp(bias), device,
+                                           ctypes.byref(p)))
+        self._op = p
+
+    def run(self, x, out=None, stream=None):
+        """Enqueue on x [m, cols]; returns y [m, rows]."""
+        shape = x.shape
+        if len(shape) != 2 or shape[1] != self.cols:
+            raise ValueError(f"x has shape {tuple(shape)}, not [m, {self.cols}]")
+        xs = self._rows(x, "x", shape)
+        shape = (shape[0], self.rows)
+        if out is None:
+            out, ys = self._torch.empty(shape, dtype=self.torch_dtype, device=x.device), self.rows
+        else:
+            ys = self._rows(out, "out", shape)
+        st = self._stream(stream, (x, out))
+        N.check(self.lib.sn_linear4_run(self._op, shape[0], x.data_ptr(), xs, out.data_ptr(), ys, st))
+        return out
+
+
 class BlockNorm(_Op):
     """Norms before and after a block with its gate, scale and residual.
 

@@ -57,3 +57,62 @@ def test_norm_run_refusals():
     assert run(x=p + 2) == -1                           # not on the elements' alignment
     assert L.sn_norm_run(None, 1, p, 8, 0, 0, p, 8, p, 8, p, 8, None) == -1
     assert L.sn_norm_create(None, None, None, None, None, None, -1, ctypes.byref(ctypes.c_void_p())) == -1
+
+
+def test_linear4_creation_refusals():
+    from paper_2110_06037_amd import Linear4, quantize4
+    q, scale, zero = quantize4(np.ones((4, 70)), 32, True)
+
+    def make(q=q, scale=scale, zero=zero, cols=70, group=32, **kw):
+        return Linear4("bf16", q, scale, zero=zero, cols=cols, group=group, device=kw.pop("device", -1), **kw)
+
+    make().close()
+    make(zero=None, bias=np.zeros(4), act="relu6").close()
+    assert code(lambda: make(group=48, scale=scale[:, :2], zero=None)) == -2
+    assert code(lambda: make(group=16, scale=np.ones((4, 5)), zero=None)) == -2
+    bad = scale.copy()
+    bad[1, 1] = np.inf
+    assert code(lambda: make(scale=bad)) == -1
+    assert code(lambda: make(zero=np.full_like(zero, 16))) == -1
+    assert code(lambda: make(bias=np.full(4, np.nan))) == -1
+    for wrong in (dict(cols=72), dict(scale=scale[:, :2]), dict(zero=zero[:3]), dict(bias=np.zeros(5))):
+        with pytest.raises(ValueError):
+            make(**wrong)
+    L = N.lib()
+    d = N.Linear4Desc(N.BF16, 0, 70, 32, 0)
+    p = ctypes.c_void_p()
+    assert L.sn_linear4_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -2
+    d.rows, d.act = 4, 7
+    assert L.sn_linear4_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -1
+    d.act = 0
+    assert L.sn_linear4_create(ctypes.byref(d), None, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -1
+
+
+def test_linear4_run_refusals_and_foreign_handles():
+    from paper_2110_06037_amd import Linear4, quantize4
+    L = N.lib()
+    buf = np.zeros(256, np.uint16)
+    p = buf.ctypes.data
+    h = Linear4("bf16", *quantize4(np.ones((4, 8)), 32)[:2], cols=8, group=32, device=-1)
+    norm = BlockNorm("bf16", 8, device=-1)
+
+    def run(op=h._op, m=2, x=p, xs=8, y=p, ys=4):
+        return L.sn_linear4_run(op, m, x, xs, y, ys, None)
+
+    assert run() == -5 and run(m=0, x=None, y=None) == -5
+    assert run(m=-1) == -2 and run(m=524281) == -2
+    assert run(x=None) == -1 and run(y=None) == -1 and run(x=p + 1) == -1
+    assert run(xs=7) == -2 and run(ys=3) == -2
+    assert run(op=norm._op) == -1 and run(op=None) == -1
+
+
+def test_quantize4_rounds_to_the_nearest_code():
+    from paper_2110_06037_amd import quantize4
+    w = np.array([[7.5, -7.5, 0, 1, 2, 3, -1, 0.4]], np.float32)
+    q, scale, zero = quantize4(w, 32)
+    assert zero is None and scale.shape == (1, 1) and scale[0, 0] == 1
+    codes = np.stack([q & 15, q >> 4], -1).reshape(1, -1)
+    assert codes.tolist() == [[15, 0, 8, 9, 10, 11, 7, 8]]
+    q, scale, zero = quantize4(np.array([[0.0, 15, 3, 7, 1]], np.float32), 32, True)
+    assert scale[0, 0] == 1 and zero[0, 0] == 0
+    assert np.stack([q & 15, q >> 4], -1).reshape(1, -1)[:, :5].tolist() == [[0, 15, 3, 7, 1]]

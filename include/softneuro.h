@@ -561,6 +561,58 @@ int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint1
                       const float* bias, int32_t device, sn_op** out);
 int sn_linear4_run(sn_op* op, int64_t m, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream);
 
+/* Selective state space scan with its short causal convolution.  A token's
+ * row of x holds chans = heads * head_dim + 2 * groups * state raw values,
+ * its row of dt one raw step size per head.  For each sequence and token t:
+ *
+ *   u_t = silu(conv_b + sum_{j < conv} conv_w[:, j] * raw_{t - conv + 1 + j}) = [ X | B | C ]
+ *   dt_t = log(1 + exp(dt_raw_t + dt_bias))
+ *   h_t = exp(dt_t * a) * h_{t-1} + dt_t * X_t (outer) B_t      per head, [head_dim][state]
+ *   y_t = h_t C_t + d * X_t
+ *
+ * with the B and C of group g shared by the heads of its equal part, and raw
+ * values before the first token taken from `window` [seqs][conv - 1][chans]
+ * (dtype, oldest first) and h before it from `state`
+ * [seqs][heads][head_dim][state] (float32); null for either means zeros.
+ * window_out and state_out take what follows the last token; each is its
+ * input's tensor or does not overlap it; null: not wanted.  A sequence of no
+ * tokens passes its window and state on.  `offsets` (device, seqs + 1
+ * values, not decreasing, from 0 to tokens) gives the sequences' first rows;
+ * null: all have tokens / seqs rows.  A row whose raw values hold an
+ * infinity or a NaN does not change the rows before it, and counts as NaN
+ * from there on.
+ *
+ * sn_scan_run takes any lengths; sn_scan_step is for one token per sequence
+ * (tokens = seqs, offsets null), in one kernel.                            */
+typedef struct {
+  int32_t dtype;
+  int32_t heads, head_dim, groups, state; /* state <= 256, heads % groups == 0 */
+  int32_t conv;                           /* taps, 1 .. 4 */
+  int32_t max_seqs;                       /* what one call may hold: sizes the workspace */
+  int64_t max_tokens;
+} sn_scan_desc;
+typedef struct {
+  int32_t seqs;
+  int64_t tokens;
+  const int32_t* offsets;
+  const void* x;
+  int64_t x_stride;
+  const void* dt;
+  int64_t dt_stride;
+  const void* window;
+  const float* state;
+  void* y; /* [tokens][heads * head_dim] */
+  int64_t y_stride;
+  void* window_out;
+  float* state_out;
+} sn_scan_io;
+/* conv_w: [chans][conv]; conv_b: [chans] or null; a: [heads], finite and <= 0;
+ * d, dt_bias: [heads] or null (zeros).                                     */
+int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* conv_b, const float* a,
+                   const float* d, const float* dt_bias, int32_t device, sn_op** out);
+int sn_scan_run(sn_op* op, const sn_scan_io* io, void* stream);
+int sn_scan_step(sn_op* op, const sn_scan_io* io, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

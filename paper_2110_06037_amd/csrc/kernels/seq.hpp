@@ -3,6 +3,8 @@
 // enqueues on the given stream; none allocates or synchronises.
 #pragma once
 
+#include <algorithm>
+
 #include "gemm_common.hpp"
 #include "kcommon.hpp"
 #include "launch.hpp"
@@ -46,6 +48,49 @@ struct Linear4Args {
   int64_t ys;
 };
 void linear4(const Linear4Args& a, hipStream_t st);
+
+// ------------------------------------------------------------------ selective scan
+constexpr int kScanChunk = 64;     // tokens per chunk
+constexpr int kScanUnits = 1024;   // waves that a pass is cut into segments for
+struct ScanArgs {
+  int dtype, heads, dim, groups, state, conv, chans;  // dim: of a head
+  int np;  // state columns that the workspace's rows hold (scan_np)
+  // weights
+  const float* conv_w;  // [4][chans], the last conv rows used
+  const float* conv_b;  // [chans]
+  const float* a2;      // [heads], a log2(e)
+  const float* d;       // [heads]
+  const float* dt_bias;
+  // workspace
+  float* ws_c;     // [slot][group][t][np]      C of a chunk
+  float* ws_b;     // [slot][group][np][t]      B of a chunk
+  float* ws_s;     // [slot][group][t][s]       C B^T, s in blocks not above t's
+  float* ws_dt;    // [slot][head][3][t]        step size, running sum of log2 decays (hi, lo)
+  float* ws_seg;   // [seq][segment][head][dim][state]
+  float* ws_decay; // [seq][segment][head]
+  void* wcopy;     // [seq][conv - 1][chans]    the window before the call
+  unsigned* count; // [seq][group], zero between calls
+  int64_t seg_cap; // elements of ws_seg
+  // call
+  int seqs, segs;
+  int64_t tokens;
+  const int32_t* offsets;
+  const void* x;
+  int64_t xs;
+  const void* dt;
+  int64_t dts;
+  const void* window;
+  const float* state_in;
+  void* y;
+  int64_t ys;
+  void* window_out;
+  float* state_out;
+  bool vec_x, vec_y, vec_state;  // wide accesses (set by the launcher)
+};
+inline int scan_np(int state) { return state <= 32 ? 32 : state <= 64 ? 64 : state <= 128 ? 128 : 256; }
+inline int64_t scan_slots(int64_t tokens, int seqs) { return tokens / kScanChunk + seqs + 1; }
+void scan_run(const ScanArgs& a, hipStream_t st);
+void scan_step(const ScanArgs& a, hipStream_t st);
 
 // ------------------------------------------------------------------ device helpers
 constexpr float kLog2e = 1.44269504088896340736f;

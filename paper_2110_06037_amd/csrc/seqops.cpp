@@ -17,7 +17,7 @@ using namespace sn;
     if (e_ != hipSuccess) fail(SN_E_DEVICE, std::string(#expr) + ": " + hipGetErrorString(e_)); \
   } while (0)
 
-enum OpKind { OP_NORM, OP_LINEAR4 };
+enum OpKind { OP_NORM, OP_LINEAR4, OP_SCAN };
 
 struct sn_op {
   const OpKind kind;
@@ -116,6 +116,48 @@ struct Linear4Op : sn_op {
   k::Linear4Args a{};
   using sn_op::sn_op;
 };
+
+// ------------------------------------------------------------------ scan
+struct ScanOp : sn_op {
+  k::ScanArgs a{};
+  int max_seqs = 0;
+  int64_t max_tokens = 0;
+  using sn_op::sn_op;
+};
+
+// Either one tensor or two that do not touch.
+void check_in_out(const void* in, const void* out, int64_t bytes, const char* what) {
+  const uintptr_t i = reinterpret_cast<uintptr_t>(in), o = reinterpret_cast<uintptr_t>(out);
+  if (in && out && i != o && i < o + bytes && o < i + bytes)
+    fail(SN_E_INVALID, std::string(what) + " overlaps its input without being it");
+}
+
+// The call's arguments, checked.
+k::ScanArgs scan_args(const ScanOp& op, const sn_scan_io* io, bool step) {
+  if (!io) fail(SN_E_INVALID, "null arguments");
+  k::ScanArgs a = op.a;
+  const int e = dtype_size(a.dtype);
+  if (io->seqs < 0 || io->seqs > op.max_seqs) fail(SN_E_SHAPE, "seqs outside the handle's range");
+  if (io->tokens < 0 || io->tokens > op.max_tokens) fail(SN_E_SHAPE, "tokens outside the handle's range");
+  if (io->seqs == 0 && io->tokens) fail(SN_E_SHAPE, "tokens without a sequence");
+  if (step && (io->tokens != io->seqs || io->offsets)) fail(SN_E_SHAPE, "a step takes one token per sequence");
+  if (io->seqs && !io->offsets && io->tokens % io->seqs)
+    fail(SN_E_SHAPE, "tokens are no multiple of seqs, and there are no offsets");
+  check_rows(io->x, io->x_stride, io->tokens, a.chans, a.dtype, "x");
+  check_rows(io->dt, io->dt_stride, io->tokens, a.heads, a.dtype, "dt");
+  check_rows(io->y, io->y_stride, io->tokens, (int64_t)a.heads * a.dim, a.dtype, "y");
+  for (const void* p : {io->window, (const void*)io->window_out})
+    if (reinterpret_cast<uintptr_t>(p) % e) fail(SN_E_INVALID, "window is not aligned to its elements");
+  for (const void* p : {(const void*)io->state, (const void*)io->state_out, (const void*)io->offsets})
+    if (reinterpret_cast<uintptr_t>(p) % 4) fail(SN_E_INVALID, "state or offsets are not aligned to 4 bytes");
+  check_in_out(io->window, io->window_out, (int64_t)io->seqs * (a.conv - 1) * a.chans * e, "window_out");
+  check_in_out(io->state, io->state_out, (int64_t)io->seqs * a.heads * a.dim * a.state * 4, "state_out");
+  a.seqs = io->seqs, a.tokens = io->tokens, a.offsets = io->offsets;
+  a.x = io->x, a.xs = io->x_stride, a.dt = io->dt, a.dts = io->dt_stride, a.y = io->y, a.ys = io->y_stride;
+  a.window = io->window, a.window_out = a.conv > 1 ? io->window_out : nullptr;
+  a.state_in = io->state, a.state_out = io->state_out;
+  return a;
+}
 
 }  // namespace
 
@@ -241,6 +283,93 @@ int sn_linear4_run(sn_op* p, int64_t m, const void* x, int64_t x_stride, void* y
     a.m = m, a.x = x, a.xs = x_stride, a.y = y, a.ys = y_stride;
     OnDevice on(op.device);
     k::linear4(a, static_cast<hipStream_t>(stream));
+    HIPCHK(hipGetLastError());
+  });
+}
+
+int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* conv_b, const float* a_,
+                   const float* d_, const float* dt_bias, int32_t device, sn_op** out) {
+  return guarded([&] {
+    if (!out) fail(SN_E_INVALID, "null output pointer");
+    *out = nullptr;
+    if (!desc || !conv_w || !a_) fail(SN_E_INVALID, "null description, conv_w or a");
+    const sn_scan_desc& d = *desc;
+    check_dtype(d.dtype);
+    if (d.heads < 1 || d.head_dim < 1 || d.groups < 1 || d.state < 1) fail(SN_E_SHAPE, "sizes must be positive");
+    if (d.heads % d.groups) fail(SN_E_SHAPE, "groups must divide heads");
+    if (d.state > 256) fail(SN_E_UNSUPPORTED, "state above 256");
+    if (d.conv < 1 || d.conv > 4) fail(SN_E_UNSUPPORTED, "conv must be in 1..4");
+    const int64_t chans = (int64_t)d.heads * d.head_dim + 2 * (int64_t)d.groups * d.state;
+    if (d.heads > 65535 || d.head_dim > 65535 || chans > (1 << 24)) fail(SN_E_UNSUPPORTED, "more than 2^24 channels");
+    if (d.max_seqs < 1 || d.max_seqs > 65535) fail(SN_E_SHAPE, "max_seqs must be in 1..65535");
+    if (d.max_tokens < 1 || d.max_tokens > (1 << 30)) fail(SN_E_SHAPE, "max_tokens must be in 1..2^30");
+    check_finite(conv_w, chans * d.conv, "conv_w");
+    check_finite(conv_b, chans, "conv_b");
+    check_finite(a_, d.heads, "a");
+    check_finite(d_, d.heads, "d");
+    check_finite(dt_bias, d.heads, "dt_bias");
+    for (int h = 0; h < d.heads; ++h)
+      if (a_[h] > 0.f) fail(SN_E_INVALID, "a has a positive value (states would grow)");
+    check_device(device);
+    std::unique_ptr<ScanOp> op(new ScanOp(OP_SCAN, device));
+    op->max_seqs = d.max_seqs, op->max_tokens = d.max_tokens;
+    k::ScanArgs& a = op->a;
+    a.dtype = d.dtype, a.heads = d.heads, a.dim = d.head_dim, a.groups = d.groups, a.state = d.state;
+    a.conv = d.conv, a.chans = (int)chans, a.np = k::scan_np(d.state);
+    if (device >= 0) {
+      OnDevice on(device);
+      std::vector<float> w(4 * chans, 0.f), zeros(chans, 0.f), a2(d.heads);
+      for (int64_t c = 0; c < chans; ++c)
+        for (int j = 0; j < d.conv; ++j) w[(4 - d.conv + j) * chans + c] = conv_w[c * d.conv + j];
+      for (int h = 0; h < d.heads; ++h) a2[h] = (float)((double)a_[h] * 1.4426950408889634074);
+      a.conv_w = op->upload(w.data(), w.size());
+      a.conv_b = op->upload(conv_b ? conv_b : zeros.data(), chans);
+      a.a2 = op->upload(a2.data(), d.heads);
+      a.d = op->upload(d_ ? d_ : zeros.data(), d.heads);
+      a.dt_bias = op->upload(dt_bias ? dt_bias : zeros.data(), d.heads);
+      const int64_t slots = k::scan_slots(d.max_tokens, d.max_seqs), Q = k::kScanChunk;
+      auto floats = [&](int64_t n) { return static_cast<float*>(op->alloc(n * 4)); };
+      a.ws_c = floats(slots * d.groups * Q * a.np);
+      a.ws_b = floats(slots * d.groups * Q * a.np);
+      a.ws_s = floats(slots * d.groups * Q * Q);
+      a.ws_dt = floats(slots * d.heads * 3 * Q);
+      // segments are made for fewer than kScanUnits units of at most 64
+      // columns, of at least two chunks each
+      const int64_t pairs = std::max<int64_t>(1, (d.max_tokens + Q - 1) / Q / 2);
+      a.seg_cap = std::min(int64_t(2) * k::kScanUnits * 64 * d.state,
+                           d.max_seqs * pairs * d.heads * d.head_dim * d.state);
+      a.ws_seg = floats(a.seg_cap);
+      a.ws_decay = floats(2 * k::kScanUnits);
+      a.wcopy = op->alloc(d.max_seqs * (d.conv - 1) * chans * dtype_size(d.dtype));
+      const size_t counters = (size_t)d.max_seqs * d.groups * sizeof(unsigned);
+      a.count = static_cast<unsigned*>(op->alloc(counters));
+      HIPCHK(hipMemset(a.count, 0, counters));
+      HIPCHK(hipDeviceSynchronize());
+    }
+    *out = op.release();
+  });
+}
+
+int sn_scan_run(sn_op* p, const sn_scan_io* io, void* stream) {
+  return guarded([&] {
+    ScanOp& op = op_of<ScanOp>(p, OP_SCAN);
+    const k::ScanArgs a = scan_args(op, io, false);
+    need_device(op);
+    if (!a.seqs) return;
+    OnDevice on(op.device);
+    k::scan_run(a, static_cast<hipStream_t>(stream));
+    HIPCHK(hipGetLastError());
+  });
+}
+
+int sn_scan_step(sn_op* p, const sn_scan_io* io, void* stream) {
+  return guarded([&] {
+    ScanOp& op = op_of<ScanOp>(p, OP_SCAN);
+    const k::ScanArgs a = scan_args(op, io, true);
+    need_device(op);
+    if (!a.seqs) return;
+    OnDevice on(op.device);
+    k::scan_step(a, static_cast<hipStream_t>(stream));
     HIPCHK(hipGetLastError());
   });
 }

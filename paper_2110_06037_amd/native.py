@@ -63,6 +63,20 @@ class Linear4Desc(ctypes.Structure):
                 ("group", ctypes.c_int32), ("act", ctypes.c_int32)]
 
 
+class ScanDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("state", ctypes.c_int32), ("conv", ctypes.c_int32),
+                ("max_seqs", ctypes.c_int32), ("max_tokens", ctypes.c_int64)]
+
+
+class ScanIO(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_int32), ("tokens", ctypes.c_int64), ("offsets", ctypes.c_void_p),
+                ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("dt", ctypes.c_void_p),
+                ("dt_stride", ctypes.c_int64), ("window", ctypes.c_void_p), ("state", ctypes.c_void_p),
+                ("y", ctypes.c_void_p), ("y_stride", ctypes.c_int64), ("window_out", ctypes.c_void_p),
+                ("state_out", ctypes.c_void_p)]
+
+
 # exported functions: name -> (restype, argtypes)
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -110,6 +124,10 @@ SIGNATURES = {
     "sn_norm_run": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
     "sn_linear4_create": (ctypes.c_int, [ctypes.POINTER(Linear4Desc), _P, _P, _P, _F32P, _I32, ctypes.POINTER(_P)]),
     "sn_linear4_run": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _P]),
+    "sn_scan_create": (ctypes.c_int, [ctypes.POINTER(ScanDesc), _F32P, _F32P, _F32P, _F32P, _F32P, _I32,
+                                      ctypes.POINTER(_P)]),
+    "sn_scan_run": (ctypes.c_int, [_P, ctypes.POINTER(ScanIO), _P]),
+    "sn_scan_step": (ctypes.c_int, [_P, ctypes.POINTER(ScanIO), _P]),
     "sn_last_error": (ctypes.c_char_p, []),
 }
 

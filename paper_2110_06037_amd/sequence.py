@@ -71,7 +71,7 @@ class _Op:
         if t.device != self._dev:
             raise ValueError(f"{name} is on {t.device}, the handle on {self._dev}")
         s = t.stride()
-        if s[1] != 1 and shape[1] > 1:
+        if s[1] != 1 and shape[1] > 1 and shape[0]:
             raise ValueError(f"the elements of a row of {name} are not contiguous")
         return s[0] if shape[0] > 1 else shape[1]
 
@@ -164,6 +164,93 @@ class Linear4(_Op):
         st = self._stream(stream, (x, out))
         N.check(self.lib.sn_linear4_run(self._op, shape[0], x.data_ptr(), xs, out.data_ptr(), ys, st))
         return out
+
+
+class Scan(_Op):
+    """Selective state space scan with its short causal convolution.
+
+    A token's row of ``x`` holds ``chans`` = heads * head_dim + 2 * groups *
+    state raw values, its row of ``dt`` one raw step size per head.  With
+    u_t = silu(conv_b + sum_j conv_w[:, j] * raw_{t - conv + 1 + j}) = [X | B | C]
+    and dt_t = log(1 + exp(dt_raw_t + dt_bias)), each head computes::
+
+        h_t = exp(dt_t * a) * h_{t-1} + dt_t * X_t (outer) B_t
+        y_t = h_t C_t + d * X_t
+
+    ``window`` [seqs, conv - 1, chans] holds the raw values before the first
+    token (oldest first), ``state`` [seqs, heads, head_dim, state] (float32)
+    the h before it; None means zeros.  Both come back as they are after the
+    last token, in ``window_out`` and ``state_out`` (which may be the inputs:
+    updated in place).  The workspace holds calls of up to ``max_seqs``
+    sequences and ``max_tokens`` rows in all; calls share it, so they must
+    follow each other on one stream."""
+
+    def __init__(self, dtype, heads, head_dim, groups, state, conv_w, conv_b=None, a=None, d=None, dt_bias=None,
+                 max_seqs=1, max_tokens=1, device=0):
+        super().__init__(dtype, device)
+        self.heads, self.head_dim, self.groups, self.state = heads, head_dim, groups, state
+        self.inner, self.chans = heads * head_dim, heads * head_dim + 2 * groups * state
+        conv_w = np.ascontiguousarray(conv_w, dtype=np.float32)
+        if conv_w.ndim != 2 or conv_w.shape[0] != self.chans:
+            raise ValueError(f"conv_w has shape {conv_w.shape}, not ({self.chans}, taps)")
+        self.conv = conv_w.shape[1]
+        if a is None:
+            raise ValueError("a is missing")
+        arrays = [conv_w] + [_f32(v, (n,), s) for v, n, s in ((conv_b, self.chans, "conv_b"), (a, heads, "a"),
+                                                             (d, heads, "d"), (dt_bias, heads, "dt_bias"))]
+        desc = N.ScanDesc(self.dtype, heads, head_dim, groups, state, self.conv, max_seqs, max_tokens)
+        p = ctypes.c_void_p()
+        N.check(self.lib.sn_scan_create(ctypes.byref(desc), *[_fp(v) for v in arrays], device, ctypes.byref(p)))
+        self._op = p
+
+    def _whole(self, t, name, shape, dtype):
+        if t.shape != shape or t.dtype != dtype or t.device != self._dev or not t.is_contiguous():
+            raise ValueError(f"{name} is not a contiguous {dtype} tensor {tuple(shape)} on {self._dev}")
+        return t.data_ptr()
+
+    def _call(self, f, x, dt, window, state, window_out, state_out, seqs, offsets, out, stream):
+        torch = self._torch
+        tokens = x.shape[0]
+        io = N.ScanIO()
+        io.seqs, io.tokens = seqs, tokens
+        io.x_stride, io.x = self._rows(x, "x", (tokens, self.chans)), x.data_ptr()
+        io.dt_stride, io.dt = self._rows(dt, "dt", (tokens, self.heads)), dt.data_ptr()
+        wshape, sshape = (seqs, self.conv - 1, self.chans), (seqs, self.heads, self.head_dim, self.state)
+        if window is not None:
+            io.window = self._whole(window, "window", wshape, self.torch_dtype)
+        if state is not None:
+            io.state = self._whole(state, "state", sshape, torch.float32)
+        if offsets is not None:
+            io.offsets = self._whole(offsets, "offsets", (seqs + 1,), torch.int32)
+        if out is None:
+            out = torch.empty((tokens, self.inner), dtype=self.torch_dtype, device=x.device)
+        io.y_stride, io.y = self._rows(out, "out", (tokens, self.inner)), out.data_ptr()
+        if window_out is None:
+            window_out = torch.empty(wshape, dtype=self.torch_dtype, device=x.device)
+        if state_out is None:
+            state_out = torch.empty(sshape, dtype=torch.float32, device=x.device)
+        io.window_out = self._whole(window_out, "window_out", wshape, self.torch_dtype)
+        io.state_out = self._whole(state_out, "state_out", sshape, torch.float32)
+        st = self._stream(stream, (x, dt, window, state, offsets, out, window_out, state_out))
+        N.check(f(self._op, ctypes.byref(io), st))
+        return out, window_out, state_out
+
+    def run(self, x, dt, window=None, state=None, window_out=None, state_out=None, seqs=None, offsets=None, out=None,
+            stream=None):
+        """Enqueue on the packed rows x [tokens, chans], dt [tokens, heads] of
+        one or more sequences; returns (y [tokens, heads * head_dim], window,
+        state).  ``offsets`` (int32 device tensor [seqs + 1]) gives their first
+        rows; without it ``seqs`` (default: what window or state hold, else 1)
+        sequences share the rows evenly."""
+        if seqs is None:
+            seqs = (offsets.shape[0] - 1 if offsets is not None else window.shape[0] if window is not None
+                    else state.shape[0] if state is not None else 1)
+        return self._call(self.lib.sn_scan_run, x, dt, window, state, window_out, state_out, seqs, offsets, out, stream)
+
+    def step(self, x, dt, window=None, state=None, window_out=None, state_out=None, out=None, stream=None):
+        """The same for one token of each of x.shape[0] sequences, in one kernel."""
+        return self._call(self.lib.sn_scan_step, x, dt, window, state, window_out, state_out, x.shape[0], None, out,
+                          stream)
 
 
 class BlockNorm(_Op):

@@ -116,3 +116,59 @@ def test_quantize4_rounds_to_the_nearest_code():
     q, scale, zero = quantize4(np.array([[0.0, 15, 3, 7, 1]], np.float32), 32, True)
     assert scale[0, 0] == 1 and zero[0, 0] == 0
     assert np.stack([q & 15, q >> 4], -1).reshape(1, -1)[:, :5].tolist() == [[0, 15, 3, 7, 1]]
+
+
+def _scan(**kw):
+    from paper_2110_06037_amd import Scan
+    o = dict(dtype="bf16", heads=4, head_dim=8, groups=2, state=16, conv_w=np.ones((4 * 8 + 2 * 2 * 16, 4)),
+             a=-np.ones(4), max_seqs=3, max_tokens=100, device=-1)
+    o.update(kw)
+    return Scan(o.pop("dtype"), **o)
+
+
+def test_scan_creation_refusals():
+    _scan(d=np.ones(4), dt_bias=np.zeros(4), conv_b=np.zeros(96)).close()
+    _scan(a=np.zeros(4)).close()
+    w = np.ones((4 * 8 + 2 * 3 * 16, 4))
+    assert code(lambda: _scan(groups=3, conv_w=w)) == -2
+    assert code(lambda: _scan(conv_w=np.ones((96, 5)))) == -4
+    assert code(lambda: _scan(state=257, conv_w=np.ones((32 + 4 * 257, 4)))) == -4
+    assert code(lambda: _scan(a=np.array([-1, -1, 0.5, -1]))) == -1
+    assert code(lambda: _scan(a=np.array([-1, -1, -np.inf, -1]))) == -1
+    assert code(lambda: _scan(dt_bias=np.full(4, np.nan))) == -1
+    assert code(lambda: _scan(conv_w=np.full((96, 4), np.nan))) == -1
+    assert code(lambda: _scan(max_seqs=0)) == -2 and code(lambda: _scan(max_seqs=65536)) == -2
+    assert code(lambda: _scan(max_tokens=0)) == -2 and code(lambda: _scan(max_tokens=1 << 31)) == -2
+    for wrong in (dict(conv_w=np.ones((95, 4))), dict(a=-np.ones(5)), dict(a=None), dict(d=np.ones(3))):
+        with pytest.raises(ValueError):
+            _scan(**wrong)
+
+
+def test_scan_run_refusals():
+    L = N.lib()
+    handle = _scan()
+    buf = np.zeros(1 << 16, np.uint8)
+    p = buf.ctypes.data
+
+    def call(step=False, op=handle._op, **kw):
+        io = N.ScanIO()
+        o = dict(seqs=2, tokens=2, x=p, x_stride=96, dt=p, dt_stride=4, window=p, state=p, y=p, y_stride=32, window_out=p,
+                 state_out=p)
+        o.update(kw)
+        for k, v in o.items():
+            setattr(io, k, v)
+        return (L.sn_scan_step if step else L.sn_scan_run)(op, ctypes.byref(io), None)
+
+    for step in (False, True):
+        assert call(step) == -5
+        assert call(step, seqs=-1) == -2 and call(step, seqs=4) == -2 and call(step, tokens=101) == -2
+        assert call(step, x=None) == -1 and call(step, dt=None) == -1 and call(step, y=None) == -1
+        assert call(step, x_stride=95) == -2 and call(step, y_stride=31) == -2 and call(step, dt_stride=3) == -2
+        assert call(step, window=p + 1) == -1 and call(step, state=p + 2) == -1
+        assert call(step, window_out=p + 64) == -1 and call(step, state_out=p + 64) == -1  # overlap, not in place
+        assert call(step, window=None, state=None, window_out=None, state_out=None) == -5
+        assert call(step, op=None) == -1
+    assert call(tokens=3) == -2 and call(tokens=3, offsets=p) == -5
+    assert call(seqs=0, tokens=1) == -2
+    assert call(True, tokens=4) == -2 and call(True, offsets=p) == -2
+    assert L.sn_scan_run(handle._op, None, None) == -1

@@ -247,6 +247,7 @@ int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint1
     check_dtype(d.dtype);
     if (d.rows < 1 || d.cols < 1) fail(SN_E_SHAPE, "rows and cols must be positive");
     if (d.rows > (1 << 24) || d.cols > (1 << 20)) fail(SN_E_UNSUPPORTED, "more than 2^24 rows or 2^20 cols");
+    if (k::linear4_blocks(d.rows, d.cols) >= (int64_t(1) << 28)) fail(SN_E_UNSUPPORTED, "more than 2^28 blocks of weights");
     if (d.group < 32 || d.group % 32) fail(SN_E_SHAPE, "group must be a multiple of 32");
     if (d.act < SN_ACT_NONE || d.act > SN_ACT_RELU6) fail(SN_E_INVALID, "unknown activation");
     const int64_t groups = (d.cols + (int64_t)d.group - 1) / d.group;
@@ -262,10 +263,20 @@ int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint1
     a.dtype = d.dtype, a.act = d.act, a.rows = d.rows, a.cols = d.cols, a.group = d.group;
     if (device >= 0) {
       OnDevice on(device);
-      a.q = op->upload(q, (size_t)d.rows * ((d.cols + 1) / 2));
-      a.scale = reinterpret_cast<const k::f16*>(op->upload(scale, n));
-      a.zero = op->upload(zero, n);
+      // the caller's arrays, and from them the kernels' order
+      sn_op raw(OP_LINEAR4, device);
+      const uint8_t* rq = raw.upload(q, (size_t)d.rows * ((d.cols + 1) / 2));
+      const uint16_t* rs = raw.upload(scale, n);
+      const uint8_t* rz = raw.upload(zero, n);
+      const int64_t blocks = k::linear4_blocks(d.rows, d.cols), scales = blocks * 64 / k::linear4_gs(d.group);
+      unsigned* wq = static_cast<unsigned*>(op->alloc(blocks * 1024));
+      k::f16* ws = static_cast<k::f16*>(op->alloc(scales * 2));
+      uint8_t* wz = zero ? static_cast<uint8_t*>(op->alloc(scales)) : nullptr;
+      k::linear4_pack(rq, reinterpret_cast<const k::f16*>(rs), rz, d.rows, d.cols, d.group, wq, ws, wz, nullptr);
+      HIPCHK(hipGetLastError());
+      a.wq = wq, a.ws = ws, a.wz = wz;
       a.bias = op->upload(bias, d.rows);
+      HIPCHK(hipDeviceSynchronize());
     }
     *out = op.release();
   });
@@ -275,7 +286,7 @@ int sn_linear4_run(sn_op* p, int64_t m, const void* x, int64_t x_stride, void* y
   return guarded([&] {
     Linear4Op& op = op_of<Linear4Op>(p, OP_LINEAR4);
     k::Linear4Args a = op.a;
-    if (m < 0 || m > 65535 * 8) fail(SN_E_SHAPE, "m must be in 0..524280");
+    if (m < 0 || m > 65535 * 4) fail(SN_E_SHAPE, "m must be in 0..262140");
     check_rows(x, x_stride, m, a.cols, a.dtype, "x");
     check_rows(y, y_stride, m, a.rows, a.dtype, "y");
     need_device(op);

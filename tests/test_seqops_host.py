@@ -100,7 +100,7 @@ def test_linear4_run_refusals_and_foreign_handles():
         return L.sn_linear4_run(op, m, x, xs, y, ys, None)
 
     assert run() == -5 and run(m=0, x=None, y=None) == -5
-    assert run(m=-1) == -2 and run(m=524281) == -2
+    assert run(m=-1) == -2 and run(m=262141) == -2
     assert run(x=None) == -1 and run(y=None) == -1 and run(x=p + 1) == -1
     assert run(xs=7) == -2 and run(ys=3) == -2
     assert run(op=norm._op) == -1 and run(op=None) == -1

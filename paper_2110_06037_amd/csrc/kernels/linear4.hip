@@ -25,11 +25,11 @@ namespace k {
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // ------------------------------------------------------------------ layout
-// One thread per dword of codes; scales and zero points per run of 32 GS
-// inputs: [block row][block column][16 features][4 / GS].
+// One thread per dword of codes; per run of 32 GS inputs a word of scale (low
+// half, binary16) and zero point: [block row][block column][16 features][4 / GS].
 __global__ __launch_bounds__(256) void linear4_pack_kernel(const uint8_t* q, const f16* scale, const uint8_t* zero,
-                                                           int rows, int cols, int group, int gs, unsigned* wq, f16* ws,
-                                                           uint8_t* wz) {
+                                                           int rows, int cols, int group, int gs, unsigned* wq,
+                                                           unsigned* ws) {
   const int cbs = (cols + 127) / 128, groups = (cols + group - 1) / group, pairs = (cols + 1) / 2;
   const int64_t total = (int64_t)((rows + 15) / 16) * cbs * 256, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
@@ -50,35 +50,63 @@ __global__ __launch_bounds__(256) void linear4_pack_kernel(const uint8_t* q, con
     const int cr = c0 + 32 * gs * step;
     const bool in = row < rows && cr < cols;
     const int64_t from = (int64_t)row * groups + cr / group, to = (blk * 16 + lane) * runs + step;
-    ws[to] = in ? scale[from] : (f16)0.f;
-    if (wz) wz[to] = in ? zero[from] : 8;
+    ws[to] = in ? __builtin_bit_cast(uint16_t, scale[from]) | (unsigned)(zero ? zero[from] : 8) << 16 : 0u;
   }
 }
 
 // ------------------------------------------------------------------ weights to floats
-// v_and_or_b32 takes one scalar: the mask stays in a register
-__device__ __forceinline__ unsigned and_or(unsigned w, unsigned mask, unsigned magic) { return (w & mask) | magic; }
-
-__device__ __forceinline__ f16x8 deq_f16(unsigned w, f16x2 z1024, f16x2 z64) {
+// A constant in a vector register whose value the compiler does not see: (w &
+// mask) | it is one v_and_or_b32 then (of two known constants the compiler
+// makes two instructions with literals).
+__device__ __forceinline__ unsigned vconst(unsigned v) {
+  asm("" : "+v"(v));
+  return v;
+}
+__device__ __forceinline__ float act4(float v, int act) {  // a NaN stays one
+  if (act != ACT_NONE && v < 0.f) v = 0.f;
+  return act == ACT_RELU6 && v > 6.f ? 6.f : v;
+}
+// A run's scale and zero point.
+struct Run4 {
+  float s, z;
+  unsigned z1024, z64;  // pairs of 1024 + z and 64 + z in f16
+  __device__ __forceinline__ explicit Run4(unsigned w) {
+    s = (float)__builtin_bit_cast(f16, (uint16_t)w);
+    const unsigned zi = w >> 16, zz = zi | (w & 0xffff0000u);
+    z = (float)zi;
+    z1024 = zz | 0x64006400u;
+    z64 = zz << 4 | 0x54005400u;
+  }
+};
+// The or-ed bits of 1024 + q and 64 + q, or of 128 + q (both halves of a pair).
+struct Magic {
+  unsigned a, b;
+};
+template <typename T>
+__device__ __forceinline__ Magic magic4() {
+  return std::is_same<T, f16>::value ? Magic{vconst(0x64006400u), vconst(0x54005400u)} : Magic{vconst(0x43004300u), 0u};
+}
+__device__ __forceinline__ f16x8 deq_f16(unsigned w, const Run4& c, const Magic& k) {  // q - z
+  const f16x2 a = __builtin_bit_cast(f16x2, c.z1024), b = __builtin_bit_cast(f16x2, c.z64);
   f16x2 r[4];
-  r[0] = __builtin_bit_cast(f16x2, and_or(w, 0x000f000fu, 0x64006400u)) - z1024;
-  r[1] = __builtin_bit_cast(f16x2, and_or(w, 0x00f000f0u, 0x54005400u)) - z64;
+  r[0] = __builtin_bit_cast(f16x2, (w & 0x000f000fu) | k.a) - a;
+  r[1] = __builtin_bit_cast(f16x2, (w & 0x00f000f0u) | k.b) - b;
   w >>= 8;
-  r[2] = __builtin_bit_cast(f16x2, and_or(w, 0x000f000fu, 0x64006400u)) - z1024;
-  r[3] = __builtin_bit_cast(f16x2, and_or(w, 0x00f000f0u, 0x54005400u)) - z64;
+  r[2] = __builtin_bit_cast(f16x2, (w & 0x000f000fu) | k.a) - a;
+  r[3] = __builtin_bit_cast(f16x2, (w & 0x00f000f0u) | k.b) - b;
   return __builtin_bit_cast(f16x8, r);
 }
-__device__ __forceinline__ bf16x8 deq_bf16_128(unsigned w) {  // 128 + q
+__device__ __forceinline__ bf16x8 deq_bf16_128(unsigned w, const Magic& k) {  // 128 + q
   u32x4 r;
-  r[0] = and_or(w, 0x000f000fu, 0x43004300u);
-  r[1] = and_or(w >> 4, 0x000f000fu, 0x43004300u);
-  r[2] = and_or(w >> 8, 0x000f000fu, 0x43004300u);
-  r[3] = and_or(w >> 12, 0x000f000fu, 0x43004300u);
+  r[0] = (w & 0x000f000fu) | k.a;
+  r[1] = ((w >> 4) & 0x000f000fu) | k.a;
+  r[2] = ((w >> 8) & 0x000f000fu) | k.a;
+  r[3] = ((w >> 12) & 0x000f000fu) | k.a;
   return __builtin_bit_cast(bf16x8, r);
 }
 // q - z: the two halves of a pair are the high halves of the floats 128 + q
-__device__ __forceinline__ bf16x8 deq_bf16(unsigned w, float z128) {
-  u32x4 r = __builtin_bit_cast(u32x4, deq_bf16_128(w));
+__device__ __forceinline__ bf16x8 deq_bf16(unsigned w, float z128, const Magic& k) {
+  u32x4 r = __builtin_bit_cast(u32x4, deq_bf16_128(w, k));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float lo = __builtin_bit_cast(float, r[i] << 16) - z128, hi = __builtin_bit_cast(float, r[i] & 0xffff0000u) - z128;
@@ -86,18 +114,39 @@ __device__ __forceinline__ bf16x8 deq_bf16(unsigned w, float z128) {
   }
   return __builtin_bit_cast(bf16x8, r);
 }
+template <typename T>
+__device__ __forceinline__ auto deq4(unsigned w, const Run4& c, const Magic& k) {
+  if constexpr (std::is_same<T, float>::value) return deq_bf16(w, 128.f + c.z, k);
+  else if constexpr (std::is_same<T, bf16>::value) return deq_bf16_128(w, k);
+  else return deq_f16(w, c, k);
+}
 
 // ------------------------------------------------------------------ inputs
-// 8 consecutive inputs of a row from c on, 0 past its end; vec: aligned, and
-// whole chunks of 8.
-template <typename T>
-__device__ __forceinline__ V8<T> ld_x(const T* row, int c, int cols, bool vec) {
-  if (vec) return c < cols ? ld8(row + c) : zero8<T>();
-  V8<T> r;
+// 8 consecutive inputs c .. c + 7 of a row of x, 0 past its end.  VX: rows of
+// whole aligned chunks below 2 GiB from the resource's base, one or two wide
+// loads (a resource's loads outside its range give zero); else element by
+// element.
+template <typename T, bool VX>
+struct XRow {
+  __amdgpu_buffer_rsrc_t rs;
+  const T* row;
+  unsigned off;  // of the row, in bytes (kOOB: a row of zeros)
+  __device__ __forceinline__ V8<T> get(int c, int cols) const {
+    V8<T> r;
+    if constexpr (VX) {
+      const unsigned o = c < cols ? off + (unsigned)c * (unsigned)sizeof(T) : kOOB;
+      u32x4 u[sizeof(T) / 2];
+      u[0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)o, 0, 0));
+      if constexpr (sizeof(T) == 4) u[1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)o, 16, 0));
+      __builtin_memcpy(&r, u, sizeof(r));
+    } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) r.v[j] = c + j < cols ? row[c + j] : (T)0.f;
-  return r;
-}
+      for (int j = 0; j < 8; ++j) r.v[j] = off != kOOB && c + j < cols ? row[c + j] : (T)0.f;
+    }
+    return r;
+  }
+};
+
 // Part 0, 1 or 2 of float32 values as bf16: the leading 8 significant bits,
 // the next 8, the last 8, each the value less the parts before it (exact).
 __device__ __forceinline__ float rest_f(float x) {
@@ -123,6 +172,21 @@ __device__ __forceinline__ bf16x8 part_of(V8<float> x, int part) {
   return top_bf16(x.v);
 }
 
+// The words of a feature's runs in a block.
+template <int RUNS>
+__device__ __forceinline__ void ld_runs(__amdgpu_buffer_rsrc_t rs, int voff, int soff, unsigned (&o)[RUNS]) {
+  if constexpr (RUNS == 1) {
+    o[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, voff, soff, 0);
+  } else if constexpr (RUNS == 2) {
+    const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, voff, soff, 0));
+    o[0] = v[0], o[1] = v[1];
+  } else {
+    const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, voff, soff, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = v[i];
+  }
+}
+
 template <typename T>
 struct Op4 {
   typedef typename std::conditional<std::is_same<T, f16>::value, f16, bf16>::type E;  // MFMA's element
@@ -130,218 +194,249 @@ struct Op4 {
 };
 
 // ------------------------------------------------------------------ few rows
-// A workgroup owns 16 features; its waves take the blocks of 128 inputs in
+// A workgroup owns 16 R features; its waves take the blocks of 128 inputs in
 // turn, U at a time with all their loads in flight, and their sums meet in
 // LDS.  x goes from global memory (its rows are shared by all workgroups and
 // stay in the caches) straight to the first operand: row r = 4 g + v of it is
 // row 4 v + g of x, so that up to 4 rows have all their sums in element v = 0
 // (MV = 1); in float32 v is the part and g the row.
-template <typename T, int NB, int MV, int GS>
-__global__ __launch_bounds__(1024) void linear4_rows_kernel(Linear4Args a) {
+template <typename T, int NB, int MV, int GS, bool VX, int R, int U>
+__global__ __launch_bounds__(512) void linear4_rows_kernel(Linear4Args a) {
   typedef typename Op4<T>::E E;
   typedef typename Op4<T>::frag frag;
   constexpr bool F32 = std::is_same<T, float>::value;
   constexpr bool BIASED = std::is_same<T, bf16>::value;
-  constexpr int RUNS = 4 / GS, U = NB >= 4 ? 2 : 4;
+  constexpr int RUNS = 4 / GS;
   constexpr int PER = F32 ? 4 : 4 * MV;  // rows of x per block of the first operand
   constexpr int NV = F32 ? 1 : MV;       // results per lane and block
-  extern __shared__ float red[];         // [wave][NB][NV][64]
+  extern __shared__ float red[];         // [wave][R][NB][NV][64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int col = lane & 15, g = lane >> 4, xr = lane & 15;
-  const int cbs = (a.cols + 127) / 128;
-  const int64_t blk0 = (int64_t)blockIdx.x * cbs;
-  const u32x4* wq = reinterpret_cast<const u32x4*>(a.wq) + blk0 * 64 + lane;
-  const f16* ws = a.ws + (blk0 * 16 + col) * RUNS;
-  const uint8_t* wz = a.wz ? a.wz + (blk0 * 16 + col) * RUNS : nullptr;
+  const int cbs = (a.cols + 127) / 128, rbs = (a.rows + 15) / 16;
+  const int rb0 = blockIdx.x * R;
+  // loads outside a row of blocks give zero, and meet inputs of zero
+  __amdgpu_buffer_rsrc_t rw[R], rs[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t blk = (int64_t)min(rb0 + r, rbs - 1) * cbs;
+    rw[r] = make_rsrc(a.wq + blk * 256, (long long)cbs * 1024);
+    rs[r] = make_rsrc(a.ws + blk * 16 * RUNS, (long long)cbs * 64 * RUNS);
+  }
   // this lane's rows of x
-  const T* x = static_cast<const T*>(a.x);
-  const T* xrow[NB];
-  bool on[NB];
+  const int64_t mb = (int64_t)blockIdx.y * NB * PER, left = a.m - mb;
+  const T* xb = static_cast<const T*>(a.x) + mb * a.xs;
+  XRow<T, VX> xrow[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const int v = xr & 3;
-    const int64_t m = (int64_t)(blockIdx.y * NB + nb) * PER + (F32 ? xr >> 2 : 4 * v + (xr >> 2));
-    on[nb] = m < a.m && v < (F32 ? 3 : MV);
-    xrow[nb] = x + (on[nb] ? m : 0) * a.xs;
+    const int v = xr & 3, m = nb * PER + (F32 ? xr >> 2 : 4 * v + (xr >> 2));
+    const bool on = m < left && v < (F32 ? 3 : MV);
+    if constexpr (VX) xrow[nb].rs = make_rsrc(xb, ((min(left, (int64_t)NB * PER) - 1) * a.xs + a.cols) * (int)sizeof(T));
+    xrow[nb].row = xb + (on ? m * a.xs : 0);
+    xrow[nb].off = on ? VX ? (unsigned)(m * a.xs) * (unsigned)sizeof(T) : 0u : kOOB;
   }
-  float tot[NB][NV] = {};
+  float tot[R][NB][NV] = {};
+  const Magic magic = magic4<T>();
   const frag ones = __builtin_bit_cast(frag, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
   for (int c0 = wave; c0 < cbs; c0 += waves * U) {
-    u32x4 w[U];
-    f16 sc[U][RUNS];
-    uint8_t zp[U][RUNS];
+    u32x4 w[U][R];
+    unsigned sc[U][R][RUNS];
     V8<T> xv[U][NB][4];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int cb = c0 + u * waves;
-      if (cb >= cbs) break;
-      w[u] = __builtin_nontemporal_load(wq + (int64_t)cb * 64);
-      __builtin_memcpy(sc[u], ws + (int64_t)cb * 16 * RUNS, 2 * RUNS);
-      if (wz) __builtin_memcpy(zp[u], wz + (int64_t)cb * 16 * RUNS, RUNS);
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int r = 0; r < R; ++r)  // read once: not kept in the caches for others
+        w[u][r] = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw[r], lane * 16, (c0 + u * waves) * 1024, 2));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          xv[u][nb][i] = on[nb] ? ld_x(xrow[nb], cb * 128 + 32 * i + 8 * g, a.cols, a.vec_x) : zero8<T>();
-    }
+        for (int i = 0; i < 4; ++i) xv[u][nb][i] = xrow[nb].get((c0 + u * waves) * 128 + 32 * i + 8 * g, a.cols);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        ld_runs<RUNS>(rs[r], col * 4 * RUNS, (c0 + u * waves) * 64 * RUNS, sc[u][r]);
+      }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int cb = c0 + u * waves;
-      if (cb >= cbs) break;
 #pragma unroll
       for (int run = 0; run < RUNS; ++run) {
-        const float s = (float)sc[u][run], z = wz ? (float)zp[u][run] : 8.f;
-        const f16 z1024 = (f16)(1024.f + z), z64 = (f16)(64.f + z);
-        f32x4 acc[NB], xs[NB];
+        frag xf[NB][GS];
+        f32x4 xs[NB];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) acc[nb] = xs[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int nb = 0; nb < NB; ++nb) {
+          xs[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = run * GS; i < (run + 1) * GS; ++i) {
-          frag wf;
-          if constexpr (F32) wf = deq_bf16(w[u][i], 128.f + z);
-          else if constexpr (BIASED) wf = deq_bf16_128(w[u][i]);
-          else wf = deq_f16(w[u][i], f16x2{z1024, z1024}, f16x2{z64, z64});
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            frag xf;
-            if constexpr (F32) xf = part_of(xv[u][nb][i], xr & 3);
-            else xf = __builtin_bit_cast(frag, xv[u][nb][i]);
-            acc[nb] = Mfma<E>::run(xf, wf, acc[nb]);
-            if constexpr (BIASED) xs[nb] = Mfma<E>::run(xf, ones, xs[nb]);
+          for (int i = 0; i < GS; ++i) {
+            if constexpr (F32) xf[nb][i] = part_of(xv[u][nb][run * GS + i], xr & 3);
+            else xf[nb][i] = __builtin_bit_cast(frag, xv[u][nb][run * GS + i]);
+            if constexpr (BIASED) xs[nb] = Mfma<E>::run(xf[nb][i], ones, xs[nb]);
           }
         }
-        if constexpr (F32) {
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) tot[nb][0] = fmaf(s, acc[nb][0] + (acc[nb][1] + acc[nb][2]), tot[nb][0]);
-        } else if constexpr (BIASED) {
-          // an infinity among the biased products (or a finite sum beyond the
-          // range that only the bias brings there): the run again with q - z
-          bool over = false;
+        for (int r = 0; r < R; ++r) {
+          const Run4 rc(sc[u][r][run]);
+          const float s = rc.s;
+          f32x4 acc[NB];
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
+          for (int nb = 0; nb < NB; ++nb) acc[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int v = 0; v < NV; ++v) over = over || !(fabsf(acc[nb][v]) < INFINITY);
-          float zz = 128.f + z;
-          if (__any(over)) {
+          for (int i = 0; i < GS; ++i) {
+            const frag wf = deq4<T>(w[u][r][run * GS + i], rc, magic);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) acc[nb] = xs[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int nb = 0; nb < NB; ++nb) acc[nb] = Mfma<E>::run(xf[nb][i], wf, acc[nb]);
+          }
+          if constexpr (F32) {
 #pragma unroll
-            for (int i = run * GS; i < (run + 1) * GS; ++i)
+            for (int nb = 0; nb < NB; ++nb) tot[r][nb][0] = fmaf(s, acc[nb][0] + (acc[nb][1] + acc[nb][2]), tot[r][nb][0]);
+          } else if constexpr (BIASED) {
+            // an infinity among the biased products (or a finite sum beyond
+            // the range that only the bias brings there): again with q - z
+            bool over = false;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int v = 0; v < NV; ++v) over = over || !(fabsf(acc[nb][v]) < INFINITY);
+            const float zz = 128.f + rc.z;
+            if (__any(over)) {
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                f32x4 again = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < GS; ++i) again = Mfma<E>::run(xf[nb][i], deq_bf16(w[u][r][run * GS + i], zz, magic), again);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) tot[r][nb][v] = fmaf(s, again[v], tot[r][nb][v]);
+              }
+            } else {
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb)
-                acc[nb] = Mfma<E>::run(__builtin_bit_cast(frag, xv[u][nb][i]), deq_bf16(w[u][i], zz), acc[nb]);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) tot[r][nb][v] = fmaf(s, fmaf(-zz, xs[nb][v], acc[nb][v]), tot[r][nb][v]);
+            }
+          } else {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int v = 0; v < NV; ++v) tot[r][nb][v] = fmaf(s, acc[nb][v], tot[r][nb][v]);
           }
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int v = 0; v < NV; ++v) tot[nb][v] = fmaf(s, fmaf(-zz, xs[nb][v], acc[nb][v]), tot[nb][v]);
-        } else {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int v = 0; v < NV; ++v) tot[nb][v] = fmaf(s, acc[nb][v], tot[nb][v]);
         }
       }
     }
   }
+  constexpr int SUMS = R * NB * NV * 64;
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb)
+  for (int r = 0; r < R; ++r)
 #pragma unroll
-    for (int v = 0; v < NV; ++v) red[((wave * NB + nb) * NV + v) * 64 + lane] = tot[nb][v];
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) red[wave * SUMS + ((r * NB + nb) * NV + v) * 64 + lane] = tot[r][nb][v];
   __syncthreads();
-  for (int i = threadIdx.x; i < NB * NV * 64; i += blockDim.x) {
+  for (int i = threadIdx.x; i < SUMS; i += blockDim.x) {
     float s = 0.f;
-    for (int w = 0; w < waves; ++w) s += red[w * NB * NV * 64 + i];
-    const int l = i & 63, v = (i >> 6) % NV, nb = (i >> 6) / NV;
-    const int64_t m = (int64_t)(blockIdx.y * NB + nb) * PER + (F32 ? l >> 4 : 4 * v + (l >> 4));
-    const int k = blockIdx.x * 16 + (l & 15);
-    if (m < a.m && k < a.rows)
-      static_cast<T*>(a.y)[m * a.ys + k] = from_f<T>(act_f(s + (a.bias ? a.bias[k] : 0.f), a.act));
+    for (int w = 0; w < waves; ++w) s += red[w * SUMS + i];
+    const int l = i & 63, v = (i >> 6) % NV, nb = (i >> 6) / NV % NB, r = (i >> 6) / (NV * NB);
+    const int m = nb * PER + (F32 ? l >> 4 : 4 * v + (l >> 4)), k = (rb0 + r) * 16 + (l & 15);
+    if (m < left && k < a.rows)
+      static_cast<T*>(a.y)[(mb + m) * a.ys + k] = from_f<T>(act4(s + (a.bias ? a.bias[k] : 0.f), a.act));
   }
 }
 
 // ------------------------------------------------------------------ many rows
+constexpr int kL4Stages = 3;
 // Tile of 64 rows of x by 64 RB features: each of 4 waves owns 16 RB features
 // and all 64 rows, so no weight is turned into floats twice in a workgroup,
-// and x alone goes through LDS, in the first operand's order (a wave loads its
-// 16 rows of the next 128 inputs into registers while the current ones are
-// multiplied).  bf16: the wave that loads 16 rows sums them against ones; the
-// sums wait in LDS and the bias comes off at the end, as one more product.
-template <typename T, int RB, int GS>
-__global__ __launch_bounds__(256) void linear4_tile_kernel(Linear4Args a, int tiles_m, int tiles_n) {
+// and x alone goes through LDS, in the first operand's order.  DMA (16-bit
+// types, wide rows): LDS direct loads, three blocks of 128 inputs in a ring,
+// two blocks ahead; else through registers, one block ahead (float32 is split
+// into its parts there).  bf16: sums
+// against ones, each wave for 16 of the rows, wait in LDS, and the bias comes
+// off at the end, as one more matrix product, in float32.
+template <typename T, int RB, int GS, bool VX>
+__global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int tiles_m, int tiles_n) {
   typedef typename Op4<T>::E E;
   typedef typename Op4<T>::frag frag;
-  constexpr bool F32 = std::is_same<T, float>::value;
-  constexpr bool BIASED = std::is_same<T, bf16>::value;
+  constexpr bool F32 = std::is_same<T, float>::value, BIASED = std::is_same<T, bf16>::value;
+  constexpr bool DMA = VX && !F32;
   constexpr int RUNS = 4 / GS, PARTS = F32 ? 3 : 1;
-  extern __shared__ char smem[];
-  // [stage][part][row block][step][lane] of 16 bytes, then the bias sums
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  // [stage][part][row block][step][lane] of 16 bytes, then the sums
   frag* xt = reinterpret_cast<frag*>(smem);
-  constexpr int STAGE = PARTS * 4 * 4 * 64;
-  float* xsum = reinterpret_cast<float*>(xt + 2 * STAGE);  // [run][64]
+  constexpr int STAGE = PARTS * 4 * 4 * 64, STAGES = DMA ? kL4Stages : 2;
+  float* xsum = reinterpret_cast<float*>(xt + STAGES * STAGE);  // [run][64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int cbs = (a.cols + 127) / 128, rbs = (a.rows + 15) / 16;
   int mt, nt;
   tile_of(blockIdx.x, tiles_m, tiles_n, mt, nt);
-  const int64_t m0 = (int64_t)mt * 64;
-  const T* xrow = static_cast<const T*>(a.x) + min(m0 + 16 * wave + col, a.m - 1) * a.xs;  // rows past m: any row's values
+  const int64_t m0 = (int64_t)mt * 64, left = a.m - m0;
+  // the row of x that this lane loads (past the last: the last one's values, not stored)
+  const int mx = (int)min((int64_t)(16 * wave + col), left - 1);
+  const T* xb = static_cast<const T*>(a.x) + m0 * a.xs;
+  XRow<T, VX> xrow;
+  if constexpr (VX) xrow.rs = make_rsrc(xb, ((min(left, (int64_t)64) - 1) * a.xs + a.cols) * (int)sizeof(T));
+  xrow.row = xb + mx * a.xs;
+  xrow.off = VX ? (unsigned)(mx * a.xs) * (unsigned)sizeof(T) : 0u;
   const int rb0 = (nt * 4 + wave) * RB;
-  int64_t blk[RB];  // first block of each of the wave's rows of blocks (past the last: the last's, not stored)
+  // the wave's rows of blocks (past the last: the last one's, not stored)
+  __amdgpu_buffer_rsrc_t rw[RB], rs[RB];
 #pragma unroll
-  for (int r = 0; r < RB; ++r) blk[r] = (int64_t)min(rb0 + r, rbs - 1) * cbs;
-  f32x4 tot[4][RB];
+  for (int r = 0; r < RB; ++r) {
+    const int64_t blk = (int64_t)min(rb0 + r, rbs - 1) * cbs;
+    rw[r] = make_rsrc(a.wq + blk * 256, (long long)cbs * 1024);
+    rs[r] = make_rsrc(a.ws + blk * 16 * RUNS, (long long)cbs * 64 * RUNS);
+  }
+  f32x4 tot[4][RB];  // [i]: row block (wave + i) % 4, so that each wave's own sums are those of i = 0
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int r = 0; r < RB; ++r) tot[i][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const Magic magic = magic4<T>();
   const frag ones = __builtin_bit_cast(frag, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-  V8<T> xn[4];
-  u32x4 wn[RB];
-  auto load = [&](int cb) {
-#pragma unroll
-    for (int r = 0; r < RB; ++r) wn[r] = (reinterpret_cast<const u32x4*>(a.wq) + (blk[r] + cb) * 64)[lane];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) xn[i] = ld_x(xrow, cb * 128 + 32 * i + 8 * g, a.cols, a.vec_x);
+  V8<T> xn[DMA ? 1 : 4];
+  struct W {
+    u32x4 q[RB];
+    unsigned s[RB][RUNS];
   };
-  auto put = [&](int stage, int cb) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (F32) {
-#pragma unroll
-        for (int p = 0; p < 3; ++p) xt[stage * STAGE + ((p * 4 + wave) * 4 + i) * 64 + lane] = part_of(xn[i], p);
-      } else {
-        xt[stage * STAGE + (wave * 4 + i) * 64 + lane] = __builtin_bit_cast(frag, xn[i]);
-      }
-    }
-    if constexpr (BIASED) {
-#pragma unroll
-      for (int run = 0; run < RUNS; ++run) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = run * GS; i < (run + 1) * GS; ++i) s = Mfma<E>::run(__builtin_bit_cast(frag, xn[i]), ones, s);
-        if (col == 0) *reinterpret_cast<f32x4*>(xsum + (cb * RUNS + run) * 64 + 16 * wave + 4 * g) = s;
-      }
-    }
-  };
-  load(0);
-  put(0, 0);
-  for (int cb = 0; cb < cbs; ++cb) {
-    u32x4 w[RB];
-    f16 sc[RB][RUNS];
-    uint8_t zp[RB][RUNS];
+  auto load_w = [&](int cb, W& w) {
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-      w[r] = wn[r];
-      __builtin_memcpy(sc[r], a.ws + ((blk[r] + cb) * 16 + col) * RUNS, 2 * RUNS);
-      if (a.wz) __builtin_memcpy(zp[r], a.wz + ((blk[r] + cb) * 16 + col) * RUNS, RUNS);
+      w.q[r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw[r], lane * 16, cb * 1024, 0));
+      ld_runs<RUNS>(rs[r], col * 4 * RUNS, cb * 64 * RUNS, w.s[r]);
     }
-    lds_barrier();  // the stage is written, and the other one no longer read
-    if (cb + 1 < cbs) load(cb + 1);
-    const frag* xc = xt + (cb & 1) * STAGE + lane;
+  };
+  auto load_x = [&](int cb) {  // registers, or LDS stage cb % STAGES
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = cb * 128 + 32 * i + 8 * g;
+      if constexpr (DMA) {
+        const unsigned o = c < a.cols ? xrow.off + (unsigned)c * 2u : kOOB;
+        dma16(xrow.rs, reinterpret_cast<char*>(xt + (cb % STAGES) * STAGE + (wave * 4 + i) * 64), o, 0);
+      } else {
+        xn[i] = xrow.get(c, a.cols);
+      }
+    }
+  };
+  auto put = [&](int cb) {
+    if constexpr (!DMA)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        frag* to = xt + (cb % STAGES) * STAGE + (wave * 4 + i) * 64 + lane;
+        if constexpr (F32) {
+#pragma unroll
+          for (int p = 0; p < 3; ++p) to[p * 16 * 64] = part_of(xn[i], p);
+        } else {
+          *to = __builtin_bit_cast(frag, xn[i]);
+        }
+      }
+  };
+  auto multiply = [&](int cb, const W& w) {
+    const frag* xc = xt + (cb % STAGES) * STAGE + lane;
+    auto xfrag = [&](int p, int mi, int i) { return xc[((p * 4 + ((wave + mi) & 3)) * 4 + i) * 64]; };
 #pragma unroll
     for (int run = 0; run < RUNS; ++run) {
-      f32x4 acc[4][RB];
+      f32x4 acc[4][RB], xs = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int mi = 0; mi < 4; ++mi)
 #pragma unroll
@@ -350,83 +445,77 @@ __global__ __launch_bounds__(256) void linear4_tile_kernel(Linear4Args a, int ti
       for (int i = run * GS; i < (run + 1) * GS; ++i) {
         frag wf[RB];
 #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          const float z = a.wz ? (float)zp[r][run] : 8.f;
-          if constexpr (F32) {
-            wf[r] = deq_bf16(w[r][i], 128.f + z);
-          } else if constexpr (BIASED) {
-            wf[r] = deq_bf16_128(w[r][i]);
-          } else {
-            const f16 z1024 = (f16)(1024.f + z), z64 = (f16)(64.f + z);
-            wf[r] = deq_f16(w[r][i], f16x2{z1024, z1024}, f16x2{z64, z64});
-          }
-        }
+        for (int r = 0; r < RB; ++r) wf[r] = deq4<T>(w.q[r][i], Run4(w.s[r][run]), magic);
 #pragma unroll
         for (int p = 0; p < PARTS; ++p)
 #pragma unroll
           for (int mi = 0; mi < 4; ++mi) {
-            const frag xf = xc[((p * 4 + mi) * 4 + i) * 64];
+            const frag xf = xfrag(p, mi, i);
+            if (BIASED && mi == 0) xs = Mfma<E>::run(xf, ones, xs);
 #pragma unroll
             for (int r = 0; r < RB; ++r) acc[mi][r] = Mfma<E>::run(xf, wf[r], acc[mi][r]);
           }
       }
-#pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        const float s = (float)sc[r][run];
-#pragma unroll
-        for (int mi = 0; mi < 4; ++mi)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) tot[mi][r][v] = fmaf(s, acc[mi][r][v], tot[mi][r][v]);
-      }
-    }
-    if (cb + 1 < cbs) put((cb + 1) & 1, cb + 1);
-  }
-  if constexpr (BIASED) {
-    __syncthreads();
-    for (int cb = 0; cb < cbs; ++cb)
-#pragma unroll
-      for (int run = 0; run < RUNS; ++run) {
-        f32x4 xs[4];
-#pragma unroll
-        for (int mi = 0; mi < 4; ++mi) xs[mi] = *reinterpret_cast<const f32x4*>(xsum + (cb * RUNS + run) * 64 + 16 * mi + 4 * g);
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          const int64_t at = ((blk[r] + cb) * 16 + col) * RUNS + run;
-          const float zs = (128.f + (a.wz ? (float)a.wz[at] : 8.f)) * (float)a.ws[at];
-#pragma unroll
-          for (int mi = 0; mi < 4; ++mi)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) tot[mi][r][v] = fmaf(-zs, xs[mi][v], tot[mi][r][v]);
-        }
-      }
-    // rows with an infinity or a NaN (or beyond the range by the bias alone)
-    // again, with q - z, input by input
-    bool over = false;
-#pragma unroll
-    for (int mi = 0; mi < 4; ++mi)
-#pragma unroll
-      for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) over = over || !(fabsf(tot[mi][r][v]) < INFINITY);
-    if (__any(over)) {
+      if (BIASED && col == 0) *reinterpret_cast<f32x4*>(xsum + (cb * RUNS + run) * 64 + 16 * wave + 4 * g) = xs;
 #pragma unroll
       for (int mi = 0; mi < 4; ++mi)
 #pragma unroll
-        for (int r = 0; r < RB; ++r)
+        for (int r = 0; r < RB; ++r) {
+          const float s = Run4(w.s[r][run]).s;
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            if (fabsf(tot[mi][r][v]) < INFINITY) continue;
-            const int64_t m = min(m0 + 16 * mi + 4 * g + v, a.m - 1);
-            const T* xp = static_cast<const T*>(a.x) + m * a.xs;
-            float sum = 0.f;
-            for (int c = 0; c < a.cols; ++c) {
-              const int64_t b = blk[r] + c / 128, at = (b * 16 + col) * RUNS + c % 128 / (32 * GS);
-              const unsigned dw = a.wq[(b * 64 + col + 16 * (c % 32 / 8)) * 4 + c % 128 / 32];
-              const float q = (float)(dw >> (4 * (c % 8 / 2) + 16 * (c & 1)) & 15);
-              sum = fmaf(to_f(xp[c]), (q - (a.wz ? (float)a.wz[at] : 8.f)) * (float)a.ws[at], sum);
-            }
-            tot[mi][r][v] = sum;
-          }
+          for (int v = 0; v < 4; ++v) tot[mi][r][v] = fmaf(s, acc[mi][r][v], tot[mi][r][v]);
+        }
+      if (RUNS > 1) __builtin_amdgcn_sched_barrier(0);  // one run's registers at a time
+    }
+  };
+  if constexpr (DMA) {
+    // the weights one block ahead, x two; past the last block: zeros
+    W w0, w1;
+    load_x(0), load_w(0, w0), load_x(1);
+    auto block = [&](int cb, const W& now, W& next) {
+      // x of the block is in LDS once all but the 4 loads of the next block's
+      // x have arrived; behind the barrier every wave's are, and the stage of
+      // block cb + 2 is no longer read
+      wait_vmcnt<4>();
+      dma_barrier();
+      load_w(cb + 1, next), load_x(cb + 2);
+      multiply(cb, now);
+    };
+    for (int cb = 0; cb < cbs; cb += 2) {
+      block(cb, w0, w1);
+      if (cb + 1 < cbs) block(cb + 1, w1, w0);
+    }
+  } else {
+    W w0, w1;
+    load_x(0), load_w(0, w0);
+    put(0);
+    for (int cb = 0; cb < cbs; cb += 2) {
+      lds_barrier();  // the stage is written, and the other one no longer read
+      if (cb + 1 < cbs) load_x(cb + 1), load_w(cb + 1, w1);
+      multiply(cb, w0);
+      if (cb + 1 >= cbs) break;
+      put(cb + 1);
+      lds_barrier();
+      if (cb + 2 < cbs) load_x(cb + 2), load_w(cb + 2, w0);
+      multiply(cb + 1, w1);
+      if (cb + 2 < cbs) put(cb + 2);
+    }
+  }
+  if constexpr (BIASED) {
+    __syncthreads();
+    const int runs = cbs * RUNS;
+    for (int q = 0; q < runs; q += 4) {
+      const int run = q + g;
+      float xs[4];
+#pragma unroll
+      for (int mi = 0; mi < 4; ++mi) xs[mi] = run < runs ? xsum[run * 64 + 16 * ((wave + mi) & 3) + col] : 0.f;
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        const Run4 rc(__builtin_amdgcn_raw_buffer_load_b32(rs[r], run / RUNS * 64 * RUNS + col * 4 * RUNS + run % RUNS * 4, 0, 0));
+        const float zs = run < runs ? -(128.f + rc.z) * rc.s : 0.f;
+#pragma unroll
+        for (int mi = 0; mi < 4; ++mi) tot[mi][r] = Mfma<float>::run(xs[mi], zs, tot[mi][r]);
+      }
     }
   }
 #pragma unroll
@@ -438,9 +527,36 @@ __global__ __launch_bounds__(256) void linear4_tile_kernel(Linear4Args a, int ti
     for (int mi = 0; mi < 4; ++mi)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int64_t m = m0 + 16 * mi + 4 * g + v;
-        if (m < a.m) static_cast<T*>(a.y)[m * a.ys + k] = from_f<T>(act_f(tot[mi][r][v] + b, a.act));
+        const int m = 16 * ((wave + mi) & 3) + 4 * g + v;
+        if (m < left) static_cast<T*>(a.y)[(m0 + m) * a.ys + k] = from_f<T>(act4(tot[mi][r][v] + b, a.act));
       }
+  }
+  if constexpr (BIASED) {
+    // sums that are not finite (an infinity or a NaN of x, or beyond the range
+    // by the bias alone) again, with q - z, input by input
+    uint64_t odd = 0;
+#pragma unroll
+    for (int mi = 0; mi < 4; ++mi)
+#pragma unroll
+      for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) odd |= (uint64_t)!(fabsf(tot[mi][r][v]) < INFINITY) << ((mi * RB + r) * 4 + v);
+    while (odd) {
+      const int e = __builtin_ctzll(odd), v = e & 3, r = (e >> 2) % RB, mi = (e >> 2) / RB;
+      odd &= odd - 1;
+      const int m = 16 * ((wave + mi) & 3) + 4 * g + v, k = (rb0 + r) * 16 + col;
+      if (m >= left || k >= a.rows) continue;
+      const int64_t blk = (int64_t)(rb0 + r) * cbs;
+      const T* x = xb + m * a.xs;
+      float sum = 0.f;
+      for (int c = 0; c < a.cols; ++c) {
+        const int64_t b = blk + c / 128;
+        const Run4 rc(a.ws[(b * 16 + col) * RUNS + c % 128 / (32 * GS)]);
+        const unsigned dw = a.wq[(b * 64 + col + 16 * (c % 32 / 8)) * 4 + c % 128 / 32];
+        sum = fmaf(to_f(x[c]), ((float)(dw >> (4 * (c % 8 / 2) + 16 * (c & 1)) & 15) - rc.z) * rc.s, sum);
+      }
+      static_cast<T*>(a.y)[(m0 + m) * a.ys + k] = from_f<T>(act4(sum + (a.bias ? a.bias[k] : 0.f), a.act));
+    }
   }
 }
 
@@ -449,49 +565,63 @@ int linear4_gs(int group) { return group % 128 == 0 ? 4 : group % 64 == 0 ? 2 : 
 int64_t linear4_blocks(int rows, int cols) { return (int64_t)((rows + 15) / 16) * ((cols + 127) / 128); }
 
 void linear4_pack(const uint8_t* q, const f16* scale, const uint8_t* zero, int rows, int cols, int group, unsigned* wq,
-                  f16* ws, uint8_t* wz, hipStream_t st) {
+                  unsigned* ws, hipStream_t st) {
   const int64_t blocks = linear4_blocks(rows, cols);
   check(blocks < (int64_t(1) << 31), "4-bit weights");
   SN_LAUNCH(linear4_pack_kernel, dim3((unsigned)blocks), dim3(256), 0, st, q, scale, zero, rows, cols, group,
-            linear4_gs(group), wq, ws, wz);
+            linear4_gs(group), wq, ws);
 }
 
-template <typename T, int NB, int MV, int GS>
-static void launch_rows(const Linear4Args& a, hipStream_t st) {
+template <typename T, int NB, int MV, int GS, bool VX, int R, int U>
+static void launch_rows_u(const Linear4Args& a, hipStream_t st) {
   constexpr int PER = std::is_same<T, float>::value ? 4 : 4 * MV, NV = std::is_same<T, float>::value ? 1 : MV;
   const int cbs = (a.cols + 127) / 128;
-  const int waves = cbs <= 4 ? 4 : cbs <= 64 ? 8 : 16;
-  const dim3 grid((a.rows + 15) / 16, (unsigned)((a.m + NB * PER - 1) / (NB * PER)));
-  SN_LAUNCH((linear4_rows_kernel<T, NB, MV, GS>), grid, dim3(64 * waves), waves * NB * NV * 256, st, a);
+  const int waves = std::min(8, (cbs + U - 1) / U);
+  const dim3 grid((a.rows + 16 * R - 1) / (16 * R), (unsigned)((a.m + NB * PER - 1) / (NB * PER)));
+  SN_LAUNCH((linear4_rows_kernel<T, NB, MV, GS, VX, R, U>), grid, dim3(64 * waves), waves * R * NB * NV * 256, st, a);
+}
+template <typename T, int NB, int MV, int GS, bool VX>
+static void launch_rows(const Linear4Args& a, hipStream_t st) {
+  // Several rows of blocks per workgroup share the loads of x (and its sums),
+  // as long as the workgroups still fill the chip.
+  if constexpr (VX) {
+    constexpr int U = NB == 1 ? 2 : 1;
+    const int rbs = (a.rows + 15) / 16;
+    if (rbs >= (NB == 1 ? 1024 : 512)) return launch_rows_u<T, NB, MV, GS, VX, NB == 4 && MV == 4 ? 2 : 4, U>(a, st);
+    if (rbs >= 512) return launch_rows_u<T, NB, MV, GS, VX, 2, U>(a, st);
+  }
+  launch_rows_u<T, NB, MV, GS, VX, 1, 1>(a, st);
 }
 
-template <typename T, int RB, int GS>
+template <typename T, int RB, int GS, bool VX>
 static void launch_tile(const Linear4Args& a, hipStream_t st) {
   const int tm = (int)((a.m + 63) / 64), tn = (a.rows + 64 * RB - 1) / (64 * RB), cbs = (a.cols + 127) / 128;
-  const int parts = std::is_same<T, float>::value ? 3 : 1;
-  const size_t lds = 2 * parts * 16384 + (std::is_same<T, bf16>::value ? (size_t)cbs * (4 / GS) * 256 : 0);
-  SN_LAUNCH((linear4_tile_kernel<T, RB, GS>), dim3((unsigned)(tm * tn)), dim3(256), lds, st, a, tm, tn);
+  constexpr bool F32 = std::is_same<T, float>::value, DMA = VX && !F32;
+  const size_t lds = (DMA ? kL4Stages : 2) * (F32 ? 3 : 1) * 16384 +
+                     (std::is_same<T, bf16>::value ? (size_t)cbs * (4 / GS) * 256 : 0);
+  SN_LAUNCH((linear4_tile_kernel<T, RB, GS, VX>), dim3((unsigned)(tm * tn)), dim3(256), lds, st, a, tm, tn);
 }
 
-template <typename T, int GS>
+template <typename T, int GS, bool VX>
 static void launch_linear4(const Linear4Args& a, hipStream_t st) {
   constexpr bool F32 = std::is_same<T, float>::value;
-  // the tile kernel keeps the sums of bf16 inputs in LDS: 64 KB less its stages
+  // the tile kernel keeps the sums of bf16 inputs in LDS, 256 bytes a run: with
+  // its stages at most 80 KB
   const bool fits = !std::is_same<T, bf16>::value || (int64_t)((a.cols + 127) / 128) * (4 / GS) <= 128;
   if (a.m > (F32 ? 16 : 64) && fits) {
-    if ((a.m + 63) / 64 * ((a.rows + 255) / 256) >= 256) launch_tile<T, 4, GS>(a, st);
-    else launch_tile<T, 1, GS>(a, st);
+    if ((a.m + 63) / 64 * ((a.rows + 255) / 256) >= 256) launch_tile<T, F32 ? 2 : 4, GS, VX>(a, st);
+    else launch_tile<T, 1, GS, VX>(a, st);
     return;
   }
   if constexpr (F32) {
-    if (a.m <= 4) launch_rows<T, 1, 1, GS>(a, st);
-    else if (a.m <= 8) launch_rows<T, 2, 1, GS>(a, st);
-    else launch_rows<T, 4, 1, GS>(a, st);
+    if (a.m <= 4) launch_rows<T, 1, 1, GS, VX>(a, st);
+    else if (a.m <= 8) launch_rows<T, 2, 1, GS, VX>(a, st);
+    else launch_rows<T, 4, 1, GS, VX>(a, st);
   } else {
-    if (a.m <= 4) launch_rows<T, 1, 1, GS>(a, st);
-    else if (a.m <= 16) launch_rows<T, 1, 4, GS>(a, st);
-    else if (a.m <= 32) launch_rows<T, 2, 4, GS>(a, st);
-    else launch_rows<T, 4, 4, GS>(a, st);
+    if (a.m <= 4) launch_rows<T, 1, 1, GS, VX>(a, st);
+    else if (a.m <= 16) launch_rows<T, 1, 4, GS, VX>(a, st);
+    else if (a.m <= 32) launch_rows<T, 2, 4, GS, VX>(a, st);
+    else launch_rows<T, 4, 4, GS, VX>(a, st);
   }
 }
 
@@ -499,12 +629,13 @@ void linear4(const Linear4Args& in, hipStream_t st) {
   Linear4Args a = in;
   check(a.m >= 1 && a.rows >= 1 && a.cols >= 1 && a.group >= 32 && a.group % 32 == 0 && a.m <= 65535 * 4, "4-bit product shapes");
   const int e = a.dtype == 0 ? 4 : 2;
-  a.vec_x = a.cols % 8 == 0 && al16(a.x) && al16(a.xs * e);
-#define SN_L4(T)                                         \
-  switch (linear4_gs(a.group)) {                         \
-    case 4: launch_linear4<T, 4>(a, st); break;          \
-    case 2: launch_linear4<T, 2>(a, st); break;          \
-    default: launch_linear4<T, 1>(a, st); break;         \
+  // wide loads of x: whole aligned chunks of 8, and 64 rows within a resource
+  const bool vx = a.cols % 8 == 0 && al16(a.x) && al16(a.xs * e) && (64 * a.xs + a.cols) * e < (int64_t)kOOB;
+#define SN_L4(T)                                                                                  \
+  switch (linear4_gs(a.group)) {                                                                  \
+    case 4: vx ? launch_linear4<T, 4, true>(a, st) : launch_linear4<T, 4, false>(a, st); break; \
+    case 2: vx ? launch_linear4<T, 2, true>(a, st) : launch_linear4<T, 2, false>(a, st); break; \
+    default: vx ? launch_linear4<T, 1, true>(a, st) : launch_linear4<T, 1, false>(a, st); break; \
   }
   if (a.dtype == 0) SN_L4(float)
   else if (a.dtype == 1) SN_L4(f16)

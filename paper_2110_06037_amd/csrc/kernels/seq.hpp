@@ -38,22 +38,20 @@ struct Linear4Args {
   int dtype, act;
   int64_t m;
   int rows, cols, group;
-  const unsigned* wq;  // codes, scales, zero points (or null) in the kernels' order (linear4_pack)
-  const f16* ws;
-  const uint8_t* wz;
+  const unsigned* wq;  // codes, and scales with zero points, in the kernels' order (linear4_pack)
+  const unsigned* ws;
   const float* bias;  // [rows] or null
   const void* x;
   int64_t xs;
   void* y;
   int64_t ys;
-  bool vec_x;  // wide loads of x (set by the launcher)
 };
 // Blocks of 16 features by 128 inputs: 256 dwords of codes each, and
-// 64 / linear4_gs scales (and zero points).
+// 64 / linear4_gs words of scale and zero point.
 int64_t linear4_blocks(int rows, int cols);
 int linear4_gs(int group);  // steps of 32 inputs that share a scale
 void linear4_pack(const uint8_t* q, const f16* scale, const uint8_t* zero, int rows, int cols, int group, unsigned* wq,
-                  f16* ws, uint8_t* wz, hipStream_t st);
+                  unsigned* ws, hipStream_t st);
 void linear4(const Linear4Args& a, hipStream_t st);
 
 // ------------------------------------------------------------------ selective scan

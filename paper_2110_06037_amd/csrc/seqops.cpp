@@ -270,11 +270,10 @@ int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint1
       const uint8_t* rz = raw.upload(zero, n);
       const int64_t blocks = k::linear4_blocks(d.rows, d.cols), scales = blocks * 64 / k::linear4_gs(d.group);
       unsigned* wq = static_cast<unsigned*>(op->alloc(blocks * 1024));
-      k::f16* ws = static_cast<k::f16*>(op->alloc(scales * 2));
-      uint8_t* wz = zero ? static_cast<uint8_t*>(op->alloc(scales)) : nullptr;
-      k::linear4_pack(rq, reinterpret_cast<const k::f16*>(rs), rz, d.rows, d.cols, d.group, wq, ws, wz, nullptr);
+      unsigned* ws = static_cast<unsigned*>(op->alloc(scales * 4));
+      k::linear4_pack(rq, reinterpret_cast<const k::f16*>(rs), rz, d.rows, d.cols, d.group, wq, ws, nullptr);
       HIPCHK(hipGetLastError());
-      a.wq = wq, a.ws = ws, a.wz = wz;
+      a.wq = wq, a.ws = ws;
       a.bias = op->upload(bias, d.rows);
       HIPCHK(hipDeviceSynchronize());
     }

@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
   constexpr bool DMA = VX && !F32;
   constexpr int RUNS = 4 / GS, PARTS = F32 ? 3 : 1;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  // [stage][part][row block][step][lane] of 16 bytes, then the sums
+  // [stage][part][row][slot] of 16 bytes, then the sums
   frag* xt = reinterpret_cast<frag*>(smem);
   constexpr int STAGE = PARTS * 4 * 4 * 64, STAGES = DMA ? kL4Stages : 2;
   float* xsum = reinterpret_cast<float*>(xt + STAGES * STAGE);  // [run][64]
@@ -371,13 +371,22 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
   int mt, nt;
   tile_of(blockIdx.x, tiles_m, tiles_n, mt, nt);
   const int64_t m0 = (int64_t)mt * 64, left = a.m - m0;
-  // the row of x that this lane loads (past the last: the last one's values, not stored)
-  const int mx = (int)min((int64_t)(16 * wave + col), left - 1);
+  // A stage of x in LDS: 64 rows of 16 slots of 8 inputs, chunk j of row m in
+  // slot j ^ (m % 16), so that both the loads (16 lanes to a row) and the
+  // operand reads (16 lanes to a column of chunks) meet all banks once.  This
+  // lane loads chunk (lane % 16) ^ (m % 16) of rows m = 16 wave + 4 i + lane / 16
+  // (past the last: the last one's values, not stored).
   const T* xb = static_cast<const T*>(a.x) + m0 * a.xs;
-  XRow<T, VX> xrow;
-  if constexpr (VX) xrow.rs = make_rsrc(xb, ((min(left, (int64_t)64) - 1) * a.xs + a.cols) * (int)sizeof(T));
-  xrow.row = xb + mx * a.xs;
-  xrow.off = VX ? (unsigned)(mx * a.xs) * (unsigned)sizeof(T) : 0u;
+  XRow<T, VX> xrow[4];
+  int xchunk[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = 4 * i + g, mx = (int)min((int64_t)(16 * wave + m), left - 1);
+    if constexpr (VX) xrow[i].rs = make_rsrc(xb, ((min(left, (int64_t)64) - 1) * a.xs + a.cols) * (int)sizeof(T));
+    xrow[i].row = xb + mx * a.xs;
+    xrow[i].off = VX ? (unsigned)(mx * a.xs) * (unsigned)sizeof(T) : 0u;
+    xchunk[i] = 8 * (col ^ m);
+  }
   const int rb0 = (nt * 4 + wave) * RB;
   // the wave's rows of blocks (past the last: the last one's, not stored)
   __amdgpu_buffer_rsrc_t rw[RB], rs[RB];
@@ -409,12 +418,12 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
   auto load_x = [&](int cb) {  // registers, or LDS stage cb % STAGES
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int c = cb * 128 + 32 * i + 8 * g;
+      const int c = cb * 128 + xchunk[i];
       if constexpr (DMA) {
-        const unsigned o = c < a.cols ? xrow.off + (unsigned)c * 2u : kOOB;
-        dma16(xrow.rs, reinterpret_cast<char*>(xt + (cb % STAGES) * STAGE + (wave * 4 + i) * 64), o, 0);
+        const unsigned o = c < a.cols ? xrow[i].off + (unsigned)c * 2u : kOOB;
+        dma16(xrow[i].rs, reinterpret_cast<char*>(xt + (cb % STAGES) * STAGE + (wave * 4 + i) * 64), o, 0);
       } else {
-        xn[i] = xrow.get(c, a.cols);
+        xn[i] = xrow[i].get(c, a.cols);
       }
     }
   };
@@ -432,8 +441,8 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
       }
   };
   auto multiply = [&](int cb, const W& w) {
-    const frag* xc = xt + (cb % STAGES) * STAGE + lane;
-    auto xfrag = [&](int p, int mi, int i) { return xc[((p * 4 + ((wave + mi) & 3)) * 4 + i) * 64]; };
+    const frag* xc = xt + (cb % STAGES) * STAGE + col * 16;
+    auto xfrag = [&](int p, int mi, int i) { return xc[(p * 4 + ((wave + mi) & 3)) * 256 + ((4 * i + g) ^ col)]; };
 #pragma unroll
     for (int run = 0; run < RUNS; ++run) {
       f32x4 acc[4][RB], xs = {0.f, 0.f, 0.f, 0.f};
@@ -518,18 +527,22 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
       }
     }
   }
+  // The results leave through LDS, as rows of 64 RB features: wide stores
+  // (straight from the accumulators they would be runs of 16 features, a third
+  // of the time at 2048 inputs).
+  constexpr int WIDE = 64 * RB, PITCH = WIDE + 16 / sizeof(T);
+  T* out = reinterpret_cast<T*>(smem);  // [row][feature], in place of the stages
+  wait_vmcnt<0>();
+  __syncthreads();  // nothing is on its way to the stages, and no one reads them
 #pragma unroll
   for (int r = 0; r < RB; ++r) {
     const int k = (rb0 + r) * 16 + col;
-    if (k >= a.rows) continue;
-    const float b = a.bias ? a.bias[k] : 0.f;
+    const float b = a.bias && k < a.rows ? a.bias[k] : 0.f;
 #pragma unroll
     for (int mi = 0; mi < 4; ++mi)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int m = 16 * ((wave + mi) & 3) + 4 * g + v;
-        if (m < left) static_cast<T*>(a.y)[(m0 + m) * a.ys + k] = from_f<T>(act4(tot[mi][r][v] + b, a.act));
-      }
+      for (int v = 0; v < 4; ++v)
+        out[(16 * ((wave + mi) & 3) + 4 * g + v) * PITCH + (wave * RB + r) * 16 + col] = from_f<T>(act4(tot[mi][r][v] + b, a.act));
   }
   if constexpr (BIASED) {
     // sums that are not finite (an infinity or a NaN of x, or beyond the range
@@ -555,7 +568,22 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
         const unsigned dw = a.wq[(b * 64 + col + 16 * (c % 32 / 8)) * 4 + c % 128 / 32];
         sum = fmaf(to_f(x[c]), ((float)(dw >> (4 * (c % 8 / 2) + 16 * (c & 1)) & 15) - rc.z) * rc.s, sum);
       }
-      static_cast<T*>(a.y)[(m0 + m) * a.ys + k] = from_f<T>(act4(sum + (a.bias ? a.bias[k] : 0.f), a.act));
+      out[m * PITCH + (wave * RB + r) * 16 + col] = from_f<T>(act4(sum + (a.bias ? a.bias[k] : 0.f), a.act));
+    }
+  }
+  __syncthreads();
+  const int k0 = nt * WIDE, rows = (int)min(left, (int64_t)64), wide = min(WIDE, a.rows - k0);
+  T* y = static_cast<T*>(a.y) + m0 * a.ys + k0;
+  if (a.vec_y) {
+    constexpr int PER16 = 16 / sizeof(T), CH = WIDE / PER16;
+    for (int i = threadIdx.x; i < rows * CH; i += 256) {
+      const int m = i / CH, c = i % CH * PER16;
+      if (c < wide) *reinterpret_cast<u32x4*>(y + m * a.ys + c) = *reinterpret_cast<const u32x4*>(out + m * PITCH + c);
+    }
+  } else {
+    for (int i = threadIdx.x; i < rows * WIDE; i += 256) {
+      const int m = i / WIDE, c = i % WIDE;
+      if (c < wide) y[m * a.ys + c] = out[m * PITCH + c];
     }
   }
 }
@@ -587,7 +615,7 @@ static void launch_rows(const Linear4Args& a, hipStream_t st) {
   if constexpr (VX) {
     constexpr int U = NB == 1 ? 2 : 1;
     const int rbs = (a.rows + 15) / 16;
-    if (rbs >= (NB == 1 ? 1024 : 512)) return launch_rows_u<T, NB, MV, GS, VX, NB == 4 && MV == 4 ? 2 : 4, U>(a, st);
+    if (rbs >= (NB == 1 ? 1024 : 512)) return launch_rows_u<T, NB, MV, GS, VX, 4, U>(a, st);
     if (rbs >= 512) return launch_rows_u<T, NB, MV, GS, VX, 2, U>(a, st);
   }
   launch_rows_u<T, NB, MV, GS, VX, 1, 1>(a, st);
@@ -608,8 +636,11 @@ static void launch_linear4(const Linear4Args& a, hipStream_t st) {
   // the tile kernel keeps the sums of bf16 inputs in LDS, 256 bytes a run: with
   // its stages at most 80 KB
   const bool fits = !std::is_same<T, bf16>::value || (int64_t)((a.cols + 127) / 128) * (4 / GS) <= 128;
-  if (a.m > (F32 ? 16 : 64) && fits) {
-    if ((a.m + 63) / 64 * ((a.rows + 255) / 256) >= 256) launch_tile<T, F32 ? 2 : 4, GS, VX>(a, st);
+  if (a.m > (F32 ? 16 : 32) && fits) {
+    // as wide as registers allow (more runs in a block, or parts, take more of
+    // them), if the tiles still fill the chip
+    constexpr int RB = F32 ? GS == 4 ? 2 : 1 : GS == 4 && VX ? 4 : GS == 1 && !VX ? 1 : 2;
+    if ((a.m + 63) / 64 * ((a.rows + 64 * RB - 1) / (64 * RB)) >= 256) launch_tile<T, RB, GS, VX>(a, st);
     else launch_tile<T, 1, GS, VX>(a, st);
     return;
   }
@@ -620,8 +651,7 @@ static void launch_linear4(const Linear4Args& a, hipStream_t st) {
   } else {
     if (a.m <= 4) launch_rows<T, 1, 1, GS, VX>(a, st);
     else if (a.m <= 16) launch_rows<T, 1, 4, GS, VX>(a, st);
-    else if (a.m <= 32) launch_rows<T, 2, 4, GS, VX>(a, st);
-    else launch_rows<T, 4, 4, GS, VX>(a, st);
+    else launch_rows<T, 2, 4, GS, VX>(a, st);
   }
 }
 
@@ -629,6 +659,7 @@ void linear4(const Linear4Args& in, hipStream_t st) {
   Linear4Args a = in;
   check(a.m >= 1 && a.rows >= 1 && a.cols >= 1 && a.group >= 32 && a.group % 32 == 0 && a.m <= 65535 * 4, "4-bit product shapes");
   const int e = a.dtype == 0 ? 4 : 2;
+  a.vec_y = a.rows % (16 / e) == 0 && al16(a.y) && al16(a.ys * e);
   // wide loads of x: whole aligned chunks of 8, and 64 rows within a resource
   const bool vx = a.cols % 8 == 0 && al16(a.x) && al16(a.xs * e) && (64 * a.xs + a.cols) * e < (int64_t)kOOB;
 #define SN_L4(T)                                                                                  \

@@ -45,6 +45,7 @@ struct Linear4Args {
   int64_t xs;
   void* y;
   int64_t ys;
+  bool vec_y;  // wide stores (set by the launcher)
 };
 // Blocks of 16 features by 128 inputs: 256 dwords of codes each, and
 // 64 / linear4_gs words of scale and zero point.

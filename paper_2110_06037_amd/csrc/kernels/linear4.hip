@@ -214,7 +214,8 @@ __global__ __launch_bounds__(512) void linear4_rows_kernel(Linear4Args a) {
   const int col = lane & 15, g = lane >> 4, xr = lane & 15;
   const int cbs = (a.cols + 127) / 128, rbs = (a.rows + 15) / 16;
   const int rb0 = blockIdx.x * R;
-  // loads outside a row of blocks give zero, and meet inputs of zero
+  // loads outside a row of blocks give zero, and meet inputs of zero (the whole
+  // offset in the operand that the range check compares)
   __amdgpu_buffer_rsrc_t rw[R], rs[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(512) void linear4_rows_kernel(Linear4Args a) {
 #pragma unroll
       for (int r = 0; r < R; ++r)  // read once: not kept in the caches for others
         w[u][r] = __builtin_bit_cast(
-            u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw[r], lane * 16, (c0 + u * waves) * 1024, 2));
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw[r], lane * 16 + (c0 + u * waves) * 1024, 0, 2));
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(512) void linear4_rows_kernel(Linear4Args a) {
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        ld_runs<RUNS>(rs[r], col * 4 * RUNS, (c0 + u * waves) * 64 * RUNS, sc[u][r]);
+        ld_runs<RUNS>(rs[r], col * 4 * RUNS + (c0 + u * waves) * 64 * RUNS, 0, sc[u][r]);
       }
     // all of the loads first (4096 x 16384, 4 rows of f16: 13.4 -> 10.2 us; left
     // to the compiler for bf16, where it hides them better by itself: 8.9

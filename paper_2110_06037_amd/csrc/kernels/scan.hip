@@ -23,6 +23,7 @@ namespace sn {
 namespace k {
 
 constexpr int Q = kScanChunk;
+constexpr int kScanDt = kScanDtRow;
 
 // ------------------------------------------------------------------ rows of a sequence
 // First row and length of sequence b; offsets are clamped to the call's rows,
@@ -68,21 +69,69 @@ __device__ __forceinline__ float taps4(const float (&w)[4], float bias, float r0
   return u;
 }
 
+// ------------------------------------------------------------------ operands in two halves
+// The matrix products run in f16 with float32 sums.  An operand is scaled by a
+// power of two that brings its tile's largest value below 2^14, and split in
+// hi = f16(v) and lo = f16(v - hi): 22 significant bits down to 2^-39 of the
+// tile's largest.  hi hi + hi lo + lo hi then has float32's precision (2^-23)
+// at a third of the f16 rate, five times that of the float32 instructions.
+__device__ __forceinline__ float pow2_for(float m) {  // 2^k with m 2^k in [2^13, 2^14), k at most 80
+  const int e = (__builtin_bit_cast(int, m) >> 23) & 255;
+  return __builtin_bit_cast(float, min(267 - e, 207) << 23);
+}
+__device__ __forceinline__ float inv_pow2(float s) {  // 1 / 2^k, exactly
+  return __builtin_bit_cast(float, (254 << 23) - __builtin_bit_cast(int, s));
+}
+struct HiLo {
+  f16x8 hi, lo;
+};
+__device__ __forceinline__ HiLo split8(const float (&v)[8]) {
+  HiLo r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    r.hi[i] = (f16)v[i];
+    r.lo[i] = (f16)(v[i] - (float)r.hi[i]);
+  }
+  return r;
+}
+__device__ __forceinline__ f32x4 mul3(const HiLo& a, const HiLo& b, f32x4 c) {
+  c = Mfma<f16>::run(a.lo, b.hi, c);
+  c = Mfma<f16>::run(a.hi, b.lo, c);
+  return Mfma<f16>::run(a.hi, b.hi, c);
+}
+// The larger of a running maximum and |v|, unless v is not finite.
+__device__ __forceinline__ float max_finite(float m, float v) {
+  v = fabsf(v);
+  return v < INFINITY ? fmaxf(m, v) : m;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
 // ------------------------------------------------------------------ what all heads share
-// grid (slots, groups + ceil(heads / 4) + 1).  The y index chooses: a group's
-// B, C and S; four heads' step sizes and running sums; the window's copy of
-// sequence x.
+// grid (slots, groups + ceil(heads / 16) + 1).  The y index chooses: a group's
+// B, C and S; 16 heads' step sizes and decays; the window's copy of sequence
+// x.  B and C go out as hi and lo in the order of the operands:
+//   ws_c [slot][group][tb][q][hi, lo][lane][8]: t = 16 tb + lane % 16
+//   ws_b [slot][group][nt][q][hi, lo][lane][8]: n = 16 nt + lane % 16
+// with the 8 values of step q at 32 q + 4 (lane / 16) + {0..3, 16..19} of n or
+// s: the order in which accumulator tiles hold rows.  S = C B^T in float32,
+//   ws_s [slot][group][tb][sb][lane][4]: t = 16 tb + lane % 16, s = 16 sb + 4 (lane / 16) + 0..3.
+constexpr int kPrep = 1024;
 template <typename T>
-__global__ __launch_bounds__(256) void scan_prep_kernel(ScanArgs a) {
-  const int part = blockIdx.y, hb = (a.heads + 3) / 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  const int part = blockIdx.y, hb = (a.heads + 15) / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (part == a.groups + hb) {
     const int b = blockIdx.x;
     const int64_t n = (int64_t)(a.conv - 1) * a.chans;
     if (b >= a.seqs) return;
     const T* src = static_cast<const T*>(a.window);
     T* dst = static_cast<T*>(a.wcopy) + b * n;
-    for (int64_t i = threadIdx.x; i < n; i += 256) dst[i] = src ? src[b * n + i] : from_f<T>(0.f);
+    for (int64_t i = threadIdx.x; i < n; i += kPrep) dst[i] = src ? src[b * n + i] : from_f<T>(0.f);
     return;
   }
   // the sequence of this slot: the last one whose first slot is not above it
@@ -100,7 +149,7 @@ __global__ __launch_bounds__(256) void scan_prep_kernel(ScanArgs a) {
   const int t0 = c * Q;
 
   if (part >= a.groups) {  // ---- a wave per head, a lane per token
-    const int h = (part - a.groups) * 4 + wave;
+    const int h = (part - a.groups) * 16 + wave;
     if (h >= a.heads) return;
     const int t = t0 + lane;
     float dt = 0.f, inc = 0.f;
@@ -116,19 +165,26 @@ __global__ __launch_bounds__(256) void scan_prep_kernel(ScanArgs a) {
       const float uh = __shfl_up(ch, d), ul = __shfl_up(cl, d);
       if (lane >= d) ch += uh, cl += ul;
     }
-    float* o = a.ws_dt + ((int64_t)slot * a.heads + h) * 3 * Q;
-    o[lane] = dt;
+    const float eh = __shfl(ch, 63), el = __shfl(cl, 63);
+    const float f = dt * __builtin_amdgcn_exp2f((eh - ch) + (el - cl));
+    float* o = a.ws_dt + ((int64_t)slot * a.heads + h) * kScanDt;
+    o[lane] = __builtin_amdgcn_exp2f(ch + cl);
     o[Q + lane] = ch;
     o[2 * Q + lane] = cl;
+    o[3 * Q + lane] = dt;
+    o[4 * Q + lane] = f;
+    const float dm = wave_max(max_finite(0.f, dt)), fm = wave_max(max_finite(0.f, f));
+    if (lane == 0) o[5 * Q] = eh + el, o[5 * Q + 1] = dm, o[5 * Q + 2] = fm;
     return;
   }
 
-  // ---- B and C of one group: convolution, then S = C B^T
-  const int N = a.state, NP = a.np;
-  float* C = a.ws_c + ((int64_t)slot * a.groups + part) * Q * NP;   // [t][n]
-  float* B = a.ws_b + ((int64_t)slot * a.groups + part) * Q * NP;   // [n][t]
-  float* S = a.ws_s + ((int64_t)slot * a.groups + part) * Q * Q;    // [t][s]
-  for (int i = threadIdx.x; i < 2 * NP * (Q / 4); i += 256) {
+  // ---- B and C of one group
+  const int N = a.state, NP = a.np, pitch = NP + 4;
+  float* Cs = lds;                // [t][n]
+  float* Bs = lds + Q * pitch;    // [t][n]
+  float* red = Bs + Q * pitch;    // [2][waves]
+  float mb = 0.f, mc = 0.f;
+  for (int i = threadIdx.x; i < 2 * NP * (Q / 4); i += kPrep) {
     const int e = i % (2 * NP), tq = i / (2 * NP) * 4;
     const bool isc = e >= NP;
     const int n = isc ? e - NP : e;
@@ -136,75 +192,101 @@ __global__ __launch_bounds__(256) void scan_prep_kernel(ScanArgs a) {
     if (n < N) {
       const int ch = a.heads * a.dim + (isc ? a.groups * N : 0) + part * N + n;
       float w[4], r[7];
+      const T* x = static_cast<const T*>(a.x) + s.first * a.xs + ch;
+#pragma unroll
+      for (int k = 0; k < 7; ++k) {
+        const int t = t0 + tq - 3 + k;
+        r[k] = to_f(x[min(max(t, 0), s.len - 1) * a.xs]);
+        if (t >= s.len) r[k] = 0.f;
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = a.conv_w[k * a.chans + ch];
+      if (t0 + tq == 0)
 #pragma unroll
-      for (int k = 0; k < 7; ++k) r[k] = raw_at<T>(a, s, b, t0 + tq - 3 + k, ch);
+        for (int k = 0; k < 3; ++k) r[k] = raw_at<T>(a, s, b, k - 3, ch);
 #pragma unroll
       for (int v = 0; v < 4; ++v)
-        if (t0 + tq + v < s.len) u[v] = silu_f(taps4(w, a.conv_b[ch], r[v], r[v + 1], r[v + 2], r[v + 3], a.conv));
+        if (t0 + tq + v < s.len) {
+          u[v] = silu_f(taps4(w, a.conv_b[ch], r[v], r[v + 1], r[v + 2], r[v + 3], a.conv));
+          if (isc) mc = max_finite(mc, u[v]);
+          else mb = max_finite(mb, u[v]);
+        }
     }
-    if (isc) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) C[(tq + v) * NP + n] = u[v];
-    } else {
-      *reinterpret_cast<f32x4*>(B + n * Q + tq) = f32x4{u[0], u[1], u[2], u[3]};
-    }
+    for (int v = 0; v < 4; ++v) (isc ? Cs : Bs)[(tq + v) * pitch + n] = u[v];
   }
+  mb = wave_max(mb), mc = wave_max(mc);
+  if (lane == 0) red[wave] = mb, red[kPrep / 64 + wave] = mc;
   __syncthreads();
-  const int col = lane & 15, g = lane >> 4, tb = wave;
-  for (int sb = 0; sb <= tb; ++sb) {
+  mb = wave_max(red[lane & 15]), mc = wave_max(red[16 + (lane & 15)]);
+  const float sb_ = pow2_for(mb), sc_ = pow2_for(mc);
+  const int64_t sg = (int64_t)slot * a.groups + part;
+  if (threadIdx.x == 0) a.ws_max[2 * sg] = mb, a.ws_max[2 * sg + 1] = mc;
+  const int col = lane & 15, g = lane >> 4;
+  f16* Cg = static_cast<f16*>(a.ws_c) + sg * Q * NP * 2;
+  f16* Bg = static_cast<f16*>(a.ws_b) + sg * Q * NP * 2;
+  const int NQ = NP / 32;
+  for (int f = wave; f < 4 * NQ + NP / 16 * 2; f += kPrep / 64) {
+    const bool isc = f < 4 * NQ;
+    float v[8];
+    if (isc) {
+      const int tb = f / NQ, q = f % NQ;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = sc_ * Cs[(16 * tb + col) * pitch + 32 * q + 4 * g + j + (j & 4) * 3];
+    } else {
+      const int nt = (f - 4 * NQ) >> 1, q = (f - 4 * NQ) & 1;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = sb_ * Bs[(32 * q + 4 * g + j + (j & 4) * 3) * pitch + 16 * nt + col];
+    }
+    const HiLo r = split8(v);
+    f16* o = (isc ? Cg + f * 1024 : Bg + (f - 4 * NQ) * 1024) + lane * 8;
+    *reinterpret_cast<f16x8*>(o) = r.hi;
+    *reinterpret_cast<f16x8*>(o + 512) = r.lo;
+  }
+  const int tb = wave >> 2, sb = wave & 3;
+  if (sb <= tb) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int n0 = 0; n0 < NP; n0 += 16) {
-      const f32x4 cf = *reinterpret_cast<const f32x4*>(C + (16 * tb + col) * NP + n0 + 4 * g);
+      const f32x4 bf = *reinterpret_cast<const f32x4*>(Bs + (16 * sb + col) * pitch + n0 + 4 * g);
+      const f32x4 cf = *reinterpret_cast<const f32x4*>(Cs + (16 * tb + col) * pitch + n0 + 4 * g);
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-        acc = Mfma<float>::run(cf[v], B[(n0 + 4 * g + v) * Q + 16 * sb + col], acc);
+      for (int v = 0; v < 4; ++v) acc = Mfma<float>::run(bf[v], cf[v], acc);  // rows s, columns t
     }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) S[(16 * tb + 4 * g + v) * Q + 16 * sb + col] = acc[v];
+    *reinterpret_cast<f32x4*>(a.ws_s + ((sg * 4 + tb) * 4 + sb) * 256 + lane * 4) = acc;
   }
 }
 
 // ------------------------------------------------------------------ the heads
-// A wave owns 16 PT columns p of one head and all N <= 16 NT state rows n: the
-// state lives in PT NT accumulator tiles (lane: n = 16 nt + 4 (lane / 16) + v,
-// p = p0 + PT (lane % 16) + j), whose layout is also that of the second
-// operand of the product with C, so the state never leaves the registers;
-// and a lane's convolution outputs (times 16 sb + 4 (lane / 16) + v, the
-// same p) are the second operand of both other products.  PT consecutive p
-// per lane make its row accesses vectors.
+// A wave owns 32 columns p of one head and all N <= 16 NT state rows n: the
+// state lives in 2 NT accumulator tiles (lane: n = 16 nt + 4 (lane / 16) + v,
+// p = p0 + 2 (lane % 16) + j), whose layout is also that of the second operand
+// of the product with C, so the state never leaves the registers; and a lane's
+// convolution outputs (times 16 sb + 4 (lane / 16) + v, the same p) are the
+// second operand of both other products.  Two neighbouring p per lane make
+// 4-byte row accesses; 32 columns leave registers for 2 waves per SIMD.
 // SEG: only the state that the segment adds (from zero), no outputs.
-template <typename T, int PT>
-__device__ __forceinline__ void ld_p(const T* p, int n, bool vec, float (&o)[PT]) {
-  if (vec && n >= PT) {
-    T v[PT];
-    __builtin_memcpy(v, __builtin_assume_aligned(p, sizeof(T) * PT), sizeof(T) * PT);
-#pragma unroll
-    for (int j = 0; j < PT; ++j) o[j] = to_f(v[j]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < PT; ++j) o[j] = j < n ? to_f(p[j]) : 0.f;
-  }
-}
-
-template <typename T, int NT, int PT, bool SEG>
-__global__ __launch_bounds__(256) void scan_main_kernel(ScanArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// VX: rows of x and y in whole aligned pairs.
+template <typename T, int NT, bool VX, bool SEG>
+__global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
+  constexpr int PT = 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
-  const int b = blockIdx.z, seg = blockIdx.y;
+  // segments and sequences vary fastest over the workgroups, so that (with 8 of
+  // them or a multiple) each XCD's L2 serves the chunks of its own segments
+  const int b = blockIdx.x / a.segs, seg = blockIdx.x % a.segs;
   const int each = a.heads / a.groups, pblocks = (a.dim + 16 * PT - 1) / (16 * PT);
   const int ublocks = (each * pblocks + 3) / 4;
-  const int grp = blockIdx.x / ublocks, unit = (blockIdx.x % ublocks) * 4 + wave;
+  const int grp = blockIdx.y / ublocks, unit = (blockIdx.y % ublocks) * 4 + wave;
   const Seq s = seq_of(a, b);
   const int nc = (s.len + Q - 1) / Q, per = (nc + a.segs - 1) / a.segs;
   const int c0 = min(seg * per, nc), c1 = min(c0 + per, nc);
-  const int NP = a.np, N = a.state;
+  const int N = a.state;
+  constexpr int NP = 16 * NT;
 
   if (!SEG && a.window_out) {
     // the window after the last row, shared out over the sequence's workgroups
     const int64_t n = (int64_t)(a.conv - 1) * a.chans;
-    const int blocks = gridDim.x * gridDim.y, me = blockIdx.y * gridDim.x + blockIdx.x;
+    const int blocks = a.segs * gridDim.y, me = blockIdx.y * a.segs + seg;
     T* out = static_cast<T*>(a.window_out) + b * n;
     for (int64_t i = (int64_t)me * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256) {
       const int k = (int)(i / a.chans), ch = (int)(i - (int64_t)k * a.chans), t = s.len - (a.conv - 1) + k;
@@ -214,8 +296,8 @@ __global__ __launch_bounds__(256) void scan_main_kernel(ScanArgs a) {
   }
   if (unit >= each * pblocks) return;
   const int h = grp * each + unit / pblocks;
-  const int p0 = (unit % pblocks) * 16 * PT + PT * col;  // this lane's first p
-  const int pn = a.dim - p0;                             // and how many of its PT exist (<= 0: none)
+  const int pb = (unit % pblocks) * 16 * PT, p0 = pb + PT * col;  // this lane's first p
+  const int pn = a.dim - p0;                                      // and how many of its PT exist (<= 0: none)
   const int64_t hold = (int64_t)a.dim * N;
 
   f32x4 st[NT][PT];
@@ -247,12 +329,27 @@ __global__ __launch_bounds__(256) void scan_main_kernel(ScanArgs a) {
         if (n + v < N) q[v] = r[v];
   };
   float* segst = a.ws_seg + (((int64_t)b * a.segs + seg) * a.heads + h) * hold;
+  // per column: at least the size of every value of the state (within a few
+  // powers of two).  Scales are a column's own, so no column's values have a
+  // part in another's.
+  float top[PT] = {};
+  auto col_max = [&](float v) {  // over the lanes of a column
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+  };
   if (SEG) {
     if (c1 >= nc) return;  // nothing follows: no one reads this segment's state
-  } else if (a.segs > 1) {
-    state_rw(static_cast<const float*>(segst), load);
-  } else if (a.state_in) {
-    state_rw(a.state_in + ((int64_t)b * a.heads + h) * hold, load);
+  } else {
+    if (a.segs > 1) state_rw(static_cast<const float*>(segst), load);
+    else if (a.state_in) state_rw(a.state_in + ((int64_t)b * a.heads + h) * hold, load);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < PT; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) top[j] = max_finite(top[j], st[nt][j][v]);
+#pragma unroll
+    for (int j = 0; j < PT; ++j) top[j] = col_max(top[j]);
   }
 
   // the lane's convolution
@@ -265,154 +362,283 @@ __global__ __launch_bounds__(256) void scan_main_kernel(ScanArgs a) {
     for (int k = 0; k < 4; ++k) w[k][j] = j < pn ? a.conv_w[k * a.chans + ch0 + j] : 0.f;
   }
   const float dh = a.d[h];
+  const unsigned rowb = (unsigned)a.xs * (unsigned)sizeof(T);
+  const unsigned xoff = 4 * g * rowb + (unsigned)(h * a.dim + p0) * (unsigned)sizeof(T);
   float total = 0.f;  // log2 of the segment's decay
   for (int c = c0; c < c1; ++c) {
     const int slot = slot0_of(s.first, b) + c, t0 = c * Q;
-    const float* Cm = a.ws_c + ((int64_t)slot * a.groups + grp) * Q * NP;
-    const float* Bm = a.ws_b + ((int64_t)slot * a.groups + grp) * Q * NP;
-    const float* Sm = a.ws_s + ((int64_t)slot * a.groups + grp) * Q * Q;
-    const float* dtp = a.ws_dt + ((int64_t)slot * a.heads + h) * 3 * Q;
-    // convolution outputs and Xd of the lane's 16 times
-    float u[4][PT][4], xd[4][PT][4];
-    float odd = 0.f;  // NaN if some Xd is not finite
+    const int64_t sg = (int64_t)slot * a.groups + grp;
+    const f16* Cg = static_cast<const f16*>(a.ws_c) + sg * Q * NP * 2 + lane * 8;
+    const f16* Bg = static_cast<const f16*>(a.ws_b) + sg * Q * NP * 2 + lane * 8;
+    const float* Sg = a.ws_s + sg * 16 * 256 + lane * 4;
+    const float* dtp = a.ws_dt + ((int64_t)slot * a.heads + h) * kScanDt;
+    const float maxb = a.ws_max[2 * sg], maxc = a.ws_max[2 * sg + 1];
+    const float cend = dtp[5 * Q], maxdt = dtp[5 * Q + 1], maxf = dtp[5 * Q + 2];
+    // Raw rows t0 + 16 sb + 4 g - 3 + k; loads past the end (or before the
+    // sequence) give zero.  They arrive while the state meets C.
+    T raw[4][7][PT];
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const T*>(a.x) + (s.first + t0 - 3) * a.xs,
+                                                (long long)min(s.len - t0 + 3, Q + 3) * rowb);
 #pragma unroll
-    for (int sb = 0; sb < 4; ++sb) {
-      float r[7][PT];
+    for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
       for (int k = 0; k < 7; ++k) {
-        const int t = t0 + 16 * sb + 4 * g - 3 + k;
-        if (t >= 0 && t < s.len) {
-          ld_p<T, PT>(static_cast<const T*>(a.x) + (s.first + t) * a.xs + ch0, pn, a.vec_x, r[k]);
-        } else if (t < 0 && a.conv - 1 + t >= 0) {
-          ld_p<T, PT>(static_cast<const T*>(a.wcopy) + ((int64_t)b * (a.conv - 1) + a.conv - 1 + t) * a.chans + ch0, pn,
-                      false, r[k]);
+        const bool before = sb == 0 && k < 3 && c == 0 && g == 0;
+        const unsigned row = xoff + (16 * sb + k) * rowb;  // in the offset that the range check sees
+        if constexpr (VX) {
+          const unsigned o = before || pn < PT ? kOOB : row;
+          if constexpr (sizeof(T) == 2) {
+            const unsigned v = __builtin_amdgcn_raw_buffer_load_b32(rx, (int)o, 0, 0);
+            __builtin_memcpy(raw[sb][k], &v, 4);
+          } else {
+            const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, (int)o, 0, 0));
+            __builtin_memcpy(raw[sb][k], &v, 8);
+          }
         } else {
 #pragma unroll
-          for (int j = 0; j < PT; ++j) r[k][j] = 0.f;
+          for (int j = 0; j < PT; ++j) {
+            const unsigned o = before || j >= pn ? kOOB : row + j * (unsigned)sizeof(T);
+            if constexpr (sizeof(T) == 2) {
+              const uint16_t v = __builtin_amdgcn_raw_buffer_load_b16(rx, (int)o, 0, 0);
+              __builtin_memcpy(&raw[sb][k][j], &v, 2);
+            } else {
+              const unsigned v = __builtin_amdgcn_raw_buffer_load_b32(rx, (int)o, 0, 0);
+              __builtin_memcpy(&raw[sb][k][j], &v, 4);
+            }
+          }
         }
       }
-      const f32x4 dt = *reinterpret_cast<const f32x4*>(dtp + 16 * sb + 4 * g);
+    __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
+    f32x4 acc[4][PT];
+    if constexpr (!SEG) {
+      // ---- C times the state in front of the chunk
+      float sh[PT];
+#pragma unroll
+      for (int j = 0; j < PT; ++j) sh[j] = pow2_for(top[j]);
+#pragma unroll
+      for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+        for (int j = 0; j < PT; ++j) acc[tb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int q = 0; q < NT / 2; ++q) {
+        HiLo hf[PT];
+#pragma unroll
+        for (int j = 0; j < PT; ++j) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = sh[j] * st[2 * q + (e >> 2)][j][e & 3];
+          hf[j] = split8(v);
+        }
+#pragma unroll
+        for (int tb = 0; tb < 4; ++tb) {
+          const f16* cp = Cg + (tb * (NT / 2) + q) * 1024;
+          HiLo cf;
+          cf.hi = *reinterpret_cast<const f16x8*>(cp);
+          cf.lo = *reinterpret_cast<const f16x8*>(cp + 512);
+#pragma unroll
+          for (int j = 0; j < PT; ++j) acc[tb][j] = mul3(cf, hf[j], acc[tb][j]);
+        }
+      }
+    }
+    // ---- convolution
+    __builtin_amdgcn_sched_barrier(0);
+    if (c == 0 && g == 0) {  // the window in front of the sequence
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const int i = a.conv - 4 + k;
+#pragma unroll
+        for (int j = 0; j < PT; ++j)
+          if (i >= 0 && j < pn)
+            raw[0][k][j] = static_cast<const T*>(a.wcopy)[((int64_t)b * (a.conv - 1) + i) * a.chans + ch0 + j];
+      }
+    }
+    float u[4][PT][4], sq[PT] = {}, maxu[PT], su[PT];
+#pragma unroll
+    for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
       for (int j = 0; j < PT; ++j) {
         const float wj[4] = {w[0][j], w[1][j], w[2][j], w[3][j]};
+        float r[7];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          u[sb][j][v] = silu_f(taps4(wj, cb[j], r[v][j], r[v + 1][j], r[v + 2][j], r[v + 3][j], a.conv));
-          const float x = t0 + 16 * sb + 4 * g + v < s.len ? u[sb][j][v] * dt[v] : 0.f;
-          xd[sb][j][v] = x;
-          odd = fmaf(x, 0.f, odd);
-        }
+        for (int k = 0; k < 7; ++k) r[k] = to_f(raw[sb][k][j]);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) u[sb][j][v] = silu_f(taps4(wj, cb[j], r[v], r[v + 1], r[v + 2], r[v + 3], a.conv));
       }
+    if (t0 + Q > s.len) {  // past the end: zero (a NaN would meet the zeros of earlier rows)
+#pragma unroll
+      for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+        for (int j = 0; j < PT; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (t0 + 16 * sb + 4 * g + v >= s.len) u[sb][j][v] = 0.f;
     }
+#pragma unroll
+    for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+      for (int j = 0; j < PT; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sq[j] = fmaf(u[sb][j][v], u[sb][j][v], sq[j]);
+    // A column's largest value from its sum of squares: at most 2^3 too much.
     // A value that is not finite must not meet the zeros of earlier rows (0 *
     // NaN): it leaves the products, and its column is NaN from its row on.
     int from[PT];
+    bool poison = false;
 #pragma unroll
-    for (int j = 0; j < PT; ++j) from[j] = Q;
-    const bool poison = __any(odd != 0.f);
-    if (poison) {
-#pragma unroll
-      for (int j = 0; j < PT; ++j) {
+    for (int j = 0; j < PT; ++j) {
+      sq[j] += __shfl_xor(sq[j], 16);
+      sq[j] += __shfl_xor(sq[j], 32);
+      maxu[j] = sqrtf(sq[j]);
+      from[j] = Q;
+      if (__any(!(sq[j] < INFINITY))) {  // or a value beyond 2^63
+        float m = 0.f;
 #pragma unroll
         for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
-          for (int v = 0; v < 4; ++v)
-            if (!(fabsf(xd[sb][j][v]) < INFINITY)) {
-              xd[sb][j][v] = 0.f;
+          for (int v = 0; v < 4; ++v) {
+            m = max_finite(m, u[sb][j][v]);
+            if (!(fabsf(u[sb][j][v]) < INFINITY)) {
+              u[sb][j][v] = 0.f;
               from[j] = min(from[j], 16 * sb + 4 * g + v);
             }
+          }
         from[j] = min(from[j], __shfl_xor(from[j], 16));
         from[j] = min(from[j], __shfl_xor(from[j], 32));
+        poison = poison || __any(from[j] < Q);
+        m = col_max(m);
+        if (!(sq[j] < INFINITY)) maxu[j] = 8.f * m;
       }
+      su[j] = pow2_for(maxu[j]);
     }
-    const float eh = dtp[2 * Q - 1], el = dtp[3 * Q - 1];  // c at the chunk's end
+    __builtin_amdgcn_sched_barrier(0);
     if constexpr (!SEG) {
+      // ---- earlier rows of the chunk, the row itself and the skip term
+      const float maxw = fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)), sw = pow2_for(maxw);
+      // from C h's scale to this product's, with the decay since the chunk's start
+      float to[PT];
+#pragma unroll
+      for (int j = 0; j < PT; ++j) to[j] = inv_pow2(pow2_for(maxc)) * inv_pow2(pow2_for(top[j])) * sw * su[j];
 #pragma unroll
       for (int tb = 0; tb < 4; ++tb) {
-        f32x4 acc[PT];
+        const f32x4 e = *reinterpret_cast<const f32x4*>(dtp + 16 * tb + 4 * g);
 #pragma unroll
-        for (int j = 0; j < PT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int v = 0; v < 4; ++v)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const f32x4 cf = *reinterpret_cast<const f32x4*>(Cm + (16 * tb + col) * NP + 16 * nt + 4 * g);
+          for (int j = 0; j < PT; ++j) acc[tb][j][v] *= e[v] * to[j];
+      }
 #pragma unroll
-          for (int v = 0; v < 4; ++v)
+      for (int q = 0; q < 2; ++q) {
+        HiLo uf[PT];
 #pragma unroll
-            for (int j = 0; j < PT; ++j) acc[j] = Mfma<float>::run(cf[v], st[nt][j][v], acc[j]);
+        for (int j = 0; j < PT; ++j) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = su[j] * u[2 * q + (i >> 2)][j][i & 3];
+          uf[j] = split8(v);
         }
-        const f32x4 rh = *reinterpret_cast<const f32x4*>(dtp + Q + 16 * tb + 4 * g);
-        const f32x4 rl = *reinterpret_cast<const f32x4*>(dtp + 2 * Q + 16 * tb + 4 * g);
+        f32x4 sh_[2], sl_[2], sd_[2];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const float e = __builtin_amdgcn_exp2f(rh[v] + rl[v]);
-#pragma unroll
-          for (int j = 0; j < PT; ++j) acc[j][v] *= e;
+        for (int i = 0; i < 2; ++i) {
+          const int at = 32 * q + 16 * i + 4 * g;
+          sh_[i] = *reinterpret_cast<const f32x4*>(dtp + Q + at);
+          sl_[i] = *reinterpret_cast<const f32x4*>(dtp + 2 * Q + at);
+          sd_[i] = *reinterpret_cast<const f32x4*>(dtp + 3 * Q + at) * sw;
         }
-        const int tr = 16 * tb + col;  // the row of the first operand that this lane holds
-        const float th = dtp[Q + tr], tl = dtp[2 * Q + tr];
 #pragma unroll
-        for (int sb = 0; sb <= tb; ++sb) {
-          const f32x4 sv = *reinterpret_cast<const f32x4*>(Sm + tr * Q + 16 * sb + 4 * g);
-          const f32x4 sh = *reinterpret_cast<const f32x4*>(dtp + Q + 16 * sb + 4 * g);
-          const f32x4 sl = *reinterpret_cast<const f32x4*>(dtp + 2 * Q + 16 * sb + 4 * g);
+        for (int tb = 2 * q; tb < 4; ++tb) {
+          const float th = dtp[Q + 16 * tb + col], tl = dtp[2 * Q + 16 * tb + col];
+          float m[8];
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float m =
-                16 * sb + 4 * g + v <= tr ? sv[v] * __builtin_amdgcn_exp2f((th - sh[v]) + (tl - sl[v])) : 0.f;
+          for (int i = 0; i < 2; ++i) {
+            const int sb = 2 * q + i;
+            if (sb > tb) {
 #pragma unroll
-            for (int j = 0; j < PT; ++j) acc[j] = Mfma<float>::run(m, xd[sb][j][v], acc[j]);
+              for (int v = 0; v < 4; ++v) m[4 * i + v] = 0.f;
+              continue;
+            }
+            const f32x4 sv = *reinterpret_cast<const f32x4*>(Sg + (tb * 4 + sb) * 256);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              float x = sv[v] * sd_[i][v] * __builtin_amdgcn_exp2f((th - sh_[i][v]) + (tl - sl_[i][v]));
+              if (sb == tb) {
+                if (4 * g + v == col) x = fmaf(dh, sw, x);
+                if (4 * g + v > col) x = 0.f;
+              }
+              m[4 * i + v] = x;
+            }
           }
+          const HiLo mf = split8(m);
+#pragma unroll
+          for (int j = 0; j < PT; ++j) acc[tb][j] = mul3(mf, uf[j], acc[tb][j]);
         }
+      }
+      float back[PT];
+#pragma unroll
+      for (int j = 0; j < PT; ++j) back[j] = inv_pow2(sw) * inv_pow2(su[j]);
+      T* y = static_cast<T*>(a.y) + (s.first + t0) * a.ys + ch0;
+#pragma unroll
+      for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const int t = 16 * tb + 4 * g + v;
           T o[PT];
 #pragma unroll
-          for (int j = 0; j < PT; ++j) {
-            float y = fmaf(dh, u[tb][j][v], acc[j][v]);
-            if (t >= from[j]) y = NAN;
-            o[j] = from_f<T>(y);
-          }
+          for (int j = 0; j < PT; ++j) o[j] = from_f<T>(t >= from[j] ? NAN : acc[tb][j][v] * back[j]);
           if (t0 + t < s.len) {
-            T* yp = static_cast<T*>(a.y) + (s.first + t0 + t) * a.ys + ch0;
-            if (a.vec_y && pn >= PT) {
-              __builtin_memcpy(__builtin_assume_aligned(yp, sizeof(T) * PT), o, sizeof(T) * PT);
+            if constexpr (VX) {
+              if (pn > 0) __builtin_memcpy(__builtin_assume_aligned(y + t * a.ys, sizeof(T) * PT), o, sizeof(T) * PT);
             } else {
 #pragma unroll
               for (int j = 0; j < PT; ++j)
-                if (j < pn) yp[j] = o[j];
+                if (j < pn) y[t * a.ys + j] = o[j];
             }
           }
         }
-      }
     }
-    // the state after the chunk
-    const float e = __builtin_amdgcn_exp2f(eh + el);
-    total += eh + el;
+    // ---- the state after the chunk
+    __builtin_amdgcn_sched_barrier(0);
+    const float sf = pow2_for(maxf), e = __builtin_amdgcn_exp2f(cend);
+    HiLo xf[2][PT];
 #pragma unroll
-    for (int sb = 0; sb < 4; ++sb) {
-      const f32x4 sh = *reinterpret_cast<const f32x4*>(dtp + Q + 16 * sb + 4 * g);
-      const f32x4 sl = *reinterpret_cast<const f32x4*>(dtp + 2 * Q + 16 * sb + 4 * g);
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const float f = __builtin_amdgcn_exp2f((eh - sh[v]) + (el - sl[v]));
+      for (int j = 0; j < PT; ++j) {
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < PT; ++j) xd[sb][j][v] *= f;
+        for (int i = 0; i < 2; ++i) {
+          const f32x4 f = *reinterpret_cast<const f32x4*>(dtp + 4 * Q + 32 * q + 16 * i + 4 * g);
+          // below 2^14 each: their product back to f16's range
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[4 * i + k] = (su[j] * u[2 * q + i][j][k]) * (f[k] * sf * 0x1p-14f);
+        }
+        xf[q][j] = split8(v);
       }
-    }
+    float back[PT];
+#pragma unroll
+    for (int j = 0; j < PT; ++j) back[j] = inv_pow2(pow2_for(maxb)) * inv_pow2(su[j]) * inv_pow2(sf) * 0x1p14f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      f32x4 add[PT];
 #pragma unroll
-      for (int j = 0; j < PT; ++j) st[nt][j] *= e;
+      for (int j = 0; j < PT; ++j) add[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int sb = 0; sb < 4; ++sb) {
-        const f32x4 bf = *reinterpret_cast<const f32x4*>(Bm + (16 * nt + col) * Q + 16 * sb + 4 * g);
+      for (int q = 0; q < 2; ++q) {
+        const f16* bp = Bg + (nt * 2 + q) * 1024;
+        HiLo bf;
+        bf.hi = *reinterpret_cast<const f16x8*>(bp);
+        bf.lo = *reinterpret_cast<const f16x8*>(bp + 512);
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int j = 0; j < PT; ++j) st[nt][j] = Mfma<float>::run(bf[v], xd[sb][j][v], st[nt][j]);
+        for (int j = 0; j < PT; ++j) add[j] = mul3(bf, xf[q][j], add[j]);
       }
+#pragma unroll
+      for (int j = 0; j < PT; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) st[nt][j][v] = fmaf(add[j][v], back[j], st[nt][j][v] * e);
     }
+    total += cend;
+    // |sum_s B u f| <= max B max f sum_s |u_s|, and that sum at most 8 times the root of the squares
+#pragma unroll
+    for (int j = 0; j < PT; ++j) top[j] = fmaf(top[j], e, 8.f * maxb * maxf * maxu[j]);
     if (poison) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -566,33 +792,38 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int L, int s
 }
 
 // ------------------------------------------------------------------ launchers
-template <typename T, int NT, int PT>
+template <typename T, int NT, bool VX>
 static void launch_main(const ScanArgs& a, hipStream_t st) {
-  const int each = a.heads / a.groups, pblocks = (a.dim + 16 * PT - 1) / (16 * PT);
-  const dim3 grid(a.groups * ((each * pblocks + 3) / 4), a.segs, a.seqs);
+  const int each = a.heads / a.groups, pblocks = (a.dim + 31) / 32;
+  const dim3 grid(a.segs * a.seqs, a.groups * ((each * pblocks + 3) / 4));
   if (a.segs > 1) {
-    SN_LAUNCH((scan_main_kernel<T, NT, PT, true>), grid, dim3(256), 0, st, a);
+    SN_LAUNCH((scan_main_kernel<T, NT, VX, true>), grid, dim3(256), 0, st, a);
     SN_LAUNCH((scan_carry_kernel), dim3((a.dim * a.state + 255) / 256, a.heads, a.seqs), dim3(256), 0, st, a);
   }
-  SN_LAUNCH((scan_main_kernel<T, NT, PT, false>), grid, dim3(256), 0, st, a);
+  SN_LAUNCH((scan_main_kernel<T, NT, VX, false>), grid, dim3(256), 0, st, a);
+}
+template <typename T, bool VX>
+static void launch_nt(const ScanArgs& a, hipStream_t st) {
+  if (a.np <= 32) launch_main<T, 2, VX>(a, st);
+  else if (a.np <= 64) launch_main<T, 4, VX>(a, st);
+  else if (a.np <= 128) launch_main<T, 8, VX>(a, st);
+  else launch_main<T, 16, VX>(a, st);
 }
 
 template <typename T>
 static void launch_scan(ScanArgs a, hipStream_t st) {
-  constexpr int PT = 4;
   a.vec_state = a.state % 4 == 0 && al16(a.state_in) && al16(a.state_out) && al16(a.ws_seg);
-  // a lane's PT values of a row go as one vector: rows and heads on its alignment
-  const int64_t v = sizeof(T) * PT;
+  // a lane's two values of a row as one access: rows and heads on its alignment
+  const int64_t v = sizeof(T) * 2;
   auto ok = [&](const void* p, int64_t stride) {
-    return reinterpret_cast<uintptr_t>(p) % v == 0 && stride * sizeof(T) % v == 0 && a.dim % PT == 0;
+    return reinterpret_cast<uintptr_t>(p) % v == 0 && stride * (int64_t)sizeof(T) % v == 0;
   };
-  a.vec_x = ok(a.x, a.xs), a.vec_y = ok(a.y, a.ys);
+  const bool vx = a.dim % 2 == 0 && ok(a.x, a.xs) && ok(a.y, a.ys);
   const int64_t slots = scan_slots(a.tokens, a.seqs);
-  SN_LAUNCH((scan_prep_kernel<T>), dim3((unsigned)slots, a.groups + (a.heads + 3) / 4 + 1), dim3(256), 0, st, a);
-  if (a.np <= 32) launch_main<T, 2, PT>(a, st);
-  else if (a.np <= 64) launch_main<T, 4, PT>(a, st);
-  else if (a.np <= 128) launch_main<T, 8, PT>(a, st);
-  else launch_main<T, 16, PT>(a, st);
+  const size_t lds = (2 * Q * (a.np + 4) + 2 * kPrep / 64) * sizeof(float);
+  SN_LAUNCH((scan_prep_kernel<T>), dim3((unsigned)slots, a.groups + (a.heads + 15) / 16 + 1), dim3(kPrep), lds, st, a);
+  if (vx) launch_nt<T, true>(a, st);
+  else launch_nt<T, false>(a, st);
 }
 
 template <typename T>
@@ -605,9 +836,9 @@ static void launch_step(ScanArgs a, hipStream_t st) {
 }
 
 static int scan_segments(const ScanArgs& a) {
-  // waves of a pass: units of 64 columns per head and sequence; segments until
-  // about 1024 of them (one per SIMD) run, each at least two chunks
-  const int64_t units = (int64_t)a.seqs * a.heads * ((a.dim + 63) / 64);
+  // waves of a pass: units of 32 columns per head and sequence; segments until
+  // about kScanUnits of them (two per SIMD) run, each at least two chunks
+  const int64_t units = (int64_t)a.seqs * a.heads * ((a.dim + 31) / 32);
   const int64_t chunks = (a.tokens + Q - 1) / Q;  // the most that one sequence may have
   const int64_t want = std::min<int64_t>((kScanUnits + units - 1) / units, chunks / 2);
   return (int)std::max<int64_t>(1, want);

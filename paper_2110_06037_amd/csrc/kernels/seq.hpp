@@ -57,7 +57,8 @@ void linear4(const Linear4Args& a, hipStream_t st);
 
 // ------------------------------------------------------------------ selective scan
 constexpr int kScanChunk = 64;     // tokens per chunk
-constexpr int kScanUnits = 1024;   // waves that a pass is cut into segments for
+constexpr int kScanUnits = 2048;   // waves that a pass is cut into segments for
+constexpr int kScanDtRow = 5 * kScanChunk + 16;  // floats per head and chunk of ws_dt
 struct ScanArgs {
   int dtype, heads, dim, groups, state, conv, chans;  // dim: of a head
   int np;  // state columns that the workspace's rows hold (scan_np)
@@ -68,10 +69,13 @@ struct ScanArgs {
   const float* d;       // [heads]
   const float* dt_bias;
   // workspace
-  float* ws_c;     // [slot][group][t][np]      C of a chunk
-  float* ws_b;     // [slot][group][np][t]      B of a chunk
-  float* ws_s;     // [slot][group][t][s]       C B^T, s in blocks not above t's
-  float* ws_dt;    // [slot][head][3][t]        step size, running sum of log2 decays (hi, lo)
+  void* ws_c;      // [slot][group] C of a chunk, 2 x 64 np f16 (scan_prep_kernel)
+  void* ws_b;      // [slot][group] B of a chunk, likewise
+  float* ws_s;     // [slot][group] C B^T, 64 x 64
+  float* ws_max;   // [slot][group][2] largest sizes in B and C
+  float* ws_dt;    // [slot][head][kScanDtRow]: 64 each of the decay since the chunk's start, its log2 as
+                   // hi and lo, the step size, the step size times the decay to the chunk's end; then
+                   // the chunk's log2 decay and the largest of the step sizes and of the last array
   float* ws_seg;   // [seq][segment][head][dim][state]
   float* ws_decay; // [seq][segment][head]
   void* wcopy;     // [seq][conv - 1][chans]    the window before the call
@@ -91,7 +95,7 @@ struct ScanArgs {
   int64_t ys;
   void* window_out;
   float* state_out;
-  bool vec_x, vec_y, vec_state;  // wide accesses (set by the launcher)
+  bool vec_state;  // wide accesses of the state (set by the launcher)
 };
 inline int scan_np(int state) { return state <= 32 ? 32 : state <= 64 ? 64 : state <= 128 ? 128 : 256; }
 inline int64_t scan_slots(int64_t tokens, int seqs) { return tokens / kScanChunk + seqs + 1; }

@@ -144,6 +144,8 @@ k::ScanArgs scan_args(const ScanOp& op, const sn_scan_io* io, bool step) {
   if (io->seqs && !io->offsets && io->tokens % io->seqs)
     fail(SN_E_SHAPE, "tokens are no multiple of seqs, and there are no offsets");
   check_rows(io->x, io->x_stride, io->tokens, a.chans, a.dtype, "x");
+  // 67 rows of x are addressed with 32-bit offsets
+  if (io->x_stride * e * 68 >= (int64_t(1) << 31)) fail(SN_E_UNSUPPORTED, "x: row stride above 2^31 / 68 bytes");
   check_rows(io->dt, io->dt_stride, io->tokens, a.heads, a.dtype, "dt");
   check_rows(io->y, io->y_stride, io->tokens, (int64_t)a.heads * a.dim, a.dtype, "y");
   for (const void* p : {io->window, (const void*)io->window_out})
@@ -339,14 +341,15 @@ int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* c
       a.dt_bias = op->upload(dt_bias ? dt_bias : zeros.data(), d.heads);
       const int64_t slots = k::scan_slots(d.max_tokens, d.max_seqs), Q = k::kScanChunk;
       auto floats = [&](int64_t n) { return static_cast<float*>(op->alloc(n * 4)); };
-      a.ws_c = floats(slots * d.groups * Q * a.np);
-      a.ws_b = floats(slots * d.groups * Q * a.np);
+      a.ws_c = op->alloc(slots * d.groups * Q * a.np * 4);
+      a.ws_b = op->alloc(slots * d.groups * Q * a.np * 4);
       a.ws_s = floats(slots * d.groups * Q * Q);
-      a.ws_dt = floats(slots * d.heads * 3 * Q);
-      // segments are made for fewer than kScanUnits units of at most 64
+      a.ws_max = floats(slots * d.groups * 2);
+      a.ws_dt = floats(slots * d.heads * k::kScanDtRow);
+      // segments are made for fewer than kScanUnits units of at most 32
       // columns, of at least two chunks each
       const int64_t pairs = std::max<int64_t>(1, (d.max_tokens + Q - 1) / Q / 2);
-      a.seg_cap = std::min(int64_t(2) * k::kScanUnits * 64 * d.state,
+      a.seg_cap = std::min(int64_t(2) * k::kScanUnits * 32 * d.state,
                            d.max_seqs * pairs * d.heads * d.head_dim * d.state);
       a.ws_seg = floats(a.seg_cap);
       a.ws_decay = floats(2 * k::kScanUnits);

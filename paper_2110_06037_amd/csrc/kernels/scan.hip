@@ -377,6 +377,8 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
     // Raw rows t0 + 16 sb + 4 g - 3 + k; loads past the end (or before the
     // sequence) give zero.  They arrive while the state meets C.
     T raw[4][7][PT];
+    unsigned xo = xoff;  // per chunk: kept out of the loop, its 28 sums would fill the registers
+    asm volatile("" : "+v"(xo));
     const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const T*>(a.x) + (s.first + t0 - 3) * a.xs,
                                                 (long long)min(s.len - t0 + 3, Q + 3) * rowb);
 #pragma unroll
@@ -384,7 +386,7 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
 #pragma unroll
       for (int k = 0; k < 7; ++k) {
         const bool before = sb == 0 && k < 3 && c == 0 && g == 0;
-        const unsigned row = xoff + (16 * sb + k) * rowb;  // in the offset that the range check sees
+        const unsigned row = xo + (16 * sb + k) * rowb;  // in the offset that the range check sees
         if constexpr (VX) {
           const unsigned o = before || pn < PT ? kOOB : row;
           if constexpr (sizeof(T) == 2) {
@@ -575,7 +577,12 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
       float back[PT];
 #pragma unroll
       for (int j = 0; j < PT; ++j) back[j] = inv_pow2(sw) * inv_pow2(su[j]);
-      T* y = static_cast<T*>(a.y) + (s.first + t0) * a.ys + ch0;
+      // stores past the last row (or column) are outside the range, and dropped
+      const unsigned yrow = (unsigned)a.ys * (unsigned)sizeof(T);
+      const __amdgpu_buffer_rsrc_t ry =
+          make_rsrc(static_cast<T*>(a.y) + (s.first + t0) * a.ys, (long long)min(s.len - t0, Q) * yrow);
+      unsigned yo = 4 * g * yrow + (unsigned)ch0 * (unsigned)sizeof(T);
+      asm volatile("" : "+v"(yo));
 #pragma unroll
       for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
@@ -584,13 +591,19 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
           T o[PT];
 #pragma unroll
           for (int j = 0; j < PT; ++j) o[j] = from_f<T>(t >= from[j] ? NAN : acc[tb][j][v] * back[j]);
-          if (t0 + t < s.len) {
-            if constexpr (VX) {
-              if (pn > 0) __builtin_memcpy(__builtin_assume_aligned(y + t * a.ys, sizeof(T) * PT), o, sizeof(T) * PT);
+          const unsigned off = yo + (16 * tb + v) * yrow;
+          if constexpr (VX) {
+            if constexpr (sizeof(T) == 2) {
+              __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o), ry, (int)(pn > 0 ? off : kOOB), 0, 0);
             } else {
+              __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, o), ry, (int)(pn > 0 ? off : kOOB), 0, 0);
+            }
+          } else {
 #pragma unroll
-              for (int j = 0; j < PT; ++j)
-                if (j < pn) y[t * a.ys + j] = o[j];
+            for (int j = 0; j < PT; ++j) {
+              const int to_ = (int)(j < pn ? off + j * (unsigned)sizeof(T) : kOOB);
+              if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, o[j]), ry, to_, 0, 0);
+              else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o[j]), ry, to_, 0, 0);
             }
           }
         }

@@ -144,8 +144,9 @@ k::ScanArgs scan_args(const ScanOp& op, const sn_scan_io* io, bool step) {
   if (io->seqs && !io->offsets && io->tokens % io->seqs)
     fail(SN_E_SHAPE, "tokens are no multiple of seqs, and there are no offsets");
   check_rows(io->x, io->x_stride, io->tokens, a.chans, a.dtype, "x");
-  // 67 rows of x are addressed with 32-bit offsets
-  if (io->x_stride * e * 68 >= (int64_t(1) << 31)) fail(SN_E_UNSUPPORTED, "x: row stride above 2^31 / 68 bytes");
+  // 67 rows of x and 64 of y are addressed with 32-bit offsets
+  if (std::max(io->x_stride, io->y_stride) * e * 68 >= (int64_t(1) << 31))
+    fail(SN_E_UNSUPPORTED, "row stride above 2^31 / 68 bytes");
   check_rows(io->dt, io->dt_stride, io->tokens, a.heads, a.dtype, "dt");
   check_rows(io->y, io->y_stride, io->tokens, (int64_t)a.heads * a.dim, a.dtype, "y");
   for (const void* p : {io->window, (const void*)io->window_out})

@@ -33,7 +33,7 @@ struct Seq {
   int len;
 };
 __device__ __forceinline__ int64_t seq_start(const ScanArgs& a, int b) {
-  if (!a.offsets) return (int64_t)b * (a.tokens / a.seqs);
+  if (!a.offsets) return (int64_t)b * a.each;
   const int64_t o = a.offsets[b];
   return o < 0 ? 0 : o > a.tokens ? a.tokens : o;
 }
@@ -118,7 +118,7 @@ __device__ __forceinline__ float wave_max(float v) {
 //   ws_b [slot][group][nt][q][hi, lo][lane][8]: n = 16 nt + lane % 16
 // with the 8 values of step q at 32 q + 4 (lane / 16) + {0..3, 16..19} of n or
 // s: the order in which accumulator tiles hold rows.  S = C B^T in float32,
-//   ws_s [slot][group][tb][sb][lane][4]: t = 16 tb + lane % 16, s = 16 sb + 4 (lane / 16) + 0..3.
+//   ws_s [slot][group][tb][sb <= tb][lane][4]: t = 16 tb + lane % 16, s = 16 sb + 4 (lane / 16) + 0..3.
 constexpr int kPrep = 1024;
 template <typename T>
 __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) acc = Mfma<float>::run(bf[v], cf[v], acc);  // rows s, columns t
     }
-    *reinterpret_cast<f32x4*>(a.ws_s + ((sg * 4 + tb) * 4 + sb) * 256 + lane * 4) = acc;
+    *reinterpret_cast<f32x4*>(a.ws_s + sg * kScanS + (tb * (tb + 1) / 2 + sb) * 256 + lane * 4) = acc;
   }
 }
 
@@ -266,17 +266,37 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // 4-byte row accesses; 32 columns leave registers for 2 waves per SIMD.
 // SEG: only the state that the segment adds (from zero), no outputs.
 // VX: rows of x and y in whole aligned pairs.
+//
+// The waves of a workgroup share the group's C, B and S of a chunk in LDS, and
+// each has its head's decays there, all brought by LDS direct loads while the
+// chunk before (C, decays) or the product with C (B, S) is computed: two
+// barriers per chunk, behind which one set has arrived and the other is free.
+constexpr int kScanWaves = 8;
+constexpr int kDtBytes = 5 * Q * 4;
+template <int NT, bool SEG>
+constexpr int scan_lds(int waves) {  // C, B, S, two decay rows per wave
+  return (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + waves * 2 * kDtBytes;
+}
 template <typename T, int NT, bool VX, bool SEG>
-__global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
+__global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) {
   constexpr int PT = 2;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  char* const ldsB = smem;
+  char* const ldsC = smem + 4096 * NT;                    // not with SEG
+  char* const ldsS = smem + 8192 * NT;                    // not with SEG
+  const int waves = blockDim.x >> 6;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   // segments and sequences vary fastest over the workgroups, so that (with 8 of
   // them or a multiple) each XCD's L2 serves the chunks of its own segments
   const int b = blockIdx.x / a.segs, seg = blockIdx.x % a.segs;
   const int each = a.heads / a.groups, pblocks = (a.dim + 16 * PT - 1) / (16 * PT);
-  const int ublocks = (each * pblocks + 3) / 4;
-  const int grp = blockIdx.y / ublocks, unit = (blockIdx.y % ublocks) * 4 + wave;
+  const int ublocks = (each * pblocks + waves - 1) / waves;
+  const int grp = blockIdx.y / ublocks, unit_ = (blockIdx.y % ublocks) * waves + wave;
+  // a wave beyond the last unit works on the last one, for the barriers' sake, and stores nothing
+  const bool live = unit_ < each * pblocks;
+  const int unit = min(unit_, each * pblocks - 1);
+  char* const ldsD = smem + (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + wave * 2 * kDtBytes;
   const Seq s = seq_of(a, b);
   const int nc = (s.len + Q - 1) / Q, per = (nc + a.segs - 1) / a.segs;
   const int c0 = min(seg * per, nc), c1 = min(c0 + per, nc);
@@ -288,16 +308,15 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
     const int64_t n = (int64_t)(a.conv - 1) * a.chans;
     const int blocks = a.segs * gridDim.y, me = blockIdx.y * a.segs + seg;
     T* out = static_cast<T*>(a.window_out) + b * n;
-    for (int64_t i = (int64_t)me * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256) {
+    for (int64_t i = (int64_t)me * blockDim.x + threadIdx.x; i < n; i += (int64_t)blocks * blockDim.x) {
       const int k = (int)(i / a.chans), ch = (int)(i - (int64_t)k * a.chans), t = s.len - (a.conv - 1) + k;
       out[i] = t >= 0 ? static_cast<const T*>(a.x)[(s.first + t) * a.xs + ch]
                       : static_cast<const T*>(a.wcopy)[b * n + (int64_t)(a.conv - 1 + t) * a.chans + ch];
     }
   }
-  if (unit >= each * pblocks) return;
   const int h = grp * each + unit / pblocks;
   const int pb = (unit % pblocks) * 16 * PT, p0 = pb + PT * col;  // this lane's first p
-  const int pn = a.dim - p0;                                      // and how many of its PT exist (<= 0: none)
+  const int pn = live ? a.dim - p0 : 0;                           // and how many of its PT exist (<= 0: none)
   const int64_t hold = (int64_t)a.dim * N;
 
   f32x4 st[NT][PT];
@@ -365,15 +384,42 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
   const unsigned rowb = (unsigned)a.xs * (unsigned)sizeof(T);
   const unsigned xoff = 4 * g * rowb + (unsigned)(h * a.dim + p0) * (unsigned)sizeof(T);
   float total = 0.f;  // log2 of the segment's decay
+  const int slot0 = slot0_of(s.first, b);
+  auto fetch = [&](char* to, const void* from, int kbytes) {  // shared by the waves, 1 KB an instruction
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(from, kbytes * 1024);
+    for (int i = wave; i < kbytes; i += waves) dma16(r, to + i * 1024, lane * 16 + i * 1024, 0);
+  };
+  auto fetch_c = [&](int c) {  // C, and the wave's decays
+    const int64_t sg = (int64_t)(slot0 + c) * a.groups + grp;
+    if (!SEG) fetch(ldsC, static_cast<const char*>(a.ws_c) + sg * 4096 * NT, 4 * NT);
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.ws_dt + ((int64_t)(slot0 + c) * a.heads + h) * kScanDt, kDtBytes);
+    char* to = ldsD + (c & 1) * kDtBytes;
+    dma16(r, to, lane * 16, 0);
+    if (lane < 16) dma16(r, to + 1024, lane * 16 + 1024, 0);
+  };
+  auto fetch_b = [&](int c) {  // B and S (its tiles on and below the diagonal, packed)
+    const int64_t sg = (int64_t)(slot0 + c) * a.groups + grp;
+    fetch(ldsB, static_cast<const char*>(a.ws_b) + sg * 4096 * NT, 4 * NT);
+    if (!SEG) fetch(ldsS, a.ws_s + sg * kScanS, 10);
+  };
+  auto arrived = [&] {  // this wave's loads, then every wave's; and all reads of LDS so far are done
+    wait_vmcnt<0>();
+    dma_barrier();
+  };
+  if (c0 < c1) {
+    fetch_c(c0), fetch_b(c0);
+    arrived();
+  }
   for (int c = c0; c < c1; ++c) {
-    const int slot = slot0_of(s.first, b) + c, t0 = c * Q;
+    const int slot = slot0 + c, t0 = c * Q;
     const int64_t sg = (int64_t)slot * a.groups + grp;
-    const f16* Cg = static_cast<const f16*>(a.ws_c) + sg * Q * NP * 2 + lane * 8;
-    const f16* Bg = static_cast<const f16*>(a.ws_b) + sg * Q * NP * 2 + lane * 8;
-    const float* Sg = a.ws_s + sg * 16 * 256 + lane * 4;
-    const float* dtp = a.ws_dt + ((int64_t)slot * a.heads + h) * kScanDt;
+    const f16* Cg = reinterpret_cast<const f16*>(ldsC) + lane * 8;
+    const f16* Bg = reinterpret_cast<const f16*>(ldsB) + lane * 8;
+    const float* Sg = reinterpret_cast<const float*>(ldsS) + lane * 4;
+    const float* dtp = reinterpret_cast<const float*>(ldsD + (c & 1) * kDtBytes);
+    const float* dts = a.ws_dt + ((int64_t)slot * a.heads + h) * kScanDt + 5 * Q;
     const float maxb = a.ws_max[2 * sg], maxc = a.ws_max[2 * sg + 1];
-    const float cend = dtp[5 * Q], maxdt = dtp[5 * Q + 1], maxf = dtp[5 * Q + 2];
+    const float cend = dts[0], maxdt = dts[1], maxf = dts[2];
     // Raw rows t0 + 16 sb + 4 g - 3 + k; loads past the end (or before the
     // sequence) give zero.  They arrive while the state meets C.
     T raw[4][7][PT];
@@ -442,6 +488,8 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
         }
       }
     }
+    arrived();  // B and S of this chunk are there, C is free
+    if (c + 1 < c1) fetch_c(c + 1);
     // ---- convolution
     __builtin_amdgcn_sched_barrier(0);
     if (c == 0 && g == 0) {  // the window in front of the sequence
@@ -558,7 +606,7 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
               for (int v = 0; v < 4; ++v) m[4 * i + v] = 0.f;
               continue;
             }
-            const f32x4 sv = *reinterpret_cast<const f32x4*>(Sg + (tb * 4 + sb) * 256);
+            const f32x4 sv = *reinterpret_cast<const f32x4*>(Sg + (tb * (tb + 1) / 2 + sb) * 256);
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               float x = sv[v] * sd_[i][v] * __builtin_amdgcn_exp2f((th - sh_[i][v]) + (tl - sl_[i][v]));
@@ -659,10 +707,12 @@ __global__ __launch_bounds__(256, 2) void scan_main_kernel(ScanArgs a) {
         for (int j = 0; j < PT; ++j)
           if (from[j] < Q) st[nt][j] = f32x4{NAN, NAN, NAN, NAN};
     }
+    arrived();  // C and the decays of the next chunk are there, B and S are free
+    if (c + 1 < c1) fetch_b(c + 1);
   }
   if (SEG) {
     state_rw(segst, store);
-    if (lane == 0 && unit % pblocks == 0) a.ws_decay[((int64_t)b * a.segs + seg) * a.heads + h] = total;
+    if (lane == 0 && live && unit % pblocks == 0) a.ws_decay[((int64_t)b * a.segs + seg) * a.heads + h] = total;
   } else if (a.state_out && (c1 == nc && (c0 < c1 || seg == 0))) {
     // the segment with the sequence's last chunk (segment 0 of a sequence without rows)
     state_rw(a.state_out + ((int64_t)b * a.heads + h) * hold, store);
@@ -807,13 +857,13 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int L, int s
 // ------------------------------------------------------------------ launchers
 template <typename T, int NT, bool VX>
 static void launch_main(const ScanArgs& a, hipStream_t st) {
-  const int each = a.heads / a.groups, pblocks = (a.dim + 31) / 32;
-  const dim3 grid(a.segs * a.seqs, a.groups * ((each * pblocks + 3) / 4));
+  const int units = a.heads / a.groups * ((a.dim + 31) / 32), waves = std::min(kScanWaves, units);
+  const dim3 grid(a.segs * a.seqs, a.groups * ((units + waves - 1) / waves));
   if (a.segs > 1) {
-    SN_LAUNCH((scan_main_kernel<T, NT, VX, true>), grid, dim3(256), 0, st, a);
+    SN_LAUNCH((scan_main_kernel<T, NT, VX, true>), grid, dim3(64 * waves), (scan_lds<NT, true>(waves)), st, a);
     SN_LAUNCH((scan_carry_kernel), dim3((a.dim * a.state + 255) / 256, a.heads, a.seqs), dim3(256), 0, st, a);
   }
-  SN_LAUNCH((scan_main_kernel<T, NT, VX, false>), grid, dim3(256), 0, st, a);
+  SN_LAUNCH((scan_main_kernel<T, NT, VX, false>), grid, dim3(64 * waves), (scan_lds<NT, false>(waves)), st, a);
 }
 template <typename T, bool VX>
 static void launch_nt(const ScanArgs& a, hipStream_t st) {
@@ -863,6 +913,7 @@ void scan_run(const ScanArgs& in, hipStream_t st) {
             a.conv >= 1 && a.conv <= 4 && a.seqs >= 1 && a.seqs <= 65535 && a.tokens >= 0,
         "scan shapes");
   a.segs = scan_segments(a);
+  a.each = a.tokens / a.seqs;
   check(a.segs == 1 || a.seqs * (int64_t)a.segs * a.heads * a.dim * a.state <= a.seg_cap, "scan segments");
   if (a.dtype == 0) launch_scan<float>(a, st);
   else if (a.dtype == 1) launch_scan<f16>(a, st);

@@ -344,7 +344,7 @@ int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* c
       auto floats = [&](int64_t n) { return static_cast<float*>(op->alloc(n * 4)); };
       a.ws_c = op->alloc(slots * d.groups * Q * a.np * 4);
       a.ws_b = op->alloc(slots * d.groups * Q * a.np * 4);
-      a.ws_s = floats(slots * d.groups * Q * Q);
+      a.ws_s = floats(slots * d.groups * k::kScanS);
       a.ws_max = floats(slots * d.groups * 2);
       a.ws_dt = floats(slots * d.heads * k::kScanDtRow);
       // segments are made for fewer than kScanUnits units of at most 32

@@ -120,7 +120,7 @@ __device__ __forceinline__ float wave_max(float v) {
 // s: the order in which accumulator tiles hold rows.  S = C B^T in float32,
 //   ws_s [slot][group][tb][sb <= tb][lane][4]: t = 16 tb + lane % 16, s = 16 sb + 4 (lane / 16) + 0..3.
 constexpr int kPrep = 1024;
-template <typename T>
+template <typename T, int NP>
 __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int part = blockIdx.y, hb = (a.heads + 15) / 16;
@@ -172,48 +172,52 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
     o[Q + lane] = ch;
     o[2 * Q + lane] = cl;
     o[3 * Q + lane] = dt;
-    o[4 * Q + lane] = f;
     const float dm = wave_max(max_finite(0.f, dt)), fm = wave_max(max_finite(0.f, f));
+    o[4 * Q + lane] = f * (pow2_for(fm) * 0x1p-14f);  // below 1
     if (lane == 0) o[5 * Q] = eh + el, o[5 * Q + 1] = dm, o[5 * Q + 2] = fm;
     return;
   }
 
   // ---- B and C of one group
-  const int N = a.state, NP = a.np, pitch = NP + 4;
+  const int N = a.state;
+  constexpr int pitch = NP + 4, ITEMS = NP / 32;  // channels by 4 times per thread
   float* Cs = lds;                // [t][n]
   float* Bs = lds + Q * pitch;    // [t][n]
   float* red = Bs + Q * pitch;    // [2][waves]
   float mb = 0.f, mc = 0.f;
-  for (int i = threadIdx.x; i < 2 * NP * (Q / 4); i += kPrep) {
-    const int e = i % (2 * NP), tq = i / (2 * NP) * 4;
+  float w[ITEMS][4], bias[ITEMS];
+  T r[ITEMS][7];
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {  // all loads first
+    const int i = threadIdx.x + kPrep * k, e = i % (2 * NP), tq = i / (2 * NP) * 4;
+    const int n = min(e % NP, N - 1), ch = a.heads * a.dim + (e >= NP ? a.groups * N : 0) + part * N + n;
+    const T* x = static_cast<const T*>(a.x) + s.first * a.xs + ch;
+#pragma unroll
+    for (int j = 0; j < 7; ++j) r[k][j] = x[min(max(t0 + tq - 3 + j, 0), s.len - 1) * a.xs];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[k][j] = a.conv_w[j * a.chans + ch];
+    bias[k] = a.conv_b[ch];
+  }
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int i = threadIdx.x + kPrep * k, e = i % (2 * NP), tq = i / (2 * NP) * 4, n = e % NP;
     const bool isc = e >= NP;
-    const int n = isc ? e - NP : e;
-    float u[4] = {0.f, 0.f, 0.f, 0.f};
-    if (n < N) {
-      const int ch = a.heads * a.dim + (isc ? a.groups * N : 0) + part * N + n;
-      float w[4], r[7];
-      const T* x = static_cast<const T*>(a.x) + s.first * a.xs + ch;
+    float v[7];
 #pragma unroll
-      for (int k = 0; k < 7; ++k) {
-        const int t = t0 + tq - 3 + k;
-        r[k] = to_f(x[min(max(t, 0), s.len - 1) * a.xs]);
-        if (t >= s.len) r[k] = 0.f;
-      }
+    for (int j = 0; j < 7; ++j) v[j] = to_f(r[k][j]);
+    if (t0 + tq == 0) {
+      const int ch = a.heads * a.dim + (isc ? a.groups * N : 0) + part * N + min(n, N - 1);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] = a.conv_w[k * a.chans + ch];
-      if (t0 + tq == 0)
-#pragma unroll
-        for (int k = 0; k < 3; ++k) r[k] = raw_at<T>(a, s, b, k - 3, ch);
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        if (t0 + tq + v < s.len) {
-          u[v] = silu_f(taps4(w, a.conv_b[ch], r[v], r[v + 1], r[v + 2], r[v + 3], a.conv));
-          if (isc) mc = max_finite(mc, u[v]);
-          else mb = max_finite(mb, u[v]);
-        }
+      for (int j = 0; j < 3; ++j) v[j] = raw_at<T>(a, s, b, j - 3, ch);
     }
 #pragma unroll
-    for (int v = 0; v < 4; ++v) (isc ? Cs : Bs)[(tq + v) * pitch + n] = u[v];
+    for (int j = 0; j < 4; ++j) {
+      float u = 0.f;  // past the end, and in columns that only fill the tile
+      if (t0 + tq + j < s.len && n < N) u = silu_f(taps4(w[k], bias[k], v[j], v[j + 1], v[j + 2], v[j + 3], a.conv));
+      if (isc) mc = max_finite(mc, u);
+      else mb = max_finite(mb, u);
+      (isc ? Cs : Bs)[(tq + j) * pitch + n] = u;
+    }
   }
   mb = wave_max(mb), mc = wave_max(mc);
   if (lane == 0) red[wave] = mb, red[kPrep / 64 + wave] = mc;
@@ -225,7 +229,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
   const int col = lane & 15, g = lane >> 4;
   f16* Cg = static_cast<f16*>(a.ws_c) + sg * Q * NP * 2;
   f16* Bg = static_cast<f16*>(a.ws_b) + sg * Q * NP * 2;
-  const int NQ = NP / 32;
+  constexpr int NQ = NP / 32;
   for (int f = wave; f < 4 * NQ + NP / 16 * 2; f += kPrep / 64) {
     const bool isc = f < 4 * NQ;
     float v[8];
@@ -246,6 +250,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
   const int tb = wave >> 2, sb = wave & 3;
   if (sb <= tb) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int n0 = 0; n0 < NP; n0 += 16) {
       const f32x4 bf = *reinterpret_cast<const f32x4*>(Bs + (16 * sb + col) * pitch + n0 + 4 * g);
       const f32x4 cf = *reinterpret_cast<const f32x4*>(Cs + (16 * tb + col) * pitch + n0 + 4 * g);
@@ -366,7 +371,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 #pragma unroll
       for (int j = 0; j < PT; ++j)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) top[j] = max_finite(top[j], st[nt][j][v]);
+        for (int v = 0; v < 4; ++v) top[j] = fmaxf(top[j], fabsf(st[nt][j][v]));
 #pragma unroll
     for (int j = 0; j < PT; ++j) top[j] = col_max(top[j]);
   }
@@ -503,6 +508,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       }
     }
     float u[4][PT][4], sq[PT] = {}, maxu[PT], su[PT];
+    auto convolve = [&](int conv) {
 #pragma unroll
     for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
@@ -512,8 +518,17 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 #pragma unroll
         for (int k = 0; k < 7; ++k) r[k] = to_f(raw[sb][k][j]);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) u[sb][j][v] = silu_f(taps4(wj, cb[j], r[v], r[v + 1], r[v + 2], r[v + 3], a.conv));
+        for (int v = 0; v < 4; ++v) u[sb][j][v] = taps4(wj, cb[j], r[v], r[v + 1], r[v + 2], r[v + 3], conv);
       }
+    };
+    if (a.conv == 4) convolve(4);  // without the tests for absent taps
+    else convolve(a.conv);
+#pragma unroll
+    for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+      for (int j = 0; j < PT; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) u[sb][j][v] = silu_f(u[sb][j][v]);
     if (t0 + Q > s.len) {  // past the end: zero (a NaN would meet the zeros of earlier rows)
 #pragma unroll
       for (int sb = 0; sb < 4; ++sb)
@@ -625,6 +640,15 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       float back[PT];
 #pragma unroll
       for (int j = 0; j < PT; ++j) back[j] = inv_pow2(sw) * inv_pow2(su[j]);
+      if (poison) {
+#pragma unroll
+        for (int tb = 0; tb < 4; ++tb)
+#pragma unroll
+          for (int j = 0; j < PT; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+              if (16 * tb + 4 * g + v >= from[j]) acc[tb][j][v] = NAN;
+      }
       // stores past the last row (or column) are outside the range, and dropped
       const unsigned yrow = (unsigned)a.ys * (unsigned)sizeof(T);
       const __amdgpu_buffer_rsrc_t ry =
@@ -635,10 +659,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const int t = 16 * tb + 4 * g + v;
           T o[PT];
 #pragma unroll
-          for (int j = 0; j < PT; ++j) o[j] = from_f<T>(t >= from[j] ? NAN : acc[tb][j][v] * back[j]);
+          for (int j = 0; j < PT; ++j) o[j] = from_f<T>(acc[tb][j][v] * back[j]);
           const unsigned off = yo + (16 * tb + v) * yrow;
           if constexpr (VX) {
             if constexpr (sizeof(T) == 2) {
@@ -658,7 +681,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     }
     // ---- the state after the chunk
     __builtin_amdgcn_sched_barrier(0);
-    const float sf = pow2_for(maxf), e = __builtin_amdgcn_exp2f(cend);
+    const float sf = inv_pow2(pow2_for(maxf)) * 0x1p14f, e = __builtin_amdgcn_exp2f(cend);
     HiLo xf[2][PT];
 #pragma unroll
     for (int q = 0; q < 2; ++q)
@@ -668,15 +691,14 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const f32x4 f = *reinterpret_cast<const f32x4*>(dtp + 4 * Q + 32 * q + 16 * i + 4 * g);
-          // below 2^14 each: their product back to f16's range
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[4 * i + k] = (su[j] * u[2 * q + i][j][k]) * (f[k] * sf * 0x1p-14f);
+          for (int k = 0; k < 4; ++k) v[4 * i + k] = (su[j] * u[2 * q + i][j][k]) * f[k];
         }
         xf[q][j] = split8(v);
       }
     float back[PT];
 #pragma unroll
-    for (int j = 0; j < PT; ++j) back[j] = inv_pow2(pow2_for(maxb)) * inv_pow2(su[j]) * inv_pow2(sf) * 0x1p14f;
+    for (int j = 0; j < PT; ++j) back[j] = inv_pow2(pow2_for(maxb)) * inv_pow2(su[j]) * sf;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       f32x4 add[PT];
@@ -860,7 +882,10 @@ static void launch_main(const ScanArgs& a, hipStream_t st) {
   const int units = a.heads / a.groups * ((a.dim + 31) / 32), waves = std::min(kScanWaves, units);
   const dim3 grid(a.segs * a.seqs, a.groups * ((units + waves - 1) / waves));
   if (a.segs > 1) {
-    SN_LAUNCH((scan_main_kernel<T, NT, VX, true>), grid, dim3(64 * waves), (scan_lds<NT, true>(waves)), st, a);
+    // half the waves: three of its workgroups fit a CU
+    const int ws = std::min(kScanWaves / 2, units);
+    const dim3 gs(a.segs * a.seqs, a.groups * ((units + ws - 1) / ws));
+    SN_LAUNCH((scan_main_kernel<T, NT, VX, true>), gs, dim3(64 * ws), (scan_lds<NT, true>(ws)), st, a);
     SN_LAUNCH((scan_carry_kernel), dim3((a.dim * a.state + 255) / 256, a.heads, a.seqs), dim3(256), 0, st, a);
   }
   SN_LAUNCH((scan_main_kernel<T, NT, VX, false>), grid, dim3(64 * waves), (scan_lds<NT, false>(waves)), st, a);
@@ -883,8 +908,12 @@ static void launch_scan(ScanArgs a, hipStream_t st) {
   };
   const bool vx = a.dim % 2 == 0 && ok(a.x, a.xs) && ok(a.y, a.ys);
   const int64_t slots = scan_slots(a.tokens, a.seqs);
+  const dim3 grid((unsigned)slots, a.groups + (a.heads + 15) / 16 + 1);
   const size_t lds = (2 * Q * (a.np + 4) + 2 * kPrep / 64) * sizeof(float);
-  SN_LAUNCH((scan_prep_kernel<T>), dim3((unsigned)slots, a.groups + (a.heads + 15) / 16 + 1), dim3(kPrep), lds, st, a);
+  if (a.np == 32) SN_LAUNCH((scan_prep_kernel<T, 32>), grid, dim3(kPrep), lds, st, a);
+  else if (a.np == 64) SN_LAUNCH((scan_prep_kernel<T, 64>), grid, dim3(kPrep), lds, st, a);
+  else if (a.np == 128) SN_LAUNCH((scan_prep_kernel<T, 128>), grid, dim3(kPrep), lds, st, a);
+  else SN_LAUNCH((scan_prep_kernel<T, 256>), grid, dim3(kPrep), lds, st, a);
   if (vx) launch_nt<T, true>(a, st);
   else launch_nt<T, false>(a, st);
 }

@@ -18,6 +18,7 @@
 // float32 sum would lose the differences of neighbours late in a chunk of
 // strong decays.
 #include "seq.hpp"
+#include <cstdlib>
 
 namespace sn {
 namespace k {
@@ -262,29 +263,28 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 }
 
 // ------------------------------------------------------------------ the heads
-// A wave owns 32 columns p of one head and all N <= 16 NT state rows n: the
-// state lives in 2 NT accumulator tiles (lane: n = 16 nt + 4 (lane / 16) + v,
-// p = p0 + 2 (lane % 16) + j), whose layout is also that of the second operand
+// A wave owns 16 PT columns p of one head and all N <= 16 NT state rows n: the
+// state lives in PT NT accumulator tiles (lane: n = 16 nt + 4 (lane / 16) + v,
+// p = p0 + PT (lane % 16) + j), whose layout is also that of the second operand
 // of the product with C, so the state never leaves the registers; and a lane's
 // convolution outputs (times 16 sb + 4 (lane / 16) + v, the same p) are the
-// second operand of both other products.  Two neighbouring p per lane make
-// 4-byte row accesses; 32 columns leave registers for 2 waves per SIMD.
+// second operand of both other products.
 // SEG: only the state that the segment adds (from zero), no outputs.
-// VX: rows of x and y in whole aligned pairs.
+// PT: 1, or 2 in 16-bit types with rows of x and y in whole aligned pairs.
 //
 // The waves of a workgroup share the group's C, B and S of a chunk in LDS, and
 // each has its head's decays there, all brought by LDS direct loads while the
 // chunk before (C, decays) or the product with C (B, S) is computed: two
 // barriers per chunk, behind which one set has arrived and the other is free.
-constexpr int kScanWaves = 8;
+constexpr int kScanWaves = 8;  // of a workgroup: 2 per SIMD
 constexpr int kDtBytes = 5 * Q * 4;
-template <int NT, bool SEG>
-constexpr int scan_lds(int waves) {  // C, B, S, two decay rows per wave
-  return (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + waves * 2 * kDtBytes;
+constexpr int kMixBytes = 6 * 2048;  // a head's 6 operands of the mix of a chunk's rows, hi and lo
+template <int NT, bool SHARE, bool SEG>
+constexpr int scan_lds(int waves) {  // B, C, S, two decay rows per wave, the mix of every 4 waves
+  return (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + waves * 2 * kDtBytes + (SHARE && !SEG ? waves / 4 * kMixBytes : 0);
 }
-template <typename T, int NT, bool VX, bool SEG>
+template <typename T, int NT, int PT, bool SHARE, bool SEG>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) {
-  constexpr int PT = 2;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   char* const ldsB = smem;
   char* const ldsC = smem + 4096 * NT;                    // not with SEG
@@ -301,6 +301,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   // a wave beyond the last unit works on the last one, for the barriers' sake, and stores nothing
   const bool live = unit_ < each * pblocks;
   const int unit = min(unit_, each * pblocks - 1);
+  char* const ldsM = smem + scan_lds<NT, false, SEG>(waves) + (wave >> 2) * kMixBytes;  // with SHARE
   char* const ldsD = smem + (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + wave * 2 * kDtBytes;
   const Seq s = seq_of(a, b);
   const int nc = (s.len + Q - 1) / Q, per = (nc + a.segs - 1) / a.segs;
@@ -329,28 +330,40 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int j = 0; j < PT; ++j) st[nt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto state_rw = [&](auto* p, auto&& f) {  // f(element pointer, tile register) over the lane's state
+  // the lane's part of a head's state; what is outside it has an offset out of range
+  auto at_state = [&](int nt, int j, int v) {
+    const int n = 16 * nt + 4 * g + v;
+    return (int)(j < pn && n < N ? ((unsigned)(p0 + j) * (unsigned)N + (unsigned)n) * 4u : kOOB);
+  };
+  auto load_state = [&](const float* p) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, hold * 4);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int j = 0; j < PT; ++j) {
-        const int n = 16 * nt + 4 * g;
-        auto* q = p + (int64_t)(p0 + j) * N + n;
-        if (j < pn && n < N) f(q, st[nt][j], n);
-      }
-  };
-  auto load = [&](const float* q, f32x4& r, int n) {
-    if (a.vec_state) r = *reinterpret_cast<const f32x4*>(q);
-    else
+      for (int j = 0; j < PT; ++j)
+        if (a.vec_state) {
+          st[nt][j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at_state(nt, j, 0), 0, 0));
+        } else {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) r[v] = n + v < N ? q[v] : 0.f;
+          for (int v = 0; v < 4; ++v)
+            st[nt][j][v] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at_state(nt, j, v), 0, 0));
+        }
   };
-  auto store = [&](float* q, f32x4& r, int n) {
-    if (a.vec_state) *reinterpret_cast<f32x4*>(q) = r;
-    else
+  auto store_state = [&](float* p) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p, hold * 4);
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-        if (n + v < N) q[v] = r[v];
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < PT; ++j)
+        if (a.vec_state) {
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, st[nt][j]), r, at_state(nt, j, 0), 0, 0);
+        } else {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float one = st[nt][j][v];  // (a bit cast of the element itself reads element 0)
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, one), r, at_state(nt, j, v), 0, 0);
+          }
+        }
   };
   float* segst = a.ws_seg + (((int64_t)b * a.segs + seg) * a.heads + h) * hold;
   // per column: at least the size of every value of the state (within a few
@@ -361,21 +374,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     v = fmaxf(v, __shfl_xor(v, 16));
     return fmaxf(v, __shfl_xor(v, 32));
   };
-  if (SEG) {
-    if (c1 >= nc) return;  // nothing follows: no one reads this segment's state
-  } else {
-    if (a.segs > 1) state_rw(static_cast<const float*>(segst), load);
-    else if (a.state_in) state_rw(a.state_in + ((int64_t)b * a.heads + h) * hold, load);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int j = 0; j < PT; ++j)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) top[j] = fmaxf(top[j], fabsf(st[nt][j][v]));
-#pragma unroll
-    for (int j = 0; j < PT; ++j) top[j] = col_max(top[j]);
-  }
-
+  if (SEG && c1 >= nc) return;  // nothing follows: no one reads this segment's state
   // the lane's convolution
   const int ch0 = h * a.dim + p0;
   float w[4][PT], cb[PT];
@@ -394,27 +393,68 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     const __amdgpu_buffer_rsrc_t r = make_rsrc(from, kbytes * 1024);
     for (int i = wave; i < kbytes; i += waves) dma16(r, to + i * 1024, lane * 16 + i * 1024, 0);
   };
-  auto fetch_c = [&](int c) {  // C, and the wave's decays
+  auto fetch_c = [&](int c) {  // C, the wave's decays, and S (its tiles on and below the diagonal, packed) with SHARE
     const int64_t sg = (int64_t)(slot0 + c) * a.groups + grp;
     if (!SEG) fetch(ldsC, static_cast<const char*>(a.ws_c) + sg * 4096 * NT, 4 * NT);
+    if (!SEG && SHARE) fetch(ldsS, a.ws_s + sg * kScanS, 10);
     const __amdgpu_buffer_rsrc_t r = make_rsrc(a.ws_dt + ((int64_t)(slot0 + c) * a.heads + h) * kScanDt, kDtBytes);
     char* to = ldsD + (c & 1) * kDtBytes;
     dma16(r, to, lane * 16, 0);
     if (lane < 16) dma16(r, to + 1024, lane * 16 + 1024, 0);
   };
-  auto fetch_b = [&](int c) {  // B and S (its tiles on and below the diagonal, packed)
+  auto fetch_b = [&](int c) {  // B, and S without SHARE
     const int64_t sg = (int64_t)(slot0 + c) * a.groups + grp;
     fetch(ldsB, static_cast<const char*>(a.ws_b) + sg * 4096 * NT, 4 * NT);
-    if (!SEG) fetch(ldsS, a.ws_s + sg * kScanS, 10);
+    if (!SEG && !SHARE) fetch(ldsS, a.ws_s + sg * kScanS, 10);
   };
-  auto arrived = [&] {  // this wave's loads, then every wave's; and all reads of LDS so far are done
-    wait_vmcnt<0>();
-    dma_barrier();
+  // Raw rows 16 sb + 4 g - 3 + k of a chunk; rows past the end (or before the
+  // sequence) give zero, and so does a chunk past the segment.
+  T raw[4][7][PT];
+  auto load_raw = [&](int c) {
+    unsigned xo = xoff;  // per chunk: kept out of the loop, its 28 sums would fill the registers
+    asm volatile("" : "+v"(xo));
+    const int t0 = c * Q;
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const T*>(a.x) + (s.first + t0 - 3) * a.xs,
+                                                c < c1 ? (long long)min(s.len - t0 + 3, Q + 3) * rowb : 0);
+#pragma unroll
+    for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+      for (int k = 0; k < 7; ++k) {
+        const bool before = sb == 0 && k < 3 && c == 0 && g == 0;
+        const unsigned row = xo + (16 * sb + k) * rowb;  // in the offset that the range check sees
+        const unsigned o = before || pn < PT ? kOOB : row;
+        if constexpr (sizeof(T) * PT == 2) {
+          const uint16_t v = __builtin_amdgcn_raw_buffer_load_b16(rx, (int)o, 0, 0);
+          __builtin_memcpy(raw[sb][k], &v, 2);
+        } else {
+          const unsigned v = __builtin_amdgcn_raw_buffer_load_b32(rx, (int)o, 0, 0);
+          __builtin_memcpy(raw[sb][k], &v, 4);
+        }
+      }
   };
-  if (c0 < c1) {
-    fetch_c(c0), fetch_b(c0);
-    arrived();
+  // The next chunk's raw rows are loaded a chunk ahead, where registers allow.
+  constexpr bool AHEAD = PT == 1;
+  // Accesses of a chunk that follow its loads of the next chunk's C and decays:
+  // the raw rows, and the stores of y.
+  constexpr int AFTER = (AHEAD ? 28 : 0) + (SEG ? 0 : 16);
+  if (c0 < c1) fetch_c(c0), fetch_b(c0);
+  if (!SEG) {
+    if (a.segs > 1) load_state(segst);
+    else if (a.state_in) load_state(a.state_in + ((int64_t)b * a.heads + h) * hold);
   }
+  if (AHEAD) load_raw(c0);
+  if (!SEG) {
+#pragma unroll
+    for (int j = 0; j < PT; ++j) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) top[j] = fmaxf(top[j], fabsf(st[nt][j][v]));
+      top[j] = col_max(top[j]);
+    }
+  }
+  wait_vmcnt<0>();
+  dma_barrier();
   for (int c = c0; c < c1; ++c) {
     const int slot = slot0 + c, t0 = c * Q;
     const int64_t sg = (int64_t)slot * a.groups + grp;
@@ -425,43 +465,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     const float* dts = a.ws_dt + ((int64_t)slot * a.heads + h) * kScanDt + 5 * Q;
     const float maxb = a.ws_max[2 * sg], maxc = a.ws_max[2 * sg + 1];
     const float cend = dts[0], maxdt = dts[1], maxf = dts[2];
-    // Raw rows t0 + 16 sb + 4 g - 3 + k; loads past the end (or before the
-    // sequence) give zero.  They arrive while the state meets C.
-    T raw[4][7][PT];
-    unsigned xo = xoff;  // per chunk: kept out of the loop, its 28 sums would fill the registers
-    asm volatile("" : "+v"(xo));
-    const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const T*>(a.x) + (s.first + t0 - 3) * a.xs,
-                                                (long long)min(s.len - t0 + 3, Q + 3) * rowb);
-#pragma unroll
-    for (int sb = 0; sb < 4; ++sb)
-#pragma unroll
-      for (int k = 0; k < 7; ++k) {
-        const bool before = sb == 0 && k < 3 && c == 0 && g == 0;
-        const unsigned row = xo + (16 * sb + k) * rowb;  // in the offset that the range check sees
-        if constexpr (VX) {
-          const unsigned o = before || pn < PT ? kOOB : row;
-          if constexpr (sizeof(T) == 2) {
-            const unsigned v = __builtin_amdgcn_raw_buffer_load_b32(rx, (int)o, 0, 0);
-            __builtin_memcpy(raw[sb][k], &v, 4);
-          } else {
-            const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, (int)o, 0, 0));
-            __builtin_memcpy(raw[sb][k], &v, 8);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < PT; ++j) {
-            const unsigned o = before || j >= pn ? kOOB : row + j * (unsigned)sizeof(T);
-            if constexpr (sizeof(T) == 2) {
-              const uint16_t v = __builtin_amdgcn_raw_buffer_load_b16(rx, (int)o, 0, 0);
-              __builtin_memcpy(&raw[sb][k][j], &v, 2);
-            } else {
-              const unsigned v = __builtin_amdgcn_raw_buffer_load_b32(rx, (int)o, 0, 0);
-              __builtin_memcpy(&raw[sb][k][j], &v, 4);
-            }
-          }
-        }
-      }
-    __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
+    if (!AHEAD) {
+      load_raw(c);
+      __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
+    }
     f32x4 acc[4][PT];
     if constexpr (!SEG) {
       // ---- C times the state in front of the chunk
@@ -493,10 +500,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
         }
       }
     }
-    arrived();  // B and S of this chunk are there, C is free
-    if (c + 1 < c1) fetch_c(c + 1);
     // ---- convolution
-    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
     if (c == 0 && g == 0) {  // the window in front of the sequence
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
@@ -529,6 +534,47 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       for (int j = 0; j < PT; ++j)
 #pragma unroll
         for (int v = 0; v < 4; ++v) u[sb][j][v] = silu_f(u[sb][j][v]);
+    const float sw = pow2_for(fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)));
+    // The mix of rows 16 tb .. + 15 with rows 32 q .. + 31: S, the decay between
+    // them and the step size; on the diagonal the skip term, above it nothing.
+    auto mix = [&](int tb, int q) {
+      const float th = dtp[Q + 16 * tb + col], tl = dtp[2 * Q + 16 * tb + col];
+      float m[8];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int sb = 2 * q + i, at = 16 * sb + 4 * g;
+        const f32x4 sh_ = *reinterpret_cast<const f32x4*>(dtp + Q + at);
+        const f32x4 sl_ = *reinterpret_cast<const f32x4*>(dtp + 2 * Q + at);
+        const f32x4 sd_ = *reinterpret_cast<const f32x4*>(dtp + 3 * Q + at);
+        const f32x4 sv = *reinterpret_cast<const f32x4*>(Sg + (tb * (tb + 1) / 2 + min(sb, tb)) * 256);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          float x = sv[v] * (sd_[v] * sw) * __builtin_amdgcn_exp2f((th - sh_[v]) + (tl - sl_[v]));
+          if (at + v == 16 * tb + col) x = fmaf(dh, sw, x);
+          m[4 * i + v] = at + v > 16 * tb + col ? 0.f : x;
+        }
+      }
+      return split8(m);
+    };
+    f16x8* const mixes = reinterpret_cast<f16x8*>(ldsM) + lane;  // [operand][hi, lo][lane]; operand 4 q + tb - 2 q
+    if constexpr (SHARE && !SEG) {
+      // the four waves of a head make 10 tiles, 2 or 3 each
+      auto put = [&](int tb, int q) {
+        const HiLo m = mix(tb, q);
+        mixes[(tb + 2 * q) * 128] = m.hi;
+        mixes[(tb + 2 * q) * 128 + 64] = m.lo;
+      };
+      const int w4 = wave & 3;
+      put(w4 == 3 ? 2 : w4 == 0 ? 0 : w4 + 1, w4 == 3);
+      if (w4 == 0) put(1, 0);
+      if (w4 == 3) put(3, 1);
+    }
+    // every wave's loads of B (and S) of this chunk and its share of the mix
+    // have arrived, and C (and S) is free
+    wait_vmcnt<0>();
+    dma_barrier();
+    if (c + 1 < c1) fetch_c(c + 1);
+    if (AHEAD) load_raw(c + 1);
     if (t0 + Q > s.len) {  // past the end: zero (a NaN would meet the zeros of earlier rows)
 #pragma unroll
       for (int sb = 0; sb < 4; ++sb)
@@ -578,7 +624,6 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (!SEG) {
       // ---- earlier rows of the chunk, the row itself and the skip term
-      const float maxw = fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)), sw = pow2_for(maxw);
       // from C h's scale to this product's, with the decay since the chunk's start
       float to[PT];
 #pragma unroll
@@ -601,38 +646,15 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
           for (int i = 0; i < 8; ++i) v[i] = su[j] * u[2 * q + (i >> 2)][j][i & 3];
           uf[j] = split8(v);
         }
-        f32x4 sh_[2], sl_[2], sd_[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int at = 32 * q + 16 * i + 4 * g;
-          sh_[i] = *reinterpret_cast<const f32x4*>(dtp + Q + at);
-          sl_[i] = *reinterpret_cast<const f32x4*>(dtp + 2 * Q + at);
-          sd_[i] = *reinterpret_cast<const f32x4*>(dtp + 3 * Q + at) * sw;
-        }
 #pragma unroll
         for (int tb = 2 * q; tb < 4; ++tb) {
-          const float th = dtp[Q + 16 * tb + col], tl = dtp[2 * Q + 16 * tb + col];
-          float m[8];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int sb = 2 * q + i;
-            if (sb > tb) {
-#pragma unroll
-              for (int v = 0; v < 4; ++v) m[4 * i + v] = 0.f;
-              continue;
-            }
-            const f32x4 sv = *reinterpret_cast<const f32x4*>(Sg + (tb * (tb + 1) / 2 + sb) * 256);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              float x = sv[v] * sd_[i][v] * __builtin_amdgcn_exp2f((th - sh_[i][v]) + (tl - sl_[i][v]));
-              if (sb == tb) {
-                if (4 * g + v == col) x = fmaf(dh, sw, x);
-                if (4 * g + v > col) x = 0.f;
-              }
-              m[4 * i + v] = x;
-            }
+          HiLo mf;
+          if constexpr (SHARE) {
+            mf.hi = mixes[(tb + 2 * q) * 128];
+            mf.lo = mixes[(tb + 2 * q) * 128 + 64];
+          } else {
+            mf = mix(tb, q);
           }
-          const HiLo mf = split8(m);
 #pragma unroll
           for (int j = 0; j < PT; ++j) acc[tb][j] = mul3(mf, uf[j], acc[tb][j]);
         }
@@ -663,20 +685,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 #pragma unroll
           for (int j = 0; j < PT; ++j) o[j] = from_f<T>(acc[tb][j][v] * back[j]);
           const unsigned off = yo + (16 * tb + v) * yrow;
-          if constexpr (VX) {
-            if constexpr (sizeof(T) == 2) {
-              __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o), ry, (int)(pn > 0 ? off : kOOB), 0, 0);
-            } else {
-              __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, o), ry, (int)(pn > 0 ? off : kOOB), 0, 0);
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < PT; ++j) {
-              const int to_ = (int)(j < pn ? off + j * (unsigned)sizeof(T) : kOOB);
-              if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, o[j]), ry, to_, 0, 0);
-              else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o[j]), ry, to_, 0, 0);
-            }
-          }
+          const int to_ = (int)(pn > 0 ? off : kOOB);
+          if constexpr (sizeof(T) * PT == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, o), ry, to_, 0, 0);
+          else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o), ry, to_, 0, 0);
         }
     }
     // ---- the state after the chunk
@@ -729,15 +740,18 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
         for (int j = 0; j < PT; ++j)
           if (from[j] < Q) st[nt][j] = f32x4{NAN, NAN, NAN, NAN};
     }
-    arrived();  // C and the decays of the next chunk are there, B and S are free
+    // every wave's loads of C and its decays for the next chunk have arrived
+    // (the newest AFTER are not among them), and B and S are free
+    wait_vmcnt<AFTER>();
+    dma_barrier();
     if (c + 1 < c1) fetch_b(c + 1);
   }
   if (SEG) {
-    state_rw(segst, store);
+    store_state(segst);
     if (lane == 0 && live && unit % pblocks == 0) a.ws_decay[((int64_t)b * a.segs + seg) * a.heads + h] = total;
   } else if (a.state_out && (c1 == nc && (c0 < c1 || seg == 0))) {
     // the segment with the sequence's last chunk (segment 0 of a sequence without rows)
-    state_rw(a.state_out + ((int64_t)b * a.heads + h) * hold, store);
+    store_state(a.state_out + ((int64_t)b * a.heads + h) * hold);
   }
 }
 
@@ -877,36 +891,30 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int L, int s
 }
 
 // ------------------------------------------------------------------ launchers
-template <typename T, int NT, bool VX>
+template <typename T, int NT, int PT, bool SHARE>
 static void launch_main(const ScanArgs& a, hipStream_t st) {
-  const int units = a.heads / a.groups * ((a.dim + 31) / 32), waves = std::min(kScanWaves, units);
+  const int units = a.heads / a.groups * ((a.dim + 16 * PT - 1) / (16 * PT)), waves = std::min(kScanWaves, units);
   const dim3 grid(a.segs * a.seqs, a.groups * ((units + waves - 1) / waves));
   if (a.segs > 1) {
     // half the waves: three of its workgroups fit a CU
-    const int ws = std::min(kScanWaves / 2, units);
+    const int ws = std::min(4, units);
     const dim3 gs(a.segs * a.seqs, a.groups * ((units + ws - 1) / ws));
-    SN_LAUNCH((scan_main_kernel<T, NT, VX, true>), gs, dim3(64 * ws), (scan_lds<NT, true>(ws)), st, a);
+    SN_LAUNCH((scan_main_kernel<T, NT, PT, false, true>), gs, dim3(64 * ws), (scan_lds<NT, false, true>(ws)), st, a);
     SN_LAUNCH((scan_carry_kernel), dim3((a.dim * a.state + 255) / 256, a.heads, a.seqs), dim3(256), 0, st, a);
   }
-  SN_LAUNCH((scan_main_kernel<T, NT, VX, false>), grid, dim3(64 * waves), (scan_lds<NT, false>(waves)), st, a);
+  SN_LAUNCH((scan_main_kernel<T, NT, PT, SHARE, false>), grid, dim3(64 * waves), (scan_lds<NT, SHARE, false>(waves)), st, a);
 }
-template <typename T, bool VX>
-static void launch_nt(const ScanArgs& a, hipStream_t st) {
-  if (a.np <= 32) launch_main<T, 2, VX>(a, st);
-  else if (a.np <= 64) launch_main<T, 4, VX>(a, st);
-  else if (a.np <= 128) launch_main<T, 8, VX>(a, st);
-  else launch_main<T, 16, VX>(a, st);
+template <typename T, int PT, bool SHARE>
+static void launch_cols(const ScanArgs& a, hipStream_t st) {
+  if (a.np == 32) launch_main<T, 2, PT, SHARE>(a, st);
+  else if (a.np == 64) launch_main<T, 4, PT, SHARE>(a, st);
+  else if (a.np == 128) launch_main<T, 8, PT, SHARE>(a, st);
+  else if constexpr (PT == 1 && !SHARE) launch_main<T, 16, PT, SHARE>(a, st);
 }
 
 template <typename T>
 static void launch_scan(ScanArgs a, hipStream_t st) {
   a.vec_state = a.state % 4 == 0 && al16(a.state_in) && al16(a.state_out) && al16(a.ws_seg);
-  // a lane's two values of a row as one access: rows and heads on its alignment
-  const int64_t v = sizeof(T) * 2;
-  auto ok = [&](const void* p, int64_t stride) {
-    return reinterpret_cast<uintptr_t>(p) % v == 0 && stride * (int64_t)sizeof(T) % v == 0;
-  };
-  const bool vx = a.dim % 2 == 0 && ok(a.x, a.xs) && ok(a.y, a.ys);
   const int64_t slots = scan_slots(a.tokens, a.seqs);
   const dim3 grid((unsigned)slots, a.groups + (a.heads + 15) / 16 + 1);
   const size_t lds = (2 * Q * (a.np + 4) + 2 * kPrep / 64) * sizeof(float);
@@ -914,8 +922,12 @@ static void launch_scan(ScanArgs a, hipStream_t st) {
   else if (a.np == 64) SN_LAUNCH((scan_prep_kernel<T, 64>), grid, dim3(kPrep), lds, st, a);
   else if (a.np == 128) SN_LAUNCH((scan_prep_kernel<T, 128>), grid, dim3(kPrep), lds, st, a);
   else SN_LAUNCH((scan_prep_kernel<T, 256>), grid, dim3(kPrep), lds, st, a);
-  if (vx) launch_nt<T, true>(a, st);
-  else launch_nt<T, false>(a, st);
+  if constexpr (sizeof(T) == 2) {
+    if (a.cols == 32) return launch_cols<T, 2, false>(a, st);
+  }
+  // with 64 columns per head or a multiple, four waves of one share its mix
+  if ((a.dim + 15) / 16 % 4 == 0 && a.np <= 128) launch_cols<T, 1, true>(a, st);
+  else launch_cols<T, 1, false>(a, st);
 }
 
 template <typename T>
@@ -927,13 +939,22 @@ static void launch_step(ScanArgs a, hipStream_t st) {
   SN_LAUNCH((scan_step_kernel<T>), dim3((unsigned)(a.heads * splits), a.seqs), dim3(256), 0, st, a, L, splits);
 }
 
-static int scan_segments(const ScanArgs& a) {
-  // waves of a pass: units of 32 columns per head and sequence; segments until
-  // about kScanUnits of them (two per SIMD) run, each at least two chunks
-  const int64_t units = (int64_t)a.seqs * a.heads * ((a.dim + 31) / 32);
+// Columns per wave and segments.  A wave of 32 columns does less per column
+// (the products' masks and decays are a head's, not a column's), one of 16
+// makes more waves of a short call and leaves room for 256 state rows.
+static void scan_split(ScanArgs& a) {
   const int64_t chunks = (a.tokens + Q - 1) / Q;  // the most that one sequence may have
-  const int64_t want = std::min<int64_t>((kScanUnits + units - 1) / units, chunks / 2);
-  return (int)std::max<int64_t>(1, want);
+  auto units = [&](int cols) { return (int64_t)a.seqs * a.heads * ((a.dim + cols - 1) / cols); };
+  // waves of a pass: segments until about kScanUnits run, each of at least two chunks
+  auto segs = [&](int cols) {
+    return std::max<int64_t>(1, std::min((kScanUnits + units(cols) - 1) / units(cols), chunks / 2));
+  };
+  const int e = a.dtype == 0 ? 4 : 2;
+  auto pairs = [&](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 2 == 0; };
+  const bool can = e == 2 && a.np <= 128 && a.dim % 2 == 0 && pairs(a.x, a.xs) && pairs(a.y, a.ys);
+  a.cols = can && units(32) * segs(32) >= kScanUnits ? 32 : 16;
+  if (getenv("SCOLS") && can) a.cols = atoi(getenv("SCOLS"));
+  a.segs = (int)segs(a.cols);
 }
 
 void scan_run(const ScanArgs& in, hipStream_t st) {
@@ -941,7 +962,7 @@ void scan_run(const ScanArgs& in, hipStream_t st) {
   check(a.heads >= 1 && a.groups >= 1 && a.heads % a.groups == 0 && a.dim >= 1 && a.state >= 1 && a.state <= 256 &&
             a.conv >= 1 && a.conv <= 4 && a.seqs >= 1 && a.seqs <= 65535 && a.tokens >= 0,
         "scan shapes");
-  a.segs = scan_segments(a);
+  scan_split(a);
   a.each = a.tokens / a.seqs;
   check(a.segs == 1 || a.seqs * (int64_t)a.segs * a.heads * a.dim * a.state <= a.seg_cap, "scan segments");
   if (a.dtype == 0) launch_scan<float>(a, st);

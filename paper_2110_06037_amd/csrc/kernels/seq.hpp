@@ -83,7 +83,7 @@ struct ScanArgs {
   unsigned* count; // [seq][group], zero between calls
   int64_t seg_cap; // elements of ws_seg
   // call
-  int seqs, segs;
+  int seqs, segs, cols;  // segments per sequence and columns per wave are set by the launcher
   int64_t each;  // rows per sequence without offsets (set by the launcher)
   int64_t tokens;
   const int32_t* offsets;

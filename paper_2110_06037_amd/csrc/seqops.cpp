@@ -347,8 +347,8 @@ int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* c
       a.ws_s = floats(slots * d.groups * k::kScanS);
       a.ws_max = floats(slots * d.groups * 2);
       a.ws_dt = floats(slots * d.heads * k::kScanDtRow);
-      // segments are made for fewer than kScanUnits units of at most 32
-      // columns, of at least two chunks each
+      // segments are made for fewer than kScanUnits units of at
+      // most 32 columns, of at least two chunks each
       const int64_t pairs = std::max<int64_t>(1, (d.max_tokens + Q - 1) / Q / 2);
       a.seg_cap = std::min(int64_t(2) * k::kScanUnits * 32 * d.state,
                            d.max_seqs * pairs * d.heads * d.head_dim * d.state);

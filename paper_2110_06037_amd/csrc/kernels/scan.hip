@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
   mb = wave_max(red[lane & 15]), mc = wave_max(red[16 + (lane & 15)]);
   const float sb_ = pow2_for(mb), sc_ = pow2_for(mc);
   const int64_t sg = (int64_t)slot * a.groups + part;
-  if (threadIdx.x == 0) a.ws_max[2 * sg] = mb, a.ws_max[2 * sg + 1] = mc;
+  if (threadIdx.x == 0) a.ws_max[sg * kScanMax] = mb, a.ws_max[sg * kScanMax + 1] = mc;
   const int col = lane & 15, g = lane >> 4;
   f16* Cg = static_cast<f16*>(a.ws_c) + sg * Q * NP * 2;
   f16* Bg = static_cast<f16*>(a.ws_b) + sg * Q * NP * 2;
@@ -277,11 +277,12 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // chunk before (C, decays) or the product with C (B, S) is computed: two
 // barriers per chunk, behind which one set has arrived and the other is free.
 constexpr int kScanWaves = 8;  // of a workgroup: 2 per SIMD
-constexpr int kDtBytes = 5 * Q * 4;
+constexpr int kDtBytes = kScanDt * 4;      // with its three scalars
+constexpr int kMaxBytes = kScanMax * 4;
 constexpr int kMixBytes = 6 * 2048;  // a head's 6 operands of the mix of a chunk's rows, hi and lo
 template <int NT, bool SHARE, bool SEG>
-constexpr int scan_lds(int waves) {  // B, C, S, two decay rows per wave, the mix of every 4 waves
-  return (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + waves * 2 * kDtBytes + (SHARE && !SEG ? waves / 4 * kMixBytes : 0);
+constexpr int scan_lds(int waves) {  // B, C, S, two sets of largest sizes, two decay rows per wave, the mix of every 4 waves
+  return (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + 2 * kMaxBytes + waves * 2 * kDtBytes + (SHARE && !SEG ? waves / 4 * kMixBytes : 0);
 }
 template <typename T, int NT, int PT, bool SHARE, bool SEG>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) {
@@ -302,7 +303,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   const bool live = unit_ < each * pblocks;
   const int unit = min(unit_, each * pblocks - 1);
   char* const ldsM = smem + scan_lds<NT, false, SEG>(waves) + (wave >> 2) * kMixBytes;  // with SHARE
-  char* const ldsD = smem + (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + wave * 2 * kDtBytes;
+  char* const ldsX = smem + (SEG ? 4096 * NT : 8192 * NT + 10 * 1024);
+  char* const ldsD = ldsX + 2 * kMaxBytes + wave * 2 * kDtBytes;
   const Seq s = seq_of(a, b);
   const int nc = (s.len + Q - 1) / Q, per = (nc + a.segs - 1) / a.segs;
   const int c0 = min(seg * per, nc), c1 = min(c0 + per, nc);
@@ -400,7 +402,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     const __amdgpu_buffer_rsrc_t r = make_rsrc(a.ws_dt + ((int64_t)(slot0 + c) * a.heads + h) * kScanDt, kDtBytes);
     char* to = ldsD + (c & 1) * kDtBytes;
     dma16(r, to, lane * 16, 0);
-    if (lane < 16) dma16(r, to + 1024, lane * 16 + 1024, 0);
+    if (lane < (kDtBytes - 1024) / 16) dma16(r, to + 1024, lane * 16 + 1024, 0);
+    if (wave == 0 && lane < kMaxBytes / 16)
+      dma16(make_rsrc(a.ws_max + sg * kScanMax, kMaxBytes), ldsX + (c & 1) * kMaxBytes, lane * 16, 0);
   };
   auto fetch_b = [&](int c) {  // B, and S without SHARE
     const int64_t sg = (int64_t)(slot0 + c) * a.groups + grp;
@@ -456,15 +460,14 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   wait_vmcnt<0>();
   dma_barrier();
   for (int c = c0; c < c1; ++c) {
-    const int slot = slot0 + c, t0 = c * Q;
-    const int64_t sg = (int64_t)slot * a.groups + grp;
+    const int t0 = c * Q;
     const f16* Cg = reinterpret_cast<const f16*>(ldsC) + lane * 8;
     const f16* Bg = reinterpret_cast<const f16*>(ldsB) + lane * 8;
     const float* Sg = reinterpret_cast<const float*>(ldsS) + lane * 4;
     const float* dtp = reinterpret_cast<const float*>(ldsD + (c & 1) * kDtBytes);
-    const float* dts = a.ws_dt + ((int64_t)slot * a.heads + h) * kScanDt + 5 * Q;
-    const float maxb = a.ws_max[2 * sg], maxc = a.ws_max[2 * sg + 1];
-    const float cend = dts[0], maxdt = dts[1], maxf = dts[2];
+    // (from LDS: scalar loads here would hold up every wait for LDS)
+    const float* maxes = reinterpret_cast<const float*>(ldsX + (c & 1) * kMaxBytes);
+    const float maxb = maxes[0], maxc = maxes[1], cend = dtp[5 * Q], maxdt = dtp[5 * Q + 1], maxf = dtp[5 * Q + 2];
     if (!AHEAD) {
       load_raw(c);
       __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)

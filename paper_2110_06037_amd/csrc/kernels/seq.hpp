@@ -59,6 +59,7 @@ void linear4(const Linear4Args& a, hipStream_t st);
 constexpr int kScanChunk = 64;     // tokens per chunk
 constexpr int kScanUnits = 2048;   // waves that a pass is cut into segments for
 constexpr int kScanDtRow = 5 * kScanChunk + 16;  // floats per head and chunk of ws_dt
+constexpr int kScanMax = 4;                      // floats per group and chunk of ws_max
 constexpr int kScanS = 10 * 256;                 // floats per group and chunk of ws_s
 struct ScanArgs {
   int dtype, heads, dim, groups, state, conv, chans;  // dim: of a head
@@ -73,7 +74,7 @@ struct ScanArgs {
   void* ws_c;      // [slot][group] C of a chunk, 2 x 64 np f16 (scan_prep_kernel)
   void* ws_b;      // [slot][group] B of a chunk, likewise
   float* ws_s;     // [slot][group] C B^T, its 10 tiles on and below the diagonal
-  float* ws_max;   // [slot][group][2] largest sizes in B and C
+  float* ws_max;   // [slot][group][kScanMax] largest sizes in B and C
   float* ws_dt;    // [slot][head][kScanDtRow]: 64 each of the decay since the chunk's start, its log2 as
                    // hi and lo, the step size, the step size times the decay to the chunk's end; then
                    // the chunk's log2 decay and the largest of the step sizes and of the last array

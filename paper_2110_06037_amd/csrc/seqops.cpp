@@ -345,7 +345,7 @@ int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* c
       a.ws_c = op->alloc(slots * d.groups * Q * a.np * 4);
       a.ws_b = op->alloc(slots * d.groups * Q * a.np * 4);
       a.ws_s = floats(slots * d.groups * k::kScanS);
-      a.ws_max = floats(slots * d.groups * 2);
+      a.ws_max = floats(slots * d.groups * k::kScanMax);
       a.ws_dt = floats(slots * d.heads * k::kScanDtRow);
       // segments are made for fewer than kScanUnits units of at
       // most 32 columns, of at least two chunks each

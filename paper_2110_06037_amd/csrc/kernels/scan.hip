@@ -18,7 +18,6 @@
 // float32 sum would lose the differences of neighbours late in a chunk of
 // strong decays.
 #include "seq.hpp"
-#include <cstdlib>
 
 namespace sn {
 namespace k {
@@ -49,6 +48,12 @@ __device__ __forceinline__ Seq seq_of(const ScanArgs& a, int b) {
 // rows has at most floor((first + n) / 64) - floor(first / 64) + 1 chunks, so
 // slots of different sequences differ and stay below tokens / 64 + seqs + 1.
 __device__ __forceinline__ int slot0_of(int64_t first, int b) { return (int)(first / Q) + b; }
+
+// Likewise segment i of its sequence, of `per` chunks, has slot segment0 + i,
+// below (tokens / 64 + seqs) / per + seqs + 1.
+__device__ __forceinline__ int64_t segment0_of(const ScanArgs& a, int64_t first, int b) {
+  return slot0_of(first, b) / a.per + b;
+}
 
 // Raw value of channel ch at time t of a sequence: before 0 from the window,
 // past the end 0.
@@ -263,14 +268,15 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 }
 
 // ------------------------------------------------------------------ the heads
-// A wave owns 16 PT columns p of one head and all N <= 16 NT state rows n: the
-// state lives in PT NT accumulator tiles (lane: n = 16 nt + 4 (lane / 16) + v,
-// p = p0 + PT (lane % 16) + j), whose layout is also that of the second operand
+// A wave owns 16 columns p of one head and all N <= 16 NT state rows n: the
+// state lives in NT accumulator tiles (lane: n = 16 nt + 4 (lane / 16) + v, p =
+// p0 + lane % 16), whose layout is also that of the second operand
 // of the product with C, so the state never leaves the registers; and a lane's
 // convolution outputs (times 16 sb + 4 (lane / 16) + v, the same p) are the
 // second operand of both other products.
 // SEG: only the state that the segment adds (from zero), no outputs.
-// PT: 1, or 2 in 16-bit types with rows of x and y in whole aligned pairs.
+// SHARE: the four waves of 64 columns of a head make its mix of a chunk's rows
+// together.
 //
 // The waves of a workgroup share the group's C, B and S of a chunk in LDS, and
 // each has its head's decays there, all brought by LDS direct loads while the
@@ -284,8 +290,12 @@ template <int NT, bool SHARE, bool SEG>
 constexpr int scan_lds(int waves) {  // B, C, S, two sets of largest sizes, two decay rows per wave, the mix of every 4 waves
   return (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + 2 * kMaxBytes + waves * 2 * kDtBytes + (SHARE && !SEG ? waves / 4 * kMixBytes : 0);
 }
-template <typename T, int NT, int PT, bool SHARE, bool SEG>
+template <typename T, int NT, bool SHARE, bool SEG>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) {
+  // Columns per lane.  Two (waves of 32 columns) measured 129 us against 130 at
+  // 4096 tokens of 64 heads, but 437 against 351 at 8 sequences of 2048: fewer
+  // waves, and no registers left for the rows ahead.
+  constexpr int PT = 1;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   char* const ldsB = smem;
   char* const ldsC = smem + 4096 * NT;                    // not with SEG
@@ -293,9 +303,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   const int waves = blockDim.x >> 6;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
-  // segments and sequences vary fastest over the workgroups, so that (with 8 of
-  // them or a multiple) each XCD's L2 serves the chunks of its own segments
-  const int b = blockIdx.x / a.segs, seg = blockIdx.x % a.segs;
+  // sequences and segments vary fastest over the workgroups, so that (with 8 of
+  // them or a multiple) each XCD's L2 serves the chunks of its own; sequences
+  // first: the first segments, which all have, spread over the XCDs
+  const int b = blockIdx.x % a.seqs, seg = blockIdx.x / a.seqs;
   const int each = a.heads / a.groups, pblocks = (a.dim + 16 * PT - 1) / (16 * PT);
   const int ublocks = (each * pblocks + waves - 1) / waves;
   const int grp = blockIdx.y / ublocks, unit_ = (blockIdx.y % ublocks) * waves + wave;
@@ -306,8 +317,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   char* const ldsX = smem + (SEG ? 4096 * NT : 8192 * NT + 10 * 1024);
   char* const ldsD = ldsX + 2 * kMaxBytes + wave * 2 * kDtBytes;
   const Seq s = seq_of(a, b);
-  const int nc = (s.len + Q - 1) / Q, per = (nc + a.segs - 1) / a.segs;
-  const int c0 = min(seg * per, nc), c1 = min(c0 + per, nc);
+  const int nc = (s.len + Q - 1) / Q;
+  const int c0 = min(seg * a.per, nc), c1 = min(c0 + a.per, nc);
   const int N = a.state;
   constexpr int NP = 16 * NT;
 
@@ -367,7 +378,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
           }
         }
   };
-  float* segst = a.ws_seg + (((int64_t)b * a.segs + seg) * a.heads + h) * hold;
+  const int64_t head_seg = (segment0_of(a, s.first, b) + seg) * a.heads + h;
+  float* segst = a.ws_seg + head_seg * hold;
   // per column: at least the size of every value of the state (within a few
   // powers of two).  Scales are a column's own, so no column's values have a
   // part in another's.
@@ -376,7 +388,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     v = fmaxf(v, __shfl_xor(v, 16));
     return fmaxf(v, __shfl_xor(v, 32));
   };
-  if (SEG && c1 >= nc) return;  // nothing follows: no one reads this segment's state
+  // the whole workgroup: a segment that nothing follows (no one reads its
+  // state), or behind the sequence's last one (which has no slot)
+  if (SEG ? c1 >= nc : seg > 0 && c0 >= nc) return;
   // the lane's convolution
   const int ch0 = h * a.dim + p0;
   float w[4][PT], cb[PT];
@@ -427,7 +441,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
         const bool before = sb == 0 && k < 3 && c == 0 && g == 0;
         const unsigned row = xo + (16 * sb + k) * rowb;  // in the offset that the range check sees
         const unsigned o = before || pn < PT ? kOOB : row;
-        if constexpr (sizeof(T) * PT == 2) {
+        if constexpr (sizeof(T) == 2) {
           const uint16_t v = __builtin_amdgcn_raw_buffer_load_b16(rx, (int)o, 0, 0);
           __builtin_memcpy(raw[sb][k], &v, 2);
         } else {
@@ -436,17 +450,15 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
         }
       }
   };
-  // The next chunk's raw rows are loaded a chunk ahead, where registers allow.
-  constexpr bool AHEAD = PT == 1;
   // Accesses of a chunk that follow its loads of the next chunk's C and decays:
   // the raw rows, and the stores of y.
-  constexpr int AFTER = (AHEAD ? 28 : 0) + (SEG ? 0 : 16);
+  constexpr int AFTER = 28 + (SEG ? 0 : 16);
   if (c0 < c1) fetch_c(c0), fetch_b(c0);
   if (!SEG) {
     if (a.segs > 1) load_state(segst);
     else if (a.state_in) load_state(a.state_in + ((int64_t)b * a.heads + h) * hold);
   }
-  if (AHEAD) load_raw(c0);
+  load_raw(c0);
   if (!SEG) {
 #pragma unroll
     for (int j = 0; j < PT; ++j) {
@@ -468,10 +480,6 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     // (from LDS: scalar loads here would hold up every wait for LDS)
     const float* maxes = reinterpret_cast<const float*>(ldsX + (c & 1) * kMaxBytes);
     const float maxb = maxes[0], maxc = maxes[1], cend = dtp[5 * Q], maxdt = dtp[5 * Q + 1], maxf = dtp[5 * Q + 2];
-    if (!AHEAD) {
-      load_raw(c);
-      __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
-    }
     f32x4 acc[4][PT];
     if constexpr (!SEG) {
       // ---- C times the state in front of the chunk
@@ -577,7 +585,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     wait_vmcnt<0>();
     dma_barrier();
     if (c + 1 < c1) fetch_c(c + 1);
-    if (AHEAD) load_raw(c + 1);
+    load_raw(c + 1);
     if (t0 + Q > s.len) {  // past the end: zero (a NaN would meet the zeros of earlier rows)
 #pragma unroll
       for (int sb = 0; sb < 4; ++sb)
@@ -624,7 +632,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       }
       su[j] = pow2_for(maxu[j]);
     }
-    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
     if constexpr (!SEG) {
       // ---- earlier rows of the chunk, the row itself and the skip term
       // from C h's scale to this product's, with the decay since the chunk's start
@@ -689,7 +697,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
           for (int j = 0; j < PT; ++j) o[j] = from_f<T>(acc[tb][j][v] * back[j]);
           const unsigned off = yo + (16 * tb + v) * yrow;
           const int to_ = (int)(pn > 0 ? off : kOOB);
-          if constexpr (sizeof(T) * PT == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, o), ry, to_, 0, 0);
+          if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, o), ry, to_, 0, 0);
           else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o), ry, to_, 0, 0);
         }
     }
@@ -751,7 +759,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   }
   if (SEG) {
     store_state(segst);
-    if (lane == 0 && live && unit % pblocks == 0) a.ws_decay[((int64_t)b * a.segs + seg) * a.heads + h] = total;
+    if (lane == 0 && live && unit % pblocks == 0) a.ws_decay[head_seg] = total;
   } else if (a.state_out && (c1 == nc && (c0 < c1 || seg == 0))) {
     // the segment with the sequence's last chunk (segment 0 of a sequence without rows)
     store_state(a.state_out + ((int64_t)b * a.heads + h) * hold);
@@ -764,13 +772,16 @@ __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
   const int64_t hold = (int64_t)a.dim * a.state, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int b = blockIdx.z, h = blockIdx.y;
   if (e >= hold) return;
-  const int nc = (seq_of(a, b).len + Q - 1) / Q, per = (nc + a.segs - 1) / a.segs;
+  const Seq s = seq_of(a, b);
+  const int nc = (s.len + Q - 1) / Q;
+  const int64_t seg0 = segment0_of(a, s.first, b);
   float v = a.state_in ? a.state_in[((int64_t)b * a.heads + h) * hold + e] : 0.f;
-  for (int i = 0; i < a.segs; ++i) {
-    float* p = a.ws_seg + (((int64_t)b * a.segs + i) * a.heads + h) * hold + e;
-    const bool more = (i + 1) * per < nc;  // another segment follows with chunks of its own
+  for (int i = 0;; ++i) {
+    const int64_t at = (seg0 + i) * a.heads + h;
+    float* p = a.ws_seg + at * hold + e;
+    const bool more = (i + 1) * a.per < nc;  // another segment follows
     float add = 0.f, f = 0.f;
-    if (more) add = *p, f = __builtin_amdgcn_exp2f(a.ws_decay[((int64_t)b * a.segs + i) * a.heads + h]);
+    if (more) add = *p, f = __builtin_amdgcn_exp2f(a.ws_decay[at]);
     *p = v;
     if (!more) return;
     v = fmaf(v, f, add);
@@ -894,25 +905,25 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int L, int s
 }
 
 // ------------------------------------------------------------------ launchers
-template <typename T, int NT, int PT, bool SHARE>
+template <typename T, int NT, bool SHARE>
 static void launch_main(const ScanArgs& a, hipStream_t st) {
-  const int units = a.heads / a.groups * ((a.dim + 16 * PT - 1) / (16 * PT)), waves = std::min(kScanWaves, units);
+  const int units = a.heads / a.groups * ((a.dim + 15) / 16), waves = std::min(kScanWaves, units);
   const dim3 grid(a.segs * a.seqs, a.groups * ((units + waves - 1) / waves));
   if (a.segs > 1) {
     // half the waves: three of its workgroups fit a CU
     const int ws = std::min(4, units);
     const dim3 gs(a.segs * a.seqs, a.groups * ((units + ws - 1) / ws));
-    SN_LAUNCH((scan_main_kernel<T, NT, PT, false, true>), gs, dim3(64 * ws), (scan_lds<NT, false, true>(ws)), st, a);
+    SN_LAUNCH((scan_main_kernel<T, NT, false, true>), gs, dim3(64 * ws), (scan_lds<NT, false, true>(ws)), st, a);
     SN_LAUNCH((scan_carry_kernel), dim3((a.dim * a.state + 255) / 256, a.heads, a.seqs), dim3(256), 0, st, a);
   }
-  SN_LAUNCH((scan_main_kernel<T, NT, PT, SHARE, false>), grid, dim3(64 * waves), (scan_lds<NT, SHARE, false>(waves)), st, a);
+  SN_LAUNCH((scan_main_kernel<T, NT, SHARE, false>), grid, dim3(64 * waves), (scan_lds<NT, SHARE, false>(waves)), st, a);
 }
-template <typename T, int PT, bool SHARE>
-static void launch_cols(const ScanArgs& a, hipStream_t st) {
-  if (a.np == 32) launch_main<T, 2, PT, SHARE>(a, st);
-  else if (a.np == 64) launch_main<T, 4, PT, SHARE>(a, st);
-  else if (a.np == 128) launch_main<T, 8, PT, SHARE>(a, st);
-  else if constexpr (PT == 1 && !SHARE) launch_main<T, 16, PT, SHARE>(a, st);
+template <typename T, bool SHARE>
+static void launch_np(const ScanArgs& a, hipStream_t st) {
+  if (a.np == 32) launch_main<T, 2, SHARE>(a, st);
+  else if (a.np == 64) launch_main<T, 4, SHARE>(a, st);
+  else if (a.np == 128) launch_main<T, 8, SHARE>(a, st);
+  else if constexpr (!SHARE) launch_main<T, 16, SHARE>(a, st);
 }
 
 template <typename T>
@@ -925,12 +936,11 @@ static void launch_scan(ScanArgs a, hipStream_t st) {
   else if (a.np == 64) SN_LAUNCH((scan_prep_kernel<T, 64>), grid, dim3(kPrep), lds, st, a);
   else if (a.np == 128) SN_LAUNCH((scan_prep_kernel<T, 128>), grid, dim3(kPrep), lds, st, a);
   else SN_LAUNCH((scan_prep_kernel<T, 256>), grid, dim3(kPrep), lds, st, a);
-  if constexpr (sizeof(T) == 2) {
-    if (a.cols == 32) return launch_cols<T, 2, false>(a, st);
-  }
-  // with 64 columns per head or a multiple, four waves of one share its mix
-  if ((a.dim + 15) / 16 % 4 == 0 && a.np <= 128) launch_cols<T, 1, true>(a, st);
-  else launch_cols<T, 1, false>(a, st);
+  // with 64 columns per head or a multiple, four waves of one share its mix (70
+  // us against 81 for the second pass over 4096 tokens of 64 heads); beside 256
+  // state rows LDS has no room for it
+  if ((a.dim + 15) / 16 % 4 == 0 && a.np <= 128) launch_np<T, true>(a, st);
+  else launch_np<T, false>(a, st);
 }
 
 template <typename T>
@@ -942,22 +952,18 @@ static void launch_step(ScanArgs a, hipStream_t st) {
   SN_LAUNCH((scan_step_kernel<T>), dim3((unsigned)(a.heads * splits), a.seqs), dim3(256), 0, st, a, L, splits);
 }
 
-// Columns per wave and segments.  A wave of 32 columns does less per column
-// (the products' masks and decays are a head's, not a column's), one of 16
-// makes more waves of a short call and leaves room for 256 state rows.
+// Segments: as many chunks to each as leave kScanUnits waves, at least two (a
+// segment's chunks but the last one's are read twice, and its state is written
+// and read); one if there are more waves anyhow, or the states found no room.
 static void scan_split(ScanArgs& a) {
-  const int64_t chunks = (a.tokens + Q - 1) / Q;  // the most that one sequence may have
-  auto units = [&](int cols) { return (int64_t)a.seqs * a.heads * ((a.dim + cols - 1) / cols); };
-  // waves of a pass: segments until about kScanUnits run, each of at least two chunks
-  auto segs = [&](int cols) {
-    return std::max<int64_t>(1, std::min((kScanUnits + units(cols) - 1) / units(cols), chunks / 2));
-  };
-  const int e = a.dtype == 0 ? 4 : 2;
-  auto pairs = [&](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride % 2 == 0; };
-  const bool can = e == 2 && a.np <= 128 && a.dim % 2 == 0 && pairs(a.x, a.xs) && pairs(a.y, a.ys);
-  a.cols = can && units(32) * segs(32) >= kScanUnits ? 32 : 16;
-  if (getenv("SCOLS") && can) a.cols = atoi(getenv("SCOLS"));
-  a.segs = (int)segs(a.cols);
+  a.each = a.tokens / a.seqs;
+  const int64_t slots = scan_slots(a.tokens, a.seqs), units = (int64_t)a.heads * ((a.dim + 15) / 16);
+  const int64_t chunks = ((a.offsets ? a.tokens : a.each) + Q - 1) / Q;  // the most that one sequence may have
+  const int64_t hold = (int64_t)a.heads * a.dim * a.state;
+  int64_t per = std::max<int64_t>(2, ((a.tokens + Q - 1) / Q * units + kScanUnits - 1) / kScanUnits);
+  while (per < chunks && scan_segment_slots(slots, a.seqs, (int)per) * hold > a.seg_cap) ++per;
+  a.per = (int)std::max<int64_t>(1, std::min(per, chunks));
+  a.segs = (int)std::max<int64_t>(1, (chunks + a.per - 1) / a.per);
 }
 
 void scan_run(const ScanArgs& in, hipStream_t st) {
@@ -966,8 +972,6 @@ void scan_run(const ScanArgs& in, hipStream_t st) {
             a.conv >= 1 && a.conv <= 4 && a.seqs >= 1 && a.seqs <= 65535 && a.tokens >= 0,
         "scan shapes");
   scan_split(a);
-  a.each = a.tokens / a.seqs;
-  check(a.segs == 1 || a.seqs * (int64_t)a.segs * a.heads * a.dim * a.state <= a.seg_cap, "scan segments");
   if (a.dtype == 0) launch_scan<float>(a, st);
   else if (a.dtype == 1) launch_scan<f16>(a, st);
   else launch_scan<bf16>(a, st);

@@ -78,13 +78,14 @@ struct ScanArgs {
   float* ws_dt;    // [slot][head][kScanDtRow]: 64 each of the decay since the chunk's start, its log2 as
                    // hi and lo, the step size, the step size times the decay to the chunk's end; then
                    // the chunk's log2 decay and the largest of the step sizes and of the last array
-  float* ws_seg;   // [seq][segment][head][dim][state]
-  float* ws_decay; // [seq][segment][head]
+  float* ws_seg;   // [segment slot][head][dim][state]
+  float* ws_decay; // [segment slot][head]
   void* wcopy;     // [seq][conv - 1][chans]    the window before the call
   unsigned* count; // [seq][group], zero between calls
   int64_t seg_cap; // elements of ws_seg
   // call
-  int seqs, segs, cols;  // segments per sequence and columns per wave are set by the launcher
+  int seqs;
+  int segs, per;  // segments of the longest sequence, chunks of a segment (set by the launcher)
   int64_t each;  // rows per sequence without offsets (set by the launcher)
   int64_t tokens;
   const int32_t* offsets;
@@ -102,6 +103,7 @@ struct ScanArgs {
 };
 inline int scan_np(int state) { return state <= 32 ? 32 : state <= 64 ? 64 : state <= 128 ? 128 : 256; }
 inline int64_t scan_slots(int64_t tokens, int seqs) { return tokens / kScanChunk + seqs + 1; }
+inline int64_t scan_segment_slots(int64_t slots, int seqs, int per) { return slots / per + seqs + 1; }
 void scan_run(const ScanArgs& a, hipStream_t st);
 void scan_step(const ScanArgs& a, hipStream_t st);
 

@@ -347,13 +347,12 @@ int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* c
       a.ws_s = floats(slots * d.groups * k::kScanS);
       a.ws_max = floats(slots * d.groups * k::kScanMax);
       a.ws_dt = floats(slots * d.heads * k::kScanDtRow);
-      // segments are made for fewer than kScanUnits units of at
-      // most 32 columns, of at least two chunks each
-      const int64_t pairs = std::max<int64_t>(1, (d.max_tokens + Q - 1) / Q / 2);
-      a.seg_cap = std::min(int64_t(2) * k::kScanUnits * 32 * d.state,
-                           d.max_seqs * pairs * d.heads * d.head_dim * d.state);
+      // segments' states: kScanUnits waves of 16 columns and as much again for
+      // the sequences' last ones, if calls can be so long (two chunks at least)
+      const int64_t hold = (int64_t)d.heads * d.head_dim * d.state, most = k::scan_segment_slots(slots, d.max_seqs, 2);
+      a.seg_cap = std::min(int64_t(2) * k::kScanUnits * 16 * d.state, most * hold);
       a.ws_seg = floats(a.seg_cap);
-      a.ws_decay = floats(2 * k::kScanUnits);
+      a.ws_decay = floats(std::max<int64_t>(1, a.seg_cap / hold) * d.heads);
       a.wcopy = op->alloc(d.max_seqs * (d.conv - 1) * chans * dtype_size(d.dtype));
       const size_t counters = (size_t)d.max_seqs * d.groups * sizeof(unsigned);
       a.count = static_cast<unsigned*>(op->alloc(counters));

@@ -93,11 +93,21 @@ struct HiLo {
 };
 __device__ __forceinline__ HiLo split8(const float (&v)[8]) {
   HiLo r;
+  u32x4 h;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    r.hi[i] = (f16)v[i];
-    r.lo[i] = (f16)(v[i] - (float)r.hi[i]);
+  for (int i = 0; i < 4; ++i) {
+    typedef f16 f16x2 __attribute__((ext_vector_type(2)));
+    h[i] = __builtin_bit_cast(unsigned, f16x2{(f16)v[2 * i], (f16)v[2 * i + 1]});
+    // lo is taken from the packed halves as they are: the compiler may fold the
+    // product that makes v into one conversion of two (one rounding instead of
+    // two), and near a tie hi and the hi that lo completes would differ
+    unsigned one = h[i];
+    asm("" : "+v"(one));
+    h[i] = one;
   }
+  r.hi = __builtin_bit_cast(f16x8, h);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.lo[i] = (f16)(v[i] - (float)r.hi[i]);
   return r;
 }
 __device__ __forceinline__ f32x4 mul3(const HiLo& a, const HiLo& b, f32x4 c) {

@@ -155,6 +155,19 @@ def test_long_sequences_in_segments(dtype, lens):
     once(dtype, lens, heads=4, dim=64, state=64)
 
 
+@pytest.mark.parametrize("dtype,lens,conv", [("f16", [1, 79], 2), ("f32", [42, 2, 9, 28], 4), ("bf16", [157, 73], 3)])
+def test_the_state_has_float32_precision_throughout(dtype, lens, conv):
+    # A term's dozen roundings of at most 2^-24 each, uniform and independent,
+    # have a root mean square of sqrt(12 / 3) = 2 of 2^-24, and a sum's errors
+    # add like their squares: 4 of 2^-24 of the sizes in the mean over all
+    # elements leaves a factor of 2 -- and shows a few terms of 11 bits among
+    # many of 24, which the bound for single elements does not.
+    c = Case(dtype, lens, heads=8, dim=64, state=128, conv=conv, first=False, seed=11)
+    _, _, h, _, size = c.exact()
+    err = host(c.run(c.op())[2]) - h
+    assert np.linalg.norm(err) <= 4 * 2.0 ** -24 * np.linalg.norm(size)
+
+
 @pytest.mark.parametrize("step,rate", [((1e-6, 1e-5), (1e-3, 1e-2)), ((0.5, 4), (4, 16)), ((20, 60), (16, 64)),
                                        ((1e-3, 0.1), (0, 0))])
 def test_decays_from_none_to_vanishing(step, rate):

@@ -44,6 +44,7 @@ class _Op:
         self.torch_dtype = self._types[self.dtype]
         self.device = device
         self._dev = torch.device("cuda", device) if device >= 0 else None
+        self._current = torch.cuda.current_stream
 
     def close(self):
         if getattr(self, "_op", None):
@@ -62,23 +63,25 @@ class _Op:
     def __exit__(self, *exc):
         self.close()
 
-    def _rows(self, t, name, shape, dtype=None):
-        """The row stride of a device tensor [rows, n] that a kernel may use as it is."""
-        if t.dtype != (dtype or self.torch_dtype):
-            raise TypeError(f"{name} is {t.dtype}, not {dtype or self.torch_dtype}")
-        if t.shape != shape:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-        if t.device != self._dev:
-            raise ValueError(f"{name} is on {t.device}, the handle on {self._dev}")
-        s = t.stride()
-        if s[1] != 1 and shape[1] > 1 and shape[0]:
+    def _rows(self, t, name, rows, cols, dtype):
+        """The row stride of a device tensor [rows, cols] that a kernel may use
+        as it is.  (A call of a small operator is a few microseconds: the one
+        test that all sound tensors pass comes first.)"""
+        if t.dtype is dtype and t.get_device() == self.device and t.shape == (rows, cols):
+            s, e = t.stride()
+            if e == 1 or cols <= 1 or not rows:
+                return s if rows > 1 else cols
             raise ValueError(f"the elements of a row of {name} are not contiguous")
-        return s[0] if shape[0] > 1 else shape[1]
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+        if t.shape != (rows, cols):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {(rows, cols)}")
+        raise ValueError(f"{name} is on {t.device}, the handle on {self._dev}")
 
     def _stream(self, stream, tensors):
         """The stream's pointer; on another stream than the current one the
         tensors' memory is kept from reuse until its work is done."""
-        cur = self._torch.cuda.current_stream(self._dev)
+        cur = self._current(self.device)
         if stream is None:
             return cur.cuda_stream
         if isinstance(stream, int):
@@ -148,21 +151,20 @@ class Linear4(_Op):
         N.check(self.lib.sn_linear4_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data,
                                            None if zero is None else zero.ctypes.data, _fp(bias), device,
                                            ctypes.byref(p)))
-        self._op = p
+        self._op, self._run = p, self.lib.sn_linear4_run
 
     def run(self, x, out=None, stream=None):
         """Enqueue on x [m, cols]; returns y [m, rows]."""
-        shape = x.shape
-        if len(shape) != 2 or shape[1] != self.cols:
-            raise ValueError(f"x has shape {tuple(shape)}, not [m, {self.cols}]")
-        xs = self._rows(x, "x", shape)
-        shape = (shape[0], self.rows)
+        m = x.shape[0]
+        xs = self._rows(x, "x", m, self.cols, self.torch_dtype)
         if out is None:
-            out, ys = self._torch.empty(shape, dtype=self.torch_dtype, device=x.device), self.rows
+            out, ys = x.new_empty((m, self.rows)), self.rows
         else:
-            ys = self._rows(out, "out", shape)
+            ys = self._rows(out, "out", m, self.rows, self.torch_dtype)
         st = self._stream(stream, (x, out))
-        N.check(self.lib.sn_linear4_run(self._op, shape[0], x.data_ptr(), xs, out.data_ptr(), ys, st))
+        rc = self._run(self._op, m, x.data_ptr(), xs, out.data_ptr(), ys, st)
+        if rc:
+            N.check(rc)
         return out
 
 
@@ -202,37 +204,39 @@ class Scan(_Op):
         p = ctypes.c_void_p()
         N.check(self.lib.sn_scan_create(ctypes.byref(desc), *[_fp(v) for v in arrays], device, ctypes.byref(p)))
         self._op = p
+        self._io = N.ScanIO()  # one call's arguments: filled anew by every call
+        self._io_ref = ctypes.byref(self._io)
 
     def _whole(self, t, name, shape, dtype):
-        if t.shape != shape or t.dtype != dtype or t.device != self._dev or not t.is_contiguous():
-            raise ValueError(f"{name} is not a contiguous {dtype} tensor {tuple(shape)} on {self._dev}")
-        return t.data_ptr()
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self.device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name} is not a contiguous {dtype} tensor {tuple(shape)} on {self._dev}")
 
     def _call(self, f, x, dt, window, state, window_out, state_out, seqs, offsets, out, stream):
-        torch = self._torch
-        tokens = x.shape[0]
-        io = N.ScanIO()
+        tokens, kind, f32 = x.shape[0], self.torch_dtype, self._torch.float32
+        io = self._io
         io.seqs, io.tokens = seqs, tokens
-        io.x_stride, io.x = self._rows(x, "x", (tokens, self.chans)), x.data_ptr()
-        io.dt_stride, io.dt = self._rows(dt, "dt", (tokens, self.heads)), dt.data_ptr()
+        io.x_stride, io.x = self._rows(x, "x", tokens, self.chans, kind), x.data_ptr()
+        io.dt_stride, io.dt = self._rows(dt, "dt", tokens, self.heads, kind), dt.data_ptr()
         wshape, sshape = (seqs, self.conv - 1, self.chans), (seqs, self.heads, self.head_dim, self.state)
-        if window is not None:
-            io.window = self._whole(window, "window", wshape, self.torch_dtype)
-        if state is not None:
-            io.state = self._whole(state, "state", sshape, torch.float32)
-        if offsets is not None:
-            io.offsets = self._whole(offsets, "offsets", (seqs + 1,), torch.int32)
+        io.window = None if window is None else self._whole(window, "window", wshape, kind)
+        io.state = None if state is None else self._whole(state, "state", sshape, f32)
+        io.offsets = None if offsets is None else self._whole(offsets, "offsets", (seqs + 1,), self._torch.int32)
         if out is None:
-            out = torch.empty((tokens, self.inner), dtype=self.torch_dtype, device=x.device)
-        io.y_stride, io.y = self._rows(out, "out", (tokens, self.inner)), out.data_ptr()
+            out = x.new_empty((tokens, self.inner))
+            io.y_stride, io.y = self.inner, out.data_ptr()
+        else:
+            io.y_stride, io.y = self._rows(out, "out", tokens, self.inner, kind), out.data_ptr()
         if window_out is None:
-            window_out = torch.empty(wshape, dtype=self.torch_dtype, device=x.device)
+            window_out = x.new_empty(wshape)
         if state_out is None:
-            state_out = torch.empty(sshape, dtype=torch.float32, device=x.device)
-        io.window_out = self._whole(window_out, "window_out", wshape, self.torch_dtype)
-        io.state_out = self._whole(state_out, "state_out", sshape, torch.float32)
+            state_out = x.new_empty(sshape, dtype=f32)
+        io.window_out = self._whole(window_out, "window_out", wshape, kind)
+        io.state_out = self._whole(state_out, "state_out", sshape, f32)
         st = self._stream(stream, (x, dt, window, state, offsets, out, window_out, state_out))
-        N.check(f(self._op, ctypes.byref(io), st))
+        rc = f(self._op, self._io_ref, st)
+        if rc:
+            N.check(rc)
         return out, window_out, state_out
 
     def run(self, x, dt, window=None, state=None, window_out=None, state_out=None, seqs=None, offsets=None, out=None,
@@ -282,30 +286,34 @@ class BlockNorm(_Op):
                        1.0 if scale is None or vector else float(scale))
         p = ctypes.c_void_p()
         N.check(self.lib.sn_norm_create(ctypes.byref(d), *[_fp(a) for a in arrays], device, ctypes.byref(p)))
-        self._op = p
+        self._op, self._run = p, self.lib.sn_norm_run
 
     def run(self, x, gate=None, residual=None, out=None, res_out=None, stream=None):
         """Enqueue on x [rows, dim]; returns (y, res_out), None for the one that
         the handle does not have.  ``out`` may be x and ``res_out`` residual."""
-        shape = x.shape
-        if len(shape) != 2 or shape[1] != self.dim:
-            raise ValueError(f"x has shape {tuple(shape)}, not [rows, {self.dim}]")
-        xs = self._rows(x, "x", shape)
+        rows, dim, kind = x.shape[0], self.dim, self.torch_dtype
+        xs = self._rows(x, "x", rows, dim, kind)
         gp = gs = rp = rs = op = os = yp = ys = 0
         if gate is not None:
-            gp, gs = gate.data_ptr(), self._rows(gate, "gate", shape)
-        if residual is not None:
-            if self.res_dtype is None:
-                raise ValueError("a residual given to a handle without one")
-            rp, rs = residual.data_ptr(), self._rows(residual, "residual", shape, self.res_dtype)
+            gp, gs = gate.data_ptr(), self._rows(gate, "gate", rows, dim, kind)
         if self.res_dtype is not None:
+            if residual is not None:
+                rp, rs = residual.data_ptr(), self._rows(residual, "residual", rows, dim, self.res_dtype)
             if res_out is None:
-                res_out = self._torch.empty(shape, dtype=self.res_dtype, device=x.device)
-            op, os = res_out.data_ptr(), self._rows(res_out, "res_out", shape, self.res_dtype)
+                res_out, os = x.new_empty((rows, dim), dtype=self.res_dtype), dim
+            else:
+                os = self._rows(res_out, "res_out", rows, dim, self.res_dtype)
+            op = res_out.data_ptr()
+        elif residual is not None:
+            raise ValueError("a residual given to a handle without one")
         if self.has_y:
             if out is None:
-                out = self._torch.empty(shape, dtype=self.torch_dtype, device=x.device)
-            yp, ys = out.data_ptr(), self._rows(out, "out", shape)
+                out, ys = x.new_empty((rows, dim)), dim
+            else:
+                ys = self._rows(out, "out", rows, dim, kind)
+            yp = out.data_ptr()
         st = self._stream(stream, (x, gate, residual, out, res_out))
-        N.check(self.lib.sn_norm_run(self._op, shape[0], x.data_ptr(), xs, gp, gs, rp, rs, op, os, yp, ys, st))
+        rc = self._run(self._op, rows, x.data_ptr(), xs, gp, gs, rp, rs, op, os, yp, ys, st)
+        if rc:
+            N.check(rc)
         return out, res_out

@@ -1,0 +1,98 @@
+"""A net of gated sequence blocks on the GPU: all operators together against
+the same net in 64 bits, prompts against tokens one by one, packed prompts
+against single ones, and captured steps against eager ones."""
+
+import numpy as np
+import pytest
+
+from paper_2110_06037_amd import SequenceNet
+from tests.gpu_util import TOL
+from tests.seq_util import device, host, rounded
+from workloads.sequence import sequence_config, sequence_weights
+
+pytestmark = pytest.mark.gpu
+CONFIG = sequence_config(dim=96, heads=4, head_dim=40, groups=2, state=24, conv=4, group=32)
+
+
+def dense(p, cols, group):
+    q, scale, zero = p
+    code = np.stack([q & 15, q >> 4], -1).reshape(q.shape[0], -1)[:, :cols].astype(np.float64)
+    at = np.arange(cols) // group
+    return (code - (8.0 if zero is None else zero[:, at])) * scale[:, at].astype(np.float64)
+
+
+def silu(v):
+    return v / (1 + np.exp(-v))
+
+
+def norm(v, w, groups=1):
+    g = v.reshape(v.shape[0], groups, -1)
+    return (g / np.sqrt((g * g).mean(-1, keepdims=True) + 1e-5)).reshape(v.shape) * w
+
+
+def exact(weights, x):
+    """One sequence from zeros, in 64 bits without any rounding between the operators."""
+    h, u = x, norm(x, weights["norm"].astype(np.float64))
+    for w in weights["blocks"]:
+        c = w["config"]
+        H, P, G, S = c["heads"], c["head_dim"], c["groups"], c["state"]
+        inner, chans = H * P, H * P + 2 * G * S
+        p = u @ dense(w["in_proj"], c["dim"], c["group"]).T
+        z, raw, dt = p[:, :inner], p[:, inner:inner + chans], np.logaddexp(0, p[:, inner + chans:] + w["dt_bias"])
+        pad = np.concatenate([np.zeros((c["conv"] - 1, chans)), raw])
+        v = silu(sum(pad[j:j + len(x)] * w["conv_w"][:, j] for j in range(c["conv"])) + w["conv_b"])
+        X = v[:, :inner].reshape(-1, H, P)
+        B, C = (v[:, inner + i * G * S:inner + (i + 1) * G * S].reshape(-1, G, S).repeat(H // G, 1) for i in (0, 1))
+        s, y = np.zeros((H, P, S)), np.zeros((len(x), inner))
+        for t in range(len(x)):
+            s = s * np.exp(dt[t] * w["a"])[:, None, None] + (dt[t][:, None] * X[t])[..., None] * B[t][:, None]
+            y[t] = ((s * C[t][:, None]).sum(-1) + w["d"][:, None] * X[t]).reshape(-1)
+        o = norm(y * silu(z), w["gate_norm"], G) @ dense(w["out_proj"], inner, c["group"]).T
+        h = h + w["scale"] * o
+        u = norm(h, w["norm"].astype(np.float64))
+    return u
+
+
+def off(a, b):
+    return float(np.linalg.norm(a - b) / np.linalg.norm(b))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_prompts_and_tokens_against_64_bits(dtype):
+    weights = sequence_weights(CONFIG, 2, seed=3)
+    r = np.random.default_rng(4)
+    xs = [rounded(r.standard_normal((n, 96)), dtype) for n in (70, 1, 33)]
+    want = [exact(weights, x) for x in xs]
+    net = SequenceNet(dtype, weights, max_seqs=3, max_tokens=104)
+    import torch
+    # packed prompts
+    state = net.new_state(3)
+    offsets = torch.tensor([0, 70, 71, 104], dtype=torch.int32, device="cuda")
+    got = host(net.run(device(np.concatenate(xs), dtype), state, offsets))
+    for g, w in zip(np.split(got, [70, 71]), want):
+        assert off(g, w) <= TOL[dtype]
+    # a prompt, then tokens
+    state = net.new_state(1)
+    x = device(xs[0], dtype)
+    parts = [net.run(x[:50], state)] + [net.step(x[t:t + 1], state) for t in range(50, 70)]
+    assert off(host(torch.cat(parts)), want[0]) <= TOL[dtype]
+    net.close()
+
+
+def test_captured_steps_equal_eager_ones():
+    import torch
+    weights = sequence_weights(CONFIG, 3, seed=5, zero=False)
+    net = SequenceNet("bf16", weights, max_seqs=2, max_tokens=16)
+    eager, captured = net.new_state(2), net.new_state(2)
+    x = torch.randn(16, 96, device="cuda").bfloat16()
+    net.run(x, eager), net.run(x, captured)
+    token, out, replay = net.capture_step(captured)
+    for _ in range(4):
+        t = torch.randn(2, 96, device="cuda").bfloat16()
+        token.copy_(t)
+        replay()
+        want = net.step(t, eager)
+        torch.cuda.synchronize()
+        assert torch.equal(want, out)
+    assert all(torch.equal(a, b) for a, b in zip(eager.states + eager.windows, captured.states + captured.windows))
+    net.close()

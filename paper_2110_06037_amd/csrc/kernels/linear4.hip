@@ -201,7 +201,7 @@ struct Op4 {
 // row 4 v + g of x, so that up to 4 rows have all their sums in element v = 0
 // (MV = 1); in float32 v is the part and g the row.
 template <typename T, int NB, int MV, int GS, bool VX, int R, int U>
-__global__ __launch_bounds__(512) void linear4_rows_kernel(Linear4Args a) {
+__global__ __launch_bounds__(R == 1 && NB < 4 ? 1024 : 512) void linear4_rows_kernel(Linear4Args a) {
   typedef typename Op4<T>::E E;
   typedef typename Op4<T>::frag frag;
   constexpr bool F32 = std::is_same<T, float>::value;
@@ -609,7 +609,8 @@ template <typename T, int NB, int MV, int GS, bool VX, int R, int U>
 static void launch_rows_u(const Linear4Args& a, hipStream_t st) {
   constexpr int PER = std::is_same<T, float>::value ? 4 : 4 * MV, NV = std::is_same<T, float>::value ? 1 : MV;
   const int cbs = (a.cols + 127) / 128;
-  const int waves = std::min(8, (cbs + U - 1) / U);
+  // one row of blocks per workgroup: few features, so more waves for each
+  const int waves = std::min(R == 1 && NB < 4 ? 16 : 8, (cbs + U - 1) / U);
   const dim3 grid((a.rows + 16 * R - 1) / (16 * R), (unsigned)((a.m + NB * PER - 1) / (NB * PER)));
   SN_LAUNCH((linear4_rows_kernel<T, NB, MV, GS, VX, R, U>), grid, dim3(64 * waves), waves * R * NB * NV * 256, st, a);
 }
@@ -620,7 +621,7 @@ static void launch_rows(const Linear4Args& a, hipStream_t st) {
   if constexpr (VX) {
     constexpr int U = NB == 1 ? 2 : 1;
     const int rbs = (a.rows + 15) / 16;
-    if (rbs >= (NB == 1 ? 1024 : 512)) return launch_rows_u<T, NB, MV, GS, VX, 4, U>(a, st);
+    if (rbs >= (NB == 1 ? 1024 : 512)) return launch_rows_u<T, NB, MV, GS, VX, NB == 4 ? 2 : 4, U>(a, st);
     if (rbs >= 512) return launch_rows_u<T, NB, MV, GS, VX, 2, U>(a, st);
   }
   launch_rows_u<T, NB, MV, GS, VX, 1, 1>(a, st);

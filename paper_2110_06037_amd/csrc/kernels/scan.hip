@@ -127,9 +127,9 @@ __device__ __forceinline__ float wave_max(float v) {
 }
 
 // ------------------------------------------------------------------ what all heads share
-// grid (slots, groups + ceil(heads / 16) + 1).  The y index chooses: a group's
-// B, C and S; 16 heads' step sizes and decays; the window's copy of sequence
-// x.  B and C go out as hi and lo in the order of the operands:
+// grid (slots, groups + ceil(heads / 16) + copies).  The y index chooses: a
+// group's B, C and S; 16 heads' step sizes and decays; a share of the windows'
+// copy.  B and C go out as hi and lo in the order of the operands:
 //   ws_c [slot][group][tb][q][hi, lo][lane][8]: t = 16 tb + lane % 16
 //   ws_b [slot][group][nt][q][hi, lo][lane][8]: n = 16 nt + lane % 16
 // with the 8 values of step q at 32 q + 4 (lane / 16) + {0..3, 16..19} of n or
@@ -141,13 +141,12 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int part = blockIdx.y, hb = (a.heads + 15) / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (part == a.groups + hb) {
-    const int b = blockIdx.x;
-    const int64_t n = (int64_t)(a.conv - 1) * a.chans;
-    if (b >= a.seqs) return;
+  if (part >= a.groups + hb) {
+    const int64_t n = (int64_t)a.seqs * (a.conv - 1) * a.chans, step = (int64_t)(gridDim.y - a.groups - hb) * gridDim.x * kPrep;
     const T* src = static_cast<const T*>(a.window);
-    T* dst = static_cast<T*>(a.wcopy) + b * n;
-    for (int64_t i = threadIdx.x; i < n; i += kPrep) dst[i] = src ? src[b * n + i] : from_f<T>(0.f);
+    T* dst = static_cast<T*>(a.wcopy);
+    for (int64_t i = ((int64_t)(part - a.groups - hb) * gridDim.x + blockIdx.x) * kPrep + threadIdx.x; i < n; i += step)
+      dst[i] = src ? src[i] : from_f<T>(0.f);
     return;
   }
   // the sequence of this slot: the last one whose first slot is not above it
@@ -804,9 +803,10 @@ __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
 // is read first: its bytes bound the kernel.  The workgroups of a group all
 // read the window of B and C; when it is updated in place, the last of them
 // to have read it (counted per sequence and group) writes it.
-template <typename T>
+// PASS: quads of a thread.  More share the convolution of B and C among more
+// rows, fewer make more workgroups when there are few sequences.
+template <typename T, int PASS>
 __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int L, int splits) {
-  constexpr int PASS = 2;
   __shared__ float sbc[2][256], sx[256 * PASS];
   __shared__ unsigned last;
   const int b = blockIdx.y, h = blockIdx.x / splits, split = blockIdx.x % splits;
@@ -832,8 +832,8 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int L, int s
   const T* win = static_cast<const T*>(a.window);
   T* wout = static_cast<T*>(a.window_out);
   const bool in_place = a.window_out == a.window;
-  T now[4][4];  // raw values of the thread's channels, for the new window
-  constexpr int ITEMS = 4;
+  constexpr int ITEMS = PASS + 2;
+  T now[ITEMS][4];  // raw values of the thread's channels, for the new window
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
     const int it = i * 256 + threadIdx.x;
@@ -940,7 +940,8 @@ template <typename T>
 static void launch_scan(ScanArgs a, hipStream_t st) {
   a.vec_state = a.state % 4 == 0 && al16(a.state_in) && al16(a.state_out) && al16(a.ws_seg);
   const int64_t slots = scan_slots(a.tokens, a.seqs);
-  const dim3 grid((unsigned)slots, a.groups + (a.heads + 15) / 16 + 1);
+  const int64_t copies = std::min<int64_t>(8, (int64_t)a.seqs * (a.conv - 1) * a.chans / (slots * kPrep) + 1);
+  const dim3 grid((unsigned)slots, (unsigned)(a.groups + (a.heads + 15) / 16 + copies));
   const size_t lds = (2 * Q * (a.np + 4) + 2 * kPrep / 64) * sizeof(float);
   if (a.np == 32) SN_LAUNCH((scan_prep_kernel<T, 32>), grid, dim3(kPrep), lds, st, a);
   else if (a.np == 64) SN_LAUNCH((scan_prep_kernel<T, 64>), grid, dim3(kPrep), lds, st, a);
@@ -953,13 +954,23 @@ static void launch_scan(ScanArgs a, hipStream_t st) {
   else launch_np<T, false>(a, st);
 }
 
+constexpr int64_t kStepBlocks = 512;
 template <typename T>
 static void launch_step(ScanArgs a, hipStream_t st) {
   a.vec_state = a.state % 4 == 0 && al16(a.state_in) && al16(a.state_out);
   int L = 1;
   while (4 * L < a.state) L *= 2;
-  const int rows = 2 * (256 / L), splits = (a.dim + rows - 1) / rows;
-  SN_LAUNCH((scan_step_kernel<T>), dim3((unsigned)(a.heads * splits), a.seqs), dim3(256), 0, st, a, L, splits);
+  auto splits = [&](int pass) { return (a.dim + pass * (256 / L) - 1) / (pass * (256 / L)); };
+  // as many quads as a head has rows for, if that leaves kStepBlocks workgroups
+  // (64 sequences of 64 heads of 64 x 128: 61 us with eight, 70 with two; one
+  // sequence: 5.4 us with two, 7.6 with eight)
+  auto fits = [&](int pass) {
+    return pass * (256 / L) <= std::max(a.dim, 8) && (int64_t)a.seqs * a.heads * splits(pass) >= kStepBlocks;
+  };
+  auto grid = [&](int pass) { return dim3((unsigned)(a.heads * splits(pass)), a.seqs); };
+  if (fits(8)) SN_LAUNCH((scan_step_kernel<T, 8>), grid(8), dim3(256), 0, st, a, L, splits(8));
+  else if (fits(4)) SN_LAUNCH((scan_step_kernel<T, 4>), grid(4), dim3(256), 0, st, a, L, splits(4));
+  else SN_LAUNCH((scan_step_kernel<T, 2>), grid(2), dim3(256), 0, st, a, L, splits(2));
 }
 
 // Segments: as many chunks to each as leave kScanUnits waves, at least two (a

@@ -289,15 +289,16 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 //
 // The waves of a workgroup share the group's C, B and S of a chunk in LDS, and
 // each has its head's decays there, all brought by LDS direct loads while the
-// chunk before (C, decays) or the product with C (B, S) is computed: two
-// barriers per chunk, behind which one set has arrived and the other is free.
+// chunk before (C, decays; with SHARE S) or the product with C (B; else S) is
+// computed: two barriers per chunk, behind which one set has arrived and the
+// other is free.  SEG has room for two chunks' B, and one barrier per chunk.
 constexpr int kScanWaves = 8;  // of a workgroup: 2 per SIMD
 constexpr int kDtBytes = kScanDt * 4;      // with its three scalars
 constexpr int kMaxBytes = kScanMax * 4;
 constexpr int kMixBytes = 6 * 2048;  // a head's 6 operands of the mix of a chunk's rows, hi and lo
 template <int NT, bool SHARE, bool SEG>
 constexpr int scan_lds(int waves) {  // B, C, S, two sets of largest sizes, two decay rows per wave, the mix of every 4 waves
-  return (SEG ? 4096 * NT : 8192 * NT + 10 * 1024) + 2 * kMaxBytes + waves * 2 * kDtBytes + (SHARE && !SEG ? waves / 4 * kMixBytes : 0);
+  return (SEG ? 8192 * NT : 8192 * NT + 10 * 1024) + 2 * kMaxBytes + waves * 2 * kDtBytes + (SHARE && !SEG ? waves / 4 * kMixBytes : 0);
 }
 template <typename T, int NT, bool SHARE, bool SEG>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) {
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   const bool live = unit_ < each * pblocks;
   const int unit = min(unit_, each * pblocks - 1);
   char* const ldsM = smem + scan_lds<NT, false, SEG>(waves) + (wave >> 2) * kMixBytes;  // with SHARE
-  char* const ldsX = smem + (SEG ? 4096 * NT : 8192 * NT + 10 * 1024);
+  char* const ldsX = smem + (SEG ? 8192 * NT : 8192 * NT + 10 * 1024);
   char* const ldsD = ldsX + 2 * kMaxBytes + wave * 2 * kDtBytes;
   const Seq s = seq_of(a, b);
   const int nc = (s.len + Q - 1) / Q;
@@ -435,7 +436,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   };
   auto fetch_b = [&](int c) {  // B, and S without SHARE
     const int64_t sg = (int64_t)(slot0 + c) * a.groups + grp;
-    fetch(ldsB, static_cast<const char*>(a.ws_b) + sg * 4096 * NT, 4 * NT);
+    fetch(ldsB + (SEG ? (c & 1) * 4096 * NT : 0), static_cast<const char*>(a.ws_b) + sg * 4096 * NT, 4 * NT);
     if (!SEG && !SHARE) fetch(ldsS, a.ws_s + sg * kScanS, 10);
   };
   // Raw rows 16 sb + 4 g - 3 + k of a chunk; rows past the end (or before the
@@ -465,7 +466,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   };
   // Accesses of a chunk that follow its loads of the next chunk's C and decays:
   // the raw rows, and the stores of y.
-  constexpr int AFTER = 28 + (SEG ? 0 : 16);
+  constexpr int AFTER = 28 + 16;
   if (c0 < c1) fetch_c(c0), fetch_b(c0);
   if (!SEG) {
     if (a.segs > 1) load_state(segst);
@@ -487,12 +488,16 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   for (int c = c0; c < c1; ++c) {
     const int t0 = c * Q;
     const f16* Cg = reinterpret_cast<const f16*>(ldsC) + lane * 8;
-    const f16* Bg = reinterpret_cast<const f16*>(ldsB) + lane * 8;
+    const f16* Bg = reinterpret_cast<const f16*>(ldsB + (SEG ? (c & 1) * 4096 * NT : 0)) + lane * 8;
     const float* Sg = reinterpret_cast<const float*>(ldsS) + lane * 4;
     const float* dtp = reinterpret_cast<const float*>(ldsD + (c & 1) * kDtBytes);
     // (from LDS: scalar loads here would hold up every wait for LDS)
     const float* maxes = reinterpret_cast<const float*>(ldsX + (c & 1) * kMaxBytes);
-    const float maxb = maxes[0], maxc = maxes[1], cend = dtp[5 * Q], maxdt = dtp[5 * Q + 1], maxf = dtp[5 * Q + 2];
+    float maxb, maxc, cend, maxdt, maxf;
+    auto scalars = [&] {
+      maxb = maxes[0], maxc = maxes[1], cend = dtp[5 * Q], maxdt = dtp[5 * Q + 1], maxf = dtp[5 * Q + 2];
+    };
+    if constexpr (!SEG) scalars();
     f32x4 acc[4][PT];
     if constexpr (!SEG) {
       // ---- C times the state in front of the chunk
@@ -558,7 +563,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       for (int j = 0; j < PT; ++j)
 #pragma unroll
         for (int v = 0; v < 4; ++v) u[sb][j][v] = silu_f(u[sb][j][v]);
-    const float sw = pow2_for(fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)));
+    const float sw = SEG ? 1.f : pow2_for(fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)));
     // The mix of rows 16 tb .. + 15 with rows 32 q .. + 31: S, the decay between
     // them and the step size; on the diagonal the skip term, above it nothing.
     auto mix = [&](int tb, int q) {
@@ -593,11 +598,16 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       if (w4 == 0) put(1, 0);
       if (w4 == 3) put(3, 1);
     }
-    // every wave's loads of B (and S) of this chunk and its share of the mix
-    // have arrived, and C (and S) is free
+    // Every wave's loads of B (and S) of this chunk and its share of the mix
+    // have arrived, and C (and S) is free.  (SEG: everything of this chunk has,
+    // and the other buffers are free.)
     wait_vmcnt<0>();
     dma_barrier();
-    if (c + 1 < c1) fetch_c(c + 1);
+    if (c + 1 < c1) {
+      fetch_c(c + 1);
+      if (SEG) fetch_b(c + 1);
+    }
+    if constexpr (SEG) scalars();
     load_raw(c + 1);
     if (t0 + Q > s.len) {  // past the end: zero (a NaN would meet the zeros of earlier rows)
 #pragma unroll
@@ -764,11 +774,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
         for (int j = 0; j < PT; ++j)
           if (from[j] < Q) st[nt][j] = f32x4{NAN, NAN, NAN, NAN};
     }
-    // every wave's loads of C and its decays for the next chunk have arrived
-    // (the newest AFTER are not among them), and B and S are free
-    wait_vmcnt<AFTER>();
-    dma_barrier();
-    if (c + 1 < c1) fetch_b(c + 1);
+    if constexpr (!SEG) {
+      // every wave's loads of C and its decays for the next chunk have arrived
+      // (the newest AFTER are not among them), and B (and S) is free
+      wait_vmcnt<AFTER>();
+      dma_barrier();
+      if (c + 1 < c1) fetch_b(c + 1);
+    }
   }
   if (SEG) {
     store_state(segst);

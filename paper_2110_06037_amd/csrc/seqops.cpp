@@ -310,6 +310,7 @@ int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* c
     check_dtype(d.dtype);
     if (d.heads < 1 || d.head_dim < 1 || d.groups < 1 || d.state < 1) fail(SN_E_SHAPE, "sizes must be positive");
     if (d.heads % d.groups) fail(SN_E_SHAPE, "groups must divide heads");
+    if (d.groups > 16384) fail(SN_E_UNSUPPORTED, "more than 16384 groups");
     if (d.state > 256) fail(SN_E_UNSUPPORTED, "state above 256");
     if (d.conv < 1 || d.conv > 4) fail(SN_E_UNSUPPORTED, "conv must be in 1..4");
     const int64_t chans = (int64_t)d.heads * d.head_dim + 2 * (int64_t)d.groups * d.state;

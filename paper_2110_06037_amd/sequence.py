@@ -44,7 +44,9 @@ class _Op:
         self.torch_dtype = self._types[self.dtype]
         self.device = device
         self._dev = torch.device("cuda", device) if device >= 0 else None
-        self._current = torch.cuda.current_stream
+        # the current stream's pointer, without making a Stream object of it (1 us)
+        self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
 
     def close(self):
         if getattr(self, "_op", None):
@@ -83,12 +85,12 @@ class _Op:
         tensors' memory is kept from reuse until its work is done."""
         cur = self._current(self.device)
         if stream is None:
-            return cur.cuda_stream
+            return cur
         if isinstance(stream, int):
-            if stream == cur.cuda_stream:
+            if stream == cur:
                 return stream
             stream = self._torch.cuda.ExternalStream(stream, device=self._dev)
-        if stream.cuda_stream != cur.cuda_stream:
+        if stream.cuda_stream != cur:
             for t in tensors:
                 if t is not None:
                     t.record_stream(stream)

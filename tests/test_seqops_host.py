@@ -132,6 +132,7 @@ def test_scan_creation_refusals():
     w = np.ones((4 * 8 + 2 * 3 * 16, 4))
     assert code(lambda: _scan(groups=3, conv_w=w)) == -2
     assert code(lambda: _scan(conv_w=np.ones((96, 5)))) == -4
+    assert code(lambda: _scan(heads=20000, head_dim=1, groups=20000, state=1, conv_w=np.ones((60000, 1)), a=np.zeros(20000))) == -4
     assert code(lambda: _scan(state=257, conv_w=np.ones((32 + 4 * 257, 4)))) == -4
     assert code(lambda: _scan(a=np.array([-1, -1, 0.5, -1]))) == -1
     assert code(lambda: _scan(a=np.array([-1, -1, -np.inf, -1]))) == -1

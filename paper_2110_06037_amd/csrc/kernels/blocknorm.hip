@@ -22,7 +22,7 @@ __global__ __launch_bounds__(WPR < 4 ? 256 : 64 * WPR) void block_norm_kernel(No
   const int slot = threadIdx.x / TPR;
   const int D = a.dim / a.groups;
   const int64_t units = a.rows * a.groups;
-  const int64_t unit = (int64_t)blockIdx.x * ROWS + slot;
+  const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + slot;
   const bool on = unit < units;  // threads without a row take part in the barriers
   const int64_t row = on ? unit / a.groups : 0;
   const int col = on ? (int)(unit - row * a.groups) * D : 0;
@@ -173,7 +173,11 @@ template <typename T, typename R, bool VEC>
 static void launch_norm(const NormArgs& a, hipStream_t st) {
   const int D = a.dim / a.groups;
   const int64_t units = a.rows * a.groups;
-  const auto grid = [&](int rows_per_block) { return dim3((unsigned)((units + rows_per_block - 1) / rows_per_block)); };
+  // in two dimensions: one takes fewer than 2^32 threads
+  const auto grid = [&](int rows_per_block) {
+    const int64_t blocks = (units + rows_per_block - 1) / rows_per_block, x = std::min<int64_t>(blocks, 1 << 20);
+    return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+  };
 #define SN_NORM(WPR, NV)                                                                               \
   SN_LAUNCH((block_norm_kernel<T, R, VEC, WPR, NV>), grid(WPR < 4 ? 4 / WPR : 1), \
             dim3(WPR < 4 ? 256 : 64 * WPR), 0, st, a)

@@ -199,3 +199,15 @@ def test_graph_replays_equal_eager_runs():
         torch.cuda.synchronize()
         ey, er = op.run(x, residual=r)
         assert torch.equal(ey, y) and torch.equal(er, ro)
+
+
+def test_more_rows_than_one_grid_dimension_has_threads_for():
+    import torch
+    op = BlockNorm("bf16", 8, post=np.arange(1, 9))
+    rows = (1 << 26) + 5
+    x = torch.empty(rows, 8, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(3))
+    y = torch.zeros_like(x)
+    op.run(x, out=y)
+    for at in (0, (1 << 22) - 2, (1 << 25) + 7, (1 << 26) - 30, rows - 40):
+        assert torch.equal(y[at:at + 40], op.run(x[at:at + 40])[0])
+    assert bool((y != 0).any(dim=1).all())

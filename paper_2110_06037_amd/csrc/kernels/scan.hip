@@ -291,14 +291,21 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // each has its head's decays there, all brought by LDS direct loads while the
 // chunk before (C, decays; with SHARE S) or the product with C (B; else S) is
 // computed: two barriers per chunk, behind which one set has arrived and the
-// other is free.  SEG has room for two chunks' B, and one barrier per chunk.
+// other is free.  SEG up to 128 state rows has room for two chunks' B, and one
+// barrier per chunk (4096 tokens of 64 heads of 64 x 128: 33.5 us against 35.5;
+// at 256 rows two chunks leave one workgroup per CU: 105 us for the whole scan
+// against 98).
 constexpr int kScanWaves = 8;  // of a workgroup: 2 per SIMD
 constexpr int kDtBytes = kScanDt * 4;      // with its three scalars
 constexpr int kMaxBytes = kScanMax * 4;
 constexpr int kMixBytes = 6 * 2048;  // a head's 6 operands of the mix of a chunk's rows, hi and lo
+template <int NT, bool SEG>
+constexpr bool scan_two() { return SEG && NT <= 8; }
+template <int NT, bool SEG>
+constexpr int scan_tiles() { return SEG ? (scan_two<NT, SEG>() ? 8192 : 4096) * NT : 8192 * NT + 10 * 1024; }
 template <int NT, bool SHARE, bool SEG>
 constexpr int scan_lds(int waves) {  // B, C, S, two sets of largest sizes, two decay rows per wave, the mix of every 4 waves
-  return (SEG ? 8192 * NT : 8192 * NT + 10 * 1024) + 2 * kMaxBytes + waves * 2 * kDtBytes + (SHARE && !SEG ? waves / 4 * kMixBytes : 0);
+  return scan_tiles<NT, SEG>() + 2 * kMaxBytes + waves * 2 * kDtBytes + (SHARE && !SEG ? waves / 4 * kMixBytes : 0);
 }
 template <typename T, int NT, bool SHARE, bool SEG>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) {
@@ -306,6 +313,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   // 4096 tokens of 64 heads, but 437 against 351 at 8 sequences of 2048: fewer
   // waves, and no registers left for the rows ahead.
   constexpr int PT = 1;
+  constexpr bool TWO = scan_two<NT, SEG>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
   char* const ldsB = smem;
   char* const ldsC = smem + 4096 * NT;                    // not with SEG
@@ -328,7 +336,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   const bool live = unit_ < each * pblocks;
   const int unit = min(unit_, each * pblocks - 1);
   char* const ldsM = smem + scan_lds<NT, false, SEG>(waves) + (wave >> 2) * kMixBytes;  // with SHARE
-  char* const ldsX = smem + (SEG ? 8192 * NT : 8192 * NT + 10 * 1024);
+  char* const ldsX = smem + scan_tiles<NT, SEG>();
   char* const ldsD = ldsX + 2 * kMaxBytes + wave * 2 * kDtBytes;
   const Seq s = seq_of(a, b);
   const int nc = (s.len + Q - 1) / Q;
@@ -436,7 +444,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   };
   auto fetch_b = [&](int c) {  // B, and S without SHARE
     const int64_t sg = (int64_t)(slot0 + c) * a.groups + grp;
-    fetch(ldsB + (SEG ? (c & 1) * 4096 * NT : 0), static_cast<const char*>(a.ws_b) + sg * 4096 * NT, 4 * NT);
+    fetch(ldsB + (TWO ? (c & 1) * 4096 * NT : 0), static_cast<const char*>(a.ws_b) + sg * 4096 * NT, 4 * NT);
     if (!SEG && !SHARE) fetch(ldsS, a.ws_s + sg * kScanS, 10);
   };
   // Raw rows 16 sb + 4 g - 3 + k of a chunk; rows past the end (or before the
@@ -466,7 +474,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   };
   // Accesses of a chunk that follow its loads of the next chunk's C and decays:
   // the raw rows, and the stores of y.
-  constexpr int AFTER = 28 + 16;
+  constexpr int AFTER = 28 + (SEG ? 0 : 16);
   if (c0 < c1) fetch_c(c0), fetch_b(c0);
   if (!SEG) {
     if (a.segs > 1) load_state(segst);
@@ -488,7 +496,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   for (int c = c0; c < c1; ++c) {
     const int t0 = c * Q;
     const f16* Cg = reinterpret_cast<const f16*>(ldsC) + lane * 8;
-    const f16* Bg = reinterpret_cast<const f16*>(ldsB + (SEG ? (c & 1) * 4096 * NT : 0)) + lane * 8;
+    const f16* Bg = reinterpret_cast<const f16*>(ldsB + (TWO ? (c & 1) * 4096 * NT : 0)) + lane * 8;
     const float* Sg = reinterpret_cast<const float*>(ldsS) + lane * 4;
     const float* dtp = reinterpret_cast<const float*>(ldsD + (c & 1) * kDtBytes);
     // (from LDS: scalar loads here would hold up every wait for LDS)
@@ -544,16 +552,16 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     float u[4][PT][4], sq[PT] = {}, maxu[PT], su[PT];
     auto convolve = [&](int conv) {
 #pragma unroll
-    for (int sb = 0; sb < 4; ++sb)
+      for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
-      for (int j = 0; j < PT; ++j) {
-        const float wj[4] = {w[0][j], w[1][j], w[2][j], w[3][j]};
-        float r[7];
+        for (int j = 0; j < PT; ++j) {
+          const float wj[4] = {w[0][j], w[1][j], w[2][j], w[3][j]};
+          float r[7];
 #pragma unroll
-        for (int k = 0; k < 7; ++k) r[k] = to_f(raw[sb][k][j]);
+          for (int k = 0; k < 7; ++k) r[k] = to_f(raw[sb][k][j]);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) u[sb][j][v] = taps4(wj, cb[j], r[v], r[v + 1], r[v + 2], r[v + 3], conv);
-      }
+          for (int v = 0; v < 4; ++v) u[sb][j][v] = taps4(wj, cb[j], r[v], r[v + 1], r[v + 2], r[v + 3], conv);
+        }
     };
     if (a.conv == 4) convolve(4);  // without the tests for absent taps
     else convolve(a.conv);
@@ -599,13 +607,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       if (w4 == 3) put(3, 1);
     }
     // Every wave's loads of B (and S) of this chunk and its share of the mix
-    // have arrived, and C (and S) is free.  (SEG: everything of this chunk has,
+    // have arrived, and C (and S) is free.  (TWO: everything of this chunk has,
     // and the other buffers are free.)
     wait_vmcnt<0>();
     dma_barrier();
     if (c + 1 < c1) {
       fetch_c(c + 1);
-      if (SEG) fetch_b(c + 1);
+      if (TWO) fetch_b(c + 1);
     }
     if constexpr (SEG) scalars();
     load_raw(c + 1);
@@ -774,7 +782,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
         for (int j = 0; j < PT; ++j)
           if (from[j] < Q) st[nt][j] = f32x4{NAN, NAN, NAN, NAN};
     }
-    if constexpr (!SEG) {
+    if constexpr (!TWO) {
       // every wave's loads of C and its decays for the next chunk have arrived
       // (the newest AFTER are not among them), and B (and S) is free
       wait_vmcnt<AFTER>();
@@ -1008,6 +1016,9 @@ void scan_run(const ScanArgs& in, hipStream_t st) {
             a.conv >= 1 && a.conv <= 4 && a.seqs >= 1 && a.seqs <= 65535 && a.tokens >= 0,
         "scan shapes");
   scan_split(a);
+  check((int64_t)a.segs * a.seqs * a.groups * ((a.heads / a.groups * (int64_t)((a.dim + 15) / 16) + 3) / 4) * 64 * kScanWaves <
+            (int64_t(1) << 32),
+        "scan of more workgroups than a launch takes");
   if (a.dtype == 0) launch_scan<float>(a, st);
   else if (a.dtype == 1) launch_scan<f16>(a, st);
   else launch_scan<bf16>(a, st);

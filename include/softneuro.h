@@ -497,8 +497,9 @@ const char* sn_last_error(void);
  *    workspace, calls of one scan handle must follow each other on one stream
  *    (or be ordered by events); norm and product handles have no workspace.
  *  - Rows of a tensor are `stride` elements apart (stride >= the row's
- *    length) and each row is contiguous.  Any alignment of whole elements is
- *    accepted; 16-byte aligned rows take the wide loads.
+ *    length; a single row's is not looked at) and each row is contiguous.
+ *    Any alignment of whole elements is accepted; 16-byte aligned rows take
+ *    the wide loads.
  *  - device = -1 makes a host-only handle: its runs check their arguments
  *    and then return SN_E_DEVICE.
  *  - Zero rows (m, rows or tokens of 0) are allowed and write nothing but
@@ -586,10 +587,10 @@ int sn_linear4_run(sn_op* op, int64_t m, const void* x, int64_t x_stride, void* 
  * (tokens = seqs, offsets null), in one kernel.                            */
 typedef struct {
   int32_t dtype;
-  int32_t heads, head_dim, groups, state; /* state <= 256, heads % groups == 0 */
+  int32_t heads, head_dim, groups, state; /* state <= 256, groups <= 16384, heads % groups == 0 */
   int32_t conv;                           /* taps, 1 .. 4 */
   int32_t max_seqs;                       /* what one call may hold: sizes the workspace */
-  int64_t max_tokens;
+  int64_t max_tokens;                     /* at most 2^27 */
 } sn_scan_desc;
 typedef struct {
   int32_t seqs;

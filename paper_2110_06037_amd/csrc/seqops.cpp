@@ -92,13 +92,16 @@ Op& op_of(sn_op* p, OpKind kind) {
 }
 
 // A tensor of `rows` rows of `n` elements: given, rows that do not overlap,
-// elements on their own alignment.
-void check_rows(const void* p, int64_t stride, int64_t rows, int64_t n, int dtype, const char* what) {
-  if (rows == 0) return;
+// elements on their own alignment.  Returns the stride to use: that of one row
+// means nothing to the caller, but the kernels' ranges are made from it.
+int64_t check_rows(const void* p, int64_t stride, int64_t rows, int64_t n, int dtype, const char* what) {
+  if (rows == 0) return n;
   if (!p) fail(SN_E_INVALID, std::string(what) + " is null");
-  if (rows > 1 && stride < n) fail(SN_E_SHAPE, std::string(what) + ": row stride below the row's length");
-  if (stride < 0 || stride > (int64_t(1) << 40)) fail(SN_E_SHAPE, std::string(what) + ": row stride out of range");
+  if (rows == 1) stride = n;
+  if (stride < n) fail(SN_E_SHAPE, std::string(what) + ": row stride below the row's length");
+  if (stride > (int64_t(1) << 40)) fail(SN_E_SHAPE, std::string(what) + ": row stride out of range");
   if (reinterpret_cast<uintptr_t>(p) % dtype_size(dtype)) fail(SN_E_INVALID, std::string(what) + " is not aligned to its elements");
+  return stride;
 }
 
 void need_device(const sn_op& op) {
@@ -143,12 +146,11 @@ k::ScanArgs scan_args(const ScanOp& op, const sn_scan_io* io, bool step) {
   if (step && (io->tokens != io->seqs || io->offsets)) fail(SN_E_SHAPE, "a step takes one token per sequence");
   if (io->seqs && !io->offsets && io->tokens % io->seqs)
     fail(SN_E_SHAPE, "tokens are no multiple of seqs, and there are no offsets");
-  check_rows(io->x, io->x_stride, io->tokens, a.chans, a.dtype, "x");
+  a.xs = check_rows(io->x, io->x_stride, io->tokens, a.chans, a.dtype, "x");
+  a.dts = check_rows(io->dt, io->dt_stride, io->tokens, a.heads, a.dtype, "dt");
+  a.ys = check_rows(io->y, io->y_stride, io->tokens, (int64_t)a.heads * a.dim, a.dtype, "y");
   // 67 rows of x and 64 of y are addressed with 32-bit offsets
-  if (std::max(io->x_stride, io->y_stride) * e * 68 >= (int64_t(1) << 31))
-    fail(SN_E_UNSUPPORTED, "row stride above 2^31 / 68 bytes");
-  check_rows(io->dt, io->dt_stride, io->tokens, a.heads, a.dtype, "dt");
-  check_rows(io->y, io->y_stride, io->tokens, (int64_t)a.heads * a.dim, a.dtype, "y");
+  if (std::max(a.xs, a.ys) * e * 68 >= (int64_t(1) << 31)) fail(SN_E_UNSUPPORTED, "row stride above 2^31 / 68 bytes");
   for (const void* p : {io->window, (const void*)io->window_out})
     if (reinterpret_cast<uintptr_t>(p) % e) fail(SN_E_INVALID, "window is not aligned to its elements");
   for (const void* p : {(const void*)io->state, (const void*)io->state_out, (const void*)io->offsets})
@@ -156,7 +158,7 @@ k::ScanArgs scan_args(const ScanOp& op, const sn_scan_io* io, bool step) {
   check_in_out(io->window, io->window_out, (int64_t)io->seqs * (a.conv - 1) * a.chans * e, "window_out");
   check_in_out(io->state, io->state_out, (int64_t)io->seqs * a.heads * a.dim * a.state * 4, "state_out");
   a.seqs = io->seqs, a.tokens = io->tokens, a.offsets = io->offsets;
-  a.x = io->x, a.xs = io->x_stride, a.dt = io->dt, a.dts = io->dt_stride, a.y = io->y, a.ys = io->y_stride;
+  a.x = io->x, a.dt = io->dt, a.y = io->y;
   a.window = io->window, a.window_out = a.conv > 1 ? io->window_out : nullptr;
   a.state_in = io->state, a.state_out = io->state_out;
   return a;
@@ -216,24 +218,23 @@ int sn_norm_run(sn_op* p, int64_t rows, const void* x, int64_t x_stride, const v
     k::NormArgs a = op.a;
     if (rows < 0 || rows >= (int64_t(1) << 31) || rows * a.groups >= (int64_t(1) << 31)) fail(SN_E_SHAPE, "rows out of range");
     const bool has_y = a.pre_w || a.rdtype < 0;
-    check_rows(x, x_stride, rows, a.dim, a.dtype, "x");
-    if (a.gate) check_rows(gate, gate_stride, rows, a.dim, a.dtype, "gate");
+    a.xs = check_rows(x, x_stride, rows, a.dim, a.dtype, "x");
+    if (a.gate) a.gs = check_rows(gate, gate_stride, rows, a.dim, a.dtype, "gate");
     else if (gate) fail(SN_E_INVALID, "a gate given to a handle without one");
     if (a.rdtype >= 0) {
-      check_rows(res, res_stride, rows, a.dim, a.rdtype, "res");
-      check_rows(res_out, res_out_stride, rows, a.dim, a.rdtype, "res_out");
-      if (res == res_out && res_stride != res_out_stride) fail(SN_E_SHAPE, "res in place needs one stride");
+      a.rs = check_rows(res, res_stride, rows, a.dim, a.rdtype, "res");
+      a.ros = check_rows(res_out, res_out_stride, rows, a.dim, a.rdtype, "res_out");
+      if (res == res_out && a.rs != a.ros) fail(SN_E_SHAPE, "res in place needs one stride");
     } else if (res || res_out) {
       fail(SN_E_INVALID, "a residual given to a handle without one");
     }
-    if (has_y) check_rows(y, y_stride, rows, a.dim, a.dtype, "y");
+    if (has_y) a.ys = check_rows(y, y_stride, rows, a.dim, a.dtype, "y");
     else if (y) fail(SN_E_INVALID, "y given to a handle without a pre norm (its output is res_out)");
-    if (y && y == x && x_stride != y_stride) fail(SN_E_SHAPE, "y in place needs one stride");
+    if (y && y == x && a.xs != a.ys) fail(SN_E_SHAPE, "y in place needs one stride");
     need_device(op);
     if (!rows) return;
     a.rows = rows;
-    a.x = x, a.xs = x_stride, a.g = gate, a.gs = gate_stride, a.r = res, a.rs = res_stride;
-    a.ro = res_out, a.ros = res_out_stride, a.y = y, a.ys = y_stride;
+    a.x = x, a.g = gate, a.r = res, a.ro = res_out, a.y = y;
     OnDevice on(op.device);
     k::block_norm(a, static_cast<hipStream_t>(stream));
     HIPCHK(hipGetLastError());
@@ -289,11 +290,11 @@ int sn_linear4_run(sn_op* p, int64_t m, const void* x, int64_t x_stride, void* y
     Linear4Op& op = op_of<Linear4Op>(p, OP_LINEAR4);
     k::Linear4Args a = op.a;
     if (m < 0 || m > 65535 * 4) fail(SN_E_SHAPE, "m must be in 0..262140");
-    check_rows(x, x_stride, m, a.cols, a.dtype, "x");
-    check_rows(y, y_stride, m, a.rows, a.dtype, "y");
+    a.xs = check_rows(x, x_stride, m, a.cols, a.dtype, "x");
+    a.ys = check_rows(y, y_stride, m, a.rows, a.dtype, "y");
     need_device(op);
     if (!m) return;
-    a.m = m, a.x = x, a.xs = x_stride, a.y = y, a.ys = y_stride;
+    a.m = m, a.x = x, a.y = y;
     OnDevice on(op.device);
     k::linear4(a, static_cast<hipStream_t>(stream));
     HIPCHK(hipGetLastError());
@@ -316,7 +317,7 @@ int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* c
     const int64_t chans = (int64_t)d.heads * d.head_dim + 2 * (int64_t)d.groups * d.state;
     if (d.heads > 65535 || d.head_dim > 65535 || chans > (1 << 24)) fail(SN_E_UNSUPPORTED, "more than 2^24 channels");
     if (d.max_seqs < 1 || d.max_seqs > 65535) fail(SN_E_SHAPE, "max_seqs must be in 1..65535");
-    if (d.max_tokens < 1 || d.max_tokens > (1 << 30)) fail(SN_E_SHAPE, "max_tokens must be in 1..2^30");
+    if (d.max_tokens < 1 || d.max_tokens > (1 << 27)) fail(SN_E_SHAPE, "max_tokens must be in 1..2^27");
     check_finite(conv_w, chans * d.conv, "conv_w");
     check_finite(conv_b, chans, "conv_b");
     check_finite(a_, d.heads, "a");

@@ -385,3 +385,22 @@ def test_no_rows_and_refusals():
     for bad in (lambda: op.step(x, dt), lambda: op.run(x, dt, seqs=2)):
         with pytest.raises(N.SNError):  # more than max_seqs
             bad()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_stride_of_a_single_row_is_not_looked_at(dtype):
+    import torch
+    c = Case(dtype, [1], heads=2, first=True)
+    op = c.op()
+    for call, kw in ((op.step, {}), (op.run, {"seqs": 1})):
+        f = op.lib.sn_scan_step if call == op.step else op.lib.sn_scan_run
+        win, h = c.carried()
+        x, dt = device(c.x, dtype), device(c.dt, dtype)
+        y, w, s = call(x, dt, win, h, **kw)
+        want = [t.clone() for t in (y, w, s)]
+        for t in (y, w, s):
+            t.fill_(7)
+        io = op._io  # the same call again, with strides that say nothing
+        io.x_stride = io.dt_stride = io.y_stride = 0
+        N.check(f(op._op, io, torch.cuda.current_stream().cuda_stream))
+        assert all(torch.equal(a, b) for a, b in zip(want, (y, w, s)))

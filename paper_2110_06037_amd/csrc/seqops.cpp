@@ -251,7 +251,8 @@ int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint1
     check_dtype(d.dtype);
     if (d.rows < 1 || d.cols < 1) fail(SN_E_SHAPE, "rows and cols must be positive");
     if (d.rows > (1 << 24) || d.cols > (1 << 20)) fail(SN_E_UNSUPPORTED, "more than 2^24 rows or 2^20 cols");
-    if (k::linear4_blocks(d.rows, d.cols) >= (int64_t(1) << 28)) fail(SN_E_UNSUPPORTED, "more than 2^28 blocks of weights");
+    // (one launch lays them out, with fewer than 2^32 threads)
+    if (k::linear4_blocks(d.rows, d.cols) >= (int64_t(1) << 24)) fail(SN_E_UNSUPPORTED, "more than 2^24 blocks of 2048 weights");
     if (d.group < 32 || d.group % 32) fail(SN_E_SHAPE, "group must be a multiple of 32");
     if (d.act < SN_ACT_NONE || d.act > SN_ACT_RELU6) fail(SN_E_INVALID, "unknown activation");
     const int64_t groups = (d.cols + (int64_t)d.group - 1) / d.group;

@@ -206,6 +206,10 @@ struct Op4 {
 // stay in the caches) straight to the first operand: row r = 4 g + v of it is
 // row 4 v + g of x, so that up to 4 rows have all their sums in element v = 0
 // (MV = 1); in float32 v is the part and g the row.
+//
+// Bound by the weights' bytes, and by the one trip to memory that every wave
+// makes: 4 rows of 4096 inputs and 16384 features in f16, weights from HBM, @R4.
+// One row of 2048 and 8512 features in bf16, weights in the caches, @R1.
 template <typename T, int NB, int MV, int GS, bool VX, int R, int U>
 __global__ __launch_bounds__(R == 1 && NB < 4 ? 1024 : 512) void linear4_rows_kernel(Linear4Args a) {
   typedef typename Op4<T>::E E;
@@ -362,9 +366,14 @@ constexpr int kL4Stages = 3;
 // and x alone goes through LDS, in the first operand's order.  DMA (16-bit
 // types, wide rows): LDS direct loads, three blocks of 128 inputs in a ring,
 // two blocks ahead; else through registers, one block ahead (float32 is split
-// into its parts there).  bf16: sums
-// against ones, each wave for 16 of the rows, wait in LDS, and the bias comes
-// off at the end, as one more matrix product, in float32.
+// into its parts there).  bf16: sums against ones, each wave for 16 of the rows,
+// wait in LDS, and the bias comes off at the end, as one more matrix product, in
+// float32.
+//
+// Bound by instruction issue: matrix instructions fill a third of the cycles, the
+// codes' way to floats and the runs' scales two fifths more (counted); HBM
+// traffic is small.  1500 rows of 2048 inputs
+// and 8512 features: @T.
 template <typename T, int RB, int GS, bool VX>
 __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int tiles_m, int tiles_n) {
   typedef typename Op4<T>::E E;

@@ -135,6 +135,10 @@ __device__ __forceinline__ float wave_max(float v) {
 // with the 8 values of step q at 32 q + 4 (lane / 16) + {0..3, 16..19} of n or
 // s: the order in which accumulator tiles hold rows.  S = C B^T in float32,
 //   ws_s [slot][group][tb][sb <= tb][lane][4]: t = 16 tb + lane % 16, s = 16 sb + 4 (lane / 16) + 0..3.
+// Once per chunk and group instead of once per wave of the heads.  Bound by
+// latency: one workgroup per chunk and part, the raw rows from memory, then the
+// convolution, the maxima and S one after the other, 11.5 us for 4096 tokens of
+// 64 heads and one group.
 constexpr int kPrep = 1024;
 template <typename T, int NP>
 __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
@@ -291,10 +295,17 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // each has its head's decays there, all brought by LDS direct loads while the
 // chunk before (C, decays; with SHARE S) or the product with C (B; else S) is
 // computed: two barriers per chunk, behind which one set has arrived and the
-// other is free.  SEG up to 128 state rows has room for two chunks' B, and one
-// barrier per chunk (4096 tokens of 64 heads of 64 x 128: 33.5 us against 35.5;
-// at 256 rows two chunks leave one workgroup per CU: 105 us for the whole scan
-// against 98).
+// other is free.  Bound by the latency of one chunk after the other: about 5 us
+// for a lone wave, 1.5 more for each further wave of a SIMD, whose registers
+// (170) leave room for two; 4096 tokens of 64 heads of 64 x 128 in bf16: 33.5 us
+// for the first pass, 68 for the second, with matrix instructions in 17% of the
+// cycles and other vector instructions in 44%; 8 sequences of 2048, which need no
+// first pass, 367 us all told.  Twelve or sixteen waves, or more or fewer
+// segments, were not faster.
+//
+// SEG up to 128 state rows has room for two chunks' B, and one barrier per chunk
+// (33.5 us against 35.5; at 256 rows two chunks leave one workgroup per CU: 105
+// us for the whole scan against 98).
 constexpr int kScanWaves = 8;  // of a workgroup: 2 per SIMD
 constexpr int kDtBytes = kScanDt * 4;      // with its three scalars
 constexpr int kMaxBytes = kScanMax * 4;
@@ -800,7 +811,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 }
 
 // States over the segments: slot i of a head's segments takes the state in
-// front of segment i.  Segments after the sequence's end are not read.
+// front of segment i.  Segments after the sequence's end are not read.  Bound by
+// the chain of loads, one per segment (8 segments of 64 heads of 64 x 128: 8 us).
 __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
   const int64_t hold = (int64_t)a.dim * a.state, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int b = blockIdx.z, h = blockIdx.y;
@@ -829,6 +841,9 @@ __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
 // to have read it (counted per sequence and group) writes it.
 // PASS: quads of a thread.  More share the convolution of B and C among more
 // rows, fewer make more workgroups when there are few sequences.
+// 64 heads of 64 x 128 in bf16: 64 sequences 61 us, 4.4 TB/s (a copy of gigabytes
+// reaches 4.8); 8 sequences 12 us; one 5.4 us, most of it the launch and the way
+// from the window over the convolution to the state.
 template <typename T, int PASS>
 __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int L, int splits) {
   __shared__ float sbc[2][256], sx[256 * PASS];

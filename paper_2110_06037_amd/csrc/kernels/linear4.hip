@@ -208,8 +208,9 @@ struct Op4 {
 // (MV = 1); in float32 v is the part and g the row.
 //
 // Bound by the weights' bytes, and by the one trip to memory that every wave
-// makes: 4 rows of 4096 inputs and 16384 features in f16, weights from HBM, @R4.
-// One row of 2048 and 8512 features in bf16, weights in the caches, @R1.
+// makes: 4 rows of 4096 inputs and 16384 features in f16, weights from HBM, 10.0
+// us, 3.5 TB/s; one row in bf16 8.9 us, 3.9 TB/s; of 2048 inputs and 8512 features
+// 5.3 us, of which an empty launch is 2.3.
 template <typename T, int NB, int MV, int GS, bool VX, int R, int U>
 __global__ __launch_bounds__(R == 1 && NB < 4 ? 1024 : 512) void linear4_rows_kernel(Linear4Args a) {
   typedef typename Op4<T>::E E;
@@ -373,7 +374,8 @@ constexpr int kL4Stages = 3;
 // Bound by instruction issue: matrix instructions fill a third of the cycles, the
 // codes' way to floats and the runs' scales two fifths more (counted); HBM
 // traffic is small.  1500 rows of 2048 inputs
-// and 8512 features: @T.
+// and 8512 features: 80 us in bf16, 650 TFLOP/s (a plain library
+// product of 8192^3 reaches 1236); 341 us in float32.
 template <typename T, int RB, int GS, bool VX>
 __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int tiles_m, int tiles_n) {
   typedef typename Op4<T>::E E;

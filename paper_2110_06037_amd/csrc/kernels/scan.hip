@@ -10,8 +10,8 @@
 // i.e. three small matrix products per chunk and head on MFMA, chunk after
 // chunk with the state in registers.  Sequences of many chunks are cut into
 // segments so that few heads still fill the chip: a first pass finds the
-// state that every segment adds, a small kernel carries the states over the
-// segments, and the second pass starts every segment from its own state.
+// state that every segment adds, and the second pass starts every segment from
+// its own state, summed up from those, by a small kernel if they are many.
 //
 // All decays are at most 1 (a <= 0).  c is held as hi + lo with hi in steps of
 // 1/256, so that differences of hi are exact and those of lo small: a plain
@@ -287,7 +287,8 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // of the product with C, so the state never leaves the registers; and a lane's
 // convolution outputs (times 16 sb + 4 (lane / 16) + v, the same p) are the
 // second operand of both other products.
-// SEG: only the state that the segment adds (from zero), no outputs.
+// SEG: only the state that the segment adds (from zero; segment 0 from the
+// sequence's, which it copies), no outputs.
 // SHARE: the four waves of 64 columns of a head make its mix of a chunk's rows
 // together.
 //
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // (170) leave room for two; 4096 tokens of 64 heads of 64 x 128 in bf16: 33.5 us
 // for the first pass, 68 for the second, with matrix instructions in 17% of the
 // cycles and other vector instructions in 44%; 8 sequences of 2048, which need no
-// first pass, 367 us all told.  Twelve or sixteen waves, or more or fewer
+// first pass, 350 us all told.  Twelve or sixteen waves, or more or fewer
 // segments, were not faster.
 //
 // SEG up to 128 state rows has room for two chunks' B, and one barrier per chunk
@@ -381,18 +382,18 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     const int n = 16 * nt + 4 * g + v;
     return (int)(j < pn && n < N ? ((unsigned)(p0 + j) * (unsigned)N + (unsigned)n) * 4u : kOOB);
   };
-  auto load_state = [&](const float* p) {
+  auto load_state = [&](const float* p, f32x4 (&to)[NT][PT]) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, hold * 4);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int j = 0; j < PT; ++j)
         if (a.vec_state) {
-          st[nt][j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at_state(nt, j, 0), 0, 0));
+          to[nt][j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at_state(nt, j, 0), 0, 0));
         } else {
 #pragma unroll
           for (int v = 0; v < 4; ++v)
-            st[nt][j][v] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at_state(nt, j, v), 0, 0));
+            to[nt][j][v] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at_state(nt, j, v), 0, 0));
         }
   };
   auto store_state = [&](float* p) {
@@ -411,8 +412,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
           }
         }
   };
-  const int64_t head_seg = (segment0_of(a, s.first, b) + seg) * a.heads + h;
-  float* segst = a.ws_seg + head_seg * hold;
+  // the head's slot of segment i
+  const int64_t head_seg0 = segment0_of(a, s.first, b) * a.heads + h;
+  auto seg_slot = [&](int i) { return head_seg0 + (int64_t)i * a.heads; };
+  auto seg_state = [&](int i) { return a.ws_seg + seg_slot(i) * hold; };
   // per column: at least the size of every value of the state (within a few
   // powers of two).  Scales are a column's own, so no column's values have a
   // part in another's.
@@ -488,8 +491,30 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   constexpr int AFTER = 28 + (SEG ? 0 : 16);
   if (c0 < c1) fetch_c(c0), fetch_b(c0);
   if (!SEG) {
-    if (a.segs > 1) load_state(segst);
-    else if (a.state_in) load_state(a.state_in + ((int64_t)b * a.heads + h) * hold);
+    const float* in = a.state_in ? a.state_in + ((int64_t)b * a.heads + h) * hold : nullptr;
+    if (nc <= a.per) {
+      if (in) load_state(in, st);
+    } else if (seg == 0) {
+      // the copy: by now the sequence's last segment may have written its state in place
+      if (in) load_state(seg_state(0), st);
+    } else {
+      const int from = a.carried ? seg : 1;
+      load_state(seg_state(from), st);
+      for (int i = from + 1; i <= seg; ++i) {
+        f32x4 add[NT][PT];
+        load_state(seg_state(i), add);
+        const float f = __builtin_amdgcn_exp2f(a.ws_decay[seg_slot(i)]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int j = 0; j < PT; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) st[nt][j][v] = fmaf(st[nt][j][v], f, add[nt][j][v]);
+      }
+    }
+  } else if (seg == 0 && a.state_in) {
+    load_state(a.state_in + ((int64_t)b * a.heads + h) * hold, st);
+    store_state(seg_state(0));
   }
   load_raw(c0);
   if (!SEG) {
@@ -802,34 +827,31 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     }
   }
   if (SEG) {
-    store_state(segst);
-    if (lane == 0 && live && unit % pblocks == 0) a.ws_decay[head_seg] = total;
+    store_state(seg_state(seg + 1));
+    if (lane == 0 && live && unit % pblocks == 0) a.ws_decay[seg_slot(seg + 1)] = total;
   } else if (a.state_out && (c1 == nc && (c0 < c1 || seg == 0))) {
     // the segment with the sequence's last chunk (segment 0 of a sequence without rows)
     store_state(a.state_out + ((int64_t)b * a.heads + h) * hold);
   }
 }
 
-// States over the segments: slot i of a head's segments takes the state in
-// front of segment i.  Segments after the sequence's end are not read.  Bound by
-// the chain of loads, one per segment (8 segments of 64 heads of 64 x 128: 8 us).
+// States over the segments, if there are many: slot i, with what segment i - 1
+// adds (with segment 0's whole state for i = 1), takes the state in front of
+// segment i.  Bound by the chain of loads, one per segment.
 __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
   const int64_t hold = (int64_t)a.dim * a.state, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int b = blockIdx.z, h = blockIdx.y;
   if (e >= hold) return;
   const Seq s = seq_of(a, b);
   const int nc = (s.len + Q - 1) / Q;
-  const int64_t seg0 = segment0_of(a, s.first, b);
-  float v = a.state_in ? a.state_in[((int64_t)b * a.heads + h) * hold + e] : 0.f;
-  for (int i = 0;; ++i) {
-    const int64_t at = (seg0 + i) * a.heads + h;
-    float* p = a.ws_seg + at * hold + e;
-    const bool more = (i + 1) * a.per < nc;  // another segment follows
-    float add = 0.f, f = 0.f;
-    if (more) add = *p, f = __builtin_amdgcn_exp2f(a.ws_decay[at]);
+  if (2 * a.per >= nc) return;
+  const int64_t slot = segment0_of(a, s.first, b) * a.heads + h;
+  float* p = a.ws_seg + (slot + a.heads) * hold + e;
+  float v = *p;
+  for (int i = 2; i * a.per < nc; ++i) {
+    p += a.heads * hold;
+    v = fmaf(v, __builtin_amdgcn_exp2f(a.ws_decay[slot + (int64_t)i * a.heads]), *p);
     *p = v;
-    if (!more) return;
-    v = fmaf(v, f, add);
   }
 }
 
@@ -962,7 +984,7 @@ static void launch_main(const ScanArgs& a, hipStream_t st) {
     // half the waves: three of its workgroups fit a CU
     const int ws = std::min(4, units);
     SN_LAUNCH((scan_main_kernel<T, NT, false, true>), grid(ws), dim3(64 * ws), (scan_lds<NT, false, true>(ws)), st, a);
-    SN_LAUNCH((scan_carry_kernel), dim3((a.dim * a.state + 255) / 256, a.heads, a.seqs), dim3(256), 0, st, a);
+    if (a.carried) SN_LAUNCH((scan_carry_kernel), dim3((a.dim * a.state + 255) / 256, a.heads, a.seqs), dim3(256), 0, st, a);
   }
   SN_LAUNCH((scan_main_kernel<T, NT, SHARE, false>), grid(waves), dim3(64 * waves), (scan_lds<NT, SHARE, false>(waves)), st, a);
 }
@@ -1011,6 +1033,13 @@ static void launch_step(ScanArgs a, hipStream_t st) {
   else SN_LAUNCH((scan_step_kernel<T, 2>), grid(2), dim3(256), 0, st, a, L, splits(2));
 }
 
+// Up to this many state rows of segments, each segment finds the state in front
+// of it from those that the earlier ones add by itself, instead of a launch that
+// does so for all: 2 segments of 128 rows 47.1 -> 44.8 us, 4 of 64 43.5 -> 42.4,
+// 8 of 16 (counted as 32) 83.2 -> 80.0; but 8 of 64 97.9 -> 98.7, 8 of 128 121.4
+// -> 124.9 and 32 of 256 99 -> 186, a load's latency and more for each.
+constexpr int kScanCarry = 256;
+
 // Segments: as many chunks to each as leave kScanUnits waves, at least two (a
 // segment's chunks but the last one's are read twice, and its state is written
 // and read); one if there are more waves anyhow, or the states found no room.
@@ -1023,6 +1052,7 @@ static void scan_split(ScanArgs& a) {
   while (per < chunks && scan_segment_slots(slots, a.seqs, (int)per) * hold > a.seg_cap) ++per;
   a.per = (int)std::max<int64_t>(1, std::min(per, chunks));
   a.segs = (int)std::max<int64_t>(1, (chunks + a.per - 1) / a.per);
+  a.carried = a.segs * a.np > kScanCarry;
 }
 
 void scan_run(const ScanArgs& in, hipStream_t st) {

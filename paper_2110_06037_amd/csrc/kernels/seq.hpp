@@ -78,14 +78,16 @@ struct ScanArgs {
   float* ws_dt;    // [slot][head][kScanDtRow]: 64 each of the decay since the chunk's start, its log2 as
                    // hi and lo, the step size, the step size times the decay to the chunk's end; then
                    // the chunk's log2 decay and the largest of the step sizes and of the last array
-  float* ws_seg;   // [segment slot][head][dim][state]
-  float* ws_decay; // [segment slot][head]
+  float* ws_seg;   // [segment slot][head][dim][state]: slot 0 of a sequence its state before the call, slot i + 1
+                   // what segment i adds
+  float* ws_decay; // [segment slot][head], likewise: log2 of segment i's decay
   void* wcopy;     // [seq][conv - 1][chans]    the window before the call
   unsigned* count; // [seq][group], zero between calls
   int64_t seg_cap; // elements of ws_seg
   // call
   int seqs;
   int segs, per;  // segments of the longest sequence, chunks of a segment (set by the launcher)
+  bool carried;   // states over the segments by a launch of their own (set by the launcher)
   int64_t each;  // rows per sequence without offsets (set by the launcher)
   int64_t tokens;
   const int32_t* offsets;

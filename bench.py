@@ -113,9 +113,9 @@ KERNEL_SOURCES = {
     "dw3x3_kernel": ("dwconv.hip", "gemm_common.hpp", "kcommon.hpp", "launch.hpp"),
     "wino_fused_kernel": ("wino_fused.hip", "wino.hpp", "gemm_common.hpp", "kcommon.hpp", "launch.hpp"),
 }
-ALL_KERNEL_SOURCES = ("conv.hip", "conv_igemm_bf16.hip", "conv_igemm_f16.hip", "conv1x1_stream.hip", "conv_ksplit.hip",
-                      "conv_patch.hip", "conv_smallc.hip", "convert.hip", "dwconv.hip", "fc.hip", "igemm.hpp", "misc.hip",
-                      "wino.hpp", "wino_fused.hip",
+ALL_KERNEL_SOURCES = ("blocknorm.hip", "conv.hip", "conv_igemm_bf16.hip", "conv_igemm_f16.hip", "conv1x1_stream.hip", "conv_ksplit.hip",
+                      "conv_patch.hip", "conv_smallc.hip", "convert.hip", "dwconv.hip", "fc.hip", "igemm.hpp", "linear4.hip",
+                      "misc.hip", "scan.hip", "seq.hpp", "wino.hpp", "wino_fused.hip",
                       "gemm_common.hpp",
                       "kcommon.hpp", "launch.hpp")
 

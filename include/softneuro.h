@@ -557,10 +557,10 @@ typedef struct {
   int32_t cols;  /* input features */
   int32_t group;
   int32_t act;   /* sn_act */
-} sn_linear4_desc;
-int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint16_t* scale, const uint8_t* zero,
+} sn_qlinear_desc;
+int sn_qlinear_create(const sn_qlinear_desc* desc, const uint8_t* q, const uint16_t* scale, const uint8_t* zero,
                       const float* bias, int32_t device, sn_op** out);
-int sn_linear4_run(sn_op* op, int64_t m, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream);
+int sn_qlinear_run(sn_op* op, int64_t m, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream);
 
 /* Selective state space scan with its short causal convolution.  A token's
  * row of x holds chans = heads * head_dim + 2 * groups * state raw values,

@@ -287,8 +287,8 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // of the product with C, so the state never leaves the registers; and a lane's
 // convolution outputs (times 16 sb + 4 (lane / 16) + v, the same p) are the
 // second operand of both other products.
-// SEG: only the state that the segment adds (from zero; segment 0 from the
-// sequence's, which it copies), no outputs.
+// SEG: only the state that the segment adds (from zero; unless they are carried,
+// segment 0 from the sequence's own, which it copies), no outputs.
 // SHARE: the four waves of 64 columns of a head make its mix of a chunk's rows
 // together.
 //
@@ -512,12 +512,14 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
             for (int v = 0; v < 4; ++v) st[nt][j][v] = fmaf(st[nt][j][v], f, add[nt][j][v]);
       }
     }
-  } else if (seg == 0 && a.state_in) {
-    load_state(a.state_in + ((int64_t)b * a.heads + h) * hold, st);
-    store_state(seg_state(0));
   }
   load_raw(c0);
-  if (!SEG) {
+  if (SEG) {
+    if (!a.carried && seg == 0 && a.state_in) {
+      load_state(a.state_in + ((int64_t)b * a.heads + h) * hold, st);
+      store_state(seg_state(0));
+    }
+  } else {
 #pragma unroll
     for (int j = 0; j < PT; ++j) {
 #pragma unroll
@@ -836,19 +838,20 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 }
 
 // States over the segments, if there are many: slot i, with what segment i - 1
-// adds (with segment 0's whole state for i = 1), takes the state in front of
-// segment i.  Bound by the chain of loads, one per segment.
+// adds, takes the state in front of segment i.  Bound by the chain of loads, one
+// per segment (8 segments of 64 heads of 64 x 128: 8 us).
 __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
   const int64_t hold = (int64_t)a.dim * a.state, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int b = blockIdx.z, h = blockIdx.y;
   if (e >= hold) return;
   const Seq s = seq_of(a, b);
   const int nc = (s.len + Q - 1) / Q;
-  if (2 * a.per >= nc) return;
+  if (a.per >= nc) return;  // one segment, from the sequence's own state
   const int64_t slot = segment0_of(a, s.first, b) * a.heads + h;
-  float* p = a.ws_seg + (slot + a.heads) * hold + e;
-  float v = *p;
-  for (int i = 2; i * a.per < nc; ++i) {
+  float* p = a.ws_seg + slot * hold + e;
+  float v = a.state_in ? a.state_in[((int64_t)b * a.heads + h) * hold + e] : 0.f;
+  *p = v;
+  for (int i = 1; i * a.per < nc; ++i) {
     p += a.heads * hold;
     v = fmaf(v, __builtin_amdgcn_exp2f(a.ws_decay[slot + (int64_t)i * a.heads]), *p);
     *p = v;

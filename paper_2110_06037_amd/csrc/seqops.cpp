@@ -241,13 +241,13 @@ int sn_norm_run(sn_op* p, int64_t rows, const void* x, int64_t x_stride, const v
   });
 }
 
-int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint16_t* scale, const uint8_t* zero,
+int sn_qlinear_create(const sn_qlinear_desc* desc, const uint8_t* q, const uint16_t* scale, const uint8_t* zero,
                       const float* bias, int32_t device, sn_op** out) {
   return guarded([&] {
     if (!out) fail(SN_E_INVALID, "null output pointer");
     *out = nullptr;
     if (!desc || !q || !scale) fail(SN_E_INVALID, "null description, codes or scales");
-    const sn_linear4_desc& d = *desc;
+    const sn_qlinear_desc& d = *desc;
     check_dtype(d.dtype);
     if (d.rows < 1 || d.cols < 1) fail(SN_E_SHAPE, "rows and cols must be positive");
     if (d.rows > (1 << 24) || d.cols > (1 << 20)) fail(SN_E_UNSUPPORTED, "more than 2^24 rows or 2^20 cols");
@@ -286,7 +286,7 @@ int sn_linear4_create(const sn_linear4_desc* desc, const uint8_t* q, const uint1
   });
 }
 
-int sn_linear4_run(sn_op* p, int64_t m, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream) {
+int sn_qlinear_run(sn_op* p, int64_t m, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream) {
   return guarded([&] {
     Linear4Op& op = op_of<Linear4Op>(p, OP_LINEAR4);
     k::Linear4Args a = op.a;

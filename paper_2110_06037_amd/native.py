@@ -122,8 +122,8 @@ SIGNATURES = {
     "sn_norm_create": (ctypes.c_int, [ctypes.POINTER(NormDesc), _F32P, _F32P, _F32P, _F32P, _F32P, _I32,
                                       ctypes.POINTER(_P)]),
     "sn_norm_run": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
-    "sn_linear4_create": (ctypes.c_int, [ctypes.POINTER(Linear4Desc), _P, _P, _P, _F32P, _I32, ctypes.POINTER(_P)]),
-    "sn_linear4_run": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _P]),
+    "sn_qlinear_create": (ctypes.c_int, [ctypes.POINTER(Linear4Desc), _P, _P, _P, _F32P, _I32, ctypes.POINTER(_P)]),
+    "sn_qlinear_run": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _P]),
     "sn_scan_create": (ctypes.c_int, [ctypes.POINTER(ScanDesc), _F32P, _F32P, _F32P, _F32P, _F32P, _I32,
                                       ctypes.POINTER(_P)]),
     "sn_scan_run": (ctypes.c_int, [_P, ctypes.POINTER(ScanIO), _P]),

@@ -150,10 +150,10 @@ class Linear4(_Op):
         bias = _f32(bias, (self.rows,), "bias")
         d = N.Linear4Desc(self.dtype, self.rows, self.cols, group, N.ACT[act])
         p = ctypes.c_void_p()
-        N.check(self.lib.sn_linear4_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data,
+        N.check(self.lib.sn_qlinear_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data,
                                            None if zero is None else zero.ctypes.data, _fp(bias), device,
                                            ctypes.byref(p)))
-        self._op, self._run = p, self.lib.sn_linear4_run
+        self._op, self._run = p, self.lib.sn_qlinear_run
 
     def run(self, x, out=None, stream=None):
         """Enqueue on x [m, cols]; returns y [m, rows]."""

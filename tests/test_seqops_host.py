@@ -81,11 +81,11 @@ def test_linear4_creation_refusals():
     L = N.lib()
     d = N.Linear4Desc(N.BF16, 0, 70, 32, 0)
     p = ctypes.c_void_p()
-    assert L.sn_linear4_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -2
+    assert L.sn_qlinear_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -2
     d.rows, d.act = 4, 7
-    assert L.sn_linear4_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -1
+    assert L.sn_qlinear_create(ctypes.byref(d), q.ctypes.data, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -1
     d.act = 0
-    assert L.sn_linear4_create(ctypes.byref(d), None, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -1
+    assert L.sn_qlinear_create(ctypes.byref(d), None, scale.ctypes.data, None, None, -1, ctypes.byref(p)) == -1
 
 
 def test_linear4_run_refusals_and_foreign_handles():
@@ -97,7 +97,7 @@ def test_linear4_run_refusals_and_foreign_handles():
     norm = BlockNorm("bf16", 8, device=-1)
 
     def run(op=h._op, m=2, x=p, xs=8, y=p, ys=4):
-        return L.sn_linear4_run(op, m, x, xs, y, ys, None)
+        return L.sn_qlinear_run(op, m, x, xs, y, ys, None)
 
     assert run() == -5 and run(m=0, x=None, y=None) == -5
     assert run(m=-1) == -2 and run(m=262141) == -2

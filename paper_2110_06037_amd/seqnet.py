@@ -75,8 +75,9 @@ class SequenceNet:
         return SequenceState(self, seqs)
 
     def _forward(self, x, state, scan):
+        import torch
         u, _ = self.first.run(x)
-        h = x.float()
+        h = x.to(torch.float32, copy=True)  # updated below: never the caller's x
         for b, window, s in zip(self.blocks, state.windows, state.states):
             p = b.in_proj.run(u)
             z, raw, dt = p[:, :b.inner], p[:, b.inner:b.inner + b.chans], p[:, b.inner + b.chans:]

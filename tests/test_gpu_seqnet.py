@@ -96,3 +96,21 @@ def test_captured_steps_equal_eager_ones():
         assert torch.equal(want, out)
     assert all(torch.equal(a, b) for a, b in zip(eager.states + eager.windows, captured.states + captured.windows))
     net.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_inputs_are_left_as_they_are(dtype):
+    import torch
+    net = SequenceNet(dtype, sequence_weights(CONFIG, 2, seed=6), max_seqs=2, max_tokens=20)
+    state = net.new_state(2)
+    x = device(np.random.default_rng(7).standard_normal((20, 96)), dtype)
+    before = x.clone()
+    net.run(x, state)
+    net.step(x[:2], state)
+    assert torch.equal(x, before)
+    token, out, replay = net.capture_step(state)
+    token.copy_(x[:2])
+    replay()
+    torch.cuda.synchronize()
+    assert torch.equal(token, before[:2])
+    net.close()

@@ -372,7 +372,7 @@ constexpr int kL4Stages = 3;
 // float32.
 //
 // Bound by instruction issue: matrix instructions fill a third of the cycles, the
-// codes' way to floats and the runs' scales two fifths more (counted); HBM
+// codes' way to floats and the runs' scales another third (counted); HBM
 // traffic is small.  1500 rows of 2048 inputs
 // and 8512 features: 80 us in bf16, 650 TFLOP/s (a plain library
 // product of 8192^3 reaches 1236); 341 us in float32.

@@ -300,7 +300,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // for a lone wave, 1.5 more for each further wave of a SIMD, whose registers
 // (170) leave room for two; 4096 tokens of 64 heads of 64 x 128 in bf16: 33.5 us
 // for the first pass, 68 for the second, with matrix instructions in 17% of the
-// cycles and other vector instructions in 44%; 8 sequences of 2048, which need no
+// cycles and other vector instructions in 36%; 8 sequences of 2048, which need no
 // first pass, 350 us all told.  Twelve or sixteen waves, or more or fewer
 // segments, were not faster.
 //

@@ -501,7 +501,9 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
     }
   };
   if constexpr (DMA) {
-    // the weights one block ahead, x two; past the last block: zeros
+    // the weights one block ahead (behind the last: the last one's again, not
+    // used; the block is in the scalar offset, which no range check need see), x
+    // two; past the last block: zeros
     W w0, w1;
     load_x(0), load_w(0, w0), load_x(1);
     auto block = [&](int cb, const W& now, W& next) {
@@ -510,7 +512,7 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
       // block cb + 2 is no longer read
       wait_vmcnt<4>();
       dma_barrier();
-      load_w(cb + 1, next), load_x(cb + 2);
+      load_w(min(cb + 1, cbs - 1), next), load_x(cb + 2);
       multiply(cb, now);
     };
     for (int cb = 0; cb < cbs; cb += 2) {

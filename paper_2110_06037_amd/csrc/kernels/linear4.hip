@@ -10,13 +10,16 @@
 //
 // Codes become 16-bit floats by or-ing them into the low mantissa bits of a
 // constant (two weights per instruction).  f16: 1024 + q or 64 + q, less 1024 +
-// z or 64 + z in one packed subtraction: q - z exactly.  bf16: 128 + q, and
-// the 128 + z come off the sums instead, (128 + z) sum_c x[m][c], with the
-// sums over x from an MFMA against ones: cheaper than any exact form, at a
-// cost of 2^-24 * 143 of the terms' sizes in float32, far below a bf16
-// rounding.  float32: x as the exact sum of three bf16 parts, which are three
-// rows of the first operand, times q - z exactly in bf16.  Products are exact,
-// sums float32; a group's scale multiplies the float32 sum of its run.
+// z or 64 + z in one packed subtraction: q - z exactly.  bf16: 16 + q (the code
+// in bits 3 to 6 of 7), and the 16 + z come off the sums instead, (16 + z)
+// sum_c x[m][c], with the sums over x from an MFMA against ones: cheaper than
+// any exact form.  The sums that carry it are float32 and at most 31 times their
+// inputs' sizes; it comes off after every run (few rows) or every 4 runs (many),
+// so that no sum of a whole row carries it: with inputs of one sign, 2048 of
+// them and results near 0, errors of 4 * 2^-24 of the terms' sizes.  float32: x as
+// the exact sum of three bf16 parts, which are three rows of the first operand,
+// times q - z exactly in bf16.  Products are exact, sums float32; a group's scale
+// multiplies the float32 sum of its run.
 #include "seq.hpp"
 
 namespace sn {
@@ -28,8 +31,8 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // One thread per dword of codes; per run of 32 GS inputs a word of scale (low
 // half, binary16) and zero point: [block row][block column][16 features][4 / GS].
 __global__ __launch_bounds__(256) void linear4_pack_kernel(const uint8_t* q, const f16* scale, const uint8_t* zero,
-                                                           int rows, int cols, int group, int gs, unsigned* wq,
-                                                           unsigned* ws) {
+                                                           int rows, int cols, int group, int gs, int up,
+                                                           unsigned* wq, unsigned* ws) {
   const int cbs = (cols + 127) / 128, groups = (cols + group - 1) / group, pairs = (cols + 1) / 2;
   const int64_t total = (int64_t)((rows + 15) / 16) * cbs * 256, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
@@ -44,7 +47,7 @@ __global__ __launch_bounds__(256) void linear4_pack_kernel(const uint8_t* q, con
     // dword bits: inputs 0, 2, 4, 6 from the low half up, 1, 3, 5, 7 from the high half
     w |= code << (4 * (e / 2) + 16 * (e & 1));
   }
-  wq[i] = w;
+  wq[i] = up ? w << up | w >> (32 - up) : w;  // rotated to where bf16 wants the first pair
   const int runs = 4 / gs;
   if (step < runs && lane < 16) {
     const int cr = c0 + 32 * gs * step;
@@ -78,13 +81,13 @@ struct Run4 {
     z64 = zz << 4 | 0x54005400u;
   }
 };
-// The or-ed bits of 1024 + q and 64 + q, or of 128 + q (both halves of a pair).
+// The or-ed bits of 1024 + q and 64 + q, or of 16 + q (both halves of a pair).
 struct Magic {
   unsigned a, b;
 };
 template <typename T>
 __device__ __forceinline__ Magic magic4() {
-  return std::is_same<T, f16>::value ? Magic{vconst(0x64006400u), vconst(0x54005400u)} : Magic{vconst(0x43004300u), 0u};
+  return std::is_same<T, f16>::value ? Magic{vconst(0x64006400u), vconst(0x54005400u)} : Magic{vconst(0x41804180u), 0u};
 }
 __device__ __forceinline__ f16x8 deq_f16(unsigned w, const Run4& c, const Magic& k) {  // q - z
   const f16x2 a = __builtin_bit_cast(f16x2, c.z1024), b = __builtin_bit_cast(f16x2, c.z64);
@@ -96,28 +99,30 @@ __device__ __forceinline__ f16x8 deq_f16(unsigned w, const Run4& c, const Magic&
   r[3] = __builtin_bit_cast(f16x2, (w & 0x00f000f0u) | k.b) - b;
   return __builtin_bit_cast(f16x8, r);
 }
-__device__ __forceinline__ bf16x8 deq_bf16_128(unsigned w, const Magic& k) {  // 128 + q
+constexpr int kUpBf16 = 3;   // bits that the dwords are rotated up by
+constexpr float kOff = 16.f;  // of the codes
+__device__ __forceinline__ bf16x8 deq_bf16_off(unsigned w, const Magic& k) {  // 16 + q
   u32x4 r;
-  r[0] = (w & 0x000f000fu) | k.a;
-  r[1] = ((w >> 4) & 0x000f000fu) | k.a;
-  r[2] = ((w >> 8) & 0x000f000fu) | k.a;
-  r[3] = ((w >> 12) & 0x000f000fu) | k.a;
+  r[0] = (w & 0x00780078u) | k.a;
+  r[1] = ((w >> 4) & 0x00780078u) | k.a;
+  r[2] = ((w >> 8) & 0x00780078u) | k.a;
+  r[3] = (__builtin_amdgcn_alignbit(w, w, 12) & 0x00780078u) | k.a;
   return __builtin_bit_cast(bf16x8, r);
 }
-// q - z: the two halves of a pair are the high halves of the floats 128 + q
-__device__ __forceinline__ bf16x8 deq_bf16(unsigned w, float z128, const Magic& k) {
-  u32x4 r = __builtin_bit_cast(u32x4, deq_bf16_128(w, k));
+// q - z: the two halves of a pair are the high halves of the floats 16 + q
+__device__ __forceinline__ bf16x8 deq_bf16(unsigned w, float zoff, const Magic& k) {
+  u32x4 r = __builtin_bit_cast(u32x4, deq_bf16_off(w, k));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float lo = __builtin_bit_cast(float, r[i] << 16) - z128, hi = __builtin_bit_cast(float, r[i] & 0xffff0000u) - z128;
+    const float lo = __builtin_bit_cast(float, r[i] << 16) - zoff, hi = __builtin_bit_cast(float, r[i] & 0xffff0000u) - zoff;
     r[i] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, hi), __builtin_bit_cast(unsigned, lo), 0x07060302u);
   }
   return __builtin_bit_cast(bf16x8, r);
 }
 template <typename T>
 __device__ __forceinline__ auto deq4(unsigned w, const Run4& c, const Magic& k) {
-  if constexpr (std::is_same<T, float>::value) return deq_bf16(w, 128.f + c.z, k);
-  else if constexpr (std::is_same<T, bf16>::value) return deq_bf16_128(w, k);
+  if constexpr (std::is_same<T, float>::value) return deq_bf16(w, kOff + c.z, k);
+  else if constexpr (std::is_same<T, bf16>::value) return deq_bf16_off(w, k);
   else return deq_f16(w, c, k);
 }
 
@@ -316,7 +321,7 @@ __global__ __launch_bounds__(R == 1 && NB < 4 ? 1024 : 512) void linear4_rows_ke
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
               for (int v = 0; v < NV; ++v) over = over || !(fabsf(acc[nb][v]) < INFINITY);
-            const float zz = 128.f + rc.z;
+            const float zz = kOff + rc.z;
             if (__any(over)) {
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb) {
@@ -368,14 +373,16 @@ constexpr int kL4Stages = 3;
 // types, wide rows): LDS direct loads, three blocks of 128 inputs in a ring,
 // two blocks ahead; else through registers, one block ahead (float32 is split
 // into its parts there).  bf16: sums against ones, each wave for 16 of the rows,
-// wait in LDS, and the bias comes off at the end, as one more matrix product, in
-// float32.
+// meet in LDS, and after every 4 runs the bias comes off as one more matrix
+// product in float32, whose 4 steps are the runs.
 //
 // Bound by instruction issue: matrix instructions fill a third of the cycles, the
 // codes' way to floats and the runs' scales another third (counted); HBM
 // traffic is small.  1500 rows of 2048 inputs
-// and 8512 features: 80 us in bf16, 650 TFLOP/s (a plain library
-// product of 8192^3 reaches 1236); 341 us in float32.
+// and 8512 features: 75 us in bf16, 700 TFLOP/s (a plain library
+// product of 8192^3 reaches 1236); 341 us in float32.  (The bias off the whole
+// sums at the end, from sums over x that wait in LDS, was 3 us faster, with ten
+// times the error, and had no room for rows of more than 128 runs.)
 template <typename T, int RB, int GS, bool VX>
 __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int tiles_m, int tiles_n) {
   typedef typename Op4<T>::E E;
@@ -384,10 +391,11 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
   constexpr bool DMA = VX && !F32;
   constexpr int RUNS = 4 / GS, PARTS = F32 ? 3 : 1;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  // [stage][part][row][slot] of 16 bytes, then the sums
+  // [stage][part][row][slot] of 16 bytes, then (bf16) the sums over x of the last
+  // 8 runs, and each wave's words of the last 4 (in registers they spilled)
   frag* xt = reinterpret_cast<frag*>(smem);
   constexpr int STAGE = PARTS * 4 * 4 * 64, STAGES = DMA ? kL4Stages : 2;
-  float* xsum = reinterpret_cast<float*>(xt + STAGES * STAGE);  // [run][64]
+  float* xsum = reinterpret_cast<float*>(xt + STAGES * STAGE);  // [run % 8][64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int cbs = (a.cols + 127) / 128, rbs = (a.rows + 15) / 16;
@@ -426,6 +434,32 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
     for (int r = 0; r < RB; ++r) tot[i][r] = f32x4{0.f, 0.f, 0.f, 0.f};
   const Magic magic = magic4<T>();
   const frag ones = __builtin_bit_cast(frag, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+  const int runs = cbs * RUNS;
+  constexpr int WORDS = 4 * RB * 16;
+  unsigned* const words = reinterpret_cast<unsigned*>(xsum + 8 * 64) + wave * RB * 16;  // [run % 4][wave][RB][16]
+  // The bias of runs q .. q + 3 off the sums (those behind the last do not count).
+  auto settle = [&](int q) {
+    if constexpr (BIASED) {
+      int l = lane;
+      if constexpr (BIASED) asm volatile("" : "+v"(l));
+      const int run = q + (l >> 4), c = l & 15;
+      const bool on = run < runs;
+      float xs[4];
+#pragma unroll
+      for (int mi = 0; mi < 4; ++mi) xs[mi] = on ? xsum[(run & 7) * 64 + 16 * ((wave + mi) & 3) + c] : 0.f;
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        const Run4 rc(words[(l >> 4) * WORDS + r * 16 + c]);
+        const float zs = on ? -(kOff + rc.z) * rc.s : 0.f;
+#pragma unroll
+        for (int mi = 0; mi < 4; ++mi) tot[mi][r] = Mfma<float>::run(xs[mi], zs, tot[mi][r]);
+      }
+    }
+  };
+  // Behind the barrier in front of a block: the blocks before it have left 4 new runs.
+  auto settle_before = [&](int cb) {
+    if (cb > 0 && cb * RUNS % 4 == 0) settle(cb * RUNS - 4);
+  };
   V8<T> xn[DMA ? 1 : 4];
   struct W {
     u32x4 q[RB];
@@ -464,8 +498,10 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
       }
   };
   auto multiply = [&](int cb, const W& w) {
-    const frag* xc = xt + (cb % STAGES) * STAGE + col * 16;
-    auto xfrag = [&](int p, int mi, int i) { return xc[(p * 4 + ((wave + mi) & 3)) * 256 + ((4 * i + g) ^ col)]; };
+    int l = lane;
+    if constexpr (BIASED) asm volatile("" : "+v"(l));  // 16 addresses that would stay in registers through the loop
+    const frag* xc = xt + (cb % STAGES) * STAGE + (l & 15) * 16;
+    auto xfrag = [&](int p, int mi, int i) { return xc[(p * 4 + ((wave + mi) & 3)) * 256 + ((4 * i + (l >> 4)) ^ (l & 15))]; };
 #pragma unroll
     for (int run = 0; run < RUNS; ++run) {
       f32x4 acc[4][RB], xs = {0.f, 0.f, 0.f, 0.f};
@@ -488,7 +524,12 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
             for (int r = 0; r < RB; ++r) acc[mi][r] = Mfma<E>::run(xf, wf[r], acc[mi][r]);
           }
       }
-      if (BIASED && col == 0) *reinterpret_cast<f32x4*>(xsum + (cb * RUNS + run) * 64 + 16 * wave + 4 * g) = xs;
+      if constexpr (BIASED) {
+        if (col == 0) *reinterpret_cast<f32x4*>(xsum + ((cb * RUNS + run) & 7) * 64 + 16 * wave + 4 * g) = xs;
+        if (g == 0)
+#pragma unroll
+          for (int r = 0; r < RB; ++r) words[((cb * RUNS + run) & 3) * WORDS + r * 16 + col] = w.s[r][run];
+      }
 #pragma unroll
       for (int mi = 0; mi < 4; ++mi)
 #pragma unroll
@@ -513,6 +554,7 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
       wait_vmcnt<4>();
       dma_barrier();
       load_w(min(cb + 1, cbs - 1), next), load_x(cb + 2);
+      settle_before(cb);
       multiply(cb, now);
     };
     for (int cb = 0; cb < cbs; cb += 2) {
@@ -526,31 +568,20 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
     for (int cb = 0; cb < cbs; cb += 2) {
       lds_barrier();  // the stage is written, and the other one no longer read
       if (cb + 1 < cbs) load_x(cb + 1), load_w(cb + 1, w1);
+      settle_before(cb);
       multiply(cb, w0);
       if (cb + 1 >= cbs) break;
       put(cb + 1);
       lds_barrier();
       if (cb + 2 < cbs) load_x(cb + 2), load_w(cb + 2, w0);
+      settle_before(cb + 1);
       multiply(cb + 1, w1);
       if (cb + 2 < cbs) put(cb + 2);
     }
   }
   if constexpr (BIASED) {
     __syncthreads();
-    const int runs = cbs * RUNS;
-    for (int q = 0; q < runs; q += 4) {
-      const int run = q + g;
-      float xs[4];
-#pragma unroll
-      for (int mi = 0; mi < 4; ++mi) xs[mi] = run < runs ? xsum[run * 64 + 16 * ((wave + mi) & 3) + col] : 0.f;
-#pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        const Run4 rc(__builtin_amdgcn_raw_buffer_load_b32(rs[r], run / RUNS * 64 * RUNS + col * 4 * RUNS + run % RUNS * 4, 0, 0));
-        const float zs = run < runs ? -(128.f + rc.z) * rc.s : 0.f;
-#pragma unroll
-        for (int mi = 0; mi < 4; ++mi) tot[mi][r] = Mfma<float>::run(xs[mi], zs, tot[mi][r]);
-      }
-    }
+    settle((cbs - 1) * RUNS / 4 * 4);
   }
   // The results leave through LDS, as rows of 64 RB features: wide stores
   // (straight from the accumulators they would be runs of 16 features, a third
@@ -591,7 +622,8 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
         const int64_t b = blk + c / 128;
         const Run4 rc(a.ws[(b * 16 + col) * RUNS + c % 128 / (32 * GS)]);
         const unsigned dw = a.wq[(b * 64 + col + 16 * (c % 32 / 8)) * 4 + c % 128 / 32];
-        sum = fmaf(to_f(x[c]), ((float)(dw >> (4 * (c % 8 / 2) + 16 * (c & 1)) & 15) - rc.z) * rc.s, sum);
+        const unsigned code = __builtin_amdgcn_alignbit(dw, dw, kUpBf16 + 4 * (c % 8 / 2) + 16 * (c & 1)) & 15;
+        sum = fmaf(to_f(x[c]), ((float)code - rc.z) * rc.s, sum);
       }
       out[m * PITCH + (wave * RB + r) * 16 + col] = from_f<T>(act4(sum + (a.bias ? a.bias[k] : 0.f), a.act));
     }
@@ -617,12 +649,12 @@ __global__ __launch_bounds__(256, 2) void linear4_tile_kernel(Linear4Args a, int
 int linear4_gs(int group) { return group % 128 == 0 ? 4 : group % 64 == 0 ? 2 : 1; }
 int64_t linear4_blocks(int rows, int cols) { return (int64_t)((rows + 15) / 16) * ((cols + 127) / 128); }
 
-void linear4_pack(const uint8_t* q, const f16* scale, const uint8_t* zero, int rows, int cols, int group, unsigned* wq,
-                  unsigned* ws, hipStream_t st) {
+void linear4_pack(int dtype, const uint8_t* q, const f16* scale, const uint8_t* zero, int rows, int cols, int group,
+                  unsigned* wq, unsigned* ws, hipStream_t st) {
   const int64_t blocks = linear4_blocks(rows, cols);
   check(blocks < (int64_t(1) << 31), "4-bit weights");
   SN_LAUNCH(linear4_pack_kernel, dim3((unsigned)blocks), dim3(256), 0, st, q, scale, zero, rows, cols, group,
-            linear4_gs(group), wq, ws);
+            linear4_gs(group), dtype == 1 ? 0 : kUpBf16, wq, ws);
 }
 
 template <typename T, int NB, int MV, int GS, bool VX, int R, int U>
@@ -649,20 +681,17 @@ static void launch_rows(const Linear4Args& a, hipStream_t st) {
 
 template <typename T, int RB, int GS, bool VX>
 static void launch_tile(const Linear4Args& a, hipStream_t st) {
-  const int tm = (int)((a.m + 63) / 64), tn = (a.rows + 64 * RB - 1) / (64 * RB), cbs = (a.cols + 127) / 128;
+  const int tm = (int)((a.m + 63) / 64), tn = (a.rows + 64 * RB - 1) / (64 * RB);
   constexpr bool F32 = std::is_same<T, float>::value, DMA = VX && !F32;
   const size_t lds = (DMA ? kL4Stages : 2) * (F32 ? 3 : 1) * 16384 +
-                     (std::is_same<T, bf16>::value ? (size_t)cbs * (4 / GS) * 256 : 0);
+                     (std::is_same<T, bf16>::value ? 8 * 256 + 4 * 4 * RB * 64 : 0);
   SN_LAUNCH((linear4_tile_kernel<T, RB, GS, VX>), dim3((unsigned)(tm * tn)), dim3(256), lds, st, a, tm, tn);
 }
 
 template <typename T, int GS, bool VX>
 static void launch_linear4(const Linear4Args& a, hipStream_t st) {
   constexpr bool F32 = std::is_same<T, float>::value;
-  // the tile kernel keeps the sums of bf16 inputs in LDS, 256 bytes a run: with
-  // its stages at most 80 KB
-  const bool fits = !std::is_same<T, bf16>::value || (int64_t)((a.cols + 127) / 128) * (4 / GS) <= 128;
-  if (a.m > (F32 ? 16 : 32) && fits) {
+  if (a.m > (F32 ? 16 : 32)) {
     // as wide as registers allow (more runs in a block, or parts, take more of
     // them), if the tiles still fill the chip
     constexpr int RB = F32 ? GS == 4 ? 2 : 1 : GS == 4 && VX ? 4 : GS == 1 && !VX ? 1 : 2;

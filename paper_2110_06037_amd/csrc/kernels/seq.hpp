@@ -51,8 +51,8 @@ struct Linear4Args {
 // 64 / linear4_gs words of scale and zero point.
 int64_t linear4_blocks(int rows, int cols);
 int linear4_gs(int group);  // steps of 32 inputs that share a scale
-void linear4_pack(const uint8_t* q, const f16* scale, const uint8_t* zero, int rows, int cols, int group, unsigned* wq,
-                  unsigned* ws, hipStream_t st);
+void linear4_pack(int dtype, const uint8_t* q, const f16* scale, const uint8_t* zero, int rows, int cols, int group,
+                  unsigned* wq, unsigned* ws, hipStream_t st);
 void linear4(const Linear4Args& a, hipStream_t st);
 
 // ------------------------------------------------------------------ selective scan

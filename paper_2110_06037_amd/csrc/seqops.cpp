@@ -276,7 +276,7 @@ int sn_qlinear_create(const sn_qlinear_desc* desc, const uint8_t* q, const uint1
       const int64_t blocks = k::linear4_blocks(d.rows, d.cols), scales = blocks * 64 / k::linear4_gs(d.group);
       unsigned* wq = static_cast<unsigned*>(op->alloc(blocks * 1024));
       unsigned* ws = static_cast<unsigned*>(op->alloc(scales * 4));
-      k::linear4_pack(rq, reinterpret_cast<const k::f16*>(rs), rz, d.rows, d.cols, d.group, wq, ws, nullptr);
+      k::linear4_pack(d.dtype, rq, reinterpret_cast<const k::f16*>(rs), rz, d.rows, d.cols, d.group, wq, ws, nullptr);
       HIPCHK(hipGetLastError());
       a.wq = wq, a.ws = ws;
       a.bias = op->upload(bias, d.rows);

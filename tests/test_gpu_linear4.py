@@ -153,3 +153,33 @@ def test_another_stream_and_graph_replays():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(op.run(x), y)
+
+
+@pytest.mark.parametrize("m,cols,group", [(20, 2048, 128), (70, 2048, 128), (70, 4096, 64), (70, 2040, 32), (70, 2048, 96),
+                                          (70, 8192, 32)])
+def test_sums_of_bf16_inputs_have_float32_precision(m, cols, group):
+    # Inputs of one sign whose second half repeats the first, against weights
+    # that are its negative: every exact result is 0, and what comes out is the
+    # error of the sums, almost unrounded.
+    #
+    # A rounding of a partial sum v is at most 2^-24 |v|, 2^-24 |v| / sqrt(3) in
+    # the root mean square, and the errors of different roundings add like
+    # their squares.  Codes may be summed around an offset that leaves them
+    # below 32 (exact in bf16 beside 4 bits of code): the sums of 512 inputs
+    # reach 24 * 512 * 1.5 scales, with up to 8 roundings of that size and 16 for each
+    # 128 of them at a quarter of it: sqrt(8 + 4 * 16 / 16) * 18432 / sqrt(3) =
+    # 36900 for 512 inputs.  Their terms' sizes are 3.7 * 1.5 in the mean, 2870
+    # for 512: 13 of 2^-24 of the sizes, and 2048 inputs, four times, halve
+    # that ratio: 6.5.  A factor of 2.5 above it: 16.
+    r = np.random.default_rng(cols + group)
+    rows, half = 80, cols // 2
+    d = r.integers(-7, 8, (rows, half))
+    code = np.concatenate([8 + d, 8 - d], 1).astype(np.uint8)
+    x = rounded(1 + r.random((m, half)), "bf16")
+    x = np.concatenate([x, x], 1)
+    scale = np.ones((rows, -(-cols // group)), np.float16)
+    op = Linear4("bf16", code[:, 0::2] | (code[:, 1::2] << 4), scale, cols=cols, group=group)
+    got = host(op.run(device(x, "bf16")))
+    size = x @ np.abs(code.astype(np.float64) - 8).T
+    assert np.linalg.norm(got) <= 16 * 2.0 ** -24 * np.linalg.norm(size)
+    op.close()

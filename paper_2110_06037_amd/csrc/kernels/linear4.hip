@@ -33,7 +33,8 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 __global__ __launch_bounds__(256) void linear4_pack_kernel(const uint8_t* q, const f16* scale, const uint8_t* zero,
                                                            int rows, int cols, int group, int gs, int up,
                                                            unsigned* wq, unsigned* ws) {
-  const int cbs = (cols + 127) / 128, groups = (cols + group - 1) / group, pairs = (cols + 1) / 2;
+  // (a group may be nearly 2^31 wide: unsigned, the sum does not overflow)
+  const int cbs = (cols + 127) / 128, groups = ((unsigned)cols + (unsigned)group - 1) / group, pairs = (cols + 1) / 2;
   const int64_t total = (int64_t)((rows + 15) / 16) * cbs * 256, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
   const int step = (int)(i & 3), lane = (int)(i >> 2) & 63;

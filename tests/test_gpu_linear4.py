@@ -183,3 +183,11 @@ def test_sums_of_bf16_inputs_have_float32_precision(m, cols, group):
     size = x @ np.abs(code.astype(np.float64) - 8).T
     assert np.linalg.norm(got) <= 16 * 2.0 ** -24 * np.linalg.norm(size)
     op.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_groups_wider_than_the_rows(dtype):
+    # one scale and zero point per row, up to the largest group there is
+    for group in (1024, 1 << 30, (1 << 31) - 32):
+        run_case(dtype, 3, 300, 40, group, True)
+        run_case(dtype, 40, 300, 40, group, True)

@@ -9,6 +9,7 @@ current stream of the handle's device, or on ``stream``, and returns at once.
 from __future__ import annotations
 
 import ctypes
+import operator
 
 import numpy as np
 
@@ -23,6 +24,14 @@ def _f32(v, shape, name):
     if a.shape != tuple(shape):
         raise ValueError(f"{name} has shape {a.shape}, not {tuple(shape)}")
     return a
+
+
+def _int(v, name, least=-(1 << 31)):
+    """A whole number that fits the C ABI's int32 (ctypes would cut it to 32 bits)."""
+    v = operator.index(v)
+    if not least <= v < 1 << 31:
+        raise ValueError(f"{name} is out of range: {v}")
+    return v
 
 
 def _fp(a):
@@ -42,7 +51,7 @@ class _Op:
         if self.dtype not in self._types:
             raise ValueError(f"unknown dtype {dtype!r}")
         self.torch_dtype = self._types[self.dtype]
-        self.device = device
+        self.device = device = _int(device, "device")
         self._dev = torch.device("cuda", device) if device >= 0 else None
         # the current stream's pointer, without making a Stream object of it (1 us)
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -135,8 +144,9 @@ class Linear4(_Op):
     def __init__(self, dtype, q, scale, zero=None, bias=None, cols=None, group=128, act="none", device=0):
         super().__init__(dtype, device)
         q = np.ascontiguousarray(q, dtype=np.uint8)
+        group = _int(group, "group", 1)
         self.rows = q.shape[0]
-        self.cols = 2 * q.shape[1] if cols is None else cols
+        self.cols = 2 * q.shape[1] if cols is None else _int(cols, "cols")
         if q.shape[1] != (self.cols + 1) // 2:
             raise ValueError(f"{q.shape[1]} bytes of codes a row do not hold {self.cols} columns")
         scale = np.ascontiguousarray(scale, dtype=np.float16)
@@ -192,6 +202,9 @@ class Scan(_Op):
     def __init__(self, dtype, heads, head_dim, groups, state, conv_w, conv_b=None, a=None, d=None, dt_bias=None,
                  max_seqs=1, max_tokens=1, device=0):
         super().__init__(dtype, device)
+        heads, head_dim, groups, state, max_seqs = (
+            _int(v, n) for v, n in ((heads, "heads"), (head_dim, "head_dim"), (groups, "groups"), (state, "state"),
+                                    (max_seqs, "max_seqs")))
         self.heads, self.head_dim, self.groups, self.state = heads, head_dim, groups, state
         self.inner, self.chans = heads * head_dim, heads * head_dim + 2 * groups * state
         conv_w = np.ascontiguousarray(conv_w, dtype=np.float32)
@@ -278,13 +291,13 @@ class BlockNorm(_Op):
                  gate="none", groups=1, eps=1e-5, residual=None, device=0):
         super().__init__(dtype, device)
         rd = -1 if residual is None else N.DTYPE[residual] if isinstance(residual, str) else residual
-        self.dim, self.gate = dim, gate
+        self.dim, self.gate = _int(dim, "dim"), gate
         self.res_dtype = None if rd < 0 else self._types[rd]
         self.has_y = pre is not None or rd < 0
         vector = scale is not None and np.ndim(scale) > 0
         arrays = [_f32(v, (dim,), n) for v, n in ((post, "post"), (post_bias, "post_bias"), (pre, "pre"),
                                                   (pre_bias, "pre_bias"), (scale if vector else None, "scale"))]
-        d = N.NormDesc(self.dtype, rd, dim, groups, N.NORM[kind], N.GATE[gate], eps,
+        d = N.NormDesc(self.dtype, rd, dim, _int(groups, "groups"), N.NORM[kind], N.GATE[gate], eps,
                        1.0 if scale is None or vector else float(scale))
         p = ctypes.c_void_p()
         N.check(self.lib.sn_norm_create(ctypes.byref(d), *[_fp(a) for a in arrays], device, ctypes.byref(p)))

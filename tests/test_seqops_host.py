@@ -173,3 +173,18 @@ def test_scan_run_refusals():
     assert call(seqs=0, tokens=1) == -2
     assert call(True, tokens=4) == -2 and call(True, offsets=p) == -2
     assert L.sn_scan_run(handle._op, None, None) == -1
+
+
+def test_numbers_beyond_int32_are_refused():
+    # they would arrive cut to 32 bits: a group of 2^32 + 32 as 32, with the
+    # scales of one group per row
+    from paper_2110_06037_amd import Linear4, quantize4
+    q, scale, _ = quantize4(np.ones((4, 64)), 64)
+    for group in ((1 << 32) + 32, 0, -32):
+        with pytest.raises(ValueError):
+            Linear4("bf16", q, scale, cols=64, group=group, device=-1)
+    for wrong in (dict(max_seqs=(1 << 32) + 3), dict(device=(1 << 32) - 1)):
+        with pytest.raises(ValueError):
+            _scan(**wrong)
+    with pytest.raises(ValueError):
+        BlockNorm("bf16", 8, groups=(1 << 32) + 1, device=-1)

@@ -16,7 +16,9 @@
 // All decays are at most 1 (a <= 0).  c is held as hi + lo with hi in steps of
 // 1/256, so that differences of hi are exact and those of lo small: a plain
 // float32 sum would lose the differences of neighbours late in a chunk of
-// strong decays.
+// strong decays.  A step's log2 decay counts as at least -1000: 2^-1000 is 0
+// beside anything in float32, and 64 steps stay below 2^16, up to where float32
+// holds every multiple of 1/256.
 #include "seq.hpp"
 
 namespace sn {
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
       const float v = to_f(static_cast<const T*>(a.dt)[(s.first + t) * a.dts + h]) + a.dt_bias[h];
       dt = v > 20.f ? v : log1pf(expf(v));  // beyond 20 the difference is below a unit
       inc = dt * a.a2[h];
-      if (inc < -1e4f) inc = -1e4f;  // 2^-1e4 is 0: keeps the sums finite, NaN stays
+      if (inc < -1000.f) inc = -1000.f;  // still 0, and the sums' hi exact; NaN stays
     }
     float ch = rintf(inc * 256.f) * (1.f / 256.f), cl = inc - ch;
 #pragma unroll

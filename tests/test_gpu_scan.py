@@ -404,3 +404,16 @@ def test_the_stride_of_a_single_row_is_not_looked_at(dtype):
         io.x_stride = io.dt_stride = io.y_stride = 0
         N.check(f(op._op, io, torch.cuda.current_stream().cuda_stream))
         assert all(torch.equal(a, b) for a, b in zip(want, (y, w, s)))
+
+
+@pytest.mark.parametrize("strong,dt", [(30, 200.0), (50, 120.0), (60, 1e4), (10, 1e4), (63, 50.0)])
+def test_weak_decays_behind_strong_ones(strong, dt):
+    # rows whose decay leaves nothing, then rows of a tenth and less in the same
+    # chunk: the decays among the latter come from differences of the chunk's sums
+    c = Case("f32", [64, 100], heads=4, dim=16, state=16, rate=(16, 16))
+    c.dt[:strong] = dt
+    c.dt[64:64 + strong] = dt
+    c.dt_bias[:] = 0
+    c.dt[strong:64] = -4.6
+    c.dt[64 + strong:] = -4.6
+    c.check(c.run(c.op()))

@@ -655,6 +655,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       fetch_c(c + 1);
       if (TWO) fetch_b(c + 1);
     }
+    // the AFTER accesses that follow stay behind these
+    asm volatile("" ::: "memory");
     if constexpr (SEG) scalars();
     load_raw(c + 1);
     if (t0 + Q > s.len) {  // past the end: zero (a NaN would meet the zeros of earlier rows)

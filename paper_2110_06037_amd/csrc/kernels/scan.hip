@@ -323,10 +323,6 @@ constexpr int scan_lds(int waves) {  // B, C, S, two sets of largest sizes, two 
 }
 template <typename T, int NT, bool SHARE, bool SEG>
 __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) {
-  // Columns per lane.  Two (waves of 32 columns) measured 129 us against 130 at
-  // 4096 tokens of 64 heads, but 437 against 351 at 8 sequences of 2048: fewer
-  // waves, and no registers left for the rows ahead.
-  constexpr int PT = 1;
   constexpr bool TWO = scan_two<NT, SEG>();
   extern __shared__ __attribute__((aligned(16))) char smem[];
   char* const ldsB = smem;
@@ -340,7 +336,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   // offsets, segments vary slowest: most sequences have none of the later ones,
   // and workgroups without work at regular places leave whole shader engines
   // idle (8 sequences of 2048 rows: 981 us against 357).
-  const int each = a.heads / a.groups, pblocks = (a.dim + 16 * PT - 1) / (16 * PT);
+  const int each = a.heads / a.groups, pblocks = (a.dim + 15) / 16;
   const int ublocks = (each * pblocks + waves - 1) / waves, yblocks = a.groups * ublocks;
   const unsigned rest = blockIdx.x / a.seqs;
   const int b = blockIdx.x % a.seqs;
@@ -370,49 +366,43 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     }
   }
   const int h = grp * each + unit / pblocks;
-  const int pb = (unit % pblocks) * 16 * PT, p0 = pb + PT * col;  // this lane's first p
-  const int pn = live ? a.dim - p0 : 0;                           // and how many of its PT exist (<= 0: none)
+  const int p0 = unit % pblocks * 16 + col;  // this lane's p
+  const bool have = live && p0 < a.dim;      // whether it exists
   const int64_t hold = (int64_t)a.dim * N;
 
-  f32x4 st[NT][PT];
+  f32x4 st[NT];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int j = 0; j < PT; ++j) st[nt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int nt = 0; nt < NT; ++nt) st[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
   // the lane's part of a head's state; what is outside it has an offset out of range
-  auto at_state = [&](int nt, int j, int v) {
+  auto at_state = [&](int nt, int v) {
     const int n = 16 * nt + 4 * g + v;
-    return (int)(j < pn && n < N ? ((unsigned)(p0 + j) * (unsigned)N + (unsigned)n) * 4u : kOOB);
+    return (int)(have && n < N ? ((unsigned)p0 * (unsigned)N + (unsigned)n) * 4u : kOOB);
   };
-  auto load_state = [&](const float* p, f32x4 (&to)[NT][PT]) {
+  auto load_state = [&](const float* p, f32x4 (&to)[NT]) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, hold * 4);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
+      if (a.vec_state) {
+        to[nt] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at_state(nt, 0), 0, 0));
+      } else {
 #pragma unroll
-      for (int j = 0; j < PT; ++j)
-        if (a.vec_state) {
-          to[nt][j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at_state(nt, j, 0), 0, 0));
-        } else {
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            to[nt][j][v] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at_state(nt, j, v), 0, 0));
-        }
+        for (int v = 0; v < 4; ++v)
+          to[nt][v] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at_state(nt, v), 0, 0));
+      }
   };
   auto store_state = [&](float* p) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p, hold * 4);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
+      if (a.vec_state) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, st[nt]), r, at_state(nt, 0), 0, 0);
+      } else {
 #pragma unroll
-      for (int j = 0; j < PT; ++j)
-        if (a.vec_state) {
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, st[nt][j]), r, at_state(nt, j, 0), 0, 0);
-        } else {
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float one = st[nt][j][v];  // (a bit cast of the element itself reads element 0)
-            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, one), r, at_state(nt, j, v), 0, 0);
-          }
+        for (int v = 0; v < 4; ++v) {
+          const float one = st[nt][v];  // (a bit cast of the element itself reads element 0)
+          __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, one), r, at_state(nt, v), 0, 0);
         }
+      }
   };
   // the head's slot of segment i
   const int64_t head_seg0 = segment0_of(a, s.first, b) * a.heads + h;
@@ -421,7 +411,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   // per column: at least the size of every value of the state (within a few
   // powers of two).  Scales are a column's own, so no column's values have a
   // part in another's.
-  float top[PT] = {};
+  float top = 0.f;
   auto col_max = [&](float v) {  // over the lanes of a column
     v = fmaxf(v, __shfl_xor(v, 16));
     return fmaxf(v, __shfl_xor(v, 32));
@@ -431,13 +421,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   if (SEG ? c1 >= nc : seg > 0 && c0 >= nc) return;
   // the lane's convolution
   const int ch0 = h * a.dim + p0;
-  float w[4][PT], cb[PT];
+  float w[4];
+  const float cb = have ? a.conv_b[ch0] : 0.f;
 #pragma unroll
-  for (int j = 0; j < PT; ++j) {
-    cb[j] = j < pn ? a.conv_b[ch0 + j] : 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k][j] = j < pn ? a.conv_w[k * a.chans + ch0 + j] : 0.f;
-  }
+  for (int k = 0; k < 4; ++k) w[k] = have ? a.conv_w[k * a.chans + ch0] : 0.f;
   const float dh = a.d[h];
   const unsigned rowb = (unsigned)a.xs * (unsigned)sizeof(T);
   const unsigned xoff = 4 * g * rowb + (unsigned)(h * a.dim + p0) * (unsigned)sizeof(T);
@@ -465,7 +452,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   };
   // Raw rows 16 sb + 4 g - 3 + k of a chunk; rows past the end (or before the
   // sequence) give zero, and so does a chunk past the segment.
-  T raw[4][7][PT];
+  T raw[4][7];
   auto load_raw = [&](int c) {
     unsigned xo = xoff;  // per chunk: kept out of the loop, its 28 sums would fill the registers
     asm volatile("" : "+v"(xo));
@@ -478,13 +465,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       for (int k = 0; k < 7; ++k) {
         const bool before = sb == 0 && k < 3 && c == 0 && g == 0;
         const unsigned row = xo + (16 * sb + k) * rowb;  // in the offset that the range check sees
-        const unsigned o = before || pn < PT ? kOOB : row;
+        const unsigned o = before || !have ? kOOB : row;
         if constexpr (sizeof(T) == 2) {
           const uint16_t v = __builtin_amdgcn_raw_buffer_load_b16(rx, (int)o, 0, 0);
-          __builtin_memcpy(raw[sb][k], &v, 2);
+          __builtin_memcpy(&raw[sb][k], &v, 2);
         } else {
           const unsigned v = __builtin_amdgcn_raw_buffer_load_b32(rx, (int)o, 0, 0);
-          __builtin_memcpy(raw[sb][k], &v, 4);
+          __builtin_memcpy(&raw[sb][k], &v, 4);
         }
       }
   };
@@ -503,15 +490,13 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       const int from = a.carried ? seg : 1;
       load_state(seg_state(from), st);
       for (int i = from + 1; i <= seg; ++i) {
-        f32x4 add[NT][PT];
+        f32x4 add[NT];
         load_state(seg_state(i), add);
         const float f = __builtin_amdgcn_exp2f(a.ws_decay[seg_slot(i)]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int j = 0; j < PT; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) st[nt][j][v] = fmaf(st[nt][j][v], f, add[nt][j][v]);
+          for (int v = 0; v < 4; ++v) st[nt][v] = fmaf(st[nt][v], f, add[nt][v]);
       }
     }
   }
@@ -523,13 +508,10 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < PT; ++j) {
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) top[j] = fmaxf(top[j], fabsf(st[nt][j][v]));
-      top[j] = col_max(top[j]);
-    }
+      for (int v = 0; v < 4; ++v) top = fmaxf(top, fabsf(st[nt][v]));
+    top = col_max(top);
   }
   wait_vmcnt<0>();
   dma_barrier();
@@ -546,34 +528,25 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       maxb = maxes[0], maxc = maxes[1], cend = dtp[5 * Q], maxdt = dtp[5 * Q + 1], maxf = dtp[5 * Q + 2];
     };
     if constexpr (!SEG) scalars();
-    f32x4 acc[4][PT];
+    f32x4 acc[4];
     if constexpr (!SEG) {
       // ---- C times the state in front of the chunk
-      float sh[PT];
+      const float sh = pow2_for(top);
 #pragma unroll
-      for (int j = 0; j < PT; ++j) sh[j] = pow2_for(top[j]);
-#pragma unroll
-      for (int tb = 0; tb < 4; ++tb)
-#pragma unroll
-        for (int j = 0; j < PT; ++j) acc[tb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int tb = 0; tb < 4; ++tb) acc[tb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int q = 0; q < NT / 2; ++q) {
-        HiLo hf[PT];
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < PT; ++j) {
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = sh[j] * st[2 * q + (e >> 2)][j][e & 3];
-          hf[j] = split8(v);
-        }
+        for (int e = 0; e < 8; ++e) v[e] = sh * st[2 * q + (e >> 2)][e & 3];
+        const HiLo hf = split8(v);
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb) {
           const f16* cp = Cg + (tb * (NT / 2) + q) * 1024;
           HiLo cf;
           cf.hi = *reinterpret_cast<const f16x8*>(cp);
           cf.lo = *reinterpret_cast<const f16x8*>(cp + 512);
-#pragma unroll
-          for (int j = 0; j < PT; ++j) acc[tb][j] = mul3(cf, hf[j], acc[tb][j]);
+          acc[tb] = mul3(cf, hf, acc[tb]);
         }
       }
     }
@@ -583,34 +556,26 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
         const int i = a.conv - 4 + k;
-#pragma unroll
-        for (int j = 0; j < PT; ++j)
-          if (i >= 0 && j < pn)
-            raw[0][k][j] = static_cast<const T*>(a.wcopy)[((int64_t)b * (a.conv - 1) + i) * a.chans + ch0 + j];
+        if (i >= 0 && have) raw[0][k] = static_cast<const T*>(a.wcopy)[((int64_t)b * (a.conv - 1) + i) * a.chans + ch0];
       }
     }
-    float u[4][PT][4], sq[PT] = {}, maxu[PT], su[PT];
+    float u[4][4], sq = 0.f;
     auto convolve = [&](int conv) {
 #pragma unroll
-      for (int sb = 0; sb < 4; ++sb)
+      for (int sb = 0; sb < 4; ++sb) {
+        float r[7];
 #pragma unroll
-        for (int j = 0; j < PT; ++j) {
-          const float wj[4] = {w[0][j], w[1][j], w[2][j], w[3][j]};
-          float r[7];
+        for (int k = 0; k < 7; ++k) r[k] = to_f(raw[sb][k]);
 #pragma unroll
-          for (int k = 0; k < 7; ++k) r[k] = to_f(raw[sb][k][j]);
-#pragma unroll
-          for (int v = 0; v < 4; ++v) u[sb][j][v] = taps4(wj, cb[j], r[v], r[v + 1], r[v + 2], r[v + 3], conv);
-        }
+        for (int v = 0; v < 4; ++v) u[sb][v] = taps4(w, cb, r[v], r[v + 1], r[v + 2], r[v + 3], conv);
+      }
     };
     if (a.conv == 4) convolve(4);  // without the tests for absent taps
     else convolve(a.conv);
 #pragma unroll
     for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
-      for (int j = 0; j < PT; ++j)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) u[sb][j][v] = silu_f(u[sb][j][v]);
+      for (int v = 0; v < 4; ++v) u[sb][v] = silu_f(u[sb][v]);
     const float sw = SEG ? 1.f : pow2_for(fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)));
     // The mix of rows 16 tb .. + 15 with rows 32 q .. + 31: S, the decay between
     // them and the step size; on the diagonal the skip term, above it nothing.
@@ -663,73 +628,57 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 #pragma unroll
       for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
-        for (int j = 0; j < PT; ++j)
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            if (t0 + 16 * sb + 4 * g + v >= s.len) u[sb][j][v] = 0.f;
+        for (int v = 0; v < 4; ++v)
+          if (t0 + 16 * sb + 4 * g + v >= s.len) u[sb][v] = 0.f;
     }
 #pragma unroll
     for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
-      for (int j = 0; j < PT; ++j)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sq[j] = fmaf(u[sb][j][v], u[sb][j][v], sq[j]);
+      for (int v = 0; v < 4; ++v) sq = fmaf(u[sb][v], u[sb][v], sq);
     // A column's largest value from its sum of squares: at most 2^3 too much.
     // A value that is not finite must not meet the zeros of earlier rows (0 *
     // NaN): it leaves the products, and its column is NaN from its row on.
-    int from[PT];
     bool poison = false;
+    sq += __shfl_xor(sq, 16);
+    sq += __shfl_xor(sq, 32);
+    float maxu = sqrtf(sq);
+    int from = Q;
+    if (__any(!(sq < INFINITY))) {  // or a value beyond 2^63
+      float m = 0.f;
 #pragma unroll
-    for (int j = 0; j < PT; ++j) {
-      sq[j] += __shfl_xor(sq[j], 16);
-      sq[j] += __shfl_xor(sq[j], 32);
-      maxu[j] = sqrtf(sq[j]);
-      from[j] = Q;
-      if (__any(!(sq[j] < INFINITY))) {  // or a value beyond 2^63
-        float m = 0.f;
+      for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
-        for (int sb = 0; sb < 4; ++sb)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            m = max_finite(m, u[sb][j][v]);
-            if (!(fabsf(u[sb][j][v]) < INFINITY)) {
-              u[sb][j][v] = 0.f;
-              from[j] = min(from[j], 16 * sb + 4 * g + v);
-            }
+        for (int v = 0; v < 4; ++v) {
+          m = max_finite(m, u[sb][v]);
+          if (!(fabsf(u[sb][v]) < INFINITY)) {
+            u[sb][v] = 0.f;
+            from = min(from, 16 * sb + 4 * g + v);
           }
-        from[j] = min(from[j], __shfl_xor(from[j], 16));
-        from[j] = min(from[j], __shfl_xor(from[j], 32));
-        poison = poison || __any(from[j] < Q);
-        m = col_max(m);
-        if (!(sq[j] < INFINITY)) maxu[j] = 8.f * m;
-      }
-      su[j] = pow2_for(maxu[j]);
+        }
+      from = min(from, __shfl_xor(from, 16));
+      from = min(from, __shfl_xor(from, 32));
+      poison = __any(from < Q);
+      m = col_max(m);
+      if (!(sq < INFINITY)) maxu = 8.f * m;
     }
+    const float su = pow2_for(maxu);
     __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
     if constexpr (!SEG) {
       // ---- earlier rows of the chunk, the row itself and the skip term
       // from C h's scale to this product's, with the decay since the chunk's start
-      float to[PT];
-#pragma unroll
-      for (int j = 0; j < PT; ++j) to[j] = inv_pow2(pow2_for(maxc)) * inv_pow2(pow2_for(top[j])) * sw * su[j];
+      const float to = inv_pow2(pow2_for(maxc)) * inv_pow2(pow2_for(top)) * sw * su;
 #pragma unroll
       for (int tb = 0; tb < 4; ++tb) {
         const f32x4 e = *reinterpret_cast<const f32x4*>(dtp + 16 * tb + 4 * g);
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int j = 0; j < PT; ++j) acc[tb][j][v] *= e[v] * to[j];
+        for (int v = 0; v < 4; ++v) acc[tb][v] *= e[v] * to;
       }
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        HiLo uf[PT];
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < PT; ++j) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = su[j] * u[2 * q + (i >> 2)][j][i & 3];
-          uf[j] = split8(v);
-        }
+        for (int i = 0; i < 8; ++i) v[i] = su * u[2 * q + (i >> 2)][i & 3];
+        const HiLo uf = split8(v);
 #pragma unroll
         for (int tb = 2 * q; tb < 4; ++tb) {
           HiLo mf;
@@ -739,21 +688,16 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
           } else {
             mf = mix(tb, q);
           }
-#pragma unroll
-          for (int j = 0; j < PT; ++j) acc[tb][j] = mul3(mf, uf[j], acc[tb][j]);
+          acc[tb] = mul3(mf, uf, acc[tb]);
         }
       }
-      float back[PT];
-#pragma unroll
-      for (int j = 0; j < PT; ++j) back[j] = inv_pow2(sw) * inv_pow2(su[j]);
+      const float back = inv_pow2(sw) * inv_pow2(su);
       if (poison) {
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
-          for (int j = 0; j < PT; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-              if (16 * tb + 4 * g + v >= from[j]) acc[tb][j][v] = NAN;
+          for (int v = 0; v < 4; ++v)
+            if (16 * tb + 4 * g + v >= from) acc[tb][v] = NAN;
       }
       // stores past the last row (or column) are outside the range, and dropped
       const unsigned yrow = (unsigned)a.ys * (unsigned)sizeof(T);
@@ -765,11 +709,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          T o[PT];
-#pragma unroll
-          for (int j = 0; j < PT; ++j) o[j] = from_f<T>(acc[tb][j][v] * back[j]);
+          const T o = from_f<T>(acc[tb][v] * back);
           const unsigned off = yo + (16 * tb + v) * yrow;
-          const int to_ = (int)(pn > 0 ? off : kOOB);
+          const int to_ = (int)(have ? off : kOOB);
           if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, o), ry, to_, 0, 0);
           else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o), ry, to_, 0, 0);
         }
@@ -777,52 +719,40 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     // ---- the state after the chunk
     __builtin_amdgcn_sched_barrier(0);
     const float sf = inv_pow2(pow2_for(maxf)) * 0x1p14f, e = __builtin_amdgcn_exp2f(cend);
-    HiLo xf[2][PT];
+    HiLo xf[2];
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
+    for (int q = 0; q < 2; ++q) {
+      float v[8];
 #pragma unroll
-      for (int j = 0; j < PT; ++j) {
-        float v[8];
+      for (int i = 0; i < 2; ++i) {
+        const f32x4 f = *reinterpret_cast<const f32x4*>(dtp + 4 * Q + 32 * q + 16 * i + 4 * g);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const f32x4 f = *reinterpret_cast<const f32x4*>(dtp + 4 * Q + 32 * q + 16 * i + 4 * g);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) v[4 * i + k] = (su[j] * u[2 * q + i][j][k]) * f[k];
-        }
-        xf[q][j] = split8(v);
+        for (int k = 0; k < 4; ++k) v[4 * i + k] = (su * u[2 * q + i][k]) * f[k];
       }
-    float back[PT];
-#pragma unroll
-    for (int j = 0; j < PT; ++j) back[j] = inv_pow2(pow2_for(maxb)) * inv_pow2(su[j]) * sf;
+      xf[q] = split8(v);
+    }
+    const float back = inv_pow2(pow2_for(maxb)) * inv_pow2(su) * sf;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      f32x4 add[PT];
-#pragma unroll
-      for (int j = 0; j < PT; ++j) add[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 add = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const f16* bp = Bg + (nt * 2 + q) * 1024;
         HiLo bf;
         bf.hi = *reinterpret_cast<const f16x8*>(bp);
         bf.lo = *reinterpret_cast<const f16x8*>(bp + 512);
-#pragma unroll
-        for (int j = 0; j < PT; ++j) add[j] = mul3(bf, xf[q][j], add[j]);
+        add = mul3(bf, xf[q], add);
       }
 #pragma unroll
-      for (int j = 0; j < PT; ++j)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) st[nt][j][v] = fmaf(add[j][v], back[j], st[nt][j][v] * e);
+      for (int v = 0; v < 4; ++v) st[nt][v] = fmaf(add[v], back, st[nt][v] * e);
     }
     total += cend;
     // |sum_s B u f| <= max B max f sum_s |u_s|, and that sum at most 8 times the root of the squares
-#pragma unroll
-    for (int j = 0; j < PT; ++j) top[j] = fmaf(top[j], e, 8.f * maxb * maxf * maxu[j]);
+    top = fmaf(top, e, 8.f * maxb * maxf * maxu);
     if (poison) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < PT; ++j)
-          if (from[j] < Q) st[nt][j] = f32x4{NAN, NAN, NAN, NAN};
+        if (from < Q) st[nt] = f32x4{NAN, NAN, NAN, NAN};
     }
     if constexpr (!TWO) {
       // every wave's loads of C and its decays for the next chunk have arrived

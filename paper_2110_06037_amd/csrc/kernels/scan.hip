@@ -83,13 +83,14 @@ __device__ __forceinline__ float taps4(const float (&w)[4], float bias, float r0
 // hi = f16(v) and lo = f16(v - hi): 22 significant bits down to 2^-39 of the
 // tile's largest.  hi hi + hi lo + lo hi then has float32's precision (2^-23)
 // at a third of the f16 rate, five times that of the float32 instructions.
-__device__ __forceinline__ float pow2_for(float m) {  // 2^k with m 2^k in [2^13, 2^14), k at most 80
+// Scales are kept as exponents: a product's comes off as their sum in one
+// ldexp, where the product of two powers, or of two inverses, may leave
+// float32's range.
+__device__ __forceinline__ int exp_for(float m) {  // k with m 2^k in [2^13, 2^14), at most 126
   const int e = (__builtin_bit_cast(int, m) >> 23) & 255;
-  return __builtin_bit_cast(float, min(267 - e, 207) << 23);
+  return min(140 - e, 126);
 }
-__device__ __forceinline__ float inv_pow2(float s) {  // 1 / 2^k, exactly
-  return __builtin_bit_cast(float, (254 << 23) - __builtin_bit_cast(int, s));
-}
+__device__ __forceinline__ float pow2(int k) { return __builtin_bit_cast(float, (k + 127) << 23); }
 struct HiLo {
   f16x8 hi, lo;
 };
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
     o[2 * Q + lane] = cl;
     o[3 * Q + lane] = dt;
     const float dm = wave_max(max_finite(0.f, dt)), fm = wave_max(max_finite(0.f, f));
-    o[4 * Q + lane] = f * (pow2_for(fm) * 0x1p-14f);  // below 1
+    o[4 * Q + lane] = f * pow2(exp_for(fm) - 14);  // below 1
     if (lane == 0) o[5 * Q] = eh + el, o[5 * Q + 1] = dm, o[5 * Q + 2] = fm;
     return;
   }
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
   if (lane == 0) red[wave] = mb, red[kPrep / 64 + wave] = mc;
   __syncthreads();
   mb = wave_max(red[lane & 15]), mc = wave_max(red[16 + (lane & 15)]);
-  const float sb_ = pow2_for(mb), sc_ = pow2_for(mc);
+  const float sb_ = pow2(exp_for(mb)), sc_ = pow2(exp_for(mc));
   const int64_t sg = (int64_t)slot * a.groups + part;
   if (threadIdx.x == 0) a.ws_max[sg * kScanMax] = mb, a.ws_max[sg * kScanMax + 1] = mc;
   const int col = lane & 15, g = lane >> 4;
@@ -529,9 +530,11 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     };
     if constexpr (!SEG) scalars();
     f32x4 acc[4];
+    int kh = 0;
     if constexpr (!SEG) {
       // ---- C times the state in front of the chunk
-      const float sh = pow2_for(top);
+      kh = exp_for(top);
+      const float sh = pow2(kh);
 #pragma unroll
       for (int tb = 0; tb < 4; ++tb) acc[tb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -576,7 +579,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
       for (int v = 0; v < 4; ++v) u[sb][v] = silu_f(u[sb][v]);
-    const float sw = SEG ? 1.f : pow2_for(fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)));
+    const int kw = SEG ? 0 : exp_for(fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)));
+    const float sw = pow2(kw);
     // The mix of rows 16 tb .. + 15 with rows 32 q .. + 31: S, the decay between
     // them and the step size; on the diagonal the skip term, above it nothing.
     auto mix = [&](int tb, int q) {
@@ -661,18 +665,14 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       m = col_max(m);
       if (!(sq < INFINITY)) maxu = 8.f * m;
     }
-    const float su = pow2_for(maxu);
+    const int ku = exp_for(maxu);
+    const float su = pow2(ku);
     __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
     if constexpr (!SEG) {
       // ---- earlier rows of the chunk, the row itself and the skip term
-      // from C h's scale to this product's, with the decay since the chunk's start
-      const float to = inv_pow2(pow2_for(maxc)) * inv_pow2(pow2_for(top)) * sw * su;
+      f32x4 sum[4];
 #pragma unroll
-      for (int tb = 0; tb < 4; ++tb) {
-        const f32x4 e = *reinterpret_cast<const f32x4*>(dtp + 16 * tb + 4 * g);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[tb][v] *= e[v] * to;
-      }
+      for (int tb = 0; tb < 4; ++tb) sum[tb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         float v[8];
@@ -688,10 +688,18 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
           } else {
             mf = mix(tb, q);
           }
-          acc[tb] = mul3(mf, uf, acc[tb]);
+          sum[tb] = mul3(mf, uf, sum[tb]);
         }
       }
-      const float back = inv_pow2(sw) * inv_pow2(su);
+      // to C h with the decay since the chunk's start, each with its own scale
+      const int kch = -(exp_for(maxc) + kh), kwu = -(kw + ku);
+#pragma unroll
+      for (int tb = 0; tb < 4; ++tb) {
+        const f32x4 e = *reinterpret_cast<const f32x4*>(dtp + 16 * tb + 4 * g);
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          acc[tb][v] = __builtin_ldexpf(acc[tb][v] * e[v], kch) + __builtin_ldexpf(sum[tb][v], kwu);
+      }
       if (poison) {
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
@@ -709,7 +717,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       for (int tb = 0; tb < 4; ++tb)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const T o = from_f<T>(acc[tb][v] * back);
+          const T o = from_f<T>(acc[tb][v]);
           const unsigned off = yo + (16 * tb + v) * yrow;
           const int to_ = (int)(have ? off : kOOB);
           if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, o), ry, to_, 0, 0);
@@ -718,7 +726,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     }
     // ---- the state after the chunk
     __builtin_amdgcn_sched_barrier(0);
-    const float sf = inv_pow2(pow2_for(maxf)) * 0x1p14f, e = __builtin_amdgcn_exp2f(cend);
+    const float e = __builtin_amdgcn_exp2f(cend);
     HiLo xf[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -731,7 +739,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       }
       xf[q] = split8(v);
     }
-    const float back = inv_pow2(pow2_for(maxb)) * inv_pow2(su) * sf;
+    const int kadd = 14 - (exp_for(maxb) + ku + exp_for(maxf));
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       f32x4 add = {0.f, 0.f, 0.f, 0.f};
@@ -744,7 +752,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
         add = mul3(bf, xf[q], add);
       }
 #pragma unroll
-      for (int v = 0; v < 4; ++v) st[nt][v] = fmaf(add[v], back, st[nt][v] * e);
+      for (int v = 0; v < 4; ++v) st[nt][v] = fmaf(st[nt][v], e, __builtin_ldexpf(add[v], kadd));
     }
     total += cend;
     // |sum_s B u f| <= max B max f sum_s |u_s|, and that sum at most 8 times the root of the squares

@@ -417,3 +417,23 @@ def test_weak_decays_behind_strong_ones(strong, dt):
     c.dt[strong:64] = -4.6
     c.dt[64 + strong:] = -4.6
     c.check(c.run(c.op()))
+
+
+@pytest.mark.parametrize("dim", [16, 64])
+@pytest.mark.parametrize("raw_dt", [-20.0, -30.0, -100.0])
+@pytest.mark.parametrize("lens", [[1, 64, 40], [700]])
+def test_states_held_by_vanishing_steps(lens, raw_dt, dim):
+    # columns of zeros, no skip term, steps of almost nothing: y = C h alone,
+    # beside products whose largest terms are 0 or far below one
+    c = Case("f32", lens, heads=2, dim=dim, state=16, d=False, seed=5)
+    c.conv_b[:] = 0
+    c.dt_bias[:] = 0
+    c.dt[:] = raw_dt
+    c.x[:, :c.inner], c.window[:, :, :c.inner] = 0, 0
+    exact = c.exact()
+    op = c.op()
+    c.check(c.run(op), exact)
+    if lens[0] == 1:  # the same from the one-token kernel
+        win, h = c.carried()
+        y = op.step(device(c.x[:1], "f32"), device(c.dt[:1], "f32"), win[:1], h[:1])[0]
+        assert_close(y, exact[0][:1], exact[3][:1], "f32", COUNT, "step")

@@ -24,6 +24,8 @@
 namespace sn {
 namespace k {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int Q = kScanChunk;
 constexpr int kScanDt = kScanDtRow;
 
@@ -79,10 +81,15 @@ __device__ __forceinline__ float taps4(const float (&w)[4], float bias, float r0
 
 // ------------------------------------------------------------------ operands in two halves
 // The matrix products run in f16 with float32 sums.  An operand is scaled by a
-// power of two that brings its tile's largest value below 2^14, and split in
-// hi = f16(v) and lo = f16(v - hi): 22 significant bits down to 2^-39 of the
-// tile's largest.  hi hi + hi lo + lo hi then has float32's precision (2^-23)
-// at a third of the f16 rate, five times that of the float32 instructions.
+// power of two that brings its largest value below 2^14, and split in hi =
+// f16(v) and lo = f16(v - hi).  hi hi + hi lo + lo hi then has 22 significant
+// bits, float32's precision but for 2, at a third of the f16 rate, five times that
+// of the float32 instructions.  Values have all 22 bits down to 2^-17 of the
+// largest beside them, and fewer below: an error of 2^-39 of that.  It is taken
+// over as little as shares a sum, from the values themselves (a product of maxima
+// that lie in different rows would be far above any): a row of the mix; a
+// column's state; a column's convolved values and, apart from them, those values
+// times step and decay, in a chunk; B and C over a chunk of their group.
 // Scales are kept as exponents: a product's comes off as their sum in one
 // ldexp, where the product of two powers, or of two inverses, may leave
 // float32's range.
@@ -127,6 +134,24 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int d = 32; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
   return v;
+}
+// Over the four lanes l % 16 + 16 i.  (A swap of v's halves, or rows of 16 lanes,
+// with another register that holds v leaves each side's in one of the two.)
+template <class F>
+__device__ __forceinline__ unsigned over_rows(unsigned v, F f) {
+  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  const unsigned w = f((unsigned)a[0], (unsigned)a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+  return f((unsigned)b[0], (unsigned)b[1]);
+}
+// The largest of values >= 0 (as bits, which have the same order; a NaN counts as largest).
+__device__ __forceinline__ float rows_max(float v) {
+  return __builtin_bit_cast(float, over_rows(__builtin_bit_cast(unsigned, v), [](unsigned a, unsigned b) { return max(a, b); }));
+}
+__device__ __forceinline__ float rows_sum(float v) {
+  return __builtin_bit_cast(float, over_rows(__builtin_bit_cast(unsigned, v), [](unsigned a, unsigned b) {
+    return __builtin_bit_cast(unsigned, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+  }));
 }
 
 // ------------------------------------------------------------------ what all heads share
@@ -194,9 +219,8 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
     o[Q + lane] = ch;
     o[2 * Q + lane] = cl;
     o[3 * Q + lane] = dt;
-    const float dm = wave_max(max_finite(0.f, dt)), fm = wave_max(max_finite(0.f, f));
-    o[4 * Q + lane] = f * pow2(exp_for(fm) - 14);  // below 1
-    if (lane == 0) o[5 * Q] = eh + el, o[5 * Q + 1] = dm, o[5 * Q + 2] = fm;
+    o[4 * Q + lane] = f;
+    if (lane == 0) o[5 * Q] = eh + el;
     return;
   }
 
@@ -311,9 +335,9 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // (33.5 us against 35.5; at 256 rows two chunks leave one workgroup per CU: 105
 // us for the whole scan against 98).
 constexpr int kScanWaves = 8;  // of a workgroup: 2 per SIMD
-constexpr int kDtBytes = kScanDt * 4;      // with its three scalars
+constexpr int kDtBytes = kScanDt * 4;
 constexpr int kMaxBytes = kScanMax * 4;
-constexpr int kMixBytes = 6 * 2048;  // a head's 6 operands of the mix of a chunk's rows, hi and lo
+constexpr int kMixBytes = 6 * (2048 + 64);  // a head's 6 operands of the mix of a chunk's rows, hi and lo, and their rows' scales
 template <int NT, bool SEG>
 constexpr bool scan_two() { return SEG && NT <= 8; }
 template <int NT, bool SEG>
@@ -409,14 +433,6 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   const int64_t head_seg0 = segment0_of(a, s.first, b) * a.heads + h;
   auto seg_slot = [&](int i) { return head_seg0 + (int64_t)i * a.heads; };
   auto seg_state = [&](int i) { return a.ws_seg + seg_slot(i) * hold; };
-  // per column: at least the size of every value of the state (within a few
-  // powers of two).  Scales are a column's own, so no column's values have a
-  // part in another's.
-  float top = 0.f;
-  auto col_max = [&](float v) {  // over the lanes of a column
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
-  };
   // the whole workgroup: a segment that nothing follows (no one reads its
   // state), or behind the sequence's last one (which has no slot)
   if (SEG ? c1 >= nc : seg > 0 && c0 >= nc) return;
@@ -426,7 +442,7 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
   const float cb = have ? a.conv_b[ch0] : 0.f;
 #pragma unroll
   for (int k = 0; k < 4; ++k) w[k] = have ? a.conv_w[k * a.chans + ch0] : 0.f;
-  const float dh = a.d[h];
+  const float dh = SEG ? 0.f : a.d[h];
   const unsigned rowb = (unsigned)a.xs * (unsigned)sizeof(T);
   const unsigned xoff = 4 * g * rowb + (unsigned)(h * a.dim + p0) * (unsigned)sizeof(T);
   float total = 0.f;  // log2 of the segment's decay
@@ -507,12 +523,6 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       load_state(a.state_in + ((int64_t)b * a.heads + h) * hold, st);
       store_state(seg_state(0));
     }
-  } else {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) top = fmaxf(top, fabsf(st[nt][v]));
-    top = col_max(top);
   }
   wait_vmcnt<0>();
   dma_barrier();
@@ -524,16 +534,19 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     const float* dtp = reinterpret_cast<const float*>(ldsD + (c & 1) * kDtBytes);
     // (from LDS: scalar loads here would hold up every wait for LDS)
     const float* maxes = reinterpret_cast<const float*>(ldsX + (c & 1) * kMaxBytes);
-    float maxb, maxc, cend, maxdt, maxf;
-    auto scalars = [&] {
-      maxb = maxes[0], maxc = maxes[1], cend = dtp[5 * Q], maxdt = dtp[5 * Q + 1], maxf = dtp[5 * Q + 2];
-    };
+    float maxb, maxc, cend;
+    auto scalars = [&] { maxb = maxes[0], maxc = maxes[1], cend = dtp[5 * Q]; };
     if constexpr (!SEG) scalars();
     f32x4 acc[4];
     int kh = 0;
     if constexpr (!SEG) {
       // ---- C times the state in front of the chunk
-      kh = exp_for(top);
+      float top = 0.f;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) top = fmaxf(top, fabsf(st[nt][v]));
+      kh = exp_for(rows_max(top));
       const float sh = pow2(kh);
 #pragma unroll
       for (int tb = 0; tb < 4; ++tb) acc[tb] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -579,13 +592,12 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     for (int sb = 0; sb < 4; ++sb)
 #pragma unroll
       for (int v = 0; v < 4; ++v) u[sb][v] = silu_f(u[sb][v]);
-    const int kw = SEG ? 0 : exp_for(fmaf((float)N * maxb * maxc, maxdt, fabsf(dh)));
-    const float sw = pow2(kw);
     // The mix of rows 16 tb .. + 15 with rows 32 q .. + 31: S, the decay between
-    // them and the step size; on the diagonal the skip term, above it nothing.
-    auto mix = [&](int tb, int q) {
+    // them and the step size, above the diagonal nothing; scaled by 2^k, a row's
+    // own (the lane's: row 16 tb + lane % 16).
+    auto mix = [&](int tb, int q, int& k) {
       const float th = dtp[Q + 16 * tb + col], tl = dtp[2 * Q + 16 * tb + col];
-      float m[8];
+      float m[8], most = 0.f;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int sb = 2 * q + i, at = 16 * sb + 4 * g;
@@ -595,20 +607,28 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
         const f32x4 sv = *reinterpret_cast<const f32x4*>(Sg + (tb * (tb + 1) / 2 + min(sb, tb)) * 256);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          float x = sv[v] * (sd_[v] * sw) * __builtin_amdgcn_exp2f((th - sh_[v]) + (tl - sl_[v]));
-          if (at + v == 16 * tb + col) x = fmaf(dh, sw, x);
+          const float x = sv[v] * sd_[v] * __builtin_amdgcn_exp2f((th - sh_[v]) + (tl - sl_[v]));
           m[4 * i + v] = at + v > 16 * tb + col ? 0.f : x;
+          most = fmaxf(most, fabsf(m[4 * i + v]));
         }
       }
+      k = exp_for(rows_max(most));
+      const float s = pow2(k);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] *= s;
       return split8(m);
     };
-    f16x8* const mixes = reinterpret_cast<f16x8*>(ldsM) + lane;  // [operand][hi, lo][lane]; operand 4 q + tb - 2 q
+    // [operand][hi, lo][lane], operand tb + 2 q; then [operand][16] scales
+    f16x8* const mixes = reinterpret_cast<f16x8*>(ldsM) + lane;
+    int* const mixk = reinterpret_cast<int*>(ldsM + 6 * 2048);
     if constexpr (SHARE && !SEG) {
       // the four waves of a head make 10 tiles, 2 or 3 each
       auto put = [&](int tb, int q) {
-        const HiLo m = mix(tb, q);
+        int k;
+        const HiLo m = mix(tb, q, k);
         mixes[(tb + 2 * q) * 128] = m.hi;
         mixes[(tb + 2 * q) * 128 + 64] = m.lo;
+        if (g == 0) mixk[(tb + 2 * q) * 16 + col] = k;
       };
       const int w4 = wave & 3;
       put(w4 == 3 ? 2 : w4 == 0 ? 0 : w4 + 1, w4 == 3);
@@ -643,10 +663,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     // A value that is not finite must not meet the zeros of earlier rows (0 *
     // NaN): it leaves the products, and its column is NaN from its row on.
     bool poison = false;
-    sq += __shfl_xor(sq, 16);
-    sq += __shfl_xor(sq, 32);
-    float maxu = sqrtf(sq);
+    float maxu = 0.f;
     int from = Q;
+    if constexpr (!SEG) maxu = sqrtf(rows_sum(sq));
     if (__any(!(sq < INFINITY))) {  // or a value beyond 2^63
       float m = 0.f;
 #pragma unroll
@@ -662,17 +681,21 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       from = min(from, __shfl_xor(from, 16));
       from = min(from, __shfl_xor(from, 32));
       poison = __any(from < Q);
-      m = col_max(m);
-      if (!(sq < INFINITY)) maxu = 8.f * m;
+      m = rows_max(m);
+      if (!(maxu < INFINITY)) maxu = m;
     }
-    const int ku = exp_for(maxu);
-    const float su = pow2(ku);
     __builtin_amdgcn_sched_barrier(0);  // (the fences keep one phase's registers from another's)
     if constexpr (!SEG) {
-      // ---- earlier rows of the chunk, the row itself and the skip term
-      f32x4 sum[4];
+      // ---- C h with the decay since the chunk's start, and the skip term
+      const int ku = exp_for(maxu), kch = -(exp_for(maxc) + kh);
+      const float su = pow2(ku);
 #pragma unroll
-      for (int tb = 0; tb < 4; ++tb) sum[tb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int tb = 0; tb < 4; ++tb) {
+        const f32x4 e = *reinterpret_cast<const f32x4*>(dtp + 16 * tb + 4 * g);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[tb][v] = fmaf(dh, u[tb][v], __builtin_ldexpf(acc[tb][v] * e[v], kch));
+      }
+      // ---- earlier rows of the chunk, and the row itself
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         float v[8];
@@ -682,23 +705,21 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 #pragma unroll
         for (int tb = 2 * q; tb < 4; ++tb) {
           HiLo mf;
+          i32x4 k;  // of rows 16 tb + 4 g + 0..3
           if constexpr (SHARE) {
             mf.hi = mixes[(tb + 2 * q) * 128];
             mf.lo = mixes[(tb + 2 * q) * 128 + 64];
+            k = *reinterpret_cast<const i32x4*>(mixk + (tb + 2 * q) * 16 + 4 * g);
           } else {
-            mf = mix(tb, q);
+            int own;
+            mf = mix(tb, q, own);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) k[v] = __shfl(own, 4 * g + v);
           }
-          sum[tb] = mul3(mf, uf, sum[tb]);
+          const f32x4 sum = mul3(mf, uf, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int v = 0; v < 4; ++v) acc[tb][v] += __builtin_ldexpf(sum[v], -(k[v] + ku));
         }
-      }
-      // to C h with the decay since the chunk's start, each with its own scale
-      const int kch = -(exp_for(maxc) + kh), kwu = -(kw + ku);
-#pragma unroll
-      for (int tb = 0; tb < 4; ++tb) {
-        const f32x4 e = *reinterpret_cast<const f32x4*>(dtp + 16 * tb + 4 * g);
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-          acc[tb][v] = __builtin_ldexpf(acc[tb][v] * e[v], kch) + __builtin_ldexpf(sum[tb][v], kwu);
       }
       if (poison) {
 #pragma unroll
@@ -727,19 +748,26 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
     // ---- the state after the chunk
     __builtin_amdgcn_sched_barrier(0);
     const float e = __builtin_amdgcn_exp2f(cend);
+    float uf[4][4], most = 0.f;
+#pragma unroll
+    for (int sb = 0; sb < 4; ++sb) {
+      const f32x4 f = *reinterpret_cast<const f32x4*>(dtp + 4 * Q + 16 * sb + 4 * g);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        uf[sb][v] = u[sb][v] * f[v];
+        most = fmaxf(most, fabsf(uf[sb][v]));
+      }
+    }
+    const int kf = exp_for(rows_max(most)), kadd = -(exp_for(maxb) + kf);
+    const float sf = pow2(kf);
     HiLo xf[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       float v[8];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const f32x4 f = *reinterpret_cast<const f32x4*>(dtp + 4 * Q + 32 * q + 16 * i + 4 * g);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[4 * i + k] = (su * u[2 * q + i][k]) * f[k];
-      }
+      for (int i = 0; i < 8; ++i) v[i] = sf * uf[2 * q + (i >> 2)][i & 3];
       xf[q] = split8(v);
     }
-    const int kadd = 14 - (exp_for(maxb) + ku + exp_for(maxf));
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       f32x4 add = {0.f, 0.f, 0.f, 0.f};
@@ -755,8 +783,6 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
       for (int v = 0; v < 4; ++v) st[nt][v] = fmaf(st[nt][v], e, __builtin_ldexpf(add[v], kadd));
     }
     total += cend;
-    // |sum_s B u f| <= max B max f sum_s |u_s|, and that sum at most 8 times the root of the squares
-    top = fmaf(top, e, 8.f * maxb * maxf * maxu);
     if (poison) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)

@@ -58,7 +58,7 @@ void linear4(const Linear4Args& a, hipStream_t st);
 // ------------------------------------------------------------------ selective scan
 constexpr int kScanChunk = 64;     // tokens per chunk
 constexpr int kScanUnits = 2048;   // waves that a pass is cut into segments for
-constexpr int kScanDtRow = 5 * kScanChunk + 16;  // floats per head and chunk of ws_dt
+constexpr int kScanDtRow = 5 * kScanChunk + 4;  // floats per head and chunk of ws_dt
 constexpr int kScanMax = 4;                      // floats per group and chunk of ws_max
 constexpr int kScanS = 10 * 256;                 // floats per group and chunk of ws_s
 struct ScanArgs {
@@ -77,7 +77,7 @@ struct ScanArgs {
   float* ws_max;   // [slot][group][kScanMax] largest sizes in B and C
   float* ws_dt;    // [slot][head][kScanDtRow]: 64 each of the decay since the chunk's start, its log2 as
                    // hi and lo, the step size, the step size times the decay to the chunk's end; then
-                   // the chunk's log2 decay and the largest of the step sizes and of the last array
+                   // the chunk's log2 decay
   float* ws_seg;   // [segment slot][head][dim][state]: slot 0 of a sequence its state before the call, slot i + 1
                    // what segment i adds
   float* ws_decay; // [segment slot][head], likewise: log2 of segment i's decay

@@ -437,3 +437,22 @@ def test_states_held_by_vanishing_steps(lens, raw_dt, dim):
         win, h = c.carried()
         y = op.step(device(c.x[:1], "f32"), device(c.dt[:1], "f32"), win[:1], h[:1])[0]
         assert_close(y, exact[0][:1], exact[3][:1], "f32", COUNT, "step")
+
+
+@pytest.mark.parametrize("dim,state", [(16, 16), (64, 128)])
+@pytest.mark.parametrize("rate", [(0.01, 0.05), (1, 16)])
+@pytest.mark.parametrize("d", [True, False])
+@pytest.mark.parametrize("bc,x,dt", [(300, 1, 0), (1000, 1, 50), (1000, 1000, 50), (1000, 1000, 1000)])
+def test_rows_of_large_values_leave_the_others_their_precision(dim, state, rate, d, bc, x, dt):
+    # within a chunk, in different rows: large B and C, X and steps, the rows
+    # before and behind them as they always are
+    c = Case("f32", [150], heads=2, dim=dim, state=state, rate=rate, d=d, seed=8)
+    inner = c.inner
+    c.x[52, inner:] *= bc
+    c.x[110, inner:] *= bc
+    c.x[47, :inner] *= x
+    c.x[118, :inner] *= x
+    if dt:
+        c.dt[58] = dt
+        c.dt[100] = dt
+    c.check(c.run(c.op()))

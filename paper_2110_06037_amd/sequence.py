@@ -3,7 +3,14 @@
 Each class makes a handle from host weights (numpy arrays) and runs it on
 device tensors: rows are the first dimension, rows may be strided (a slice of
 a wider projection), elements of a row are contiguous.  A run enqueues on the
-current stream of the handle's device, or on ``stream``, and returns at once.
+current stream of the handle's device, or on ``stream`` (a torch stream or a
+stream's pointer), and returns at once.
+
+With another stream than the current one, the caller has that stream wait for
+what makes the tensors that are passed in, as with any work given to a stream.
+Outputs that a run makes itself are that stream's: their memory has no earlier
+use that the stream does not know of, and is not used again before the work
+on it, and on the stream that was current, is done.
 """
 
 from __future__ import annotations
@@ -89,21 +96,29 @@ class _Op:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, not {(rows, cols)}")
         raise ValueError(f"{name} is on {t.device}, the handle on {self._dev}")
 
-    def _stream(self, stream, tensors):
-        """The stream's pointer; on another stream than the current one the
-        tensors' memory is kept from reuse until its work is done."""
-        cur = self._current(self.device)
-        if stream is None:
-            return cur
+    def _side(self, stream):
+        """The stream to run on if it is another one than the current, else None."""
         if isinstance(stream, int):
-            if stream == cur:
-                return stream
-            stream = self._torch.cuda.ExternalStream(stream, device=self._dev)
-        if stream.cuda_stream != cur:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(stream)
-        return stream.cuda_stream
+            if stream == self._current(self.device):
+                return None
+            return self._torch.cuda.ExternalStream(stream, device=self._dev)
+        return None if stream.cuda_stream == self._current(self.device) else stream
+
+    def _new(self, x, shape, dtype, side):
+        """An output on another stream: from the pool of the stream that writes it (a
+        block of the current stream's may still be in use by work queued there)."""
+        with self._torch.cuda.stream(side):
+            t = x.new_empty(shape, dtype=dtype)
+        t.record_stream(self._torch.cuda.current_stream(self.device))
+        return t
+
+    def _stream(self, side, tensors):
+        """The pointer of another stream than the current one; the tensors' memory
+        is kept from reuse until its work is done."""
+        for t in tensors:
+            if t is not None:
+                t.record_stream(side)
+        return side.cuda_stream
 
 
 def quantize4(w, group=128, zero=False):
@@ -169,11 +184,13 @@ class Linear4(_Op):
         """Enqueue on x [m, cols]; returns y [m, rows]."""
         m = x.shape[0]
         xs = self._rows(x, "x", m, self.cols, self.torch_dtype)
+        side = None if stream is None else self._side(stream)
         if out is None:
-            out, ys = x.new_empty((m, self.rows)), self.rows
+            shape, ys = (m, self.rows), self.rows
+            out = x.new_empty(shape) if side is None else self._new(x, shape, x.dtype, side)
         else:
             ys = self._rows(out, "out", m, self.rows, self.torch_dtype)
-        st = self._stream(stream, (x, out))
+        st = self._current(self.device) if side is None else self._stream(side, (x, out))
         rc = self._run(self._op, m, x.data_ptr(), xs, out.data_ptr(), ys, st)
         if rc:
             N.check(rc)
@@ -237,18 +254,21 @@ class Scan(_Op):
         io.window = None if window is None else self._whole(window, "window", wshape, kind)
         io.state = None if state is None else self._whole(state, "state", sshape, f32)
         io.offsets = None if offsets is None else self._whole(offsets, "offsets", (seqs + 1,), self._torch.int32)
+        side = None if stream is None else self._side(stream)
         if out is None:
-            out = x.new_empty((tokens, self.inner))
+            shape = (tokens, self.inner)
+            out = x.new_empty(shape) if side is None else self._new(x, shape, kind, side)
             io.y_stride, io.y = self.inner, out.data_ptr()
         else:
             io.y_stride, io.y = self._rows(out, "out", tokens, self.inner, kind), out.data_ptr()
         if window_out is None:
-            window_out = x.new_empty(wshape)
+            window_out = x.new_empty(wshape) if side is None else self._new(x, wshape, kind, side)
         if state_out is None:
-            state_out = x.new_empty(sshape, dtype=f32)
+            state_out = x.new_empty(sshape, dtype=f32) if side is None else self._new(x, sshape, f32, side)
         io.window_out = self._whole(window_out, "window_out", wshape, kind)
         io.state_out = self._whole(state_out, "state_out", sshape, f32)
-        st = self._stream(stream, (x, dt, window, state, offsets, out, window_out, state_out))
+        st = self._current(self.device) if side is None else self._stream(
+            side, (x, dt, window, state, offsets, out, window_out, state_out))
         rc = f(self._op, self._io_ref, st)
         if rc:
             N.check(rc)
@@ -309,13 +329,15 @@ class BlockNorm(_Op):
         rows, dim, kind = x.shape[0], self.dim, self.torch_dtype
         xs = self._rows(x, "x", rows, dim, kind)
         gp = gs = rp = rs = op = os = yp = ys = 0
+        side = None if stream is None else self._side(stream)
         if gate is not None:
             gp, gs = gate.data_ptr(), self._rows(gate, "gate", rows, dim, kind)
         if self.res_dtype is not None:
             if residual is not None:
                 rp, rs = residual.data_ptr(), self._rows(residual, "residual", rows, dim, self.res_dtype)
             if res_out is None:
-                res_out, os = x.new_empty((rows, dim), dtype=self.res_dtype), dim
+                shape, rkind, os = (rows, dim), self.res_dtype, dim
+                res_out = x.new_empty(shape, dtype=rkind) if side is None else self._new(x, shape, rkind, side)
             else:
                 os = self._rows(res_out, "res_out", rows, dim, self.res_dtype)
             op = res_out.data_ptr()
@@ -323,11 +345,12 @@ class BlockNorm(_Op):
             raise ValueError("a residual given to a handle without one")
         if self.has_y:
             if out is None:
-                out, ys = x.new_empty((rows, dim)), dim
+                shape, ys = (rows, dim), dim
+                out = x.new_empty(shape) if side is None else self._new(x, shape, kind, side)
             else:
                 ys = self._rows(out, "out", rows, dim, kind)
             yp = out.data_ptr()
-        st = self._stream(stream, (x, gate, residual, out, res_out))
+        st = self._current(self.device) if side is None else self._stream(side, (x, gate, residual, out, res_out))
         rc = self._run(self._op, rows, x.data_ptr(), xs, gp, gs, rp, rs, op, os, yp, ys, st)
         if rc:
             N.check(rc)

@@ -46,6 +46,19 @@ class _Block:
             op.close()
 
 
+class _Replay:
+    """Replays a captured step.  The graph holds addresses only: this holds the
+    net, whose handles own weights and workspaces, and the tensors."""
+
+    def __init__(self, graph, net, *tensors):
+        self.graph, self.net, self.tensors = graph, net, tensors
+
+    def __call__(self):
+        if self.net.closed:
+            raise RuntimeError("the net of this captured step is closed")
+        self.graph.replay()
+
+
 class SequenceNet:
     """``weights``: {"norm": [dim] of the first block's input, "blocks": [...], each
     with its "config" (dim, heads, head_dim, groups, state, group), 4-bit
@@ -56,11 +69,12 @@ class SequenceNet:
 
     def __init__(self, dtype, weights, max_seqs=1, max_tokens=1, device=0, eps=1e-5):
         blocks = weights["blocks"]
-        self.device = device
+        self.device, self.closed = device, False
         self.first = BlockNorm(dtype, blocks[0]["config"]["dim"], pre=weights["norm"], eps=eps, device=device)
         self.blocks = [_Block(dtype, w, w["norm"], max_seqs, max_tokens, device, eps) for w in blocks]
 
     def close(self):
+        self.closed = True
         self.first.close()
         for b in self.blocks:
             b.close()
@@ -100,18 +114,22 @@ class SequenceNet:
     def capture_step(self, state):
         """A captured HIP graph of ``step`` on ``state``: (x, y, replay), where x
         is filled with the tokens before each replay() and y holds their outputs
-        after it.  ``state`` is as before the capture."""
+        after it.  ``state`` is as before the capture; its tensors are what every
+        replay updates.  ``replay`` keeps the net and them alive, and refuses to
+        run once the net is closed."""
         import torch
-        x = torch.zeros(state.seqs, self.first.dim, dtype=self.first.torch_dtype, device=f"cuda:{self.device}")
-        keep = [t.clone() for t in state.windows + state.states]
-        side = torch.cuda.Stream(self.device)
-        side.wait_stream(torch.cuda.current_stream(self.device))
-        with torch.cuda.stream(side):
-            self.step(x, state)
-        torch.cuda.current_stream(self.device).wait_stream(side)
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
-            y = self.step(x, state)
-        for t, k in zip(state.windows + state.states, keep):
-            t.copy_(k)
-        return x, y, graph.replay
+        with torch.cuda.device(self.device):
+            x = torch.zeros(state.seqs, self.first.dim, dtype=self.first.torch_dtype, device=f"cuda:{self.device}")
+            tensors = state.windows + state.states
+            keep = [t.clone() for t in tensors]
+            side = torch.cuda.Stream(self.device)
+            side.wait_stream(torch.cuda.current_stream(self.device))
+            with torch.cuda.stream(side):
+                self.step(x, state)
+            torch.cuda.current_stream(self.device).wait_stream(side)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                y = self.step(x, state)
+            for t, k in zip(tensors, keep):
+                t.copy_(k)
+        return x, y, _Replay(graph, self, tensors, (x, y))

@@ -114,3 +114,29 @@ def test_inputs_are_left_as_they_are(dtype):
     torch.cuda.synchronize()
     assert torch.equal(token, before[:2])
     net.close()
+
+
+def test_a_captured_step_keeps_what_it_uses():
+    import gc
+    import torch
+    import weakref
+    weights = sequence_weights(CONFIG, 2, seed=8)
+    net = SequenceNet("bf16", weights, max_seqs=2, max_tokens=2)
+    state = net.new_state(2)
+    token, out, replay = net.capture_step(state)
+    alive = [weakref.ref(net), weakref.ref(net.blocks[0].scan), weakref.ref(state.states[0]), weakref.ref(state.windows[1])]
+    del net, state
+    gc.collect()
+    assert all(r() is not None for r in alive)
+    with SequenceNet("bf16", weights, max_seqs=2, max_tokens=2) as other:
+        same = other.new_state(2)
+        for _ in range(3):
+            t = torch.randn(2, 96, device="cuda").bfloat16()
+            token.copy_(t)
+            replay()
+            want = other.step(t, same)
+            torch.cuda.synchronize()
+            assert torch.equal(want, out)
+    replay.net.close()
+    with pytest.raises(RuntimeError):
+        replay()

@@ -500,8 +500,12 @@ const char* sn_last_error(void);
  *    length; a single row's is not looked at) and each row is contiguous.
  *    Any alignment of whole elements is accepted; 16-byte aligned rows take
  *    the wide loads.
+ *  - Outputs lie apart from each other and from the inputs, except where an
+ *    operator says that one may be its input; else SN_E_INVALID (rows of
+ *    tensors with the same stride may lie between each other's, those of
+ *    different strides may not).
  *  - device = -1 makes a host-only handle: its runs check their arguments
- *    and then return SN_E_DEVICE.
+ *    (but not whether tensors overlap) and then return SN_E_DEVICE.
  *  - Zero rows (m, rows or tokens of 0) are allowed and write nothing but
  *    what is said below.
  *  - Sums, statistics and states are float32; an output is rounded once, to
@@ -523,8 +527,9 @@ void sn_op_destroy(sn_op* op);
  * norm is SN_NORM_RMS: v / sqrt(mean(v^2) + eps) * w + b, or SN_NORM_LAYER:
  * (v - mean) / sqrt(var + eps) * w + b; the post norm takes each of `groups`
  * equal parts of a row by itself (1 unless pre_w is null).  All in float32:
- * the second norm sees the residual sum before it is rounded.  y may be x,
- * and res_out may be res (same strides).  An absent tensor is null.        */
+ * the second norm sees the residual sum before it is rounded.  y and res_out
+ * may each be x, gate or res (same type and stride), but not one another.  An
+ * absent tensor is null.                                                   */
 typedef enum { SN_NORM_RMS = 0, SN_NORM_LAYER = 1 } sn_norm_kind;
 typedef enum { SN_GATE_NONE = 0, SN_GATE_BEFORE = 1, SN_GATE_AFTER = 2 } sn_gate;
 typedef struct {

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <initializer_list>
 #include <memory>
 
 #include "api_guard.hpp"
@@ -104,6 +105,36 @@ int64_t check_rows(const void* p, int64_t stride, int64_t rows, int64_t n, int d
   return stride;
 }
 
+// A tensor's place in memory: `rows` rows of `bytes`, `step` bytes apart.
+struct Place {
+  uintptr_t at;
+  int64_t rows, bytes, step;
+  Place(const void* p, int64_t rows, int64_t n, int64_t stride, int64_t e)
+      : at(reinterpret_cast<uintptr_t>(p)), rows(p ? rows : 0), bytes(n * e), step(stride * e) {}
+  Place(const void* p, int64_t n) : Place(p, n > 0, n, n, 1) {}  // in one piece
+  uintptr_t end() const { return at + (rows - 1) * step + bytes; }
+  bool same(const Place& o) const { return at == o.at && rows == o.rows && bytes == o.bytes && step == o.step; }
+};
+
+// Whether two tensors share a byte.  Rows of one step may lie between each
+// other's (slices of one wider tensor); of two steps, overlapping ranges count.
+bool meet(const Place& a, const Place& b) {
+  if (!a.rows || !b.rows || a.end() <= b.at || b.end() <= a.at) return false;
+  if (a.rows == 1 && b.rows == 1) return true;
+  const int64_t step = a.rows == 1 ? b.step : a.step;
+  if (a.rows > 1 && b.rows > 1 && a.step != b.step) return true;
+  const int64_t d = ((int64_t)(b.at - a.at) % step + step) % step;
+  return d < a.bytes || d + b.bytes > step;
+}
+
+// Other workgroups read an input while an output is written: none may lie in
+// an input, but for `in_place` kernels, where every element is read by the thread
+// that writes it, as the same tensor.
+void check_apart(const Place& out, const char* what, std::initializer_list<Place> others, bool in_place = false) {
+  for (const Place& o : others)
+    if (meet(out, o) && !(in_place && out.same(o))) fail(SN_E_INVALID, std::string(what) + " overlaps another tensor of the call");
+}
+
 void need_device(const sn_op& op) {
   if (op.device < 0) fail(SN_E_DEVICE, "host-only handle cannot run");
 }
@@ -162,6 +193,19 @@ k::ScanArgs scan_args(const ScanOp& op, const sn_scan_io* io, bool step) {
   a.window = io->window, a.window_out = a.conv > 1 ? io->window_out : nullptr;
   a.state_in = io->state, a.state_out = io->state_out;
   return a;
+}
+
+// What a call writes lies apart from what it reads (windows and states may be
+// updated in place: check_in_out).
+void check_scan_apart(const k::ScanArgs& a, const sn_scan_io& io) {
+  const int e = dtype_size(a.dtype);
+  const int64_t wbytes = (int64_t)a.seqs * (a.conv - 1) * a.chans * e, hbytes = (int64_t)a.seqs * a.heads * a.dim * a.state * 4;
+  const Place x(io.x, a.tokens, a.chans, a.xs, e), dt(io.dt, a.tokens, a.heads, a.dts, e);
+  const Place y(io.y, a.tokens, (int64_t)a.heads * a.dim, a.ys, e), offsets(io.offsets, 4 * ((int64_t)a.seqs + 1));
+  const Place w(io.window, wbytes), wo(io.window_out, wbytes), h(io.state, hbytes), ho(io.state_out, hbytes);
+  check_apart(y, "y", {x, dt, offsets, w, wo, h, ho});
+  check_apart(wo, "window_out", {x, dt, offsets, h, ho});
+  check_apart(ho, "state_out", {x, dt, offsets, w});
 }
 
 }  // namespace
@@ -233,6 +277,12 @@ int sn_norm_run(sn_op* p, int64_t rows, const void* x, int64_t x_stride, const v
     if (y && y == x && a.xs != a.ys) fail(SN_E_SHAPE, "y in place needs one stride");
     need_device(op);
     if (!rows) return;
+    const int e = dtype_size(a.dtype), er = dtype_size(std::max(a.rdtype, 0));
+    const Place px(x, rows, a.dim, a.xs, e), pg(gate, rows, a.dim, a.gs, e), pr(res, rows, a.dim, a.rs, er);
+    const Place py(y, rows, a.dim, a.ys, e), pro(res_out, rows, a.dim, a.ros, er);
+    check_apart(py, "y", {px, pg, pr}, true);
+    check_apart(pro, "res_out", {px, pg, pr}, true);
+    check_apart(py, "y", {pro});
     a.rows = rows;
     a.x = x, a.g = gate, a.r = res, a.ro = res_out, a.y = y;
     OnDevice on(op.device);
@@ -295,6 +345,8 @@ int sn_qlinear_run(sn_op* p, int64_t m, const void* x, int64_t x_stride, void* y
     a.ys = check_rows(y, y_stride, m, a.rows, a.dtype, "y");
     need_device(op);
     if (!m) return;
+    const int e = dtype_size(a.dtype);
+    check_apart(Place(y, m, a.rows, a.ys, e), "y", {Place(x, m, a.cols, a.xs, e)});
     a.m = m, a.x = x, a.y = y;
     OnDevice on(op.device);
     k::linear4(a, static_cast<hipStream_t>(stream));
@@ -372,6 +424,7 @@ int sn_scan_run(sn_op* p, const sn_scan_io* io, void* stream) {
     const k::ScanArgs a = scan_args(op, io, false);
     need_device(op);
     if (!a.seqs) return;
+    check_scan_apart(a, *io);
     OnDevice on(op.device);
     k::scan_run(a, static_cast<hipStream_t>(stream));
     HIPCHK(hipGetLastError());
@@ -384,6 +437,7 @@ int sn_scan_step(sn_op* p, const sn_scan_io* io, void* stream) {
     const k::ScanArgs a = scan_args(op, io, true);
     need_device(op);
     if (!a.seqs) return;
+    check_scan_apart(a, *io);
     OnDevice on(op.device);
     k::scan_step(a, static_cast<hipStream_t>(stream));
     HIPCHK(hipGetLastError());

@@ -206,14 +206,17 @@ static void launch_norm(const NormArgs& a, hipStream_t st) {
     SN_LAUNCH((block_norm_kernel<T, R, MODE, WPR, NV>), grid(WPR < 4 ? 4 / WPR : 1), dim3(WPR < 4 ? 256 : 64 * WPR), 0, st, a);
   };
 #define SN_NORM(WPR, NV) launch(std::integral_constant<int, WPR>(), std::integral_constant<int, NV>())
-  if constexpr (MODE == kSingle) return SN_NORM(1, 1);
-  if (D <= 512) SN_NORM(1, 1);
-  else if (D <= 1024) SN_NORM(2, 1);
-  else if (D <= 2048) SN_NORM(4, 1);
-  else if (D <= 4096) SN_NORM(4, 2);
-  else if (D <= 8192) SN_NORM(16, 1);
-  else if (D <= 16384) SN_NORM(16, 2);
-  else SN_NORM(16, 4);
+  if constexpr (MODE == kSingle) {
+    SN_NORM(1, 1);
+  } else {
+    if (D <= 512) SN_NORM(1, 1);
+    else if (D <= 1024) SN_NORM(2, 1);
+    else if (D <= 2048) SN_NORM(4, 1);
+    else if (D <= 4096) SN_NORM(4, 2);
+    else if (D <= 8192) SN_NORM(16, 1);
+    else if (D <= 16384) SN_NORM(16, 2);
+    else SN_NORM(16, 4);
+  }
 #undef SN_NORM
 }
 

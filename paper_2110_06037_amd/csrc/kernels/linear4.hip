@@ -675,7 +675,8 @@ static void launch_rows(const Linear4Args& a, hipStream_t st) {
     constexpr int U = NB == 1 ? 2 : 1;
     const int rbs = (a.rows + 15) / 16;
     if (rbs >= (NB == 1 ? 1024 : 512)) return launch_rows_u<T, NB, MV, GS, VX, NB == 4 ? 2 : 4, U>(a, st);
-    if (rbs >= 512) return launch_rows_u<T, NB, MV, GS, VX, 2, U>(a, st);
+    if constexpr (NB == 1)
+      if (rbs >= 512) return launch_rows_u<T, NB, MV, GS, VX, 2, U>(a, st);
   }
   launch_rows_u<T, NB, MV, GS, VX, 1, 1>(a, st);
 }

@@ -241,14 +241,14 @@ __global__ __launch_bounds__(R == 1 && NB < 4 ? 1024 : 512) void linear4_rows_ke
     rs[r] = make_rsrc(a.ws + blk * 16 * RUNS, (long long)cbs * 64 * RUNS);
   }
   // this lane's rows of x
-  const int64_t mb = (int64_t)blockIdx.y * NB * PER, left = a.m - mb;
-  const T* xb = static_cast<const T*>(a.x) + mb * a.xs;
+  const int rows_x = (int)a.m;  // at most NB PER
+  const T* xb = static_cast<const T*>(a.x);
   XRow<T, VX> xrow[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int v = xr & 3, m = nb * PER + (F32 ? xr >> 2 : 4 * v + (xr >> 2));
-    const bool on = m < left && v < (F32 ? 3 : MV);
-    if constexpr (VX) xrow[nb].rs = make_rsrc(xb, ((min(left, (int64_t)NB * PER) - 1) * a.xs + a.cols) * (int)sizeof(T));
+    const bool on = m < rows_x && v < (F32 ? 3 : MV);
+    if constexpr (VX) xrow[nb].rs = make_rsrc(xb, ((rows_x - 1) * a.xs + a.cols) * (int)sizeof(T));
     xrow[nb].row = xb + (on ? m * a.xs : 0);
     xrow[nb].off = on ? VX ? (unsigned)(m * a.xs) * (unsigned)sizeof(T) : 0u : kOOB;
   }
@@ -361,8 +361,8 @@ __global__ __launch_bounds__(R == 1 && NB < 4 ? 1024 : 512) void linear4_rows_ke
     for (int w = 0; w < waves; ++w) s += red[w * SUMS + i];
     const int l = i & 63, v = (i >> 6) % NV, nb = (i >> 6) / NV % NB, r = (i >> 6) / (NV * NB);
     const int m = nb * PER + (F32 ? l >> 4 : 4 * v + (l >> 4)), k = (rb0 + r) * 16 + (l & 15);
-    if (m < left && k < a.rows)
-      static_cast<T*>(a.y)[(mb + m) * a.ys + k] = from_f<T>(act4(s + (a.bias ? a.bias[k] : 0.f), a.act));
+    if (m < rows_x && k < a.rows)
+      static_cast<T*>(a.y)[m * a.ys + k] = from_f<T>(act4(s + (a.bias ? a.bias[k] : 0.f), a.act));
   }
 }
 
@@ -664,7 +664,8 @@ static void launch_rows_u(const Linear4Args& a, hipStream_t st) {
   const int cbs = (a.cols + 127) / 128;
   // one row of blocks per workgroup: few features, so more waves for each
   const int waves = std::min(R == 1 && NB < 4 ? 16 : 8, (cbs + U - 1) / U);
-  const dim3 grid((a.rows + 16 * R - 1) / (16 * R), (unsigned)((a.m + NB * PER - 1) / (NB * PER)));
+  const dim3 grid((a.rows + 16 * R - 1) / (16 * R));
+  check(a.m <= NB * PER, "rows of a few-row 4-bit product");
   SN_LAUNCH((linear4_rows_kernel<T, NB, MV, GS, VX, R, U>), grid, dim3(64 * waves), waves * R * NB * NV * 256, st, a);
 }
 template <typename T, int NB, int MV, int GS, bool VX>

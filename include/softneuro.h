@@ -509,7 +509,9 @@ const char* sn_last_error(void);
  *  - Zero rows (m, rows or tokens of 0) are allowed and write nothing but
  *    what is said below.
  *  - Sums, statistics and states are float32; an output is rounded once, to
- *    nearest-even.                                                         */
+ *    nearest-even.  The factors of a scan's products have 22 significant bits,
+ *    down to 2^-17 of the largest that they share a sum with (of a chunk of 64
+ *    tokens, in one channel, state column or group), and fewer below.      */
 typedef struct sn_op sn_op;
 void sn_op_destroy(sn_op* op);
 
@@ -555,7 +557,9 @@ int sn_norm_run(sn_op* op, int64_t rows, const void* x, int64_t x_stride, const 
  * q: [rows][ceil(cols / 2)] bytes, feature 2j in the low half of byte j;
  * scale: [rows][ceil(cols / group)] binary16 patterns; zero: codes 0 .. 15 of
  * the same shape, or null for 8; bias: [rows] float32 or null.  group is a
- * multiple of 32; a last group may be short.                               */
+ * multiple of 32; a last group may be short.  A call takes m up to 262140.
+ * Up to 128 products x (q - z), with |q - z| counted as 31, are summed before
+ * their scale: |x| up to 2^115 leaves every such sum finite.               */
 typedef struct {
   int32_t dtype; /* x and y */
   int32_t rows;  /* output features */

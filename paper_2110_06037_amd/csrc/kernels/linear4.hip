@@ -8,18 +8,19 @@
 // step i in its i-th dword.  A wave reads a block as one run of 16 bytes per
 // lane, and no weight passes through LDS.
 //
-// Codes become 16-bit floats by or-ing them into the low mantissa bits of a
-// constant (two weights per instruction).  f16: 1024 + q or 64 + q, less 1024 +
-// z or 64 + z in one packed subtraction: q - z exactly.  bf16: 16 + q (the code
-// in bits 3 to 6 of 7), and the 16 + z come off the sums instead, (16 + z)
-// sum_c x[m][c], with the sums over x from an MFMA against ones: cheaper than
-// any exact form.  The sums that carry it are float32 and at most 31 times their
-// inputs' sizes; it comes off after every run (few rows) or every 4 runs (many),
-// so that no sum of a whole row carries it: with inputs of one sign, 2048 of
-// them and results near 0, errors of 4 * 2^-24 of the terms' sizes.  float32: x as
-// the exact sum of three bf16 parts, which are three rows of the first operand,
-// times q - z exactly in bf16.  Products are exact, sums float32; a group's scale
-// multiplies the float32 sum of its run.
+// Codes become 16-bit floats by or-ing them into the mantissa of a constant, two
+// weights per instruction (the published way from small integers to floats
+// without a conversion).  f16: 1024 + q or 64 + q, less 1024 + z or 64 + z in
+// one packed subtraction: q - z exactly.  bf16: 16 + q (the code in bits 3 to 6
+// of 7), and the 16 + z come off the sums instead, (16 + z) sum_c x[m][c], with
+// the sums over x from an MFMA against ones: cheaper than any exact form.  The
+// sums that carry it are float32 and at most 31 times their inputs' sizes; it
+// comes off after every run (few rows) or every 4 runs (many), so that no sum
+// of a whole row carries it: with inputs of one sign, 2048 of them and results
+// of 0, errors of 1.5 * 2^-24 of the terms' sizes in the root mean square (few
+// rows: 0.05).  float32: x as the exact sum of three bf16 parts, which are three
+// rows of the first operand, times q - z exactly in bf16.  Products are exact,
+// sums float32; a group's scale multiplies the float32 sum of its run.
 #include "seq.hpp"
 
 namespace sn {
@@ -380,8 +381,8 @@ constexpr int kL4Stages = 3;
 // Bound by instruction issue: matrix instructions fill a third of the cycles, the
 // codes' way to floats and the runs' scales another third (counted); HBM
 // traffic is small.  1500 rows of 2048 inputs
-// and 8512 features: 75 us in bf16, 700 TFLOP/s (a plain library
-// product of 8192^3 reaches 1236); 341 us in float32.  (The bias off the whole
+// and 8512 features: 76 us in bf16, 690 TFLOP/s (a plain library
+// product of 8192^3 reaches 1236); 344 us in float32.  (The bias off the whole
 // sums at the end, from sums over x that wait in LDS, was 3 us faster, with ten
 // times the error, and had no room for rows of more than 128 runs.)
 template <typename T, int RB, int GS, bool VX>

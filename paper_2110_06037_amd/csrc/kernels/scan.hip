@@ -325,11 +325,12 @@ __global__ __launch_bounds__(kPrep) void scan_prep_kernel(ScanArgs a) {
 // computed: two barriers per chunk, behind which one set has arrived and the
 // other is free.  Bound by the latency of one chunk after the other: about 5 us
 // for a lone wave, 1.5 more for each further wave of a SIMD, whose registers
-// (170) leave room for two; 4096 tokens of 64 heads of 64 x 128 in bf16: 33.5 us
-// for the first pass, 68 for the second, with matrix instructions in 17% of the
-// cycles and other vector instructions in 36%; 8 sequences of 2048, which need no
-// first pass, 350 us all told.  Twelve or sixteen waves, or more or fewer
-// segments, were not faster.
+// (178) leave room for two; 4096 tokens of 64 heads of 64 x 128 in bf16: 33 us
+// for the first pass, 77 for the second, with matrix instructions in 16% of the
+// cycles and other vector instructions in 37%; 8 sequences of 2048, which need no
+// first pass, 275 us all told.  Twelve or sixteen waves were not faster.
+// (Scales from products of maxima instead of from the values: 8 us less for the
+// second pass, and rows of large values took the others' bits.)
 //
 // SEG up to 128 state rows has room for two chunks' B, and one barrier per chunk
 // (33.5 us against 35.5; at 256 rows two chunks leave one workgroup per CU: 105
@@ -806,8 +807,9 @@ __global__ __launch_bounds__(64 * kScanWaves) void scan_main_kernel(ScanArgs a) 
 }
 
 // States over the segments, if there are many: slot i, with what segment i - 1
-// adds, takes the state in front of segment i.  Bound by the chain of loads, one
-// per segment (8 segments of 64 heads of 64 x 128: 8 us).
+// adds, takes the state in front of segment i.  Bound by one load after the
+// other, each behind the store of the segment before it (8 segments of 64 heads
+// of 64 x 128: 8 us).
 __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
   const int64_t hold = (int64_t)a.dim * a.state, e = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int b = blockIdx.z, h = blockIdx.y;
@@ -835,7 +837,7 @@ __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a) {
 // PASS: quads of a thread.  More share the convolution of B and C among more
 // rows, fewer make more workgroups when there are few sequences.
 // 64 heads of 64 x 128 in bf16: 64 sequences 61 us, 4.4 TB/s (a copy of gigabytes
-// reaches 4.8); 8 sequences 12 us; one 5.4 us, most of it the launch and the way
+// reaches 4.8); 8 sequences 12 us; one 5.8 us, most of it the launch and the way
 // from the window over the convolution to the state.
 template <typename T, int PASS>
 __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int L, int splits) {
@@ -978,9 +980,10 @@ static void launch_scan(ScanArgs a, hipStream_t st) {
   else if (a.np == 64) SN_LAUNCH((scan_prep_kernel<T, 64>), grid, dim3(kPrep), lds, st, a);
   else if (a.np == 128) SN_LAUNCH((scan_prep_kernel<T, 128>), grid, dim3(kPrep), lds, st, a);
   else SN_LAUNCH((scan_prep_kernel<T, 256>), grid, dim3(kPrep), lds, st, a);
-  // with 64 columns per head or a multiple, four waves of one share its mix (70
-  // us against 81 for the second pass over 4096 tokens of 64 heads); beside 256
-  // state rows LDS has no room for it
+  // with 64 columns per head or a multiple, four waves of one share its mix
+  // (4096 tokens of 64 heads: 126 us against 135 for all launches; 3 x 511 of 24:
+  // 41 against 44; 4096 of 32 x 128 x 16: 79 against 90); beside 256 state rows LDS has
+  // no room for it
   if ((a.dim + 15) / 16 % 4 == 0 && a.np <= 128) launch_np<T, true>(a, st);
   else launch_np<T, false>(a, st);
 }
@@ -992,9 +995,9 @@ static void launch_step(ScanArgs a, hipStream_t st) {
   int L = 1;
   while (4 * L < a.state) L *= 2;
   auto splits = [&](int pass) { return (a.dim + pass * (256 / L) - 1) / (pass * (256 / L)); };
-  // as many quads as a head has rows for, if that leaves kStepBlocks workgroups
-  // (64 sequences of 64 heads of 64 x 128: 61 us with eight, 70 with two; one
-  // sequence: 5.4 us with two, 7.6 with eight)
+  // as many quads as a head has rows for, if that leaves kStepBlocks workgroups.
+  // 64 heads of 64 x 128, us with two, four, eight quads: 1 sequence 5.9, 7.0, 9.7;
+  // 4: 8.6, 8.5, 10.6; 8: 13.2, 11.1, 12.5; 16: 21.8, 19.8, 17.8; 64: 71, 58, 60
   auto fits = [&](int pass) {
     return pass * (256 / L) <= std::max(a.dim, 8) && (int64_t)a.seqs * a.heads * splits(pass) >= kStepBlocks;
   };
@@ -1014,6 +1017,9 @@ constexpr int kScanCarry = 256;
 // Segments: as many chunks to each as leave kScanUnits waves, at least two (a
 // segment's chunks but the last one's are read twice, and its state is written
 // and read); one if there are more waves anyhow, or the states found no room.
+// us with 1024, 2048, 4096 waves: 1024 tokens of 64 heads of 64 x 128 74, 67, 67;
+// 4096 182, 120, 135; 16384 of 8 heads 114, 92, 121; 4096 of 24 heads of 64 x 64
+// 73, 76, 70.
 static void scan_split(ScanArgs& a) {
   a.each = a.tokens / a.seqs;
   const int64_t slots = scan_slots(a.tokens, a.seqs), units = (int64_t)a.heads * ((a.dim + 15) / 16);

@@ -191,3 +191,22 @@ def test_groups_wider_than_the_rows(dtype):
     for group in (1024, 1 << 30, (1 << 31) - 32):
         run_case(dtype, 3, 300, 40, group, True)
         run_case(dtype, 40, 300, 40, group, True)
+
+
+@pytest.mark.parametrize("m,cols,group", [(3, 2048, 128), (20, 2048, 64), (70, 2048, 128), (70, 4096, 64), (70, 2048, 32)])
+def test_sums_of_bf16_inputs_of_many_magnitudes(m, cols, group):
+    # the same weights and bound as above (its ratios of partial sums to terms
+    # do not depend on the inputs' sizes), on inputs whose sums need more bits
+    # than float32 has
+    r = np.random.default_rng(cols + group)
+    rows, half = 80, cols // 2
+    d = r.integers(-7, 8, (rows, half))
+    code = np.concatenate([8 + d, 8 - d], 1).astype(np.uint8)
+    x = rounded(np.exp(r.standard_normal((m, half))), "bf16")
+    x = np.concatenate([x, x], 1)
+    op = Linear4("bf16", code[:, 0::2] | (code[:, 1::2] << 4), np.ones((rows, -(-cols // group)), np.float16), cols=cols,
+                 group=group)
+    got = host(op.run(device(x, "bf16")))
+    size = x @ np.abs(code.astype(np.float64) - 8).T
+    assert np.linalg.norm(got) <= 16 * 2.0 ** -24 * np.linalg.norm(size)
+    op.close()

@@ -623,6 +623,116 @@ int sn_scan_create(const sn_scan_desc* desc, const float* conv_w, const float* c
 int sn_scan_run(sn_op* op, const sn_scan_io* io, void* stream);
 int sn_scan_step(sn_op* op, const sn_scan_io* io, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Attention operators: what attention blocks run beside the sequence operators
+ * -- the norms of queries and keys with the position rotation, a paged cache of
+ * keys and values, and attention over it for prompts and for single tokens.
+ * They are handles as above (device -1, zero rows, strides, alignment,
+ * overlaps, streams and capture likewise).
+ *
+ *  - Rows are packed: `offsets` (device, seqs + 1 values, not decreasing, from 0
+ *    to tokens) gives the sequences' first rows; null: all have tokens / seqs
+ *    rows.  Rows behind the last sequence are left as they are.
+ *  - `past` (device, [seqs]) counts the positions of each sequence before the
+ *    call's rows: row i of sequence b stands at position past[b] + i.  A
+ *    negative count marks a slot without a sequence: nothing of it is
+ *    written to a cache, and its output rows are zeros.
+ *  - Position p of sequence b lies in the page table[b][p / page], at place
+ *    p % page of it.  A position beyond the table's width, or of an entry outside
+ *    0 .. pages - 1, has no place: it is not written, reads as zeros and is
+ *    attended by nobody.  Sequences may share pages; a place that one call
+ *    writes twice holds either's numbers.                                   */
+
+/* Norms of queries and keys for each head, with the position rotation in the
+ * same pass.  Each head_dim elements x of a row become
+ *
+ *   x = x / sqrt(mean(x^2) + eps) * w      (if norm; w: q_w or k_w [head_dim], or null for ones)
+ *   (a, b) = (a cos t - b sin t, b cos t + a sin t)     t = position * freq[j]
+ *
+ * for the rot / 2 pairs of the first rot elements: (j, j + rot / 2) with
+ * SN_PAIRS_HALVES, (2j, 2j + 1) with SN_PAIRS_NEIGHBOURS.  freq (radians,
+ * |freq| < 2^20) is float64 and the angle is exact to 2^-63 of a circle at any
+ * position.  q_out and k_out may be q and k.                               */
+typedef enum { SN_PAIRS_HALVES = 0, SN_PAIRS_NEIGHBOURS = 1 } sn_pairs;
+typedef struct {
+  int32_t dtype;
+  int32_t heads, kv_heads; /* of q and of k, at least 1 in all */
+  int32_t head_dim;        /* 1 .. 256 */
+  int32_t rot;             /* even, 0 .. head_dim */
+  int32_t pairs;           /* sn_pairs */
+  int32_t norm;            /* 0 or 1 */
+  float eps;               /* > 0 */
+} sn_headnorm_desc;
+int sn_headnorm_create(const sn_headnorm_desc* desc, const float* q_w, const float* k_w, const double* freq,
+                       int32_t device, sn_op** out);
+/* positions: device, [tokens], int32 of any sign; null if rot is 0.  Up to 2^24 - 1 tokens. */
+int sn_headnorm_run(sn_op* op, int64_t tokens, const int32_t* positions, const void* q, int64_t q_stride,
+                    const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride, void* k_out,
+                    int64_t k_out_stride, void* stream);
+
+/* A paged cache of keys and values.  Its memory is the caller's; its order is
+ * the operators' own (rows come and go through write and read):
+ * pages * kv_heads * page * head_dim elements each for k and v, and with
+ * SN_STORE_I8 pages * kv_heads * page float32 scales for each.
+ *
+ * SN_STORE_SAME keeps rows in dtype.  SN_STORE_I8 keeps each head's row x in 8 bits: the
+ * scale s = max|x| / 127 in float32 and the integers nearest to x / s, ties to
+ * even; a row stands for code * s.  Rows whose largest size is below 127 * 2^-120
+ * are zeros; one with an infinity or a NaN stands for NaN.                 */
+typedef enum { SN_STORE_SAME = 0, SN_STORE_I8 = 1 } sn_store;
+typedef struct {
+  int32_t dtype;
+  int32_t store;    /* sn_store */
+  int32_t kv_heads; /* 1 .. 4096 */
+  int32_t head_dim; /* a multiple of 8, 8 .. 256 */
+  int32_t page;     /* positions in a page: a power of two, 16 .. 4096 */
+} sn_cache_desc;
+typedef struct {
+  int64_t pages; /* below 2^31 */
+  void* k;       /* 16-byte aligned */
+  void* v;
+  float* k_scale; /* null unless SN_STORE_I8 */
+  float* v_scale;
+  int32_t seqs, width; /* of the table; width * page <= 2^30 */
+  const int32_t* table;
+  int64_t table_stride; /* any from 0: sequences may share a row */
+  const int32_t* past;
+  int64_t tokens; /* at most 2^26 */
+  const int32_t* offsets;
+} sn_cache_io;
+int sn_cache_create(const sn_cache_desc* desc, int32_t device, sn_op** out);
+/* k and v: [tokens][kv_heads * head_dim]. */
+int sn_cache_write(sn_op* op, const sn_cache_io* io, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                   void* stream);
+/* The rows of the same places, rounded once to dtype. */
+int sn_cache_read(sn_op* op, const sn_cache_io* io, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream);
+
+/* Attention over the cache.  Query head h of the row at position p (its own
+ * key and value are written before the call) sees the positions
+ * max(0, p - window + 1) .. p (window 0: 0 .. p) of key head
+ * h / (heads / kv_heads):
+ *
+ *   y = sum_j exp(scale * q k_j) v_j / sum_j exp(scale * q k_j)
+ *
+ * A row that sees no position is zeros.  What lies in places that a row does
+ * not see, infinities and NaN included, does not touch it.
+ *
+ * sn_attn_run takes any number of rows per sequence; sn_attn_step one each
+ * (tokens = seqs, offsets null).  A handle's calls share its workspace: they
+ * must follow each other on one stream.                                    */
+typedef struct {
+  sn_cache_desc cache;
+  int32_t heads;  /* a multiple of kv_heads, at most 65535 */
+  int32_t window; /* 0: none */
+  float scale;
+  int32_t max_seqs;   /* 1 .. 65535: what one call may hold */
+  int64_t max_tokens; /* at most 2^26; counts as max_seqs at least */
+} sn_attn_desc;
+int sn_attn_create(const sn_attn_desc* desc, int32_t device, sn_op** out);
+/* q and y: [tokens][heads * head_dim]. */
+int sn_attn_run(sn_op* op, const sn_cache_io* io, const void* q, int64_t q_stride, void* y, int64_t y_stride, void* stream);
+int sn_attn_step(sn_op* op, const sn_cache_io* io, const void* q, int64_t q_stride, void* y, int64_t y_stride, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,112 @@
+// Host-callable launchers of the attention operators' kernels (headnorm.hip,
+// kvcache.hip, attention.hip) and the device helpers they share.  A launcher
+// enqueues on the given stream; none allocates or synchronises.
+#pragma once
+
+#include "seq.hpp"
+
+namespace sn {
+namespace k {
+
+// ------------------------------------------------------------------ norms of heads with the position rotation
+struct HeadNormArgs {
+  int dtype, heads, kv_heads, dim, rot, pairs, norm;
+  float eps;
+  const float *q_w, *k_w;        // [dim] or null (ones)
+  const unsigned long long* turn;  // [rot / 2] turns per position, the fraction times 2^64
+  int64_t tokens;
+  const int32_t* positions;
+  const void* q;
+  int64_t qs;
+  const void* k;
+  int64_t ks;
+  void* qo;
+  int64_t qos;
+  void* ko;
+  int64_t kos;
+};
+void head_norm(const HeadNormArgs& a, hipStream_t st);
+
+// ------------------------------------------------------------------ paged cache
+constexpr int kCacheTile = 16;           // positions that V keeps together
+constexpr int kMaxPast = 1 << 30;        // positions of rows stay below 2^31
+struct CacheArgs {
+  int dtype, kv_heads, dim, shift;  // shift: log2 of a page's positions
+  bool i8;
+  int64_t pages;
+  void* k;    // [page][kv head][position][dim]
+  void* v;    // [page][kv head][position / 16][dim][position % 16]
+  float* ks;  // [page][kv head][position]
+  float* vs;
+  int seqs, width;
+  const int32_t* table;
+  int64_t ts;
+  const int32_t* past;
+  int64_t tokens;
+  const int32_t* offsets;
+  int64_t each;  // rows per sequence without offsets
+};
+struct CacheRows {
+  CacheArgs c;
+  void* k;  // [tokens][kv_heads * dim]: read by a write, written by a read
+  int64_t krs;
+  void* v;
+  int64_t vrs;
+};
+void cache_write(const CacheRows& a, hipStream_t st);
+void cache_read(const CacheRows& a, hipStream_t st);
+
+// ------------------------------------------------------------------ attention over the cache
+struct AttnArgs {
+  CacheArgs c;
+  int heads, window;
+  float scale;
+  const void* q;
+  int64_t qs;
+  void* y;
+  int64_t ys;
+};
+void attention(const AttnArgs& a, hipStream_t st);
+
+// ------------------------------------------------------------------ device helpers
+// The rows of sequence b: [first, end), within the call's rows.
+__device__ __forceinline__ void seq_rows(const CacheArgs& c, int b, int64_t& first, int64_t& end) {
+  if (c.offsets) {
+    first = min((int64_t)max(c.offsets[b], 0), c.tokens);
+    end = max(first, min((int64_t)max(c.offsets[b + 1], 0), c.tokens));
+  } else {
+    first = b * c.each;
+    end = first + c.each;
+  }
+}
+// The sequence of a row, -1 for rows of none.
+__device__ __forceinline__ int seq_of(const CacheArgs& c, int64_t row) {
+  if (!c.offsets) return (int)(row / c.each);
+  int lo = 0, hi = c.seqs;  // the last b with offsets[b] <= row
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (c.offsets[mid] <= row) lo = mid;
+    else hi = mid;
+  }
+  return c.offsets[lo] <= row && row < c.offsets[lo + 1] ? lo : -1;
+}
+// The page that holds a position of sequence b, -1 if none does.
+__device__ __forceinline__ int page_of(const CacheArgs& c, int b, int pos) {
+  const int i = pos >> c.shift;
+  if (pos < 0 || i >= c.width) return -1;
+  const int page = c.table[b * c.ts + i];
+  return (unsigned)page < (uint64_t)c.pages ? page : -1;
+}
+// Where a position's row of K and its elements of V begin (V: 16 apart), and its scales.
+__device__ __forceinline__ int64_t k_at(const CacheArgs& c, int page, int head, int slot) {
+  return ((((int64_t)page * c.kv_heads + head) << c.shift) + slot) * c.dim;
+}
+__device__ __forceinline__ int64_t v_at(const CacheArgs& c, int page, int head, int slot) {
+  return ((((int64_t)page * c.kv_heads + head) << c.shift) + (slot & ~15)) * c.dim + (slot & 15);
+}
+__device__ __forceinline__ int64_t scale_at(const CacheArgs& c, int page, int head, int slot) {
+  return (((int64_t)page * c.kv_heads + head) << c.shift) + slot;
+}
+
+}  // namespace k
+}  // namespace sn

@@ -29,6 +29,8 @@ OPT_LAYOUTS, OPT_ALGOS, OPT_PARAMS, OPT_HIPGRAPH, OPT_SEED, OPT_FLUSH, OPT_KEEP,
 DTYPE_NAME = {v: k for k, v in DTYPE.items()}
 NORM = {"rms": 0, "layer": 1}
 GATE = {"none": 0, "before": 1, "after": 2}
+PAIRS = {"halves": 0, "neighbours": 1}
+STORE = {"same": 0, "i8": 1}
 
 STATUS = {0: "SN_OK", -1: "SN_E_INVALID", -2: "SN_E_SHAPE", -3: "SN_E_STATE",
           -4: "SN_E_UNSUPPORTED", -5: "SN_E_DEVICE", -6: "SN_E_NOMEM", -7: "SN_E_INTERNAL"}
@@ -75,6 +77,29 @@ class ScanIO(ctypes.Structure):
                 ("dt_stride", ctypes.c_int64), ("window", ctypes.c_void_p), ("state", ctypes.c_void_p),
                 ("y", ctypes.c_void_p), ("y_stride", ctypes.c_int64), ("window_out", ctypes.c_void_p),
                 ("state_out", ctypes.c_void_p)]
+
+
+class HeadNormDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rot", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("norm", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("store", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page", ctypes.c_int32)]
+
+
+class CacheIO(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("seqs", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("past", ctypes.c_void_p), ("tokens", ctypes.c_int64), ("offsets", ctypes.c_void_p)]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [("cache", CacheDesc), ("heads", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("max_seqs", ctypes.c_int32), ("max_tokens", ctypes.c_int64)]
 
 
 # exported functions: name -> (restype, argtypes)
@@ -128,6 +153,14 @@ SIGNATURES = {
                                       ctypes.POINTER(_P)]),
     "sn_scan_run": (ctypes.c_int, [_P, ctypes.POINTER(ScanIO), _P]),
     "sn_scan_step": (ctypes.c_int, [_P, ctypes.POINTER(ScanIO), _P]),
+    "sn_headnorm_create": (ctypes.c_int, [ctypes.POINTER(HeadNormDesc), _F32P, _F32P, _P, _I32, ctypes.POINTER(_P)]),
+    "sn_headnorm_run": (ctypes.c_int, [_P, _I64, _P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
+    "sn_cache_create": (ctypes.c_int, [ctypes.POINTER(CacheDesc), _I32, ctypes.POINTER(_P)]),
+    "sn_cache_write": (ctypes.c_int, [_P, ctypes.POINTER(CacheIO), _P, _I64, _P, _I64, _P]),
+    "sn_cache_read": (ctypes.c_int, [_P, ctypes.POINTER(CacheIO), _P, _I64, _P, _I64, _P]),
+    "sn_attn_create": (ctypes.c_int, [ctypes.POINTER(AttnDesc), _I32, ctypes.POINTER(_P)]),
+    "sn_attn_run": (ctypes.c_int, [_P, ctypes.POINTER(CacheIO), _P, _I64, _P, _I64, _P]),
+    "sn_attn_step": (ctypes.c_int, [_P, ctypes.POINTER(CacheIO), _P, _I64, _P, _I64, _P]),
     "sn_last_error": (ctypes.c_char_p, []),
 }
 

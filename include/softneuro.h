@@ -676,7 +676,7 @@ int sn_headnorm_run(sn_op* op, int64_t tokens, const int32_t* positions, const v
  * SN_STORE_I8 pages * kv_heads * page float32 scales for each.
  *
  * SN_STORE_SAME keeps rows in dtype.  SN_STORE_I8 keeps each head's row x in 8 bits: the
- * scale s = max|x| / 127 in float32 and the integers nearest to x / s, ties to
+ * scale s = max|x| * (1 / 127), factor and product in float32, and the integers nearest to x / s, ties to
  * even; a row stands for code * s.  Rows whose largest size is below 127 * 2^-120
  * are zeros; one with an infinity or a NaN stands for NaN.                 */
 typedef enum { SN_STORE_SAME = 0, SN_STORE_I8 = 1 } sn_store;
@@ -693,7 +693,7 @@ typedef struct {
   void* v;
   float* k_scale; /* null unless SN_STORE_I8 */
   float* v_scale;
-  int32_t seqs, width; /* of the table; width * page <= 2^30 */
+  int32_t seqs, width; /* of the table; width * page <= 2^29 */
   const int32_t* table;
   int64_t table_stride; /* any from 0: sequences may share a row */
   const int32_t* past;
@@ -723,7 +723,7 @@ int sn_cache_read(sn_op* op, const sn_cache_io* io, void* k, int64_t k_stride, v
 typedef struct {
   sn_cache_desc cache;
   int32_t heads;  /* a multiple of kv_heads, at most 65535 */
-  int32_t window; /* 0: none */
+  int32_t window; /* 0: none; at most 2^29 */
   float scale;
   int32_t max_seqs;   /* 1 .. 65535: what one call may hold */
   int64_t max_tokens; /* at most 2^26; counts as max_seqs at least */

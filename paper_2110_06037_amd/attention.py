@@ -131,7 +131,7 @@ class KVCache(_Paged):
     power of two from 16) of ``kv_heads`` heads of ``head_dim``.
 
     ``store="same"`` keeps rows in dtype; "i8" in 8 bits, each head's row x as the
-    integers nearest to x / s with the float32 scale s = max|x| / 127.  Its memory
+    integers nearest to x / s with the scale s = max|x| * (1 / 127) in float32.  Its memory
     (``k``, ``v`` and with "i8" ``k_scale``, ``v_scale``) is in the operators' own
     order; rows come and go through ``write`` and ``read``."""
 

@@ -51,7 +51,7 @@ k::CacheArgs cache_args(k::CacheArgs c, const sn_cache_io* io, bool step) {
   if (step && (io->tokens != io->seqs || io->offsets)) fail(SN_E_SHAPE, "a step takes one token per sequence");
   if (io->seqs && !io->offsets && io->tokens % io->seqs) fail(SN_E_SHAPE, "tokens are no multiple of seqs, and there are no offsets");
   if (io->pages < 0 || io->pages >> 31) fail(SN_E_SHAPE, "pages must be in 0..2^31 - 1");
-  if (io->width < 0 || ((int64_t)io->width << c.shift) > k::kMaxPast) fail(SN_E_SHAPE, "width * page must be in 0..2^30");
+  if (io->width < 0 || ((int64_t)io->width << c.shift) > k::kMaxPositions) fail(SN_E_SHAPE, "width * page must be in 0..2^29");
   if (io->pages && (!io->k || !io->v || (c.i8 && (!io->k_scale || !io->v_scale)))) fail(SN_E_INVALID, "the cache's memory is null");
   if (!c.i8 && (io->k_scale || io->v_scale)) fail(SN_E_INVALID, "scales given to a cache without them");
   check_aligned(io->k, 16, "the cache's k");
@@ -99,6 +99,7 @@ int attn_call(sn_op* p, const sn_cache_io* io, const void* q, int64_t q_stride, 
     const int64_t n = (int64_t)a.heads * a.c.dim;
     a.qs = check_rows(q, q_stride, a.c.tokens, n, a.c.dtype, "q");
     a.ys = check_rows(y, y_stride, a.c.tokens, n, a.c.dtype, "y");
+    if (!step && k::attn_run_tiles(a) * a.c.kv_heads >> 24) fail(SN_E_UNSUPPORTED, "tokens * heads above 2^31 - 128 * seqs * kv_heads");
     need_device(op);
     if (!a.c.tokens) return;
     const int e = dtype_size(a.c.dtype);
@@ -107,7 +108,7 @@ int attn_call(sn_op* p, const sn_cache_io* io, const void* q, int64_t q_stride, 
                 {Place(q, a.c.tokens, n, a.qs, e), m.table, m.past, m.offsets, m.k, m.v, m.ks, m.vs});
     a.q = q, a.y = y;
     OnDevice on(op.device);
-    k::attention(a, static_cast<hipStream_t>(stream));
+    step ? k::attn_step(a, static_cast<hipStream_t>(stream)) : k::attn_run(a, static_cast<hipStream_t>(stream));
     HIPCHK(hipGetLastError());
   });
 }
@@ -249,7 +250,7 @@ int sn_attn_create(const sn_attn_desc* desc, int32_t device, sn_op** out) {
     const sn_attn_desc& d = *desc;
     const k::CacheArgs c = cache_of(d.cache);
     if (d.heads < 1 || d.heads > 65535 || d.heads % c.kv_heads) fail(SN_E_SHAPE, "heads must be a multiple of kv_heads up to 65535");
-    if (d.window < 0) fail(SN_E_SHAPE, "window must not be negative");
+    if (d.window < 0 || d.window > k::kMaxPositions) fail(SN_E_SHAPE, "window must be in 0..2^29");
     if (!std::isfinite(d.scale)) fail(SN_E_INVALID, "scale must be finite");
     if (d.max_seqs < 1 || d.max_seqs > 65535) fail(SN_E_SHAPE, "max_seqs must be in 1..65535");
     if (d.max_tokens < 1 || d.max_tokens > (1 << 26)) fail(SN_E_SHAPE, "max_tokens must be in 1..2^26");
@@ -257,6 +258,16 @@ int sn_attn_create(const sn_attn_desc* desc, int32_t device, sn_op** out) {
     std::unique_ptr<AttnOp> op(new AttnOp(OP_ATTENTION, device));
     op->max_seqs = d.max_seqs, op->max_tokens = std::max<int64_t>(d.max_tokens, d.max_seqs);
     op->a.c = c, op->a.heads = d.heads, op->a.window = d.window, op->a.scale = d.scale;
+    if (device >= 0) {
+      OnDevice on(device);
+      int64_t o, m, counts;
+      k::attn_workspace(op->a, o, m, counts);
+      op->a.ws_o = static_cast<float*>(op->alloc(o * sizeof(float)));
+      op->a.ws_m = static_cast<float*>(op->alloc(m * sizeof(float)));
+      op->a.count = static_cast<unsigned*>(op->alloc(counts * sizeof(unsigned)));
+      HIPCHK(hipMemset(op->a.count, 0, counts * sizeof(unsigned)));
+      HIPCHK(hipDeviceSynchronize());
+    }
     *out = op.release();
   });
 }

@@ -29,7 +29,8 @@ void head_norm(const HeadNormArgs& a, hipStream_t st);
 
 // ------------------------------------------------------------------ paged cache
 constexpr int kCacheTile = 16;           // positions that V keeps together
-constexpr int kMaxPast = 1 << 30;        // positions of rows stay below 2^31
+constexpr int kMaxPositions = 1 << 29;   // of a table, and of a window
+constexpr int kMaxPast = 1 << 30;        // past counts as this at most: such rows see no window of a table
 struct CacheArgs {
   int dtype, kv_heads, dim, shift;  // shift: log2 of a page's positions
   bool i8;
@@ -65,8 +66,22 @@ struct AttnArgs {
   int64_t qs;
   void* y;
   int64_t ys;
+  // workspace (attn_workspace)
+  float* ws_o;      // parts' sums of weighted values
+  float* ws_m;      // their maxima and sums of weights
+  unsigned* count;  // parts that are done, zero between calls
+  // set by the launchers
+  float scale2;   // |scale| log2(e)
+  bool negative;  // scale < 0
+  int units;      // parts that a step's keys are cut into
 };
-void attention(const AttnArgs& a, hipStream_t st);
+int64_t attn_run_tiles(const AttnArgs& a);  // bound of a prompt call's tiles of rows, per key head
+void attn_workspace(const AttnArgs& a, int64_t& o, int64_t& m, int64_t& counts);
+void attn_run(AttnArgs a, hipStream_t st);
+void attn_step(AttnArgs a, hipStream_t st);
+void attention_f32(AttnArgs& a, bool step, hipStream_t st);
+void attention_f16(AttnArgs& a, bool step, hipStream_t st);
+void attention_bf16(AttnArgs& a, bool step, hipStream_t st);
 
 // ------------------------------------------------------------------ device helpers
 // The rows of sequence b: [first, end), within the call's rows.

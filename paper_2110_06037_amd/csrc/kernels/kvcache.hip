@@ -1,5 +1,5 @@
 // The paged key-value cache: rows written to their pages, as they are or in 8
-// bits, and read back.  In 8 bits a head's row has the scale s = max|x| / 127 in
+// bits, and read back.  In 8 bits a head's row has the scale s = max|x| * (1 / 127) in
 // float32 and the codes nearest to x / s (ties to even).
 #include "attn.hpp"
 
@@ -17,11 +17,11 @@ __device__ __forceinline__ float code_of(float x, float s, float inv) {
   if (r < -h || (r == -h && odd)) c -= 1.f;
   return c;
 }
-// max|x| / 127; rows below 127 * 2^-120 count as zeros (code_of's steps stay exact),
+// max|x| * (1 / 127); rows below 127 * 2^-120 count as zeros (code_of's steps stay exact),
 // and a row with an infinity or a NaN has no numbers at all.
 __device__ __forceinline__ float scale_of(float most, bool fine) {
   if (!fine) return __builtin_nanf("");
-  const float s = most / 127.f;
+  const float s = most * (1.f / 127.f);
   return s < 0x1p-120f ? 0.f : s;
 }
 __device__ __forceinline__ float wave_max(float v) {

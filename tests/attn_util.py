@@ -27,7 +27,7 @@ def quantised(x, heads):
     h = x.reshape(x.shape[0], heads, -1)
     most = np.abs(h).max(-1)
     with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
-        s = (most / 127).astype(np.float32).astype(np.float64)
+        s = (most.astype(np.float32) * np.float32(1 / 127)).astype(np.float64)
         s = np.where(s < 2.0 ** -120, 0, s)
         code = np.where(s[..., None] > 0, np.rint(h / np.where(s > 0, s, 1)[..., None]), 0)
         out = code * s[..., None]

@@ -170,6 +170,6 @@ def test_the_oracle_of_8_bit_rows():
     x = np.concatenate([r.standard_normal((20, 16)), r.integers(-127, 128, (20, 16)) / 2]).astype(np.float32).astype(np.float64)
     want = np.zeros_like(x)
     for i, row in enumerate(x):
-        s = float(np.float32(np.abs(row).max() / 127))
+        s = float(np.float32(np.abs(row).max()) * np.float32(1 / 127))
         want[i] = [round(Fraction(v) / Fraction(s)) * s if s else 0 for v in row]
     assert np.array_equal(quantised(x, 1), want)

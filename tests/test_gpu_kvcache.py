@@ -63,7 +63,7 @@ def test_codes_at_the_middle_between_two(dtype):
     r = np.random.default_rng(3)
     rows = []
     for most in (127.0, 1.0, 254.0, 3.0, 1.984375, 100.0):
-        s = float(np.float32(most / 127))
+        s = float(np.float32(most) * np.float32(1 / 127))
         x = (r.integers(-127, 127, (16, 64)) + 0.5) * s
         x[:, 0] = most
         rows.append(np.where(r.random(x.shape) < 0.5, x, np.nextafter(x.astype(np.float32), np.float32(r.choice([-1e9, 1e9])))))

@@ -98,19 +98,37 @@ __device__ __forceinline__ float sum_x16(float v) {
 constexpr float kNone = -__builtin_huge_valf();  // a maximum of nothing
 __device__ __forceinline__ float some(float m) { return m == kNone ? 0.f : m; }
 
-// Whether this workgroup is the last of n at a counter, which it then clears.  What
-// each has written before is seen by the last one afterwards.
+// Parts of a sum that other workgroups read: stores and loads of the workspace go past
+// the XCDs' own L2 caches (cache policy sc1), a workgroup's stores are complete
+// before it counts itself in, so that no cache-wide fence is needed (with fences: 157
+// us instead of 30 for 700 workgroups).
+constexpr int kCoherent = 16;
+struct Shared {
+  __amdgpu_buffer_rsrc_t r;
+  __device__ __forceinline__ Shared(const float* p) : r(make_rsrc(p, 0x7fffffff)) {}
+  __device__ __forceinline__ void put4(int at, f32x4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, 4 * at, 0, kCoherent);
+  }
+  __device__ __forceinline__ void put(int at, float v) const {
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), r, 4 * at, 0, kCoherent);
+  }
+  __device__ __forceinline__ f32x4 get4(int at) const {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, 4 * at, 0, kCoherent));
+  }
+  __device__ __forceinline__ float get(int at) const {
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, 4 * at, 0, kCoherent));
+  }
+};
+// Whether this workgroup is the last of n at a counter, which it then clears.
 __device__ __forceinline__ bool last_of(unsigned* count, unsigned n, int* shared) {
-  __threadfence();
+  wait_vmcnt<0>();
   __syncthreads();
   if (threadIdx.x == 0) {
-    *shared = atomicAdd(count, 1u) + 1 == n;
-    if (*shared) *count = 0;
+    *shared = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == n;
+    if (*shared) __hip_atomic_exchange(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  const bool last = *shared;
-  if (last) __threadfence();
-  return last;
+  return *shared;
 }
 
 // ------------------------------------------------------------------ single tokens
@@ -356,8 +374,9 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
   __syncthreads();
   const int64_t slots = (int64_t)c.kv_heads * gridDim.z, at = (int64_t)head * gridDim.z + blockIdx.z;
   const int chunks = D / 4;
-  float* wo = a.ws_o + ((p.slot + p.part) * slots + at) * 16 * DP;
-  float* wm = a.ws_m + ((p.slot + p.part) * slots + at) * 32;
+  const Shared wo(a.ws_o), wm(a.ws_m);
+  auto o_at = [&](int part) { return (int)((p.slot + part) * slots + at) * (16 * DP); };
+  auto m_at = [&](int part) { return (int)((p.slot + part) * slots + at) * 32; };
   for (int i = threadIdx.x; i < cols * chunks; i += 64 * kStepWaves) {
     const int r = i / chunks, d = 4 * (i - r * chunks);
     float top = kNone, sum = 0.f;
@@ -378,23 +397,24 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
       for (int j = 0; j < 4; ++j) t[j] = from_f<T>(acc[j] * inv);
       __builtin_memcpy(y, t, sizeof(t));
     } else {
-      *reinterpret_cast<f32x4*>(wo + r * DP + d) = acc;
-      if (d == 0) wm[r] = top, wm[16 + r] = sum;
+      wo.put4(o_at(p.part) + r * DP + d, acc);
+      if (d == 0) wm.put(m_at(p.part) + r, top), wm.put(m_at(p.part) + 16 + r, sum);
     }
   }
   if (p.parts == 1) return;
   if (!last_of(a.count + p.slot * slots + at, p.parts, &flag)) return;
   // the last workgroup of a sequence joins its parts, in their order
-  wo = a.ws_o + (p.slot * slots + at) * 16 * DP, wm = a.ws_m + (p.slot * slots + at) * 32;
   for (int i = threadIdx.x; i < cols * chunks; i += 64 * kStepWaves) {
     const int r = i / chunks, d = 4 * (i - r * chunks);
     float top = kNone, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < p.parts; ++k) top = fmaxf(top, wm[k * slots * 32 + r]);
+#pragma unroll 8
+    for (int k = 0; k < p.parts; ++k) top = fmaxf(top, wm.get(m_at(k) + r));
+#pragma unroll 8
     for (int k = 0; k < p.parts; ++k) {
-      const float f = __builtin_amdgcn_exp2f(wm[k * slots * 32 + r] - some(top));
-      sum += f * wm[k * slots * 32 + 16 + r];
-      acc += f * *reinterpret_cast<const f32x4*>(wo + k * slots * 16 * DP + r * DP + d);
+      const float f = __builtin_amdgcn_exp2f(wm.get(m_at(k) + r) - some(top));
+      sum += f * wm.get(m_at(k) + 16 + r);
+      acc += f * wo.get4(o_at(k) + r * DP + d);
     }
     T* y = static_cast<T*>(a.y) + b * a.ys + (int64_t)(qh + r) * D + d;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -406,15 +426,13 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
 }
 
 // ------------------------------------------------------------------ prompts
-// A row of 8-bit values stands for code * s: its s goes as a power of two into the
-// codes, which every type holds exactly (f16 from 2^-24 on), and the rest of it,
-// 1 .. 2, into the weights, so that those are the only numbers that are rounded.
-// The power is at most what a row of the type may have, so that codes stay numbers
-// whatever lies where a scale that was never written would be.
-template <typename T>
+// f16 weights of 8-bit rows, which stand for code * s: s goes as a power of two into the
+// codes, which f16 holds exactly from 2^-24 on, and the rest of it, 1 .. 2, into the weights,
+// so that those are the only numbers that are rounded, and in range.  (bf16 has the range for
+// all of s in the weights.)  The power is at most a row's of f16 values, so that codes stay numbers whatever lies
+// in a place that was never written, -128 with any scale.
 __device__ __forceinline__ float power_of(float s) {
-  constexpr unsigned top = std::is_same<T, f16>::value ? 0x43800000u : 0x7b800000u;  // 2^8 (-128 lies in memory), 2^120
-  return __builtin_bit_cast(float, min(max(__builtin_bit_cast(unsigned, s) & 0x7f800000u, 0x33800000u), top));
+  return __builtin_bit_cast(float, min(max(__builtin_bit_cast(unsigned, s) & 0x7f800000u, 0x33800000u), 0x43800000u));  // 2^-24 .. 2^8
 }
 constexpr int kRunRows = 128;
 constexpr int kRunParts = 512;  // workgroups that fewer tiles than half of it are split to
@@ -423,8 +441,20 @@ constexpr int run_keys() {
   return sizeof(T) == 2 ? 64 : 32;
 }
 
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// LDS direct load: 16 bytes a lane from `bytes` at `from` (beyond them: zeros) to 1024 at
+// `to`.  (The compiler's own form makes every later read of the array wait for it; here the
+// kernel waits itself, once a block.)
+__device__ __forceinline__ void lds_load(const void* from, unsigned bytes, unsigned offset, const void* to) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(from);
+  const u32x4 rsrc = {(unsigned)p, (unsigned)(p >> 32) & 0xffffu, bytes, 0x00020000u};
+  const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)to;
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(rsrc), "s"(at) : "memory");
+}
+
 // The sequence and its tile of rows behind a number: tiles are counted over the sequences in order.
-__device__ __forceinline__ bool run_tile(const CacheArgs& c, int each, int tile, int& b, int64_t& t, int64_t& first, int64_t& n) {
+__device__ __forceinline__ bool run_tile(const CacheArgs& c, int each, int tile, int& b, int& t, int& first, int& n) {
   const int lane = threadIdx.x & 63;
   int64_t before = 0;
   for (int base = 0; base < c.seqs; base += 64) {
@@ -440,9 +470,8 @@ __device__ __forceinline__ bool run_tile(const CacheArgs& c, int each, int tile,
     const unsigned long long at = __ballot(tile < before + sum);
     if (at) {
       const int l = __ffsll(at) - 1;
-      b = __builtin_amdgcn_readfirstlane(base + l);
-      t = tile - __shfl(before + sum - own, l);
-      first = __shfl(lo, l), n = __shfl(hi - lo, l);
+      b = uniform(base + l), t = uniform(tile - (int)__shfl(before + sum - own, l));
+      first = uniform((int)__shfl(lo, l)), n = uniform((int)__shfl(hi - lo, l));
       return true;
     }
     before += __shfl(sum, 63);
@@ -450,36 +479,49 @@ __device__ __forceinline__ bool run_tile(const CacheArgs& c, int each, int tile,
   return false;
 }
 
+// K and V of a block in LDS, in granules of 16 bytes: K [key][element], V as the
+// cache has it, [16 keys][element][key].  The granules of a row lie in an order of
+// the row's own, so that 8 lanes that read one of each of 8 rows meet no bank twice.
+template <typename T, int DP>
+struct RunTile {
+  static constexpr int KB = run_keys<T>(), GE = 16 / sizeof(T), FG = 8 / GE;  // elements of a granule, granules of 8 elements
+  static constexpr int KG = DP / GE, VG = 16 / GE;                            // granules of a key's row, of an element's 16 keys
+  static constexpr int N = KB * DP / GE;                                      // of a block, each of K and V
+  static __device__ __forceinline__ int k(int key, int g) { return key * KG + (g ^ (key & ((KG < 16 ? KG : 16) - 1))); }
+  static __device__ __forceinline__ int v_order(int d) { return sizeof(T) == 2 ? (d >> 2) & 1 : (d >> 1) & 3; }
+  static __device__ __forceinline__ int v(int t16, int d, int g) { return (t16 * DP + d) * VG + (g ^ v_order(d)); }
+};
+
 template <typename T, bool I8, int DP, bool EXACT>
-__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_run_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 2)) ? 2 : 1) void attn_run_kernel(AttnArgs a) {
   typedef typename std::conditional<I8, int8_t, T>::type E;
   typedef typename Frag<T>::type F;
-  constexpr int KB = run_keys<T>(), NK = KB / 32, NS = DP / 16, ND = DP / 32, NC = DP / 8, NL = KB * NC / 256;
-  constexpr int KX = (NC < 16 ? NC : 16) - 1, VC = KB / 8, VX = VC - 1;
+  typedef RunTile<T, DP> L;
+  constexpr int KB = L::KB, NK = KB / 32, NS = DP / 16, ND = DP / 32, NG = L::N / 256, FG = L::FG;
+  constexpr int NC = DP / 8, NL = KB * NC / 256;  // chunks of 8 elements (8-bit caches)
+  constexpr bool POWER = I8 && std::is_same<T, f16>::value;  // see power_of
   // f16 weights are 2^6 times as large (2^14 at most, see kLazy)
   constexpr float LIFT = std::is_same<T, f16>::value ? 6.f : 0.f, kLazy = 8.f;
-  __shared__ __attribute__((aligned(16))) T sk[2][KB * DP];
-  __shared__ __attribute__((aligned(16))) T sv[2][KB * DP];
+  __shared__ u32x4 sk[2 * L::N], sv[2 * L::N];
   __shared__ __attribute__((aligned(16))) float sks[2][I8 ? KB : 4], svs[2][I8 ? KB : 4];
   __shared__ int flag[2];
   const CacheArgs& c = a.c;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
   const int D = EXACT ? DP : c.dim, each = a.heads / c.kv_heads;
   // heads next to each other: workgroups of one head go to one XCD where 8 divides
   // their number.  The last tiles, which see the most keys, first.
   const int head = blockIdx.x % c.kv_heads, tiles = gridDim.x / c.kv_heads, tile = tiles - 1 - blockIdx.x / c.kv_heads;
-  int b;
-  int64_t t, row0, n;
+  int b, t, row0, n;
   if (!run_tile(c, each, tile, b, t, row0, n)) return;
-  const int past = min(c.past[b], kMaxPast);
-  const int64_t rows = n * each, mine = t * kRunRows + 32 * wave + r;
-  const int64_t rr = min(mine, rows - 1);  // rows behind the last one repeat it and are not stored
-  const int token = (int)(rr / each), qh = head * each + (int)(rr - (int64_t)token * each);
+  const int past = uniform(min(c.past[b], kMaxPast));
+  const int rows = n * each, mine = t * kRunRows + 32 * wave + r;  // (below 2^31: the launcher's tiles)
+  const int rr = min(mine, rows - 1);  // rows behind the last one repeat it and are not stored
+  const int token = fdiv(rr, a.each), qh = head * each + rr - token * each;
   const int pos = past < 0 ? -1 : past + token;
-  const int top_pos = __builtin_amdgcn_readlane(pos, 63), low_pos = __builtin_amdgcn_readfirstlane(pos);  // of the wave
+  const int top_pos = __builtin_amdgcn_readlane(pos, 63), low_pos = uniform(pos);  // of the wave
   // the workgroup's keys, and this part's blocks of them
-  const int64_t r0 = t * kRunRows, r1 = min(r0 + kRunRows, rows) - 1;
-  const int pos0 = past < 0 ? -1 : past + (int)(r0 / each), pos1 = past < 0 ? -1 : past + (int)(r1 / each);
+  const int r0 = t * kRunRows, r1 = min(r0 + kRunRows, rows) - 1;
+  const int pos0 = past < 0 ? -1 : past + uniform(fdiv(r0, a.each)), pos1 = past < 0 ? -1 : past + uniform(fdiv(r1, a.each));
   const int from = a.window ? max(0, pos0 - a.window + 1) : 0, last = min(pos1, (c.width << c.shift) - 1);
   int first = from / KB, end = last < from ? first : last / KB + 1;
   if (gridDim.z > 1) {
@@ -493,78 +535,109 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_run_k
   for (int s = 0; s < NS; ++s) {
     const int d = 16 * s + 8 * h;
     V8<T> v = zero8<T>();
-    if (EXACT || d < D) v = load8(static_cast<const T*>(a.q) + (row0 + token) * a.qs + (int64_t)qh * D + d);
+    if (EXACT || d < D) v = load8(static_cast<const T*>(a.q) + (int64_t)(row0 + token) * a.qs + (int64_t)qh * D + d);
     q[s] = frag_of<T>(v);
     if (a.negative) q[s] = -q[s];
   }
 
   // lane i holds the page of the i-th 16 positions of a block
-  auto pages_at = [&](int block) { return lane < KB / 16 && block < end ? page_of(c, b, block * KB + 16 * lane) : -1; };
-  V8<E> kr[NL], vr[NL];
-  float ksr = 0.f, vsr = 0.f, vpw[I8 ? NL : 1][8];
-  auto load = [&](int block, int pages) {
+  // (its entry of the table is read two blocks ahead, and looked at one block later)
+  const int32_t* table = c.table + b * c.ts;
+  auto entry_of = [&](int block) { return min(((block * KB) >> c.shift) + ((((block * KB) & mask) + 16 * min(lane, KB / 16 - 1)) >> c.shift), c.width - 1); };
+  auto pages_of = [&](int block, int entry) {
+    return lane < KB / 16 && block * KB + 16 * lane < c.width << c.shift && (unsigned)entry < (uint64_t)c.pages ? entry : -1;
+  };
+  // where the i-th 16 positions of a block lie, in rows of dim elements
+  auto rows_at = [&](int block, int pages, int t16) {
+    const int page = max(0, __builtin_amdgcn_readlane(pages, t16));
+    return (((int64_t)page * c.kv_heads + head) << c.shift) + ((block * KB + 16 * t16) & mask);
+  };
+
+  // Caches in T: LDS direct loads.  A wave's i-th load fills the 64 granules from
+  // 256 i + 64 wave on; all lie in one 16 positions.  This lane's granule is at an
+  // offset from them that is the same in every block.
+  unsigned koff[I8 ? 1 : NG], voff[I8 ? 1 : NG];
+  if constexpr (!I8) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int x = tid + 256 * i;
-      {
-        const int key = x / NC, d = 8 * (x % NC), t16 = __builtin_amdgcn_readfirstlane(key / 16);
-        const int page = max(0, __builtin_amdgcn_readlane(pages, t16));
-        const E* p = static_cast<const E*>(c.k) +
-                     ((((int64_t)page * c.kv_heads + head) << c.shift) + ((block * KB + 16 * t16) & mask)) * D;
-        kr[i] = load8(p + (key & 15) * D + (EXACT || d < D ? d : 0));
-      }
-      {
-        const int t16 = __builtin_amdgcn_readfirstlane(x / (2 * DP)), e = x % (2 * DP);
-        const int page = max(0, __builtin_amdgcn_readlane(pages, t16));
-        const int64_t at = (((int64_t)page * c.kv_heads + head) << c.shift) + ((block * KB + 16 * t16) & mask);
-        vr[i] = load8(static_cast<const E*>(c.v) + at * D + (EXACT ? 8 * e : 8 * min(e, 2 * D - 1)));
-        if constexpr (I8) __builtin_memcpy(vpw[i], c.vs + at + 8 * (e & 1), 32);
-      }
+    for (int i = 0; i < NG; ++i) {
+      const int x = 256 * i + tid, key = x / L::KG, kg = L::k(key, x % L::KG) % L::KG;
+      koff[i] = EXACT || kg * L::GE < D ? (unsigned)(((key & 15) * D + kg * L::GE) * sizeof(T)) : kOOB;
+      const int d = x / L::VG % DP, vg = x % L::VG ^ L::v_order(d);
+      voff[i] = EXACT || d < D ? (unsigned)((d * 16 + vg * L::GE) * sizeof(T)) : kOOB;
     }
-    if constexpr (I8)
+  }
+  // 8-bit caches: through registers.
+  V8<E> kr[I8 ? NL : 1], vr[I8 ? NL : 1];
+  float ksr = 0.f, vsr = 0.f, vpw[POWER ? NL : 1][8];
+  auto load = [&](int block, int pages, int buf) {
+    if constexpr (!I8) {
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const int x = 256 * i + 64 * wave;
+        const int64_t at = rows_at(block, pages, x / L::KG / 16);
+        lds_load(static_cast<const E*>(c.k) + at * D, 16 * D * sizeof(T), koff[i], &sk[buf * L::N + x]);
+      }
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const int x = 256 * i + 64 * wave;
+        const int64_t at = rows_at(block, pages, x / (L::VG * DP));
+        lds_load(static_cast<const E*>(c.v) + at * D, 16 * D * sizeof(T), voff[i], &sv[buf * L::N + x]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int x = 256 * i + tid, w = 256 * i + 64 * wave;
+        const int d = 8 * (x % NC), e = x % (2 * DP);
+        kr[i] = load8(static_cast<const E*>(c.k) + (rows_at(block, pages, w / NC / 16) + (x / NC & 15)) * D + (EXACT || d < D ? d : 0));
+        const int64_t at = rows_at(block, pages, w / (2 * DP));
+        vr[i] = load8(static_cast<const E*>(c.v) + at * D + (EXACT ? 8 * e : 8 * min(e, 2 * D - 1)));
+        if constexpr (POWER) __builtin_memcpy(vpw[i], c.vs + at + 8 * (e & 1), 32);
+      }
       if (tid < KB) {
         const int page = max(0, __shfl(pages, tid / 16));
         const int64_t at = (((int64_t)page * c.kv_heads + head) << c.shift) + ((block * KB + tid) & mask);
         ksr = c.ks[at], vsr = c.vs[at];
       }
+    }
   };
-  // Into LDS: K [key][element], V [element][key], the chunks of 8 of a row in an order
-  // of the row's own, so that 8 lanes that read one chunk of 8 rows meet no bank twice.
-  auto store = [&](int buf, int block, bool edge) {
-    bool odd = false;
+  auto put8 = [&](u32x4* to, int at0, int at1, const F& f) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(&f);
+    to[at0] = p[0];
+    if constexpr (FG == 2) to[at1] = p[1];
+  };
+  auto store = [&](int buf) {
+    if constexpr (I8) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int x = tid + 256 * i;
-      {
-        const int key = x / NC, ch = x % NC;
+      for (int i = 0; i < NL; ++i) {
+        const int x = 256 * i + tid, key = x / NC, ch = x % NC;
         F f = frag_of<T>(kr[i]);
         if constexpr (!EXACT)
           if (8 * ch >= D) f = F{};
-        *reinterpret_cast<F*>(&sk[buf][(key * NC + (ch ^ (key & KX))) * 8]) = f;
-      }
-      {
-        const int t16 = x / (2 * DP), e = x % (2 * DP), d = e >> 1, ch = 2 * t16 + (e & 1);
-        F f;
-        if constexpr (I8) {
+        put8(sk + buf * L::N, L::k(key, FG * ch), L::k(key, FG * ch + FG - 1), f);
+        const int t16 = x / (2 * DP), e = x % (2 * DP), dd = e >> 1;
+        F g = frag_of<T>(vr[i]);
+        if constexpr (POWER) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = (T)((float)vr[i].v[j] * power_of<T>(vpw[i][j]));
-        } else {
-          f = frag_of<T>(vr[i]);
-          if (edge && (EXACT || d < D))
-#pragma unroll
-            for (int j = 0; j < 8; ++j) odd = odd || !__builtin_isfinite((float)f[j]);
+          for (int j = 0; j < 8; ++j) g[j] = (T)((float)vr[i].v[j] * power_of(vpw[i][j]));
         }
-        *reinterpret_cast<F*>(&sv[buf][(d * VC + (ch ^ (d & VX))) * 8]) = f;
+        put8(sv + buf * L::N, L::v(t16, dd, FG * (e & 1)), L::v(t16, dd, FG * (e & 1) + FG - 1), g);
       }
+      if (tid < KB) sks[buf][tid] = ksr * a.scale2, svs[buf][tid] = POWER ? vsr / power_of(vsr) : vsr;
     }
-    if constexpr (I8)
-      if (tid < KB) sks[buf][tid] = ksr * a.scale2, svs[buf][tid] = vsr / power_of<T>(vsr);
-    if (!I8 && edge && __any(odd) && lane == 0) flag[buf] = block + 1;  // (a block's own number: none is ever cleared)
   };
-  // Whether every row of the workgroup sees every key of a block.
-  auto edge_of = [&](int block, int pages) {
-    return block * KB + KB - 1 > pos0 || (a.window && block * KB < pos1 - a.window + 1) ||
-           __builtin_popcountll(__ballot(pages >= 0)) < KB / 16;
+  auto k_frag = [&](int buf, int key, int ch) {
+    F f;
+    u32x4* p = reinterpret_cast<u32x4*>(&f);
+#pragma unroll
+    for (int i = 0; i < FG; ++i) p[i] = sk[buf * L::N + L::k(key, FG * ch + i)];
+    return f;
+  };
+  auto v_frag = [&](int buf, int t16, int d) {
+    F f;
+    u32x4* p = reinterpret_cast<u32x4*>(&f);
+#pragma unroll
+    for (int i = 0; i < FG; ++i) p[i] = sv[buf * L::N + L::v(t16, d, FG * h + i)];
+    return f;
   };
 
   f32x16 o[ND];
@@ -573,21 +646,41 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_run_k
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   float m = kNone, l = 0.f;
-  int pages = pages_at(first), pages1 = pages_at(first + 1);
+  int pages = -1, pages1 = -1;
   if (tid < 2) flag[tid] = 0;
-  bool edge = edge_of(first, pages);
   if (first < end) {
-    load(first, pages);
-    __syncthreads();
-    store(0, first, edge);
+    const int entry = table[entry_of(first)], entry1 = table[entry_of(first + 1)];
+    pages = pages_of(first, entry), pages1 = pages_of(first + 1, entry1);
+    load(first, pages, 0), store(0);
   }
+  wait_vmcnt<0>();
   __syncthreads();
   for (int block = first; block < end; ++block) {
     const int buf = (block - first) & 1;
     const bool more = block + 1 < end;
-    if (more) load(block + 1, pages1);
-    const int pages2 = pages_at(block + 2);
-    const bool odd = !I8 && edge && flag[buf] == block + 1;
+    const int entry2 = table[entry_of(block + 2)];
+    if (more) load(block + 1, pages1, buf ^ 1);
+    // whether some row of the workgroup does not see some key of the block
+    const unsigned long long there = __ballot(pages >= 0);
+    const bool edge = block * KB + KB - 1 > pos0 || (a.window && block * KB < pos1 - a.window + 1) || __builtin_popcountll(there) < KB / 16;
+    bool odd = false;
+    if constexpr (!I8) {
+      // What such a row does not see takes no part in it, whatever it is: 0 times a
+      // value that is not finite would (a flag holds a block's own number, so none is ever cleared).
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const u32x4 v = sv[buf * L::N + 256 * i + tid];
+          T e[L::GE];
+          __builtin_memcpy(e, &v, 16);
+#pragma unroll
+          for (int j = 0; j < L::GE; ++j) odd = odd || !__builtin_isfinite((float)e[j]);
+        }
+        if (__any(odd) && lane == 0) flag[buf] = block + 1;
+        lds_barrier();
+        odd = flag[buf] == block + 1;
+      }
+    }
     // (a wave whose rows see none of the block has nothing to do)
     if (block * KB <= top_pos && !(a.window && block * KB + KB - 1 < low_pos - a.window + 1)) {
       f32x16 s[NK];
@@ -599,8 +692,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_run_k
         // scores in a row are then those of 8 keys in a row
         const int key = 32 * i + ((r & 19) | ((r & 4) << 1) | ((r & 8) >> 1));
 #pragma unroll
-        for (int j = 0; j < NS; ++j)
-          s[i] = mma32(*reinterpret_cast<const F*>(&sk[buf][(key * NC + ((2 * j + h) ^ (key & KX))) * 8]), q[j], s[i]);
+        for (int j = 0; j < NS; ++j) s[i] = mma32(k_frag(buf, key, 2 * j + h), q[j], s[i]);
       }
       if constexpr (I8) {
 #pragma unroll
@@ -609,7 +701,6 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_run_k
           for (int j = 0; j < 16; ++j) s[i][j] *= sks[buf][32 * i + 16 * (j >> 3) + 8 * h + (j & 7)];
       }
       if (edge) {
-        const unsigned long long there = __ballot(pages >= 0);
 #pragma unroll
         for (int i = 0; i < NK; ++i)
 #pragma unroll
@@ -652,36 +743,27 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_run_k
             s[i][j] = edge && s[i][j] == 0.f ? 0.f : w;  // (the scale of a place that is not seen may be NaN)
           }
       }
+      F w[KB / 16];
+#pragma unroll
+      for (int kk = 0; kk < KB / 16; ++kk)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[kk][j] = (T)s[kk >> 1][8 * (kk & 1) + j];
       if (I8 || !odd) {
-#pragma unroll
-        for (int kk = 0; kk < KB / 16; ++kk) {
-          F w;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = (T)s[kk >> 1][8 * (kk & 1) + j];
-#pragma unroll
-          for (int i = 0; i < ND; ++i) {
-            const int d = 32 * i + r;
-            o[i] = mma32(*reinterpret_cast<const F*>(&sv[buf][(d * VC + ((2 * kk + h) ^ (d & VX))) * 8]), w, o[i]);
-          }
-        }
-      } else {
-        // A value that is not finite lies in a block that not every row sees whole
-        // (0 times it would be NaN): the finite ones as ever, and the weights that
-        // the others have, whose signs say what becomes of the sums.
-        F w[KB / 16];
 #pragma unroll
         for (int kk = 0; kk < KB / 16; ++kk)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) w[kk][j] = (T)s[kk >> 1][8 * (kk & 1) + j];
+          for (int i = 0; i < ND; ++i) o[i] = mma32(v_frag(buf, kk, 32 * i + r), w[kk], o[i]);
+      } else {
+        // the finite values as ever, and the weights that the others have, whose
+        // signs say what becomes of the sums
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
-          const int d = 32 * i + r;
           f32x16 up, down;
 #pragma unroll
           for (int j = 0; j < 16; ++j) up[j] = down[j] = 0.f;
 #pragma unroll
           for (int kk = 0; kk < KB / 16; ++kk) {
-            const F v = *reinterpret_cast<const F*>(&sv[buf][(d * VC + ((2 * kk + h) ^ (d & VX))) * 8]);
+            const F v = v_frag(buf, kk, 32 * i + r);
             F fine, plus, minus;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -700,42 +782,43 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_run_k
         }
       }
     }
-    edge = edge_of(block + 1, pages1);
-    pages = pages1, pages1 = pages2;
-    if (more) store(buf ^ 1, block + 1, edge);
-    __syncthreads();
+    if (more) store(buf ^ 1);
+    wait_vmcnt<0>();
+    pages = pages1, pages1 = pages_of(block + 2, entry2);
+    dma_barrier();
   }
   l = sum_x32(l);
+  __syncthreads();
 
   if (gridDim.z > 1) {
     // parts: left in the lanes' order, joined by the tile's last workgroup in the parts' order
-    const int64_t slot = (int64_t)blockIdx.x * gridDim.z;
-    f32x4* wo = reinterpret_cast<f32x4*>(a.ws_o) + slot * (kRunRows * DP / 4) + tid;
-    float* wm = a.ws_m + slot * (2 * 256) + tid;
-    {
-      f32x4* w0 = wo + blockIdx.z * (kRunRows * DP / 4);
+    const int parts = gridDim.z, slot = blockIdx.x * parts;
+    const Shared wo(a.ws_o), wm(a.ws_m);
+    auto o_at = [&](int z, int i) { return ((slot + z) * (4 * ND) + i) * 1024 + 4 * tid; };
+    auto m_at = [&](int z) { return (slot + z) * 512 + tid; };
 #pragma unroll
-      for (int i = 0; i < ND; ++i)
+    for (int i = 0; i < ND; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w0[(4 * i + j) * 256] = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
-      wm[blockIdx.z * 512] = m, wm[blockIdx.z * 512 + 256] = l;
-    }
-    if (!last_of(a.count + blockIdx.x, gridDim.z, &flag[0])) return;
+      for (int j = 0; j < 4; ++j)
+        wo.put4(o_at(blockIdx.z, 4 * i + j), f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
+    wm.put(m_at(blockIdx.z), m), wm.put(m_at(blockIdx.z) + 256, l);
+    if (!last_of(a.count + blockIdx.x, parts, &flag[0])) return;
     m = kNone;
-    for (int z = 0; z < (int)gridDim.z; ++z) m = fmaxf(m, wm[z * 512]);
+#pragma unroll 4
+    for (int z = 0; z < parts; ++z) m = fmaxf(m, wm.get(m_at(z)));
     l = 0.f;
 #pragma unroll
     for (int i = 0; i < ND; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-    for (int z = 0; z < (int)gridDim.z; ++z) {
-      const float f = __builtin_amdgcn_exp2f(wm[z * 512] - some(m));
-      l += f * wm[z * 512 + 256];
+    for (int z = 0; z < parts; ++z) {
+      const float f = __builtin_amdgcn_exp2f(wm.get(m_at(z)) - some(m));
+      l += f * wm.get(m_at(z) + 256);
 #pragma unroll
       for (int i = 0; i < ND; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const f32x4 v = wo[z * (kRunRows * DP / 4) + (4 * i + j) * 256];
+          const f32x4 v = wo.get4(o_at(z, 4 * i + j));
 #pragma unroll
           for (int x = 0; x < 4; ++x) o[i][4 * j + x] += f * v[x];
         }
@@ -743,7 +826,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attn_run_k
   }
   if (mine >= rows) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* y = static_cast<T*>(a.y) + (row0 + token) * a.ys + (int64_t)qh * D;
+  T* y = static_cast<T*>(a.y) + (int64_t)(row0 + token) * a.ys + (int64_t)qh * D;
 #pragma unroll
   for (int i = 0; i < ND; ++i)
 #pragma unroll
@@ -773,6 +856,7 @@ static void launch_run(AttnArgs& a, hipStream_t st) {
   const CacheArgs& c = a.c;
   constexpr int KB = run_keys<T>();
   const int64_t wgs = attn_run_tiles(a) * c.kv_heads, blocks = (((int64_t)c.width << c.shift) + KB - 1) / KB;
+  a.each = make_fastdiv(a.heads / c.kv_heads);
   int64_t parts = 1;
   if (2 * wgs <= kRunParts) parts = std::max<int64_t>(1, std::min<int64_t>((kRunParts + wgs - 1) / wgs, blocks / 4));
   SN_LAUNCH((attn_run_kernel<T, I8, DP, EXACT>), dim3((unsigned)wgs, 1, (unsigned)parts), dim3(256), 0, st, a);

@@ -74,6 +74,7 @@ struct AttnArgs {
   float scale2;   // |scale| log2(e)
   bool negative;  // scale < 0
   int units;      // parts that a step's keys are cut into
+  FastDiv each;   // by the query heads of a key head
 };
 int64_t attn_run_tiles(const AttnArgs& a);  // bound of a prompt call's tiles of rows, per key head
 void attn_workspace(const AttnArgs& a, int64_t& o, int64_t& m, int64_t& counts);

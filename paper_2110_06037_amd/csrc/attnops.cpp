@@ -148,7 +148,8 @@ int sn_headnorm_create(const sn_headnorm_desc* desc, const float* q_w, const flo
     a.pairs = d.pairs, a.norm = d.norm, a.eps = d.eps;
     if (device >= 0) {
       OnDevice on(device);
-      a.q_w = op->upload(q_w, d.head_dim), a.k_w = op->upload(k_w, d.head_dim);
+      const std::vector<float> ones(d.head_dim, 1.f);
+      a.q_w = op->upload(q_w ? q_w : ones.data(), d.head_dim), a.k_w = op->upload(k_w ? k_w : ones.data(), d.head_dim);
       a.turn = op->upload(turn.data(), turn.size());
     }
     *out = op.release();

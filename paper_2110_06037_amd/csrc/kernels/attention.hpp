@@ -441,8 +441,6 @@ constexpr int run_keys() {
   return sizeof(T) == 2 ? 64 : 32;
 }
 
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
 // LDS direct load: 16 bytes a lane from `bytes` at `from` (beyond them: zeros) to 1024 at
 // `to`.  (The compiler's own form makes every later read of the array wait for it; here the
 // kernel waits itself, once a block.)
@@ -453,30 +451,19 @@ __device__ __forceinline__ void lds_load(const void* from, unsigned bytes, unsig
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(rsrc), "s"(at) : "memory");
 }
 
-// The sequence and its tile of rows behind a number: tiles are counted over the sequences in order.
-__device__ __forceinline__ bool run_tile(const CacheArgs& c, int each, int tile, int& b, int& t, int& first, int& n) {
-  const int lane = threadIdx.x & 63;
-  int64_t before = 0;
-  for (int base = 0; base < c.seqs; base += 64) {
-    int64_t lo = 0, hi = 0;
-    if (base + lane < c.seqs) seq_rows(c, base + lane, lo, hi);
-    const int64_t own = ((hi - lo) * each + kRunRows - 1) / kRunRows;
-    int64_t sum = own;
+// The schedule of N products whose first operands come from LDS: reads go AHEAD of the
+// products (16-bit types; the compiler's own order waits for nearly every read).
+template <typename T, int N, int AHEAD>
+__device__ __forceinline__ void reads_ahead() {
+  if constexpr (sizeof(T) == 2) {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);  // reads of LDS
 #pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const int64_t up = __shfl_up(sum, i);
-      if (lane >= i) sum += up;
+    for (int i = 0; i < N - AHEAD; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // products
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
-    const unsigned long long at = __ballot(tile < before + sum);
-    if (at) {
-      const int l = __ffsll(at) - 1;
-      b = uniform(base + l), t = uniform(tile - (int)__shfl(before + sum - own, l));
-      first = uniform((int)__shfl(lo, l)), n = uniform((int)__shfl(hi - lo, l));
-      return true;
-    }
-    before += __shfl(sum, 63);
+    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
   }
-  return false;
 }
 
 // K and V of a block in LDS, in granules of 16 bytes: K [key][element], V as the
@@ -493,7 +480,7 @@ struct RunTile {
 };
 
 template <typename T, bool I8, int DP, bool EXACT>
-__global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 2)) ? 2 : 1) void attn_run_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnArgs a) {
   typedef typename std::conditional<I8, int8_t, T>::type E;
   typedef typename Frag<T>::type F;
   typedef RunTile<T, DP> L;
@@ -504,6 +491,7 @@ __global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 
   constexpr float LIFT = std::is_same<T, f16>::value ? 6.f : 0.f, kLazy = 8.f;
   __shared__ u32x4 sk[2 * L::N], sv[2 * L::N];
   __shared__ __attribute__((aligned(16))) float sks[2][I8 ? KB : 4], svs[2][I8 ? KB : 4];
+  __shared__ __attribute__((aligned(16))) unsigned marks[I8 ? 4 : DP * 4];  // of an element: 64 keys' bits, +inf or NaN; -inf or NaN
   __shared__ int flag[2];
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
@@ -512,7 +500,7 @@ __global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 
   // their number.  The last tiles, which see the most keys, first.
   const int head = blockIdx.x % c.kv_heads, tiles = gridDim.x / c.kv_heads, tile = tiles - 1 - blockIdx.x / c.kv_heads;
   int b, t, row0, n;
-  if (!run_tile(c, each, tile, b, t, row0, n)) return;
+  if (!find_rows(c, tile, [&](int, int rows) { return ((int64_t)rows * each + kRunRows - 1) / kRunRows; }, b, t, row0, n)) return;
   const int past = uniform(min(c.past[b], kMaxPast));
   const int rows = n * each, mine = t * kRunRows + 32 * wave + r;  // (below 2^31: the launcher's tiles)
   const int rr = min(mine, rows - 1);  // rows behind the last one repeat it and are not stored
@@ -552,6 +540,7 @@ __global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 
     const int page = max(0, __builtin_amdgcn_readlane(pages, t16));
     return (((int64_t)page * c.kv_heads + head) << c.shift) + ((block * KB + 16 * t16) & mask);
   };
+  const unsigned row_bytes = D * sizeof(E), page_bytes = (unsigned)(c.kv_heads << c.shift) * row_bytes, head_bytes = (head << c.shift) * row_bytes;
 
   // Caches in T: LDS direct loads.  A wave's i-th load fills the 64 granules from
   // 256 i + 64 wave on; all lie in one 16 positions.  This lane's granule is at an
@@ -571,17 +560,20 @@ __global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 
   float ksr = 0.f, vsr = 0.f, vpw[POWER ? NL : 1][8];
   auto load = [&](int block, int pages, int buf) {
     if constexpr (!I8) {
+      int64_t at[KB / 16];
+#pragma unroll
+      for (int i = 0; i < KB / 16; ++i)
+        at[i] = (int64_t)((uint64_t)(unsigned)max(0, __builtin_amdgcn_readlane(pages, i)) * page_bytes) + head_bytes +
+                ((block * KB + 16 * i) & mask) * row_bytes;
+      // (a wave's share lies in tile i / PER + const of its own)
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         const int x = 256 * i + 64 * wave;
-        const int64_t at = rows_at(block, pages, x / L::KG / 16);
-        lds_load(static_cast<const E*>(c.k) + at * D, 16 * D * sizeof(T), koff[i], &sk[buf * L::N + x]);
-      }
-#pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const int x = 256 * i + 64 * wave;
-        const int64_t at = rows_at(block, pages, x / (L::VG * DP));
-        lds_load(static_cast<const E*>(c.v) + at * D, 16 * D * sizeof(T), voff[i], &sv[buf * L::N + x]);
+        int64_t o = at[256 * i / (16 * L::KG)];
+        if constexpr (16 * L::KG < 256)
+          if (wave >= L::KG / 4) o = at[256 * i / (16 * L::KG) + 1];
+        lds_load(static_cast<const char*>(c.k) + o, 16 * row_bytes, koff[i], &sk[buf * L::N + x]);
+        lds_load(static_cast<const char*>(c.v) + o, 16 * row_bytes, voff[i], &sv[buf * L::N + x]);
       }
     } else {
 #pragma unroll
@@ -648,6 +640,7 @@ __global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 
   float m = kNone, l = 0.f;
   int pages = -1, pages1 = -1;
   if (tid < 2) flag[tid] = 0;
+  bool odd = !I8;  // (at first: marks are cleared by the first block that looks at them)
   if (first < end) {
     const int entry = table[entry_of(first)], entry1 = table[entry_of(first + 1)];
     pages = pages_of(first, entry), pages1 = pages_of(first + 1, entry1);
@@ -663,20 +656,34 @@ __global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 
     // whether some row of the workgroup does not see some key of the block
     const unsigned long long there = __ballot(pages >= 0);
     const bool edge = block * KB + KB - 1 > pos0 || (a.window && block * KB < pos1 - a.window + 1) || __builtin_popcountll(there) < KB / 16;
-    bool odd = false;
     if constexpr (!I8) {
-      // What such a row does not see takes no part in it, whatever it is: 0 times a
-      // value that is not finite would (a flag holds a block's own number, so none is ever cleared).
+      // What a row does not see takes no part in it, whatever it is, but 0 times a value
+      // that is not finite would.  Such values become zeros in LDS, with a bit that
+      // says where they were; what they do to the rows that see them follows the product.
       if (edge) {
-#pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          const u32x4 v = sv[buf * L::N + 256 * i + tid];
-          T e[L::GE];
-          __builtin_memcpy(e, &v, 16);
-#pragma unroll
-          for (int j = 0; j < L::GE; ++j) odd = odd || !__builtin_isfinite((float)e[j]);
+        if (odd) {  // the last block's bits
+          for (int i = tid; i < DP * 4; i += 256) marks[i] = 0;
+          lds_barrier();
         }
-        if (__any(odd) && lane == 0) flag[buf] = block + 1;
+        odd = false;
+#pragma unroll 1
+        for (int i = 0; i < NG; ++i) {
+          const int x = 256 * i + tid, d = x / L::VG % DP, key = x / (L::VG * DP) * 16 + (x % L::VG ^ L::v_order(d)) * L::GE;
+          T e[L::GE];
+          __builtin_memcpy(e, &sv[buf * L::N + x], 16);
+          bool bad = false;
+#pragma unroll
+          for (int j = 0; j < L::GE; ++j) {
+            const float v = (float)e[j];
+            if (__builtin_isfinite(v)) continue;
+            if (!(v < 0.f)) atomicOr(&marks[4 * d + (key >> 5)], 1u << ((key & 31) + j));
+            if (!(v > 0.f)) atomicOr(&marks[4 * d + 2 + (key >> 5)], 1u << ((key & 31) + j));
+            e[j] = (T)0.f, bad = true;
+          }
+          if (bad) __builtin_memcpy(&sv[buf * L::N + x], e, 16);
+          odd = odd || bad;
+        }
+        if (__any(odd) && lane == 0) flag[buf] = block + 1;  // (a block's own number: never cleared)
         lds_barrier();
         odd = flag[buf] == block + 1;
       }
@@ -694,6 +701,7 @@ __global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 
 #pragma unroll
         for (int j = 0; j < NS; ++j) s[i] = mma32(k_frag(buf, key, 2 * j + h), q[j], s[i]);
       }
+      reads_ahead<T, NK * NS, 6>();
       if constexpr (I8) {
 #pragma unroll
         for (int i = 0; i < NK; ++i)
@@ -748,38 +756,29 @@ __global__ __launch_bounds__(256, DP == 64 || (DP == 128 && (I8 || sizeof(T) == 
       for (int kk = 0; kk < KB / 16; ++kk)
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[kk][j] = (T)s[kk >> 1][8 * (kk & 1) + j];
-      if (I8 || !odd) {
 #pragma unroll
-        for (int kk = 0; kk < KB / 16; ++kk)
+      for (int kk = 0; kk < KB / 16; ++kk)
 #pragma unroll
-          for (int i = 0; i < ND; ++i) o[i] = mma32(v_frag(buf, kk, 32 * i + r), w[kk], o[i]);
-      } else {
-        // the finite values as ever, and the weights that the others have, whose
-        // signs say what becomes of the sums
+        for (int i = 0; i < ND; ++i) o[i] = mma32(v_frag(buf, kk, 32 * i + r), w[kk], o[i]);
+      reads_ahead<T, KB / 16 * ND, 4>();
+      if (!I8 && edge && odd) {
+        // this row's keys of any weight, against each element's marked ones
+        unsigned seen[2] = {0u, 0u};
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-          f32x16 up, down;
+        for (int i = 0; i < NK; ++i) {
+          unsigned own = 0;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) up[j] = down[j] = 0.f;
+          for (int j = 0; j < 16; ++j) own |= s[i][j] > 0.f || s[i][j] != s[i][j] ? 1u << (16 * (j >> 3) + 8 * h + (j & 7)) : 0u;
+          seen[i] = own | __shfl_xor(own, 32);
+        }
 #pragma unroll
-          for (int kk = 0; kk < KB / 16; ++kk) {
-            const F v = v_frag(buf, kk, 32 * i + r);
-            F fine, plus, minus;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float x = (float)v[j];
-              fine[j] = __builtin_isfinite(x) ? v[j] : (T)0.f;
-              plus[j] = __builtin_isfinite(x) || x < 0.f ? (T)0.f : (T)1.f;
-              minus[j] = __builtin_isfinite(x) || x > 0.f ? (T)0.f : (T)1.f;
-            }
-            o[i] = mma32(fine, w[kk], o[i]), up = mma32(plus, w[kk], up), down = mma32(minus, w[kk], down);
-          }
+        for (int i = 0; i < ND; ++i)
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            if (up[j] > 0.f) o[i][j] += __builtin_huge_valf();
-            if (down[j] > 0.f) o[i][j] -= __builtin_huge_valf();
+            const u32x4 at = *reinterpret_cast<const u32x4*>(&marks[4 * (32 * i + 8 * (j >> 2) + 4 * h + (j & 3))]);
+            if ((at[0] & seen[0]) | (at[1] & seen[1])) o[i][j] += __builtin_huge_valf();
+            if ((at[2] & seen[0]) | (at[3] & seen[1])) o[i][j] -= __builtin_huge_valf();
           }
-        }
       }
     }
     if (more) store(buf ^ 1);

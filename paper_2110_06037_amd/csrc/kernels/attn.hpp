@@ -12,7 +12,7 @@ namespace k {
 struct HeadNormArgs {
   int dtype, heads, kv_heads, dim, rot, pairs, norm;
   float eps;
-  const float *q_w, *k_w;        // [dim] or null (ones)
+  const float *q_w, *k_w;          // [dim]
   const unsigned long long* turn;  // [rot / 2] turns per position, the fraction times 2^64
   int64_t tokens;
   const int32_t* positions;
@@ -24,6 +24,9 @@ struct HeadNormArgs {
   int64_t qos;
   void* ko;
   int64_t kos;
+  // set by the launcher
+  FastDiv all;               // by the heads of a token
+  int lanes, tokens_each;  // threads of a row, tokens of a workgroup
 };
 void head_norm(const HeadNormArgs& a, hipStream_t st);
 
@@ -53,6 +56,7 @@ struct CacheRows {
   int64_t krs;
   void* v;
   int64_t vrs;
+  int lanes;  // threads of a row (set by the launcher)
 };
 void cache_write(const CacheRows& a, hipStream_t st);
 void cache_read(const CacheRows& a, hipStream_t st);
@@ -105,6 +109,42 @@ __device__ __forceinline__ int seq_of(const CacheArgs& c, int64_t row) {
     else hi = mid;
   }
   return c.offsets[lo] <= row && row < c.offsets[lo + 1] ? lo : -1;
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// Units of work are counted over the sequences in order, count(b, rows) of each: the
+// sequence behind the number `unit`, the unit's number in it, and the sequence's rows.
+// (Every wave for itself, 64 sequences at a time.)  False: there are fewer units.
+template <typename F>
+__device__ __forceinline__ bool find_rows(const CacheArgs& c, int64_t unit, F count, int& b, int& at, int& first, int& rows) {
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int base = 0; base < c.seqs; base += 64) {
+    int64_t lo = 0, hi = 0, own = 0;
+    if (base + lane < c.seqs) {
+      seq_rows(c, base + lane, lo, hi);
+      own = count(base + lane, (int)(hi - lo));
+    }
+    int64_t sum = own;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+      const int64_t up = __shfl_up(sum, i);
+      if (lane >= i) sum += up;
+    }
+    const unsigned long long in = __ballot(unit < before + sum);
+    if (in) {
+      const int l = __ffsll(in) - 1;
+      b = uniform(base + l), at = uniform((int)(unit - __shfl(before + sum - own, l)));
+      first = uniform((int)__shfl(lo, l)), rows = uniform((int)__shfl(hi - lo, l));
+      return true;
+    }
+    before += __shfl(sum, 63);
+  }
+  return false;
+}
+// How many groups of 16 positions `rows` rows after `past` lie in.
+__device__ __forceinline__ int rows_tiles(int past, int rows) {
+  const int p = min(max(past, 0), kMaxPast) & 15;
+  return rows ? (p + rows + 15) >> 4 : 0;
 }
 // The page that holds a position of sequence b, -1 if none does.
 __device__ __forceinline__ int page_of(const CacheArgs& c, int b, int pos) {

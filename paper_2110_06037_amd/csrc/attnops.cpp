@@ -100,6 +100,7 @@ int attn_call(sn_op* p, const sn_cache_io* io, const void* q, int64_t q_stride, 
     a.qs = check_rows(q, q_stride, a.c.tokens, n, a.c.dtype, "q");
     a.ys = check_rows(y, y_stride, a.c.tokens, n, a.c.dtype, "y");
     if (!step && k::attn_run_tiles(a) * a.c.kv_heads >> 24) fail(SN_E_UNSUPPORTED, "tokens * heads above 2^31 - 128 * seqs * kv_heads");
+    if (step && !k::step_keys_fit(a.c)) fail(SN_E_UNSUPPORTED, "seqs * width * page of a step above 2^36 - 2^6 seqs");
     need_device(op);
     if (!a.c.tokens) return;
     const int e = dtype_size(a.c.dtype);

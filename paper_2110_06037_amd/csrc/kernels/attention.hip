@@ -4,6 +4,8 @@
 namespace sn {
 namespace k {
 
+bool step_keys_fit(const CacheArgs& c) { return c.seqs * ((((int64_t)c.width << c.shift) >> 5) + 2) < (int64_t(1) << 31); }
+
 int64_t attn_run_tiles(const AttnArgs& a) {
   const int each = a.heads / a.c.kv_heads;
   return a.c.tokens * each / kRunRows + a.c.seqs;
@@ -13,9 +15,8 @@ int64_t attn_run_tiles(const AttnArgs& a) {
 void attn_workspace(const AttnArgs& a, int64_t& o, int64_t& m, int64_t& counts) {
   const int64_t DP = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
   const int64_t groups = (int64_t)a.c.kv_heads * ((a.heads / a.c.kv_heads + 15) / 16);
-  const int64_t units = std::min<int64_t>(kStepUnits, (kStepTarget + groups - 1) / groups);
-  // step: a sequence of several parts has a slot for each, at most 2 * units of them per group of
-  // heads; run: at most kRunParts + kRunParts / 2 parts of tiles, which number kRunParts / 2 at most
+  const int64_t units = step_units(a, 512);
+  // step: two slots a workgroup; run: at most kRunParts + kRunParts / 2 parts of tiles, which number kRunParts / 2 at most
   const int64_t step = units > 1 ? 2 * units * groups : 0, run = kRunParts + kRunParts / 2;
   o = std::max(step * 16 * DP, run * kRunRows * DP);
   m = std::max(step * 32, run * 512);
@@ -44,7 +45,7 @@ void attn_run(AttnArgs a, hipStream_t st) {
   attention(a, false, st);
 }
 void attn_step(AttnArgs a, hipStream_t st) {
-  check(a.c.tokens == a.c.seqs && !a.c.offsets, "attention step");
+  check(a.c.tokens == a.c.seqs && !a.c.offsets && step_keys_fit(a.c), "attention step");
   attention(a, true, st);
 }
 

@@ -133,65 +133,76 @@ __device__ __forceinline__ bool last_of(unsigned* count, unsigned n, int* shared
 
 // ------------------------------------------------------------------ single tokens
 constexpr int kStepWaves = 4;
-constexpr int kStepTarget = 512;  // workgroups that the keys of all sequences are spread over
-constexpr int kStepLeast = 4;     // blocks of keys that a workgroup takes at least, one a wave
-constexpr int kStepUnits = 1024;  // bound of the parts per head group (slots: twice as many)
+constexpr int kStepLeast = 4;     // blocks of keys of a workgroup where there are workgroups enough: one a wave
+constexpr int kStepUnits = 1024;  // bound of the workgroups per group of heads
+// Workgroups that the keys of all sequences are spread over: one a compute unit, two
+// where codes are turned into numbers.  (64 sequences of up to 8192 keys, 8 key heads of
+// 128, in bf16 198 us with 256 and 204 with 512, in 8 bits 128 and 120; one of
+// 32768 keys in bf16 29 and 33.5: fewer parts to join.)
+// Two also where the tables say that each sequence can have some of its own (64 of 128 keys 9
+// us, by parts of two sequences 11); more that end at once would put the others
+// two on some units and none on others (64 of 2048 keys: 127 us, without them 101).
+inline int step_units(const AttnArgs& a, int target) {
+  const int64_t groups = (int64_t)a.c.kv_heads * ((a.heads / a.c.kv_heads + 15) / 16);
+  return (int)std::min<int64_t>(kStepUnits, (target + groups - 1) / groups);
+}
 template <typename T, bool I8, int DP>
 constexpr int step_keys() {  // keys of a block that each quarter of a wave holds: K and V take up to 64 registers each
   return I8 || DP * sizeof(T) <= 256 ? 16 : 8;
 }
 
-// What one sequence has of keys in blocks of KB: none if there are none.
+// What one sequence has of keys in blocks of KB; one block, of which nothing is seen, at least.
 struct Span {
   int from, last;  // positions
   int block, blocks;
 };
-__device__ __forceinline__ Span step_span(const AttnArgs& a, int b, int KB) {
-  const int past = a.c.past[b];
+__device__ __forceinline__ Span step_span(const AttnArgs& a, int past, int KB) {
   Span s;
   s.from = a.window ? max(0, past - a.window + 1) : 0;
   s.last = min(past, (a.c.width << a.c.shift) - 1);
   s.block = s.from / KB;
-  s.blocks = s.last < s.from ? 0 : s.last / KB - s.block + 1;
+  s.blocks = s.last < s.from ? 1 : s.last / KB - s.block + 1;
   return s;
 }
 
-// Which keys this workgroup takes.  The sequences' blocks, all together, are cut
-// into parts of `per` blocks, about `units` of them, so that a batch of very
-// different lengths is spread evenly with no length known to the host; every wave
-// finds its workgroup's part by itself, 64 sequences at a time.
+// Which keys this workgroup takes.  The blocks of all sequences stand in one row, which is
+// cut into equal parts, so that a batch of very different lengths is spread evenly with no
+// length known to the host; a part may begin and end inside sequences and hold
+// several.  Where there are workgroups enough, each sequence begins a part of its own.
+// Every wave finds its workgroup's part by itself, 64 sequences at a time.
 struct Part {
-  int b, part, parts, slot, per;  // slot: this sequence's first place in the workspace
-  Span s;
+  int per, begin, end;  // blocks of a part; this one's
+  int pad;              // a sequence counts as a multiple of pad + 1 blocks
+  int b, start;         // the sequence that it begins in, and where that begins
 };
 __device__ __forceinline__ bool step_part(const AttnArgs& a, int KB, int unit, Part& p) {
   const int lane = threadIdx.x & 63, seqs = a.c.seqs;
-  int64_t total = 0;
-  for (int base = 0; base < seqs; base += 64)
-    if (base + lane < seqs) total += step_span(a, base + lane, KB).blocks;
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) total += __shfl_xor(total, i);
-  const int per = (int)min<int64_t>(max<int64_t>((total + a.units - 1) / a.units, kStepLeast), 1 << 30);
-  int before = 0;  // parts, and slots times 2^19, of the sequences before
+  int total = 0, padded = 0, own = 0;
   for (int base = 0; base < seqs; base += 64) {
-    const int b = base + lane;
-    const int n = b < seqs ? max(1, (step_span(a, b, KB).blocks + per - 1) / per) : 0;
-    int sum = n + (n > 1 ? n << 19 : 0);
-    const int own = sum;
+    own = base + lane < seqs ? step_span(a, a.c.past[base + lane], KB).blocks : 0;
+    total += own, padded += (own + kStepLeast - 1) & -kStepLeast;
+  }
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) total += __shfl_xor(total, i), padded += __shfl_xor(padded, i);
+  total = uniform(total), padded = uniform(padded);
+  p.pad = 0, p.per = (total + a.units - 1) / a.units;
+  if (padded <= kStepLeast * a.units) p.pad = kStepLeast - 1, p.per = kStepLeast, total = padded;
+  p.begin = unit * p.per, p.end = min(p.begin + p.per, total);
+  if (p.begin >= total) return false;
+  int before = 0;
+  for (int base = 0; base < seqs; base += 64) {
+    if (seqs > 64) own = base + lane < seqs ? step_span(a, a.c.past[base + lane], KB).blocks : 0;
+    const int n = (own + p.pad) & ~p.pad;
+    int sum = n;
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) {
       const int up = __shfl_up(sum, i);
       if (lane >= i) sum += up;
     }
-    const unsigned long long at = __ballot(unit < ((before + sum) & 0x7ffff));
+    const unsigned long long at = __ballot(p.begin < before + sum);
     if (at) {
       const int l = __ffsll(at) - 1;
-      p.b = base + l, p.parts = __shfl(n, l), p.per = per;
-      const int first = __shfl(before + sum - own, l);
-      p.part = unit - (first & 0x7ffff), p.slot = first >> 19;
-      p.b = __builtin_amdgcn_readfirstlane(p.b), p.parts = __builtin_amdgcn_readfirstlane(p.parts);
-      p.part = __builtin_amdgcn_readfirstlane(p.part), p.slot = __builtin_amdgcn_readfirstlane(p.slot);
-      p.s = step_span(a, p.b, KB);
+      p.b = uniform(base + l), p.start = uniform(__shfl(before + sum - n, l));
       return true;
     }
     before += __shfl(sum, 63);
@@ -218,27 +229,14 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
   const int D = EXACT ? DP : c.dim, head = blockIdx.y, each = a.heads / c.kv_heads;
   const int cols = min(16, each - (int)blockIdx.z * 16), qh = head * each + blockIdx.z * 16;
+  const int unit = blockIdx.x;
   Part p;
-  if (!step_part(a, KB, blockIdx.x, p)) return;
-  const int b = p.b;
-  const int first = p.s.block + p.part * p.per, end = min(first + p.per, p.s.block + p.s.blocks);
+  if (!step_part(a, KB, unit, p)) return;
 
   // this lane's keys: of K's rows 4 t + ..., of V 8 u + ...
   const int ko = KPG * (col >> 2), vo = KPG * g;
   const int kslot = (ko & 15) + (col & 3), vslot = vo & 15;
   const int mask = (1 << c.shift) - 1;
-  auto page_at = [&](int block, int off) { return block < end ? page_of(c, b, block * KB + off) : -1; };
-
-  FT q[NS];
-#pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const int d = 64 * (s >> 1) + 16 * g + 8 * (s & 1);
-    V8<T> v = zero8<T>();
-    if (col < cols && (EXACT || d < D)) v = load8(static_cast<const T*>(a.q) + b * a.qs + (int64_t)(qh + col) * D + d);
-    q[s] = frag_of<T>(v);
-    if (a.negative) q[s] = -q[s];
-  }
-
   V8<E> kr[NT][NS], vr[ND][NU];
   float ks[I8 ? KPG : 1], vs[I8 ? KPG : 1];
   auto load_k = [&](int block, int page) {
@@ -268,6 +266,22 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
     }
   };
 
+  // the sequences, or parts of them, that this workgroup's blocks belong to
+  for (;;) {
+  const int b = p.b;
+  const Span span = step_span(a, uniform(c.past[b]), KB);
+  const int first = span.block + max(p.begin - p.start, 0), end = span.block + min(p.end - p.start, span.blocks);
+  auto page_at = [&](int block, int off) { return block < end ? page_of(c, b, block * KB + off) : -1; };
+  FT q[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const int d = 64 * (s >> 1) + 16 * g + 8 * (s & 1);
+    V8<T> v = zero8<T>();
+    if (col < cols && (EXACT || d < D)) v = load8(static_cast<const T*>(a.q) + b * a.qs + (int64_t)(qh + col) * D + d);
+    q[s] = frag_of<T>(v);
+    if (a.negative) q[s] = -q[s];
+  }
+
   f32x4 o[ND];
 #pragma unroll
   for (int n = 0; n < ND; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -293,7 +307,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
     if (more) load_k(block + kStepWaves, kp1);
     const int base = block * KB + vo;
     const bool there = vp >= 0;
-    const bool full = block * KB >= p.s.from && block * KB + KB - 1 <= p.s.last && __all(there);
+    const bool full = block * KB >= span.from && block * KB + KB - 1 <= span.last && __all(there);
     float v[NT][4], top = kNone;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -305,7 +319,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int pos = base + 4 * t + i;
-          if (!there || pos < p.s.from || pos > p.s.last) v[t][i] = kNone;
+          if (!there || pos < span.from || pos > span.last) v[t][i] = kNone;
         }
     }
 #pragma unroll
@@ -335,7 +349,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int pos = base + 4 * t + i;
-          if (!there || pos < p.s.from || pos > p.s.last) {
+          if (!there || pos < span.from || pos > span.last) {
             v[t][i] = 0.f;
             if constexpr (!I8) {
 #pragma unroll
@@ -367,18 +381,30 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
   l = sum_x32(sum_x16(l));
 
   // the waves' results, together
+  if (p.start > p.begin) __syncthreads();  // (the last sequence's are read)
   if (g == 0) sm[wave][col] = m, sl[wave][col] = l;
   if (col < cols)
 #pragma unroll
     for (int n = 0; n < ND; ++n) *reinterpret_cast<f32x4*>(&so[wave][col][16 * n + 4 * g]) = o[n];
   __syncthreads();
-  const int64_t slots = (int64_t)c.kv_heads * gridDim.z, at = (int64_t)head * gridDim.z + blockIdx.z;
-  const int chunks = D / 4;
+  // A sequence in several workgroups, unit0 .. unit1: each leaves its part in a slot, of
+  // which it has one for a sequence that began before it and one for a sequence that
+  // goes on behind it; the last one joins them, in their order.
+  const int unit0 = p.start / p.per, unit1 = (p.start + span.blocks - 1) / p.per;
+  const int slots = c.kv_heads * gridDim.z, at = head * gridDim.z + blockIdx.z;
   const Shared wo(a.ws_o), wm(a.ws_m);
-  auto o_at = [&](int part) { return (int)((p.slot + part) * slots + at) * (16 * DP); };
-  auto m_at = [&](int part) { return (int)((p.slot + part) * slots + at) * 32; };
+  auto slot = [&](int u) { return (u == unit0 ? 2 * u + 1 : 2 * u) * slots + at; };
+  constexpr int chunks = DP / 4;
+  auto finish = [&](int r, int d, f32x4 acc, float sum) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = from_f<T>(acc[j] * inv);
+    __builtin_memcpy(static_cast<T*>(a.y) + b * a.ys + (int64_t)(qh + r) * D + d, v, sizeof(v));
+  };
   for (int i = threadIdx.x; i < cols * chunks; i += 64 * kStepWaves) {
-    const int r = i / chunks, d = 4 * (i - r * chunks);
+    const int r = i / chunks, d = 4 * (i % chunks);
+    if (!EXACT && d >= D) continue;
     float top = kNone, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -389,39 +415,46 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
       sum += f * sl[w][r];
       acc += f * *reinterpret_cast<const f32x4*>(&so[w][r][d]);
     }
-    if (p.parts == 1) {
-      T* y = static_cast<T*>(a.y) + b * a.ys + (int64_t)(qh + r) * D + d;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      T t[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) t[j] = from_f<T>(acc[j] * inv);
-      __builtin_memcpy(y, t, sizeof(t));
+    if (unit0 == unit1) {
+      finish(r, d, acc, sum);
     } else {
-      wo.put4(o_at(p.part) + r * DP + d, acc);
-      if (d == 0) wm.put(m_at(p.part) + r, top), wm.put(m_at(p.part) + 16 + r, sum);
+      wo.put4(slot(unit) * (16 * DP) + r * DP + d, acc);
+      if (d == 0) wm.put(slot(unit) * 32 + r, top), wm.put(slot(unit) * 32 + 16 + r, sum);
     }
   }
-  if (p.parts == 1) return;
-  if (!last_of(a.count + p.slot * slots + at, p.parts, &flag)) return;
-  // the last workgroup of a sequence joins its parts, in their order
-  for (int i = threadIdx.x; i < cols * chunks; i += 64 * kStepWaves) {
-    const int r = i / chunks, d = 4 * (i - r * chunks);
-    float top = kNone, sum = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int k = 0; k < p.parts; ++k) top = fmaxf(top, wm.get(m_at(k) + r));
-#pragma unroll 8
-    for (int k = 0; k < p.parts; ++k) {
-      const float f = __builtin_amdgcn_exp2f(wm.get(m_at(k) + r) - some(top));
-      sum += f * wm.get(m_at(k) + 16 + r);
-      acc += f * wo.get4(o_at(k) + r * DP + d);
-    }
-    T* y = static_cast<T*>(a.y) + b * a.ys + (int64_t)(qh + r) * D + d;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    T t[4];
+  if (unit0 != unit1 && last_of(a.count + slot(unit0), unit1 - unit0 + 1, &flag)) {
+    for (int i = threadIdx.x; i < cols * chunks; i += 64 * kStepWaves) {
+      const int r = i / chunks, d = 4 * (i % chunks);
+      if (!EXACT && d >= D) continue;
+      float top = kNone, sum = 0.f;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      // eight parts at a time, all of their numbers in flight
+      for (int u = unit0; u <= unit1; u += 8) {
+        float ms[8], ls[8], now = top;
+        f32x4 os[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) t[j] = from_f<T>(acc[j] * inv);
-    __builtin_memcpy(y, t, sizeof(t));
+        for (int k = 0; k < 8; ++k) {
+          const int at = slot(min(u + k, unit1));
+          ms[k] = wm.get(at * 32 + r), ls[k] = wm.get(at * 32 + 16 + r), os[k] = wo.get4(at * (16 * DP) + r * DP + d);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (u + k > unit1) ms[k] = kNone;
+          now = fmaxf(now, ms[k]);
+        }
+        const float f = __builtin_amdgcn_exp2f(top - some(now));
+        sum *= f, acc *= f, top = now;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float w = __builtin_amdgcn_exp2f(ms[k] - some(now));
+          if (u + k <= unit1) sum += w * ls[k], acc += w * os[k];
+        }
+      }
+      finish(r, d, acc, sum);
+    }
+  }
+  p.start += (span.blocks + p.pad) & ~p.pad, ++p.b;
+  if (p.start >= p.end) return;
   }
 }
 
@@ -844,9 +877,11 @@ static void launch_step(AttnArgs& a, hipStream_t st) {
   const CacheArgs& c = a.c;
   constexpr int KB = 4 * step_keys<T, I8, DP>();
   const int each = a.heads / c.kv_heads, groups = (each + 15) / 16;
-  const int64_t most = ((int64_t)c.width << c.shift) / KB + 1;  // blocks of one sequence
-  a.units = (int)std::min<int64_t>(kStepUnits, (kStepTarget + (int64_t)c.kv_heads * groups - 1) / ((int64_t)c.kv_heads * groups));
-  const int64_t parts = std::min<int64_t>(a.units + (int64_t)c.seqs, c.seqs * ((most + kStepLeast - 1) / kStepLeast));
+  const int64_t most = (((int64_t)c.width << c.shift) + KB - 1) / KB + 1;  // blocks of one sequence
+  const int64_t own = c.seqs * ((most + kStepLeast - 1) / kStepLeast);     // parts, if each sequence has its own
+  a.units = step_units(a, 512);
+  if (!I8 && own > a.units) a.units = step_units(a, 256);
+  const int64_t parts = std::min<int64_t>(a.units, own);
   SN_LAUNCH((attn_step_kernel<T, I8, DP, EXACT>), dim3((unsigned)parts, c.kv_heads, groups), dim3(64 * kStepWaves), 0, st, a);
 }
 

@@ -56,7 +56,9 @@ struct CacheRows {
   int64_t krs;
   void* v;
   int64_t vrs;
-  int lanes;  // threads of a row (set by the launcher)
+  // set by the launcher
+  int lanes;              // threads of a row
+  FastDiv head_granules;  // by the 16 bytes that V has of a head's 16 positions
 };
 void cache_write(const CacheRows& a, hipStream_t st);
 void cache_read(const CacheRows& a, hipStream_t st);
@@ -77,10 +79,11 @@ struct AttnArgs {
   // set by the launchers
   float scale2;   // |scale| log2(e)
   bool negative;  // scale < 0
-  int units;      // parts that a step's keys are cut into
+  int units;      // parts that a step's keys are cut into at most
   FastDiv each;   // by the query heads of a key head
 };
 int64_t attn_run_tiles(const AttnArgs& a);  // bound of a prompt call's tiles of rows, per key head
+bool step_keys_fit(const CacheArgs& c);  // the keys of a step's sequences, in blocks of 32, are below 2^31
 void attn_workspace(const AttnArgs& a, int64_t& o, int64_t& m, int64_t& counts);
 void attn_run(AttnArgs a, hipStream_t st);
 void attn_step(AttnArgs a, hipStream_t st);

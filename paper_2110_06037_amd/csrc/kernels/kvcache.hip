@@ -40,183 +40,206 @@ __device__ __forceinline__ float max_lanes(float v, int lanes) {
   return v;
 }
 
-// A wave takes one token's row of one head, of K and of V.
+// Single rows: a wave takes one token's row of one head, of K or of V, lane l the
+// elements l, l + 64, ...; what it writes is read before the place is known.
 constexpr int kRowWaves = 4;
 template <typename T, bool I8, bool WRITE>
 __global__ __launch_bounds__(64 * kRowWaves) void cache_rows_kernel(CacheRows a) {
+  typedef typename std::conditional<I8, int8_t, T>::type E;
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & 63;
   const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRowWaves + (threadIdx.x >> 6);
-  if (unit >= c.tokens * c.kv_heads) return;
-  const int64_t row = unit / c.kv_heads;
-  const int head = (int)(unit - row * c.kv_heads), D = c.dim;
+  if (unit >= 2 * c.tokens * c.kv_heads) return;
+  const bool key = unit & 1;
+  const int64_t row = (unit >> 1) / c.kv_heads;
+  const int head = (int)((unit >> 1) - row * c.kv_heads), D = c.dim;
+  T* x = (key ? static_cast<T*>(a.k) + row * a.krs : static_cast<T*>(a.v) + row * a.vrs) + (int64_t)head * D;
+  T t[4];
+  if constexpr (WRITE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = x[min(lane + 64 * i, D - 1)];
+  }
   const int b = seq_of(c, row);
   if (b < 0) return;
   int64_t first, end;
   seq_rows(c, b, first, end);
   const int past = min(c.past[b], kMaxPast);
   const int pos = past < 0 ? -1 : past + (int)(row - first);
-  const int page = page_of(c, b, pos);
-  const int slot = pos & ((1 << c.shift) - 1);
+  const int page = page_of(c, b, pos), slot = pos & ((1 << c.shift) - 1);
+  if (WRITE && page < 0) return;
+  const int step = key ? 1 : kCacheTile;
+  E* q = static_cast<E*>(key ? c.k : c.v) + (page < 0 ? 0 : key ? k_at(c, page, head, slot) : v_at(c, page, head, slot));
+  float* scale = (key ? c.ks : c.vs) + (page < 0 || !I8 ? 0 : scale_at(c, page, head, slot));
+  if constexpr (WRITE) {
+    E e[4];
+    if constexpr (I8) {
+      float v[4], most = 0.f;
+      bool fine = true;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    T* x = which ? static_cast<T*>(a.v) + row * a.vrs : static_cast<T*>(a.k) + row * a.krs;
-    x += (int64_t)head * D;
-    const int64_t at = page < 0 ? 0 : which ? v_at(c, page, head, slot) : k_at(c, page, head, slot);
-    const int step = which ? kCacheTile : 1;
-    float* scale = which ? c.vs : c.ks;
-    if constexpr (WRITE) {
-      if (page < 0) continue;
-      if constexpr (I8) {
-        float v[4], most = 0.f;
-        bool fine = true;
+      for (int i = 0; i < 4; ++i) v[i] = to_f(t[i]), most = fmaxf(most, fabsf(v[i])), fine = fine && __builtin_isfinite(v[i]);
+      const float s = scale_of(wave_max(most), __all(fine)), inv = s > 0.f ? 1.f / s : 0.f;
+      if (lane == 0) *scale = s;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = lane + 64 * i < D ? to_f(x[lane + 64 * i]) : 0.f;
-          most = fmaxf(most, fabsf(v[i]));
-          fine = fine && __builtin_isfinite(v[i]);
-        }
-        const float s = scale_of(wave_max(most), __all(fine));
-        const float inv = s > 0.f ? 1.f / s : 0.f;
-        if (lane == 0) scale[scale_at(c, page, head, slot)] = s;
-        int8_t* q = static_cast<int8_t*>(which ? c.v : c.k) + at;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (lane + 64 * i < D) q[(lane + 64 * i) * step] = s > 0.f ? (int8_t)(int)code_of(v[i], s, inv) : (int8_t)0;
-      } else {
-        T* q = static_cast<T*>(which ? c.v : c.k) + at;
-        for (int d = lane; d < D; d += 64) q[d * step] = x[d];
-      }
+      for (int i = 0; i < 4; ++i) e[i] = s > 0.f ? (int8_t)(int)code_of(v[i], s, inv) : (int8_t)0;
     } else {
-      if constexpr (I8) {
-        const float s = page < 0 ? 0.f : scale[scale_at(c, page, head, slot)];
-        const int8_t* q = static_cast<const int8_t*>(which ? c.v : c.k) + at;
-        for (int d = lane; d < D; d += 64) x[d] = from_f<T>(page < 0 ? 0.f : (float)q[d * step] * s);
-      } else {
-        const T* q = static_cast<const T*>(which ? c.v : c.k) + at;
-        for (int d = lane; d < D; d += 64) x[d] = page < 0 ? (T)0.f : q[d * step];
-      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i] = t[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (lane + 64 * i < D) q[(lane + 64 * i) * step] = e[i];
+  } else {
+    E e[4];
+    float s = 0.f;
+    if (page >= 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i] = q[min(lane + 64 * i, D - 1) * step];
+      if constexpr (I8) s = *scale;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (lane + 64 * i >= D) continue;
+      if constexpr (I8) x[lane + 64 * i] = from_f<T>(page < 0 ? 0.f : (float)e[i] * s);
+      else x[lane + 64 * i] = page < 0 ? (T)0.f : e[i];
     }
   }
 }
 
-// Many rows: a workgroup takes the 16 positions of a sequence that V keeps together,
-// of one head or, of small ones, some; K's rows in chunks of 8, V's through LDS,
-// which turns them into rows of positions.  Positions that the call does not cover are left
-// alone: of a tile of which it covers only some, elements are written one by one.
+// Many rows: a workgroup takes the 16 positions of a sequence that V keeps together, of
+// K or of V, of one head or some; rows in chunks of 8 elements, and V's through LDS,
+// which turns them into rows of positions.  Positions that the call does not cover are
+// left alone: of a tile of which it covers only some, elements are written one by one.
+// What a thread reads is all in flight at once.
 constexpr int kTileThreads = 256;
+constexpr int kTilePasses = 2;  // (4: the same for many rows, 3 us more for few)
 template <typename T, bool I8, bool WRITE>
 __global__ __launch_bounds__(kTileThreads) void cache_tiles_kernel(CacheRows a) {
   typedef typename std::conditional<I8, int8_t, T>::type E;
-  // [8 elements' chunk j][chunk][16 positions]: threads of a row's chunks next to each other
-  __shared__ __attribute__((aligned(16))) E turn[8 * kTileThreads * 2];
+  constexpr int NP = kTilePasses, GE = 16 / sizeof(E), VG = 16 / GE;  // positions of a granule of 16 bytes, granules of an element
+  constexpr int NG = NP * kTileThreads * 8 / GE / kTileThreads;
+  // of each head [element % 8][element / 8][16 positions]: threads of a row lie next to each other
+  __shared__ u32x4 turn[NP * kTileThreads * 8 / GE];
+  E* te = reinterpret_cast<E*>(turn);
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, D = c.dim, chunks = D / 8;
   int b, tile, first, n;
   if (!find_rows(c, blockIdx.x, [&](int s, int rows) { return rows_tiles(c.past[s], rows); }, b, tile, first, n)) return;
   const int past = min(c.past[b], kMaxPast);
   const int pos0 = (max(past, 0) & ~15) + 16 * tile;  // of the tile
-  const int page = past < 0 ? -1 : page_of(c, b, pos0);
-  if (WRITE && page < 0) return;
   const int slot0 = pos0 & ((1 << c.shift) - 1);
   const bool whole = past >= 0 && pos0 >= past && pos0 + 16 <= past + n;
-  // lanes of a row of 8-element chunks, rows of one head that lie 16 * lanes threads apart
-  const int lanes = a.lanes, slots = kTileThreads / lanes, ch = tid & (lanes - 1);
+  const int row0 = pos0 - max(past, 0);  // of the sequence (a slot without one counts from 0, and reads zeros)
   const bool key = blockIdx.z == 0;
   T* rows = static_cast<T*>(key ? a.k : a.v);
   const int64_t stride = key ? a.krs : a.vrs;
+  // a pass: `slots` rows of `lanes` threads each
+  const int lanes = a.lanes, slots = kTileThreads / lanes, ch = tid & (lanes - 1), heads = NP * slots / 16, head0 = blockIdx.y * heads;
+  auto at_pass = [&](int p, int& s, int& hh) {  // position in the tile, head of the group; whether the call has the row
+    const int u = p * slots + tid / lanes;
+    s = u & 15, hh = u >> 4;
+    return ch < chunks && head0 + hh < c.kv_heads && row0 + s >= 0 && row0 + s < n;
+  };
+  auto row_at = [&](int s, int hh) { return rows + (int64_t)(first + row0 + s) * stride + (int64_t)(head0 + hh) * D + 8 * ch; };
+  V8<T> v[NP];
+  if constexpr (WRITE) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      int s, hh;
+      v[p] = zero8<T>();
+      if (at_pass(p, s, hh)) __builtin_memcpy(&v[p], row_at(s, hh), sizeof(v[p]));
+    }
+  }
+  const int page = past < 0 ? -1 : page_of(c, b, pos0);
+  if (WRITE && page < 0) return;
   E* store = static_cast<E*>(key ? c.k : c.v);
   float* scales = key ? c.ks : c.vs;
-  const int heads = max(1, slots / 16);  // of a pass
-  for (int pass = 0; pass < max(1, 16 / slots); ++pass) {
-    const int u = pass * slots + tid / lanes, s = u & 15, hh = u >> 4;  // token of the tile, head of the group
-    const int head = blockIdx.y * heads + hh;
-    const bool on = ch < chunks && head < c.kv_heads;
-    // rows of a slot without a sequence are counted from 0 (they are read as zeros)
-    const int row = pos0 + s - max(past, 0);
-    const bool mine = on && row >= 0 && row < n;
-    T* x = rows + (int64_t)(first + row) * stride + (int64_t)head * D + 8 * ch;
-    const int64_t at = ((((int64_t)max(page, 0) * c.kv_heads + min(head, c.kv_heads - 1)) << c.shift) + slot0);  // of the tile's rows
-    if constexpr (WRITE) {
-      V8<T> v = zero8<T>();
-      if (mine) __builtin_memcpy(&v, x, sizeof(v));
+  auto tile_at = [&](int hh) { return ((((int64_t)max(page, 0) * c.kv_heads + head0 + hh) << c.shift) + slot0); };
+  auto turned = [&](int s, int hh, int j) { return te + ((hh * 8 + j) * lanes + ch) * 16 + s; };
+  // V's granules, all heads of the group one after the other: in LDS, in memory
+  const int granules = min(heads, c.kv_heads - head0) * D * VG;
+  auto granule = [&](int g, u32x4*& in_lds, u32x4*& in_memory) {
+    const int hh = fdiv(g, a.head_granules), e = g - hh * (D * VG), d = e / VG, part = e % VG;
+    in_lds = turn + ((hh * 8 + (d & 7)) * lanes + (d >> 3)) * VG + part;
+    in_memory = reinterpret_cast<u32x4*>(store + tile_at(hh) * D + d * 16 + part * GE);
+  };
+  if constexpr (WRITE) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      int s, hh;
+      const bool mine = at_pass(p, s, hh);
       V8<E> q;
       if constexpr (I8) {
         float most = 0.f, f[8];
         bool fine = true;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = to_f(v.v[j]), most = fmaxf(most, fabsf(f[j])), fine = fine && __builtin_isfinite(f[j]);
+        for (int j = 0; j < 8; ++j) f[j] = to_f(v[p].v[j]), most = fmaxf(most, fabsf(f[j])), fine = fine && __builtin_isfinite(f[j]);
         if (!fine) most = __builtin_huge_valf();
         most = max_lanes(most, lanes);
         const float sc = scale_of(most, __builtin_isfinite(most)), inv = sc > 0.f ? 1.f / sc : 0.f;
-        if (mine && ch == 0) scales[at + s] = sc;
+        if (mine && ch == 0) scales[tile_at(hh) + s] = sc;
 #pragma unroll
         for (int j = 0; j < 8; ++j) q.v[j] = sc > 0.f ? (int8_t)(int)code_of(f[j], sc, inv) : (int8_t)0;
       } else {
-        q = v;
+        q = v[p];
       }
+      if (!mine) continue;
       if (key) {
-        if (mine) __builtin_memcpy(__builtin_assume_aligned(store + (at + s) * D + 8 * ch, 8), &q, sizeof(q));
+        __builtin_memcpy(__builtin_assume_aligned(store + (tile_at(hh) + s) * D + 8 * ch, 8), &q, sizeof(q));
       } else if (whole) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (on) turn[((hh * 8 + j) * lanes + ch) * 16 + s] = q.v[j];
-      } else if (mine) {
+        for (int j = 0; j < 8; ++j) *turned(s, hh, j) = q.v[j];
+      } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) store[at * D + (8 * ch + j) * 16 + s] = q.v[j];
-      }
-    } else if (key) {
-      if (mine) {
-        V8<T> v = zero8<T>();
-        if (page >= 0) {
-          V8<E> q;
-          __builtin_memcpy(&q, __builtin_assume_aligned(store + (at + s) * D + 8 * ch, 8), sizeof(q));
-          if constexpr (I8) {
-            const float sc = scales[at + s];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v.v[j] = from_f<T>((float)q.v[j] * sc);
-          } else {
-            v = q;
-          }
-        }
-        __builtin_memcpy(x, &v, sizeof(v));
+        for (int j = 0; j < 8; ++j) store[tile_at(hh) * D + (8 * ch + j) * 16 + s] = q.v[j];
       }
     }
-  }
-  if (key) return;
-  // V: granules of 16 bytes between LDS and the tile's memory, of all heads of the group
-  constexpr int GE = 16 / sizeof(E), VG = 16 / GE;  // positions of a granule, granules of an element
-  auto each_granule = [&](auto f) {
-    for (int g = tid; g < heads * D * VG; g += kTileThreads) {
-      const int hh = g / (D * VG), e = g - hh * (D * VG), d = e / VG, part = e % VG, head = blockIdx.y * heads + hh;
-      if (head >= c.kv_heads) break;
-      const int64_t at = ((((int64_t)max(page, 0) * c.kv_heads + head) << c.shift) + slot0);
-      f(turn + ((hh * 8 + (d & 7)) * lanes + (d >> 3)) * 16 + part * GE, store + at * D + d * 16 + part * GE);
-    }
-  };
-  if constexpr (WRITE) {
-    if (!whole) return;
+    if (key || !whole) return;
     __syncthreads();
-    each_granule([&](const E* from, E* to) { *reinterpret_cast<u32x4*>(to) = *reinterpret_cast<const u32x4*>(from); });
-  } else {
-    if (page >= 0) {
-      each_granule([&](E* to, const E* from) { *reinterpret_cast<u32x4*>(to) = *reinterpret_cast<const u32x4*>(from); });
-      __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      u32x4 *l, *m;
+      if (i * kTileThreads + tid >= granules) break;
+      granule(i * kTileThreads + tid, l, m);
+      *m = *l;
     }
-    for (int pass = 0; pass < max(1, 16 / slots); ++pass) {
-      const int u = pass * slots + tid / lanes, s = u & 15, hh = u >> 4, head = blockIdx.y * heads + hh, row = pos0 + s - max(past, 0);
-      if (ch >= chunks || head >= c.kv_heads || row < 0 || row >= n) continue;
-      V8<T> v = zero8<T>();
+  } else {
+    V8<E> q[NP];
+    float sc[NP];
+    if (page >= 0) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        int s, hh;
+        const bool mine = at_pass(p, s, hh);
+        if (I8 && mine) sc[p] = scales[tile_at(hh) + s];
+        if (key && mine) __builtin_memcpy(&q[p], __builtin_assume_aligned(store + (tile_at(hh) + s) * D + 8 * ch, 8), sizeof(q[p]));
+      }
+      if (!key) {
+        u32x4 r[NG], *l, *m;
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+          if (i * kTileThreads + tid < granules) granule(i * kTileThreads + tid, l, m), r[i] = *m;
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+          if (i * kTileThreads + tid < granules) granule(i * kTileThreads + tid, l, m), *l = r[i];
+        __syncthreads();
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      int s, hh;
+      if (!at_pass(p, s, hh)) continue;
+      V8<T> t = zero8<T>();
       if (page >= 0) {
-        const float sc = I8 ? scales[((((int64_t)page * c.kv_heads + head) << c.shift) + slot0) + s] : 1.f;
+        if (!key)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) q[p].v[j] = *turned(s, hh, j);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const E q = turn[((hh * 8 + j) * lanes + ch) * 16 + s];
-          if constexpr (I8) v.v[j] = from_f<T>((float)q * sc);
-          else v.v[j] = q;
+          if constexpr (I8) t.v[j] = from_f<T>((float)q[p].v[j] * sc[p]);
+          else t.v[j] = q[p].v[j];
         }
       }
-      __builtin_memcpy(rows + (int64_t)(first + row) * stride + (int64_t)head * D + 8 * ch, &v, sizeof(v));
+      __builtin_memcpy(row_at(s, hh), &t, sizeof(t));
     }
   }
 }
@@ -224,19 +247,21 @@ __global__ __launch_bounds__(kTileThreads) void cache_tiles_kernel(CacheRows a) 
 template <typename T, bool WRITE>
 static void launch_rows(CacheRows& a, hipStream_t st) {
   const CacheArgs& c = a.c;
-  // A tile of 16 positions for sequences of some rows each; single rows by waves.
-  // (At 8 rows a sequence, half a tile, both take the same time.)
-  const int64_t tiles = c.tokens / 16 + 2 * (int64_t)c.seqs;
-  if (c.tokens >= 8 * (int64_t)c.seqs) {
+  // Tiles of 16 positions for many rows of few sequences, single rows by waves.  (Written
+  // and read back, 8 heads of 128 in 8 bits: 8 sequences of 16 rows 9.4 us by tiles, 6.3 by
+  // rows; of 64 rows 10.1 and 10.9; of 512 rows 22 and 51; 64 of one row 12.4 and 5.7.)
+  if (c.tokens >= 4 * (int64_t)c.seqs && c.tokens * c.kv_heads >= 4096) {
+    const int64_t tiles = c.tokens / 16 + 2 * (int64_t)c.seqs;
     a.lanes = 1;
     while (a.lanes < c.dim / 8) a.lanes *= 2;
-    const int heads = std::max(1, kTileThreads / a.lanes / 16);
+    a.head_granules = make_fastdiv(c.dim * (c.i8 ? 1 : (int)sizeof(T)));
+    const int heads = kTilePasses * (kTileThreads / a.lanes) / 16;
     const dim3 grid((unsigned)tiles, (c.kv_heads + heads - 1) / heads, 2);
     if (c.i8) SN_LAUNCH((cache_tiles_kernel<T, true, WRITE>), grid, dim3(kTileThreads), 0, st, a);
     else SN_LAUNCH((cache_tiles_kernel<T, false, WRITE>), grid, dim3(kTileThreads), 0, st, a);
     return;
   }
-  const int64_t blocks = (c.tokens * c.kv_heads + kRowWaves - 1) / kRowWaves, x = std::min<int64_t>(blocks, 1 << 20);
+  const int64_t blocks = (2 * c.tokens * c.kv_heads + kRowWaves - 1) / kRowWaves, x = std::min<int64_t>(blocks, 1 << 20);
   const dim3 grid((unsigned)x, (unsigned)((blocks + x - 1) / x)), block(64 * kRowWaves);
   if (c.i8) SN_LAUNCH((cache_rows_kernel<T, true, WRITE>), grid, block, 0, st, a);
   else SN_LAUNCH((cache_rows_kernel<T, false, WRITE>), grid, block, 0, st, a);
@@ -246,7 +271,7 @@ static void cache_rows(const CacheRows& args, hipStream_t st) {
   CacheRows a = args;
   const CacheArgs& c = a.c;
   check(c.dim >= 8 && c.dim <= 256 && c.dim % 8 == 0 && c.kv_heads >= 1 && c.shift >= 4 && c.seqs >= 1 && c.tokens >= 1 &&
-            (c.tokens * c.kv_heads) >> 40 == 0,
+            (c.tokens * c.kv_heads) >> 39 == 0,
         "cache shapes");
   if (c.dtype == 0) launch_rows<float, WRITE>(a, st);
   else if (c.dtype == 1) launch_rows<f16, WRITE>(a, st);

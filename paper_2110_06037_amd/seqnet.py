@@ -1,6 +1,8 @@
-"""A net of gated sequence blocks on the sequence operators, for inference.
+"""A net of gated sequence blocks and attention blocks on the sequence and attention
+operators, for inference.
 
-Each block takes the normalised residual stream u and adds to the stream h::
+Each block takes the normalised residual stream u and adds to the stream h; a
+sequence block::
 
     z, raw, dt = split(in_proj(u))          # Linear4
     y = scan(raw, dt)                       # Scan: convolution, silu, state space scan
@@ -8,28 +10,63 @@ Each block takes the normalised residual stream u and adds to the stream h::
     h = h + scale * out_proj(v)             # Linear4; the sum in the BlockNorm that
     u = norm(h)                             # also makes the next block's input
 
+and an attention block::
+
+    q, k, v = split(in_proj(u))             # Linear4
+    q, k = turn(norm(q)), turn(norm(k))     # HeadNorm, in place
+    cache.write(k, v)                       # KVCache
+    y = attention(q, cache)                 # Attention
+    h = h + scale * out_proj(y)             # as above
+    u = norm(h)
+
 A prompt of any length runs with ``run``, single tokens with ``step``; both
-leave every block's convolution window and state behind in a ``SequenceState``.
+leave every block's convolution window and state, or its cache, behind in a
+``SequenceState``.
 """
 
 from __future__ import annotations
 
+from .attention import Attention, HeadNorm, KVCache
 from .sequence import BlockNorm, Linear4, Scan
 
 
 class SequenceState:
-    """The windows and states of ``seqs`` sequences in every block (zeros: before the first token)."""
+    """What ``seqs`` sequences leave behind in every block (at first nothing).
 
-    def __init__(self, net, seqs):
+    ``windows`` and ``states`` are the sequence blocks' (zeros: before the first
+    token).  For attention blocks ``past`` (int32 [seqs]) counts the tokens so far,
+    and ``caches`` hold up to ``max_positions`` of each sequence, in the pages that
+    ``tables`` say (tokens behind them are seen by no later one)."""
+
+    def __init__(self, net, seqs, max_positions=None):
         import torch
         dev = f"cuda:{net.device}"
         self.seqs = seqs
-        self.windows = [torch.zeros(seqs, b.scan.conv - 1, b.scan.chans, dtype=b.scan.torch_dtype, device=dev)
-                        for b in net.blocks]
-        self.states = [torch.zeros(seqs, b.scan.heads, b.scan.head_dim, b.scan.state, device=dev) for b in net.blocks]
+        scans = [b for b in net.blocks if not b.attends]
+        attends = [b for b in net.blocks if b.attends]
+        self.windows = [torch.zeros(seqs, b.scan.conv - 1, b.scan.chans, dtype=b.scan.torch_dtype, device=dev) for b in scans]
+        self.states = [torch.zeros(seqs, b.scan.heads, b.scan.head_dim, b.scan.state, device=dev) for b in scans]
+        self.past, self.caches, self.tables = None, [], []
+        if attends:
+            if max_positions is None:
+                raise ValueError("a net with attention blocks needs max_positions")
+            self.past = torch.zeros(seqs, dtype=torch.int32, device=dev)
+        for b in attends:
+            width = -(-max_positions // b.page)
+            self.caches.append(b.new_cache(seqs * width))
+            self.tables.append(torch.arange(seqs * width, dtype=torch.int32, device=dev).reshape(seqs, width))
+        scan, cache = iter(zip(self.windows, self.states)), iter(zip(self.caches, self.tables))
+        self.parts = [next(cache if b.attends else scan) for b in net.blocks]
+
+    def tensors(self):
+        """What a step reads and updates."""
+        held = [t for c in self.caches for t in (c.k, c.v, c.k_scale, c.v_scale) if t is not None]
+        return self.windows + self.states + ([] if self.past is None else [self.past]) + self.tables + held
 
 
 class _Block:
+    attends = False
+
     def __init__(self, dtype, w, next_norm, max_seqs, max_tokens, device, eps):
         c = w["config"]
         inner, heads = c["heads"] * c["head_dim"], c["heads"]
@@ -44,6 +81,74 @@ class _Block:
     def close(self):
         for op in (self.in_proj, self.scan, self.gate, self.out_proj, self.join):
             op.close()
+
+    def run(self, u, part, call):
+        window, s = part
+        p = self.in_proj.run(u)
+        z, raw, dt = p[:, :self.inner], p[:, self.inner:self.inner + self.chans], p[:, self.inner + self.chans:]
+        if call.step:
+            y = self.scan.step(raw, dt, window, s, window_out=window, state_out=s)[0]
+        else:
+            y = self.scan.run(raw, dt, window, s, window_out=window, state_out=s, seqs=call.state.seqs, offsets=call.offsets)[0]
+        self.gate.run(y, gate=z, out=y)
+        return self.out_proj.run(y)
+
+
+class _AttentionBlock:
+    attends = True
+
+    def __init__(self, dtype, w, next_norm, max_seqs, max_tokens, device, eps):
+        c = w["config"]
+        heads, kv, dim = c["heads"], c["kv_heads"], c["head_dim"]
+        self.page, self.nq, self.nk = c["page"], heads * dim, kv * dim
+        self.in_proj = Linear4(dtype, *w["in_proj"][:2], zero=w["in_proj"][2], cols=c["dim"], group=c["group"], device=device)
+        self.head_norm = HeadNorm(dtype, heads, kv, dim, w["q_norm"], w["k_norm"], eps=eps, rot=c["rot"], base=c["base"], device=device)
+        self.attention = Attention(dtype, heads, kv, dim, page=c["page"], store=c["store"], window=c["window"], max_seqs=max_seqs,
+                                   max_tokens=max_tokens, device=device)
+        self.out_proj = Linear4(dtype, *w["out_proj"][:2], zero=w["out_proj"][2], cols=self.nq, group=c["group"], device=device)
+        self.join = BlockNorm(dtype, c["dim"], pre=next_norm, scale=w["scale"], residual="f32", eps=eps, device=device)
+        self.new_cache = lambda pages: KVCache(dtype, kv, dim, pages, page=c["page"], store=c["store"], device=device)
+
+    def close(self):
+        for op in (self.in_proj, self.head_norm, self.attention, self.out_proj, self.join):
+            op.close()
+
+    def run(self, u, part, call):
+        cache, table = part
+        p = self.in_proj.run(u)
+        q, k, v = p[:, :self.nq], p[:, self.nq:self.nq + self.nk], p[:, self.nq + self.nk:]
+        self.head_norm.run(q, k, call.positions, q_out=q, k_out=k)
+        cache.write(k, v, table, call.state.past, offsets=call.offsets)
+        if call.step:
+            y = self.attention.step(q, cache, table, call.state.past)
+        else:
+            y = self.attention.run(q, cache, table, call.state.past, offsets=call.offsets)
+        return self.out_proj.run(y)
+
+
+class _Call:
+    """What the blocks of one run or step share; ``positions`` of the rows where blocks attend."""
+
+    def __init__(self, state, rows, offsets, step):
+        self.state, self.offsets, self.step = state, offsets, step
+        past = state.past
+        if past is None:
+            return
+        import torch
+        if step:
+            self.lens, self.positions = 1, past
+        elif offsets is None:
+            self.lens = rows // state.seqs
+            self.positions = (past[:, None] + torch.arange(self.lens, dtype=torch.int32, device=past.device)).reshape(-1)
+        else:
+            row = torch.arange(rows, dtype=torch.int32, device=past.device)
+            seq = torch.searchsorted(offsets[1:], row, right=True).clamp_(max=state.seqs - 1)
+            self.lens = offsets[1:] - offsets[:-1]
+            self.positions = past[seq] + row - offsets[:-1][seq]
+
+    def done(self):
+        if self.state.past is not None:  # slots without a sequence stay so
+            self.state.past += (self.state.past >= 0) * self.lens
 
 
 class _Replay:
@@ -64,14 +169,17 @@ class SequenceNet:
     with its "config" (dim, heads, head_dim, groups, state, group), 4-bit
     "in_proj" and "out_proj" as ``quantize4`` gives them, "conv_w", "conv_b",
     "a", "d", "dt_bias", "gate_norm", the residual's "scale", and the "norm"
-    [dim] that follows the block}.  Inputs and outputs are [rows, dim] in
+    [dim] that follows the block}.  An attention block's config has the "kind"
+    "attention" (dim, heads, kv_heads, head_dim, rot, base, window, page, store,
+    group), and beside the projections "q_norm" and "k_norm" [head_dim].  Inputs and outputs are [rows, dim] in
     ``dtype``; the residual stream between the blocks is float32."""
 
     def __init__(self, dtype, weights, max_seqs=1, max_tokens=1, device=0, eps=1e-5):
         blocks = weights["blocks"]
         self.device, self.closed = device, False
         self.first = BlockNorm(dtype, blocks[0]["config"]["dim"], pre=weights["norm"], eps=eps, device=device)
-        self.blocks = [_Block(dtype, w, w["norm"], max_seqs, max_tokens, device, eps) for w in blocks]
+        self.blocks = [(_AttentionBlock if w["config"].get("kind") == "attention" else _Block)(
+            dtype, w, w["norm"], max_seqs, max_tokens, device, eps) for w in blocks]
 
     def close(self):
         self.closed = True
@@ -85,31 +193,29 @@ class SequenceNet:
     def __exit__(self, *exc):
         self.close()
 
-    def new_state(self, seqs=1):
-        return SequenceState(self, seqs)
+    def new_state(self, seqs=1, max_positions=None):
+        """The state before the first token; attention blocks hold ``max_positions`` of each sequence."""
+        return SequenceState(self, seqs, max_positions)
 
-    def _forward(self, x, state, scan):
+    def _forward(self, x, state, offsets, step):
         import torch
         u, _ = self.first.run(x)
         h = x.to(torch.float32, copy=True)  # updated below: never the caller's x
-        for b, window, s in zip(self.blocks, state.windows, state.states):
-            p = b.in_proj.run(u)
-            z, raw, dt = p[:, :b.inner], p[:, b.inner:b.inner + b.chans], p[:, b.inner + b.chans:]
-            y = scan(b.scan, raw, dt, window, s)
-            b.gate.run(y, gate=z, out=y)
-            u, h = b.join.run(b.out_proj.run(y), residual=h, res_out=h)
+        call = _Call(state, x.shape[0], offsets, step)
+        for b, part in zip(self.blocks, state.parts):
+            u, h = b.join.run(b.run(u, part, call), residual=h, res_out=h)
+        call.done()
         return u
 
     def run(self, x, state, offsets=None):
         """The normalised outputs [tokens, dim] of prompts in packed rows x
         (``offsets``: int32 device tensor of their first rows; none: of equal
         lengths), continuing from ``state``, which is brought up to date."""
-        return self._forward(x, state, lambda op, raw, dt, w, s: op.run(
-            raw, dt, w, s, window_out=w, state_out=s, seqs=state.seqs, offsets=offsets)[0])
+        return self._forward(x, state, offsets, False)
 
     def step(self, x, state):
         """The same for one token per sequence, x [seqs, dim]."""
-        return self._forward(x, state, lambda op, raw, dt, w, s: op.step(raw, dt, w, s, window_out=w, state_out=s)[0])
+        return self._forward(x, state, None, True)
 
     def capture_step(self, state):
         """A captured HIP graph of ``step`` on ``state``: (x, y, replay), where x
@@ -120,7 +226,8 @@ class SequenceNet:
         import torch
         with torch.cuda.device(self.device):
             x = torch.zeros(state.seqs, self.first.dim, dtype=self.first.torch_dtype, device=f"cuda:{self.device}")
-            tensors = state.windows + state.states
+            # (what a step writes to a cache lies behind its sequence, until one that counts overwrites it)
+            tensors = state.windows + state.states + ([] if state.past is None else [state.past])
             keep = [t.clone() for t in tensors]
             side = torch.cuda.Stream(self.device)
             side.wait_stream(torch.cuda.current_stream(self.device))
@@ -132,4 +239,4 @@ class SequenceNet:
                 y = self.step(x, state)
             for t, k in zip(tensors, keep):
                 t.copy_(k)
-        return x, y, _Replay(graph, self, tensors, (x, y))
+        return x, y, _Replay(graph, self, state.tensors(), (x, y))

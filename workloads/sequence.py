@@ -1,7 +1,11 @@
-"""A net of gated sequence blocks with random weights, and an example that
-serves it: a batch of prompts, then tokens one by one.
+"""A net of gated sequence blocks and attention blocks with random weights, and an
+example that serves it: a batch of prompts, then tokens one by one.
 
-    python -m workloads.sequence [--dim 2048 --heads 64 --blocks 4 --prompt 1024 --tokens 32 --seqs 2]
+    python -m workloads.sequence [--dim 2048 --heads 64 --blocks 4 --prompt 1024 --tokens 32 --seqs 2
+                                  --attention 0 --store same]
+
+``--attention n`` makes every n-th block an attention block, ``--store i8`` keeps
+their caches in 8 bits.
 """
 
 import argparse
@@ -14,25 +18,44 @@ def sequence_config(dim=256, heads=8, head_dim=64, groups=1, state=64, conv=4, g
     return {"dim": dim, "heads": heads, "head_dim": head_dim, "groups": groups, "state": state, "conv": conv, "group": group}
 
 
+def attention_config(dim=256, heads=4, kv_heads=2, head_dim=64, rot=None, base=10000.0, window=0, page=64, store="same", group=64):
+    return {"kind": "attention", "dim": dim, "heads": heads, "kv_heads": kv_heads, "head_dim": head_dim,
+            "rot": head_dim if rot is None else rot, "base": base, "window": window, "page": page, "store": store, "group": group}
+
+
 def sequence_weights(config, blocks=2, seed=0, zero=True):
     """Random weights (``np.random.default_rng(seed)``) in the form that
     ``SequenceNet`` takes: He-like projections quantised to 4 bits, step sizes of
-    0.001 to 0.1 at the bias, decay rates of 1 to 16."""
+    0.001 to 0.1 at the bias, decay rates of 1 to 16.  ``config``: of all ``blocks``
+    blocks, or a list with one for each."""
     from paper_2110_06037_amd import quantize4
     r = np.random.default_rng(seed)
-    c = config
-    inner = c["heads"] * c["head_dim"]
-    chans = inner + 2 * c["groups"] * c["state"]
+    configs = list(config) if isinstance(config, (list, tuple)) else [config] * blocks
+    blocks = len(configs)
     f32 = lambda v: np.asarray(v, np.float32)
 
-    def projection(rows, cols):
+    def projection(c, rows, cols):
         return quantize4(r.standard_normal((rows, cols)) / np.sqrt(cols), c["group"], zero)
 
-    def block():
+    def attention(c):
+        heads, kv, n = c["heads"], c["kv_heads"], c["head_dim"]
+        return {"config": c,
+                "in_proj": projection(c, (heads + 2 * kv) * n, c["dim"]),
+                "out_proj": projection(c, c["dim"], heads * n),
+                "q_norm": f32(r.uniform(0.5, 1.5, n)),
+                "k_norm": f32(r.uniform(0.5, 1.5, n)),
+                "scale": 1 / np.sqrt(2 * blocks),
+                "norm": f32(r.uniform(0.5, 1.5, c["dim"]))}
+
+    def block(c):
+        if c.get("kind") == "attention":
+            return attention(c)
+        inner = c["heads"] * c["head_dim"]
+        chans = inner + 2 * c["groups"] * c["state"]
         step = np.exp(r.uniform(np.log(1e-3), np.log(1e-1), c["heads"]))
         return {"config": c,
-                "in_proj": projection(inner + chans + c["heads"], c["dim"]),
-                "out_proj": projection(c["dim"], inner),
+                "in_proj": projection(c, inner + chans + c["heads"], c["dim"]),
+                "out_proj": projection(c, c["dim"], inner),
                 "conv_w": f32(r.uniform(-1, 1, (chans, c["conv"])) / np.sqrt(c["conv"])),
                 "conv_b": f32(r.uniform(-0.1, 0.1, chans)),
                 "a": f32(-r.uniform(1, 16, c["heads"])),
@@ -42,21 +65,26 @@ def sequence_weights(config, blocks=2, seed=0, zero=True):
                 "scale": 1 / np.sqrt(2 * blocks),
                 "norm": f32(r.uniform(0.5, 1.5, c["dim"]))}
 
-    return {"norm": f32(r.uniform(0.5, 1.5, c["dim"])), "blocks": [block() for _ in range(blocks)]}
+    return {"norm": f32(r.uniform(0.5, 1.5, configs[0]["dim"])), "blocks": [block(c) for c in configs]}
 
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    for name, value in (("dim", 2048), ("heads", 64), ("blocks", 4), ("prompt", 1024), ("tokens", 32), ("seqs", 2)):
+    for name, value in (("dim", 2048), ("heads", 64), ("blocks", 4), ("prompt", 1024), ("tokens", 32), ("seqs", 2),
+                        ("attention", 0)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--store", choices=("same", "i8"), default="same")
     a = ap.parse_args()
     import torch
     from paper_2110_06037_amd import SequenceNet
     c = sequence_config(a.dim, a.heads, 2 * a.dim // a.heads, 1, 128, 4, 128)
-    net = SequenceNet("bf16", sequence_weights(c, a.blocks), max_seqs=a.seqs, max_tokens=a.seqs * a.prompt)
+    attend = attention_config(a.dim, a.dim // 64, max(1, a.dim // 256), 128, store=a.store, group=128)
+    configs = [attend if a.attention and i % a.attention == a.attention - 1 else c for i in range(a.blocks)]
+    net = SequenceNet("bf16", sequence_weights(configs), max_seqs=a.seqs, max_tokens=a.seqs * a.prompt)
+    positions = a.prompt + a.tokens + 1
     g = torch.Generator(device="cuda").manual_seed(0)
     x = torch.randn(a.seqs * a.prompt, a.dim, generator=g, device="cuda").bfloat16()
-    net.run(x, net.new_state(a.seqs))  # the first run also loads the kernels
+    net.run(x, net.new_state(a.seqs, positions))  # the first run also loads the kernels
 
     def timed(f, n):
         torch.cuda.synchronize()
@@ -66,7 +94,7 @@ def main():
         torch.cuda.synchronize()
         return (time.perf_counter() - t) / n
 
-    state = net.new_state(a.seqs)
+    state = net.new_state(a.seqs, positions)
     prompt = timed(lambda: net.run(x, state), 1)
     token, out, replay = net.capture_step(state)
 

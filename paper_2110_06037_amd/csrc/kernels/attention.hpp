@@ -828,13 +828,16 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
     const Shared wo(a.ws_o), wm(a.ws_m);
     auto o_at = [&](int z, int i) { return ((slot + z) * (4 * ND) + i) * 1024 + 4 * tid; };
     auto m_at = [&](int z) { return (slot + z) * 512 + tid; };
+    if (t * kRunRows + 32 * wave < rows) {
 #pragma unroll
-    for (int i = 0; i < ND; ++i)
+      for (int i = 0; i < ND; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        wo.put4(o_at(blockIdx.z, 4 * i + j), f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
-    wm.put(m_at(blockIdx.z), m), wm.put(m_at(blockIdx.z) + 256, l);
+        for (int j = 0; j < 4; ++j)
+          wo.put4(o_at(blockIdx.z, 4 * i + j), f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
+      wm.put(m_at(blockIdx.z), m), wm.put(m_at(blockIdx.z) + 256, l);
+    }
     if (!last_of(a.count + blockIdx.x, parts, &flag[0])) return;
+    if (t * kRunRows + 32 * wave >= rows) return;  // (a wave without rows left nothing)
     m = kNone;
 #pragma unroll 4
     for (int z = 0; z < parts; ++z) m = fmaxf(m, wm.get(m_at(z)));

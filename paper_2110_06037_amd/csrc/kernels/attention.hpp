@@ -474,14 +474,17 @@ constexpr int run_keys() {
   return sizeof(T) == 2 ? 64 : 32;
 }
 
-// LDS direct load: 16 bytes a lane from `bytes` at `from` (beyond them: zeros) to 1024 at
-// `to`.  (The compiler's own form makes every later read of the array wait for it; here the
+// LDS direct load: 16 bytes a lane from the resource (beyond its range: zeros), whose
+// offset is `offset` + `more`, to 1024 bytes at `to`.  (The compiler's own form makes every later read of the array wait for it; here the
 // kernel waits itself, once a block.)
-__device__ __forceinline__ void lds_load(const void* from, unsigned bytes, unsigned offset, const void* to) {
-  const uintptr_t p = reinterpret_cast<uintptr_t>(from);
-  const u32x4 rsrc = {(unsigned)p, (unsigned)(p >> 32) & 0xffffu, bytes, 0x00020000u};
+__device__ __forceinline__ u32x4 resource(const void* p, unsigned bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return u32x4{(unsigned)at, (unsigned)(at >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+__device__ __forceinline__ void lds_load(u32x4 rsrc, unsigned offset, unsigned more, const void* to) {
   const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)to;
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(rsrc), "s"(at) : "memory");
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(offset), "s"(rsrc), "s"(more), "s"(at)
+               : "memory");
 }
 
 // The schedule of N products whose first operands come from LDS: reads go AHEAD of the
@@ -501,14 +504,15 @@ __device__ __forceinline__ void reads_ahead() {
 
 // K and V of a block in LDS, in granules of 16 bytes: K [key][element], V as the
 // cache has it, [16 keys][element][key].  The granules of a row lie in an order of
-// the row's own, so that 8 lanes that read one of each of 8 rows meet no bank twice.
+// the row's own, so that 16 lanes that read one of each of 16 rows meet none of the 64
+// banks twice.
 template <typename T, int DP>
 struct RunTile {
   static constexpr int KB = run_keys<T>(), GE = 16 / sizeof(T), FG = 8 / GE;  // elements of a granule, granules of 8 elements
   static constexpr int KG = DP / GE, VG = 16 / GE;                            // granules of a key's row, of an element's 16 keys
   static constexpr int N = KB * DP / GE;                                      // of a block, each of K and V
-  static __device__ __forceinline__ int k(int key, int g) { return key * KG + (g ^ (key & ((KG < 16 ? KG : 16) - 1))); }
-  static __device__ __forceinline__ int v_order(int d) { return sizeof(T) == 2 ? (d >> 2) & 1 : (d >> 1) & 3; }
+  static __device__ __forceinline__ int k(int key, int g) { return key * KG + (g ^ (KG < 16 ? key >> 1 & 7 : key & 15)); }
+  static __device__ __forceinline__ int v_order(int d) { return sizeof(T) == 2 ? (d >> 3) & 1 : (d >> 2) & 3; }
   static __device__ __forceinline__ int v(int t16, int d, int g) { return (t16 * DP + d) * VG + (g ^ v_order(d)); }
 };
 
@@ -593,20 +597,28 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   float ksr = 0.f, vsr = 0.f, vpw[POWER ? NL : 1][8];
   auto load = [&](int block, int pages, int buf) {
     if constexpr (!I8) {
-      int64_t at[KB / 16];
+      // a 16 positions' place, and with pages of a whole block at least that of them all
+      auto place = [&](int t16) {
+        return (int64_t)((uint64_t)(unsigned)max(0, __builtin_amdgcn_readlane(pages, t16)) * page_bytes) + head_bytes +
+               ((block * KB + 16 * t16) & mask) * row_bytes;
+      };
+      const unsigned to = buf * L::N + 64 * wave, tile_bytes = 16 * row_bytes;
+      if (KB >> c.shift <= 1) {
+        const int64_t o = place(0);
+        const u32x4 rk = resource(static_cast<const char*>(c.k) + o, KB * row_bytes), rv = resource(static_cast<const char*>(c.v) + o, KB * row_bytes);
 #pragma unroll
-      for (int i = 0; i < KB / 16; ++i)
-        at[i] = (int64_t)((uint64_t)(unsigned)max(0, __builtin_amdgcn_readlane(pages, i)) * page_bytes) + head_bytes +
-                ((block * KB + 16 * i) & mask) * row_bytes;
-      // (a wave's share lies in tile i / PER + const of its own)
+        for (int i = 0; i < NG; ++i) {
+          const unsigned more = (256 * i + 64 * wave) / (16 * L::KG) * tile_bytes;
+          lds_load(rk, koff[i], more, &sk[to + 256 * i]);
+          lds_load(rv, voff[i], more, &sv[to + 256 * i]);
+        }
+      } else {
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const int x = 256 * i + 64 * wave;
-        int64_t o = at[256 * i / (16 * L::KG)];
-        if constexpr (16 * L::KG < 256)
-          if (wave >= L::KG / 4) o = at[256 * i / (16 * L::KG) + 1];
-        lds_load(static_cast<const char*>(c.k) + o, 16 * row_bytes, koff[i], &sk[buf * L::N + x]);
-        lds_load(static_cast<const char*>(c.v) + o, 16 * row_bytes, voff[i], &sv[buf * L::N + x]);
+        for (int i = 0; i < NG; ++i) {
+          const int64_t o = place((256 * i + 64 * wave) / (16 * L::KG));
+          lds_load(resource(static_cast<const char*>(c.k) + o, tile_bytes), koff[i], 0, &sk[to + 256 * i]);
+          lds_load(resource(static_cast<const char*>(c.v) + o, tile_bytes), voff[i], 0, &sv[to + 256 * i]);
+        }
       }
     } else {
 #pragma unroll
@@ -665,6 +677,30 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
     return f;
   };
 
+  // whether some row of the workgroup does not see some key of a block
+  auto edge_of = [&](int block, int pages) {
+    return block * KB + KB - 1 > pos0 || (a.window && block * KB < pos1 - a.window + 1) ||
+           __builtin_popcountll(__ballot(pages >= 0)) < KB / 16;
+  };
+  // What a row does not see takes no part in it, whatever it is, but 0 times a value that
+  // is not finite would: such blocks are looked through as they arrive, each thread
+  // at what it has loaded.  (A flag holds a block's own number, so none is ever cleared.)
+  auto look = [&](int block, int buf) {
+    unsigned odd = 0;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const u32x4 v = sv[buf * L::N + 256 * i + tid];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // an exponent of ones, and one more, carries into the sign
+        constexpr unsigned E1 = std::is_same<T, f16>::value ? 0x7c007c00u : sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u;
+        constexpr unsigned ONE = std::is_same<T, f16>::value ? 0x04000400u : sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+        odd |= (v[j] & E1) + ONE;
+      }
+    }
+    if (__any(odd & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u)) && lane == 0) flag[buf] = block + 1;
+  };
+
   f32x16 o[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i)
@@ -673,53 +709,44 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   float m = kNone, l = 0.f;
   int pages = -1, pages1 = -1;
   if (tid < 2) flag[tid] = 0;
-  bool odd = !I8;  // (at first: marks are cleared by the first block that looks at them)
   if (first < end) {
     const int entry = table[entry_of(first)], entry1 = table[entry_of(first + 1)];
     pages = pages_of(first, entry), pages1 = pages_of(first + 1, entry1);
     load(first, pages, 0), store(0);
   }
+  __syncthreads();  // (the flags are clear)
   wait_vmcnt<0>();
+  if (!I8 && first < end && edge_of(first, pages)) look(first, 0);
   __syncthreads();
   for (int block = first; block < end; ++block) {
     const int buf = (block - first) & 1;
     const bool more = block + 1 < end;
     const int entry2 = table[entry_of(block + 2)];
     if (more) load(block + 1, pages1, buf ^ 1);
-    // whether some row of the workgroup does not see some key of the block
     const unsigned long long there = __ballot(pages >= 0);
-    const bool edge = block * KB + KB - 1 > pos0 || (a.window && block * KB < pos1 - a.window + 1) || __builtin_popcountll(there) < KB / 16;
-    if constexpr (!I8) {
-      // What a row does not see takes no part in it, whatever it is, but 0 times a value
-      // that is not finite would.  Such values become zeros in LDS, with a bit that
-      // says where they were; what they do to the rows that see them follows the product.
-      if (edge) {
-        if (odd) {  // the last block's bits
-          for (int i = tid; i < DP * 4; i += 256) marks[i] = 0;
-          lds_barrier();
-        }
-        odd = false;
+    const bool edge = edge_of(block, pages);
+    const bool odd = !I8 && edge && flag[buf] == block + 1;
+    if (odd) {
+      // Values that are not finite become zeros in LDS, with a bit that says where they
+      // were; what they do to the rows that see them follows the product.
+      for (int i = tid; i < DP * 4; i += 256) marks[i] = 0;
+      lds_barrier();
 #pragma unroll 1
-        for (int i = 0; i < NG; ++i) {
-          const int x = 256 * i + tid, d = x / L::VG % DP, key = x / (L::VG * DP) * 16 + (x % L::VG ^ L::v_order(d)) * L::GE;
-          T e[L::GE];
-          __builtin_memcpy(e, &sv[buf * L::N + x], 16);
-          bool bad = false;
+      for (int i = 0; i < NG; ++i) {
+        const int x = 256 * i + tid, d = x / L::VG % DP, key = x / (L::VG * DP) * 16 + (x % L::VG ^ L::v_order(d)) * L::GE;
+        T e[L::GE];
+        __builtin_memcpy(e, &sv[buf * L::N + x], 16);
 #pragma unroll
-          for (int j = 0; j < L::GE; ++j) {
-            const float v = (float)e[j];
-            if (__builtin_isfinite(v)) continue;
-            if (!(v < 0.f)) atomicOr(&marks[4 * d + (key >> 5)], 1u << ((key & 31) + j));
-            if (!(v > 0.f)) atomicOr(&marks[4 * d + 2 + (key >> 5)], 1u << ((key & 31) + j));
-            e[j] = (T)0.f, bad = true;
-          }
-          if (bad) __builtin_memcpy(&sv[buf * L::N + x], e, 16);
-          odd = odd || bad;
+        for (int j = 0; j < L::GE; ++j) {
+          const float v = (float)e[j];
+          if (__builtin_isfinite(v)) continue;
+          if (!(v < 0.f)) atomicOr(&marks[4 * d + (key >> 5)], 1u << ((key & 31) + j));
+          if (!(v > 0.f)) atomicOr(&marks[4 * d + 2 + (key >> 5)], 1u << ((key & 31) + j));
+          e[j] = (T)0.f;
         }
-        if (__any(odd) && lane == 0) flag[buf] = block + 1;  // (a block's own number: never cleared)
-        lds_barrier();
-        odd = flag[buf] == block + 1;
+        __builtin_memcpy(&sv[buf * L::N + x], e, 16);
       }
+      lds_barrier();
     }
     // (a wave whose rows see none of the block has nothing to do)
     if (block * KB <= top_pos && !(a.window && block * KB + KB - 1 < low_pos - a.window + 1)) {
@@ -752,12 +779,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
           }
       }
       const float mul = I8 ? 1.f : a.scale2;
-      float top = kNone;
+      float tops[4] = {kNone, kNone, kNone, kNone};
 #pragma unroll
       for (int i = 0; i < NK; ++i)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) top = fmaxf(top, s[i][j]);
-      top = max_x32(top) * mul;
+        for (int j = 0; j < 16; ++j) tops[j & 3] = fmaxf(tops[j & 3], s[i][j]);
+      const float top = max_x32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * mul;
       // the maximum moves only when it grew by 2^kLazy: sums stay far from their type's
       // ends (each row by itself: no row's result depends on its neighbours)
       if (__any(top > m + kLazy)) {
@@ -768,13 +795,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
         m = now;
       }
       const float ref = LIFT - some(m);
+      float sums[4] = {l, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < NK; ++i)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           s[i][j] = __builtin_amdgcn_exp2f(fmaf(s[i][j], mul, ref));
-          l += s[i][j];
+          sums[j & 3] += s[i][j];
         }
+      l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
       if constexpr (I8) {
 #pragma unroll
         for (int i = 0; i < NK; ++i)
@@ -794,7 +823,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
 #pragma unroll
         for (int i = 0; i < ND; ++i) o[i] = mma32(v_frag(buf, kk, 32 * i + r), w[kk], o[i]);
       reads_ahead<T, KB / 16 * ND, 4>();
-      if (!I8 && edge && odd) {
+      if (odd) {
         // this row's keys of any weight, against each element's marked ones
         unsigned seen[2] = {0u, 0u};
 #pragma unroll
@@ -817,6 +846,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
     if (more) store(buf ^ 1);
     wait_vmcnt<0>();
     pages = pages1, pages1 = pages_of(block + 2, entry2);
+    if (!I8 && more && edge_of(block + 1, pages)) look(block + 1, buf ^ 1);
     dma_barrier();
   }
   l = sum_x32(l);

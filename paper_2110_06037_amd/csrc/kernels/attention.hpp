@@ -527,7 +527,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   // f16 weights are 2^6 times as large (2^14 at most, see kLazy)
   constexpr float LIFT = std::is_same<T, f16>::value ? 6.f : 0.f, kLazy = 8.f;
   __shared__ u32x4 sk[2 * L::N], sv[2 * L::N];
-  __shared__ __attribute__((aligned(16))) float sks[2][I8 ? KB : 4], svs[2][I8 ? KB : 4];
+  __shared__ __attribute__((aligned(16))) float sks[2][I8 ? KB : 4], svs[2][I8 ? KB : 4], powers[POWER ? KB : 4];
   __shared__ __attribute__((aligned(16))) unsigned marks[I8 ? 4 : DP * 4];  // of an element: 64 keys' bits, +inf or NaN; -inf or NaN
   __shared__ int flag[2];
   const CacheArgs& c = a.c;
@@ -594,7 +594,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   }
   // 8-bit caches: through registers.
   V8<E> kr[I8 ? NL : 1], vr[I8 ? NL : 1];
-  float ksr = 0.f, vsr = 0.f, vpw[POWER ? NL : 1][8];
+  float ksr = 0.f, vsr = 0.f;
   auto load = [&](int block, int pages, int buf) {
     if constexpr (!I8) {
       // a 16 positions' place, and with pages of a whole block at least that of them all
@@ -628,7 +628,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
         kr[i] = load8(static_cast<const E*>(c.k) + (rows_at(block, pages, w / NC / 16) + (x / NC & 15)) * D + (EXACT || d < D ? d : 0));
         const int64_t at = rows_at(block, pages, w / (2 * DP));
         vr[i] = load8(static_cast<const E*>(c.v) + at * D + (EXACT ? 8 * e : 8 * min(e, 2 * D - 1)));
-        if constexpr (POWER) __builtin_memcpy(vpw[i], c.vs + at + 8 * (e & 1), 32);
       }
       if (tid < KB) {
         const int page = max(0, __shfl(pages, tid / 16));
@@ -644,6 +643,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   };
   auto store = [&](int buf) {
     if constexpr (I8) {
+      if constexpr (POWER) {
+        if (tid < KB) powers[tid] = power_of(vsr);
+        lds_barrier();
+      }
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int x = 256 * i + tid, key = x / NC, ch = x % NC;
@@ -655,7 +658,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
         F g = frag_of<T>(vr[i]);
         if constexpr (POWER) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) g[j] = (T)((float)vr[i].v[j] * power_of(vpw[i][j]));
+          for (int j = 0; j < 8; ++j) g[j] = (T)((float)vr[i].v[j] * powers[16 * t16 + 8 * (e & 1) + j]);
         }
         put8(sv + buf * L::N, L::v(t16, dd, FG * (e & 1)), L::v(t16, dd, FG * (e & 1) + FG - 1), g);
       }

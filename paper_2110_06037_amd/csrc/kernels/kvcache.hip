@@ -6,37 +6,57 @@
 namespace sn {
 namespace k {
 
-// The integer nearest to x / s, ties to even, exactly: a rounded quotient is at
-// most one off where it falls next to the middle of two, and r = x - c s, which
-// float32 holds without rounding there, says on which side x lies.
-__device__ __forceinline__ float code_of(float x, float s, float inv) {
-  float c = rintf(x * inv);
-  const float r = fmaf(-c, s, x), h = 0.5f * s;
-  const bool odd = (int)c & 1;
-  if (r > h || (r == h && odd)) c += 1.f;
-  if (r < -h || (r == -h && odd)) c -= 1.f;
-  return c;
+// The integer nearest to x / s, ties to even, exactly, in the low 8 bits: x * inv is added
+// to 1.5 * 2^23, whose last bit counts ones, so the sum rounds to an integer c. That is at most one
+// off, where x / s falls next to the middle of two, and r = x - c s, which float32 holds
+// without rounding, says on which side x lies: beyond half of s (an odd c: from there on), c is
+// the neighbour's.
+__device__ __forceinline__ unsigned code_of(float x, float s, float inv) {
+  const float t = fmaf(x, inv, 12582912.f), r = fmaf(12582912.f - t, s, x);
+  const unsigned c = __builtin_bit_cast(unsigned, t);
+  const float half = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, 0.5f * s) - (c & 1u));
+  return c + (fabsf(r) > half ? (__builtin_bit_cast(int, r) >> 31) | 1 : 0);
+}
+__device__ __forceinline__ V8<int8_t> codes_of(const float (&x)[8], float s, float inv) {
+  V8<int8_t> q;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) q.v[j] = (int8_t)code_of(x[j], s, inv);
+  return q;
+}
+// The sizes of two numbers as integers of the same order, infinities and NaN behind all others.
+template <typename T>
+__device__ __forceinline__ unsigned size_of(const V8<T>& v) {
+  unsigned most = 0;
+  if constexpr (sizeof(T) == 2) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[j] & 0x7fff7fffu));
+    const unsigned short one = max(m[0], m[1]);
+    most = __builtin_bit_cast(unsigned, to_f(__builtin_bit_cast(T, one)));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = max(most, __builtin_bit_cast(unsigned, v.v[j]) & 0x7fffffffu);
+  }
+  return most;
 }
 // max|x| * (1 / 127); rows below 127 * 2^-120 count as zeros (code_of's steps stay exact),
 // and a row with an infinity or a NaN has no numbers at all.
-__device__ __forceinline__ float scale_of(float most, bool fine) {
-  if (!fine) return __builtin_nanf("");
-  const float s = most * (1.f / 127.f);
+__device__ __forceinline__ float scale_of(unsigned most) {
+  if (most >= 0x7f800000u) return __builtin_nanf("");
+  const float s = __builtin_bit_cast(float, most) * (1.f / 127.f);
   return s < 0x1p-120f ? 0.f : s;
 }
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int i = 32; i; i >>= 1) v = fmaxf(v, __shfl_xor(v, i));
-  return v;
-}
-
-// The largest over the 1, 2, 4 .. 32 neighbouring lanes that share a row, in all of them.
-__device__ __forceinline__ float max_lanes(float v, int lanes) {
-  if (lanes > 1) v = fmaxf(v, dpp_take<0xB1>(v));   // XOR 1
-  if (lanes > 2) v = fmaxf(v, dpp_take<0x4E>(v));   // XOR 2
-  if (lanes > 4) v = fmaxf(v, dpp_take<0x141>(v));  // the other quad of 8 lanes
-  if (lanes > 8) v = fmaxf(v, dpp_take<0x140>(v));  // the other 8 of 16
-  if (lanes > 16) v = fmaxf(v, __shfl_xor(v, 16));
+// The largest over the 1, 2, 4 .. 64 neighbouring lanes that share a row, in all of them.
+__device__ __forceinline__ unsigned max_lanes(unsigned v, int lanes) {
+  auto take = [&](unsigned o) { v = max(v, o); };
+  if (lanes > 1) take(__builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, false));   // XOR 1
+  if (lanes > 2) take(__builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, false));   // XOR 2
+  if (lanes > 4) take(__builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, false));  // the other quad of 8 lanes
+  if (lanes > 8) take(__builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, false));  // the other 8 of 16
+  if (lanes > 16) take(__shfl_xor(v, 16));
+  if (lanes > 32) take(__shfl_xor(v, 32));
   return v;
 }
 
@@ -73,14 +93,13 @@ __global__ __launch_bounds__(64 * kRowWaves) void cache_rows_kernel(CacheRows a)
   if constexpr (WRITE) {
     E e[4];
     if constexpr (I8) {
-      float v[4], most = 0.f;
-      bool fine = true;
+      unsigned most = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = to_f(t[i]), most = fmaxf(most, fabsf(v[i])), fine = fine && __builtin_isfinite(v[i]);
-      const float s = scale_of(wave_max(most), __all(fine)), inv = s > 0.f ? 1.f / s : 0.f;
+      for (int i = 0; i < 4; ++i) most = max(most, __builtin_bit_cast(unsigned, to_f(t[i])) & 0x7fffffffu);
+      const float s = scale_of(max_lanes(most, 64)), inv = s > 0.f ? 1.f / s : 0.f;
       if (lane == 0) *scale = s;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e[i] = s > 0.f ? (int8_t)(int)code_of(v[i], s, inv) : (int8_t)0;
+      for (int i = 0; i < 4; ++i) e[i] = s > 0.f ? (int8_t)code_of(to_f(t[i]), s, inv) : (int8_t)0;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) e[i] = t[i];
@@ -169,16 +188,13 @@ __global__ __launch_bounds__(kTileThreads) void cache_tiles_kernel(CacheRows a) 
       const bool mine = at_pass(p, s, hh);
       V8<E> q;
       if constexpr (I8) {
-        float most = 0.f, f[8];
-        bool fine = true;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = to_f(v[p].v[j]), most = fmaxf(most, fabsf(f[j])), fine = fine && __builtin_isfinite(f[j]);
-        if (!fine) most = __builtin_huge_valf();
-        most = max_lanes(most, lanes);
-        const float sc = scale_of(most, __builtin_isfinite(most)), inv = sc > 0.f ? 1.f / sc : 0.f;
+        const float sc = scale_of(max_lanes(size_of(v[p]), lanes)), inv = sc > 0.f ? 1.f / sc : 0.f;
         if (mine && ch == 0) scales[tile_at(hh) + s] = sc;
+        float f[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q.v[j] = sc > 0.f ? (int8_t)(int)code_of(f[j], sc, inv) : (int8_t)0;
+        for (int j = 0; j < 8; ++j) f[j] = to_f(v[p].v[j]);
+        q = codes_of(f, sc, inv);
+        if (!(sc > 0.f)) q = V8<int8_t>{};
       } else {
         q = v[p];
       }

@@ -173,13 +173,14 @@ __device__ __forceinline__ Span step_span(const AttnArgs& a, int past, int KB) {
 struct Part {
   int per, begin, end;  // blocks of a part; this one's
   int pad;              // a sequence counts as a multiple of pad + 1 blocks
-  int b, start;         // the sequence that it begins in, and where that begins
+  int b, start, past;   // the sequence that it begins in, where that begins, and its positions
 };
 __device__ __forceinline__ bool step_part(const AttnArgs& a, int KB, int unit, Part& p) {
   const int lane = threadIdx.x & 63, seqs = a.c.seqs;
-  int total = 0, padded = 0, own = 0;
+  int total = 0, padded = 0, own = 0, past = -1;
   for (int base = 0; base < seqs; base += 64) {
-    own = base + lane < seqs ? step_span(a, a.c.past[base + lane], KB).blocks : 0;
+    past = a.c.past[min(base + lane, seqs - 1)];
+    own = base + lane < seqs ? step_span(a, past, KB).blocks : 0;
     total += own, padded += (own + kStepLeast - 1) & -kStepLeast;
   }
 #pragma unroll
@@ -191,7 +192,10 @@ __device__ __forceinline__ bool step_part(const AttnArgs& a, int KB, int unit, P
   if (p.begin >= total) return false;
   int before = 0;
   for (int base = 0; base < seqs; base += 64) {
-    if (seqs > 64) own = base + lane < seqs ? step_span(a, a.c.past[base + lane], KB).blocks : 0;
+    if (seqs > 64) {
+      past = a.c.past[min(base + lane, seqs - 1)];
+      own = base + lane < seqs ? step_span(a, past, KB).blocks : 0;
+    }
     const int n = (own + p.pad) & ~p.pad;
     int sum = n;
 #pragma unroll
@@ -202,7 +206,7 @@ __device__ __forceinline__ bool step_part(const AttnArgs& a, int KB, int unit, P
     const unsigned long long at = __ballot(p.begin < before + sum);
     if (at) {
       const int l = __ffsll(at) - 1;
-      p.b = uniform(base + l), p.start = uniform(__shfl(before + sum - n, l));
+      p.b = uniform(base + l), p.start = uniform(__shfl(before + sum - n, l)), p.past = uniform(__shfl(past, l));
       return true;
     }
     before += __shfl(sum, 63);
@@ -269,18 +273,23 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
   // the sequences, or parts of them, that this workgroup's blocks belong to
   for (;;) {
   const int b = p.b;
-  const Span span = step_span(a, uniform(c.past[b]), KB);
+  const Span span = step_span(a, p.past, KB);
   const int first = span.block + max(p.begin - p.start, 0), end = span.block + min(p.end - p.start, span.blocks);
   auto page_at = [&](int block, int off) { return block < end ? page_of(c, b, block * KB + off) : -1; };
   FT q[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
     const int d = 64 * (s >> 1) + 16 * g + 8 * (s & 1);
-    V8<T> v = zero8<T>();
-    if (col < cols && (EXACT || d < D)) v = load8(static_cast<const T*>(a.q) + b * a.qs + (int64_t)(qh + col) * D + d);
-    q[s] = frag_of<T>(v);
-    if (a.negative) q[s] = -q[s];
+    // (behind no branch, whose join would wait; columns without a head repeat the last one and are not stored)
+    q[s] = frag_of<T>(load8(static_cast<const T*>(a.q) + b * a.qs + (int64_t)(qh + min(col, cols - 1)) * D + (EXACT || d < D ? d : 0)));
   }
+
+  if constexpr (!EXACT) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      if (64 * (s >> 1) + 16 * g + 8 * (s & 1) >= D) q[s] = FT{};
+  }
+  const float scale = a.negative ? -a.scale2 : a.scale2;
 
   f32x4 o[ND];
 #pragma unroll
@@ -312,7 +321,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[t][i] = s[t][i] * (I8 ? ks[I8 ? 4 * t + i : 0] * a.scale2 : a.scale2);
+      for (int i = 0; i < 4; ++i) v[t][i] = s[t][i] * (I8 ? ks[I8 ? 4 * t + i : 0] * scale : scale);
     if (!full) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -455,6 +464,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
   }
   p.start += (span.blocks + p.pad) & ~p.pad, ++p.b;
   if (p.start >= p.end) return;
+  p.past = uniform(c.past[p.b]);
   }
 }
 
@@ -559,9 +569,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
     const int d = 16 * s + 8 * h;
-    V8<T> v = zero8<T>();
-    if (EXACT || d < D) v = load8(static_cast<const T*>(a.q) + (int64_t)(row0 + token) * a.qs + (int64_t)qh * D + d);
-    q[s] = frag_of<T>(v);
+    q[s] = frag_of<T>(load8(static_cast<const T*>(a.q) + (int64_t)(row0 + token) * a.qs + (int64_t)qh * D + (EXACT || d < D ? d : 0)));
+    if (!EXACT && d >= D) q[s] = F{};
     if (a.negative) q[s] = -q[s];
   }
 

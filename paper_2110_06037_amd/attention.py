@@ -105,25 +105,23 @@ class _Paged(_Op):
             _int(v, n) for v, n in ((kv_heads, "kv_heads"), (head_dim, "head_dim"), (page, "page")))
         self.store = store
         self._desc = N.CacheDesc(self.dtype, N.STORE[store], kv_heads, head_dim, page)
-        self._geometry = (self.dtype, store, kv_heads, head_dim, page)
+        self._geometry = (self.dtype, store, kv_heads, head_dim, page, device)
         self._io = N.CacheIO()  # one call's arguments: filled anew by every call
         self._io_ref = ctypes.byref(self._io)
 
     def _fill(self, cache, table, past, tokens, offsets):
-        """The tensors' C argument; returns the tensors themselves."""
-        io, i32 = self._io, self._torch.int32
-        if table.dim() != 2:
-            raise ValueError(f"table has shape {tuple(table.shape)}, not (seqs, width)")
+        """The C argument of a call."""
+        io, i32, device = self._io, self._torch.int32, self.device
         seqs, width = table.shape
-        io.table_stride, io.table = self._rows(table, "table", seqs, width, i32), table.data_ptr()
+        if table.dtype is i32 and table.get_device() == device and (table.stride(1) == 1 or width <= 1):
+            io.table_stride, io.table = table.stride(0) if seqs > 1 else width, table.data_ptr()
+        else:
+            raise ValueError(f"table is not an int32 tensor of contiguous rows on {self._dev}")
         io.past = _list(self, past, "past", seqs)
         io.offsets = None if offsets is None else _list(self, offsets, "offsets", seqs + 1)
-        io.seqs, io.width, io.tokens, io.pages = seqs, width, tokens, cache.pages
-        io.k, io.v = cache.k.data_ptr(), cache.v.data_ptr()
-        scales = cache.k_scale, cache.v_scale
-        if scales[0] is not None:
-            io.k_scale, io.v_scale = scales[0].data_ptr(), scales[1].data_ptr()
-        return (table, past, offsets, cache.k, cache.v, *scales)
+        io.seqs, io.width, io.tokens = seqs, width, tokens
+        if cache is not self:
+            io.pages, io.k, io.v, io.k_scale, io.v_scale = cache._memory
 
 
 class KVCache(_Paged):
@@ -141,7 +139,7 @@ class KVCache(_Paged):
         p = ctypes.c_void_p()
         N.check(self.lib.sn_cache_create(ctypes.byref(self._desc), device, ctypes.byref(p)))
         self._op = p
-        self.k = self.v = self.k_scale = self.v_scale = None
+        self._tensors, self._memory = (None,) * 4, (pages, None, None, None, None)
         if device >= 0:
             torch, i8 = self._torch, store == "i8"
 
@@ -149,17 +147,24 @@ class KVCache(_Paged):
                 return torch.zeros(pages, kv_heads, *shape, dtype=kind, device=self._dev)
 
             kind = torch.int8 if i8 else self.torch_dtype
-            self.k, self.v = zeros(page, head_dim, kind=kind), zeros(page // 16, head_dim, 16, kind=kind)
-            if i8:
-                self.k_scale, self.v_scale = zeros(page, kind=torch.float32), zeros(page, kind=torch.float32)
+            scales = [zeros(page, kind=torch.float32) if i8 else None for _ in range(2)]
+            self._tensors = (zeros(page, head_dim, kind=kind), zeros(page // 16, head_dim, 16, kind=kind), *scales)
+            self._memory = (pages, *(None if t is None else t.data_ptr() for t in self._tensors))
+        io = self._io
+        io.pages, io.k, io.v, io.k_scale, io.v_scale = self._memory
+
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_scale = property(lambda self: self._tensors[2])
+    v_scale = property(lambda self: self._tensors[3])
 
     def write(self, k, v, table, past, offsets=None, stream=None):
         """Enqueue the writing of the packed rows k, v [tokens, kv_heads * head_dim] to their places."""
         tokens, n = k.shape[0], self.kv_heads * self.head_dim
         ks, vs = self._rows(k, "k", tokens, n, self.torch_dtype), self._rows(v, "v", tokens, n, self.torch_dtype)
-        tensors = self._fill(self, table, past, tokens, offsets)
+        self._fill(self, table, past, tokens, offsets)
         side = None if stream is None else self._side(stream)
-        st = self._current(self.device) if side is None else self._stream(side, (k, v, *tensors))
+        st = self._current(self.device) if side is None else self._stream(side, (k, v, table, past, offsets, *self._tensors))
         rc = self.lib.sn_cache_write(self._op, self._io_ref, k.data_ptr(), ks, v.data_ptr(), vs, st)
         if rc:
             N.check(rc)
@@ -167,16 +172,16 @@ class KVCache(_Paged):
     def read(self, table, past, tokens, offsets=None, k_out=None, v_out=None, stream=None):
         """Enqueue the reading of the same places; returns (k, v) [tokens, kv_heads * head_dim]."""
         n, kind, at, outs = self.kv_heads * self.head_dim, self.torch_dtype, [], []
-        tensors = self._fill(self, table, past, tokens, offsets)
+        self._fill(self, table, past, tokens, offsets)
         side = None if stream is None else self._side(stream)
         for out, name in ((k_out, "k_out"), (v_out, "v_out")):
             if out is None:
-                out = self.k.new_empty((tokens, n), dtype=kind) if side is None else self._new(self.k, (tokens, n), kind, side)
+                out = past.new_empty((tokens, n), dtype=kind) if side is None else self._new(past, (tokens, n), kind, side)
                 at += [out.data_ptr(), n]
             else:
                 at += [out.data_ptr(), self._rows(out, name, tokens, n, kind)]
             outs.append(out)
-        st = self._current(self.device) if side is None else self._stream(side, (*outs, *tensors))
+        st = self._current(self.device) if side is None else self._stream(side, (*outs, table, past, offsets, *self._tensors))
         rc = self.lib.sn_cache_read(self._op, self._io_ref, *at, st)
         if rc:
             N.check(rc)
@@ -210,17 +215,18 @@ class Attention(_Paged):
 
     def _call(self, f, q, cache, table, past, offsets, out, stream):
         if cache._geometry != self._geometry:
-            raise ValueError(f"the cache holds {cache._geometry}, the handle {self._geometry}")
+            raise ValueError(f"the cache is of (dtype, store, kv_heads, head_dim, page, device) {cache._geometry}, "
+                             f"the handle of {self._geometry}")
         tokens, n, kind = q.shape[0], self._n, self.torch_dtype
         qs = self._rows(q, "q", tokens, n, kind)
-        tensors = self._fill(cache, table, past, tokens, offsets)
+        self._fill(cache, table, past, tokens, offsets)
         side = None if stream is None else self._side(stream)
         if out is None:
             out = q.new_empty((tokens, n)) if side is None else self._new(q, (tokens, n), kind, side)
             ys = n
         else:
             ys = self._rows(out, "out", tokens, n, kind)
-        st = self._current(self.device) if side is None else self._stream(side, (q, out, *tensors))
+        st = self._current(self.device) if side is None else self._stream(side, (q, out, table, past, offsets, *cache._tensors))
         rc = f(self._op, self._io_ref, q.data_ptr(), qs, out.data_ptr(), ys, st)
         if rc:
             N.check(rc)

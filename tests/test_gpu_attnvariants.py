@@ -1,0 +1,168 @@
+"""What the attention operators' kernels do for large calls, at small cost: more
+sequences than a wave looks at, parts that hold several sequences and sequences in
+several parts, more tiles than are split, caches beyond 2^32 bytes, other streams,
+captured calls, calls on another stream's tensors."""
+
+import numpy as np
+import pytest
+
+from paper_2110_06037_amd import Attention, HeadNorm, KVCache
+from tests.attn_util import Paged, assert_attention, attend, i32
+from tests.seq_util import device, host, rounded
+from tests.test_gpu_attention import run_case
+from tests.test_gpu_kvcache import check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("seqs", [63, 64, 65, 130, 400])
+def test_many_sequences(store, seqs):
+    r = np.random.default_rng(seqs)
+    past = [int(n) for n in r.integers(-1, 150, seqs)]
+    run_case("bf16", store, 4, 2, 16, 16, [1] * seqs, past, step=True, seed=seqs)
+    lens = [int(n) for n in r.integers(0, 9, seqs)]
+    run_case("f16", store, 4, 2, 16, 16, lens, [max(0, p) for p in past], seed=seqs)
+    check("bf16", store, 2, 16, 16, lens, [max(0, p) for p in past], seed=seqs)
+
+
+@pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_parts_that_hold_several_sequences(dtype, store):
+    # 64 key heads leave few workgroups for each: their parts begin and end inside sequences
+    r = np.random.default_rng(2)
+    for past in ([2000, 3, 0, 700, 64, -1, 128, 1500, 31], [int(n) for n in r.integers(0, 300, 90)], [5000], [63] * 20):
+        run_case(dtype, store, 64, 64, 8, 16, [1] * len(past), past, step=True)
+        run_case(dtype, store, 64, 64, 8, 16, [1] * len(past), past, step=True, window=100)
+    # and with one key head a long sequence is in many parts
+    run_case(dtype, store, 17, 1, 8, 16, [1, 1, 1], [60000, 7, 2500], step=True)
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "same"), ("f16", "i8"), ("f32", "same")])
+def test_more_tiles_than_are_split(dtype, store):
+    run_case(dtype, store, 64, 64, 8, 16, [700, 3, 129], [0, 50, 64])
+    run_case(dtype, store, 300, 300, 8, 32, [200], [0])
+
+
+@pytest.mark.parametrize("page", [16, 64])
+def test_long_prompts_after_long_pasts(page):
+    for dtype, store in (("bf16", "same"), ("bf16", "i8"), ("f32", "i8")):
+        run_case(dtype, store, 2, 1, 128, page, [300], [5000])
+        run_case(dtype, store, 8, 1, 64, page, [33, 5], [3000, 4097])
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "same"), ("f32", "same"), ("f16", "i8")])
+def test_caches_beyond_32_bits(dtype, store):
+    # K and V of more than 2^32 bytes each, used at their far end
+    import torch
+    kv, dim, page = 8, 128, 1024
+    e = {"bf16": 2, "f32": 4, "f16": 1}[dtype]
+    pages = (1 << 32) // (kv * dim * page * e) + 40
+    cache = KVCache(dtype, kv, dim, pages, page=page, store=store)
+    assert cache.k.numel() * cache.k.element_size() > 1 << 32
+    table, past = i32([[pages - 1, pages - 30]]), i32([0])
+    r = np.random.default_rng(3)
+    k, v = (rounded(r.standard_normal((1100, kv * dim)), dtype) for _ in range(2))
+    cache.write(device(k, dtype), device(v, dtype), table, past)
+    back = [host(t) for t in cache.read(table, past, 1100)]
+    if store == "same":
+        assert np.array_equal(back[0], k) and np.array_equal(back[1], v)
+    small = KVCache(dtype, kv, dim, 2, page=page, store=store)
+    near = i32([[0, 1]])
+    small.write(device(k, dtype), device(v, dtype), near, past)
+    assert all(np.array_equal(a, host(b)) for a, b in zip(back, small.read(near, past, 1100)))
+    op = Attention(dtype, 8, kv, dim, page=page, store=store, max_tokens=60)
+    q = device(rounded(r.standard_normal((60, 8 * dim)), dtype), dtype)
+    assert torch.equal(op.run(q, cache, table, i32([1040])), op.run(q, small, near, i32([1040])))
+    assert torch.equal(op.step(q[:1], cache, table, i32([1099])), op.step(q[:1], small, near, i32([1099])))
+
+
+def head_norm():
+    import torch
+    op = HeadNorm("bf16", 8, 2, 64)
+    q, k, pos = torch.randn(64, 512, device="cuda").bfloat16(), torch.randn(64, 128, device="cuda").bfloat16(), i32(np.arange(64))
+    return lambda **kw: op.run(q, k, pos, **kw)
+
+
+def cache_read():
+    p = Paged("bf16", "i8", 2, 64, 16, [300])
+    return lambda **kw: p.cache.read(p.table, i32([0]), 300, **kw)
+
+
+def attention_run():
+    import torch
+    p = Paged("bf16", "same", 2, 64, 16, [300])
+    op = Attention("bf16", 8, 2, 64, page=16, max_tokens=100)
+    q, past = torch.randn(100, 512, device="cuda").bfloat16(), i32([200])
+    return lambda **kw: (op.run(q, p.cache, p.table, past, **kw),)
+
+
+def attention_step():
+    import torch
+    p = Paged("bf16", "same", 2, 64, 16, [300] * 4)
+    op = Attention("bf16", 8, 2, 64, page=16, max_seqs=4)
+    q, past = torch.randn(4, 512, device="cuda").bfloat16(), i32([299, 5, 77, 150])
+    return lambda **kw: (op.step(q, p.cache, p.table, past, **kw),)
+
+
+@pytest.mark.parametrize("make", [head_norm, cache_read, attention_run, attention_step])
+@pytest.mark.parametrize("pointer", [False, True])
+def test_outputs_on_another_stream(make, pointer):
+    # they do not lie in memory that work queued on the current stream still uses
+    import torch
+    run = make()
+    want = run()
+    big = torch.empty(1 << 28, device="cuda")
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    run(stream=s)
+    torch.cuda.synchronize()
+    blocks = [torch.empty_like(t) for t in want for _ in range(8)]
+    for _ in range(20):
+        big.zero_()
+    for b in blocks:
+        b.fill_(7)
+    used = {b.data_ptr() for b in blocks}
+    del b, blocks
+    got = run(stream=s.cuda_stream if pointer else s)
+    assert not used & {t.data_ptr() for t in got}
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("store", ["same", "i8"])
+def test_captured_calls(store):
+    # all operators in one graph, replayed with other inputs and positions, against eager calls
+    import torch
+    n, kv, dim = 3, 2, 64
+    p = Paged("bf16", store, kv, dim, 16, [400, 40, 90])
+    q = Paged("bf16", store, kv, dim, 16, [400, 40, 90])
+    norm, op = HeadNorm("bf16", 8, kv, dim), Attention("bf16", 8, kv, dim, page=16, store=store, max_seqs=n, max_tokens=30)
+    rows = torch.randn(30, (8 + 2 * kv) * dim, device="cuda").bfloat16()
+    past, offsets = i32([300, 0, 17]), i32([0, 3, 20, 30])
+    pos = i32(np.arange(30))
+
+    def call(c):
+        x = rows.clone()
+        a, b = norm.run(x[:, :512], x[:, 512:640], pos)
+        c.cache.write(b, x[:, 640:], c.table, past, offsets=offsets)
+        y = op.run(a, c.cache, c.table, past, offsets=offsets)
+        z = op.step(a[:n], c.cache, c.table, past)
+        return (y, z, *c.cache.read(c.table, past, 30, offsets=offsets))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(p)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        outs = call(p)
+    for i in range(5):
+        rows.copy_(torch.randn_like(rows.float()))
+        past.copy_(i32([300 - 50 * i, 10 * (i % 2), 17 + i]))
+        pos.add_(1000 * i)
+        graph.replay()
+        got = [t.clone() for t in outs]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, call(q)))

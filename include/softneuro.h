@@ -685,10 +685,10 @@ typedef struct {
   int32_t store;    /* sn_store */
   int32_t kv_heads; /* 1 .. 4096 */
   int32_t head_dim; /* a multiple of 8, 8 .. 256 */
-  int32_t page;     /* positions in a page: a power of two, 16 .. 4096 */
+  int32_t page;     /* positions in a page: a power of two, 16 .. 4096; its bytes below 2^31 */
 } sn_cache_desc;
 typedef struct {
-  int64_t pages; /* below 2^31 */
+  int64_t pages; /* below 2^31, pages * kv_heads * page below 2^40 */
   void* k;       /* 16-byte aligned */
   void* v;
   float* k_scale; /* null unless SN_STORE_I8 */
@@ -717,9 +717,14 @@ int sn_cache_read(sn_op* op, const sn_cache_io* io, void* k, int64_t k_stride, v
  * A row that sees no position is zeros.  What lies in places that a row does
  * not see, infinities and NaN included, does not touch it.
  *
- * sn_attn_run takes any number of rows per sequence; sn_attn_step one each
- * (tokens = seqs, offsets null).  A handle's calls share its workspace: they
- * must follow each other on one stream.                                    */
+ * Scores, maxima, weights and sums are float32.  With 16-bit types a prompt's weights are
+ * rounded once, to dtype, before they meet v; a step's keep 16 bits (11 with f16
+ * caches).  A row's result does not depend on the other rows of the call.
+ *
+ * sn_attn_run takes any number of rows per sequence, up to
+ * (tokens * heads / kv_heads / 128 + seqs) * kv_heads < 2^24; sn_attn_step one each
+ * (tokens = seqs, offsets null; seqs * (width * page + 64) below 2^35).  A handle's calls share
+ * its workspace: they must follow each other on one stream.                */
 typedef struct {
   sn_cache_desc cache;
   int32_t heads;  /* a multiple of kv_heads, at most 65535 */

@@ -62,6 +62,8 @@ class HeadNorm(_Op):
         """Enqueue on q [tokens, heads * head_dim], k [tokens, kv_heads * head_dim]
         (None where the handle has no such heads) and positions (int32 device
         tensor [tokens]); returns (q_out, k_out), which may be q and k."""
+        if q is None and k is None:
+            raise ValueError("neither q nor k is given")
         tokens, kind = (k if q is None else q).shape[0], self.torch_dtype
         side = None if stream is None else self._side(stream)
         at = [0] * 8

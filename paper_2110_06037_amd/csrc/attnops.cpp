@@ -35,6 +35,8 @@ k::CacheArgs cache_of(const sn_cache_desc& d) {
   k::CacheArgs c{};
   c.dtype = d.dtype, c.i8 = d.store == SN_STORE_I8, c.kv_heads = d.kv_heads, c.dim = d.head_dim;
   while ((1 << c.shift) < d.page) ++c.shift;
+  // (places within a page are 32-bit offsets)
+  if ((int64_t)d.kv_heads * d.page * d.head_dim * (c.i8 ? 1 : dtype_size(d.dtype)) >> 31) fail(SN_E_UNSUPPORTED, "a page of 2^31 bytes or more");
   return c;
 }
 
@@ -51,6 +53,7 @@ k::CacheArgs cache_args(k::CacheArgs c, const sn_cache_io* io, bool step) {
   if (step && (io->tokens != io->seqs || io->offsets)) fail(SN_E_SHAPE, "a step takes one token per sequence");
   if (io->seqs && !io->offsets && io->tokens % io->seqs) fail(SN_E_SHAPE, "tokens are no multiple of seqs, and there are no offsets");
   if (io->pages < 0 || io->pages >> 31) fail(SN_E_SHAPE, "pages must be in 0..2^31 - 1");
+  if ((io->pages * c.kv_heads << c.shift) >> 40) fail(SN_E_SHAPE, "more than 2^40 rows of heads in the cache");
   if (io->width < 0 || ((int64_t)io->width << c.shift) > k::kMaxPositions) fail(SN_E_SHAPE, "width * page must be in 0..2^29");
   if (io->pages && (!io->k || !io->v || (c.i8 && (!io->k_scale || !io->v_scale)))) fail(SN_E_INVALID, "the cache's memory is null");
   if (!c.i8 && (io->k_scale || io->v_scale)) fail(SN_E_INVALID, "scales given to a cache without them");
@@ -100,7 +103,7 @@ int attn_call(sn_op* p, const sn_cache_io* io, const void* q, int64_t q_stride, 
     a.qs = check_rows(q, q_stride, a.c.tokens, n, a.c.dtype, "q");
     a.ys = check_rows(y, y_stride, a.c.tokens, n, a.c.dtype, "y");
     if (!step && k::attn_run_tiles(a) * a.c.kv_heads >> 24) fail(SN_E_UNSUPPORTED, "tokens * heads above 2^31 - 128 * seqs * kv_heads");
-    if (step && !k::step_keys_fit(a.c)) fail(SN_E_UNSUPPORTED, "seqs * width * page of a step above 2^36 - 2^6 seqs");
+    if (step && !k::step_keys_fit(a.c)) fail(SN_E_UNSUPPORTED, "seqs * (width * page + 64) of a step not below 2^35");
     need_device(op);
     if (!a.c.tokens) return;
     const int e = dtype_size(a.c.dtype);

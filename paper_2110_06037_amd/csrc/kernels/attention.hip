@@ -4,7 +4,7 @@
 namespace sn {
 namespace k {
 
-bool step_keys_fit(const CacheArgs& c) { return c.seqs * ((((int64_t)c.width << c.shift) >> 5) + 2) < (int64_t(1) << 31); }
+bool step_keys_fit(const CacheArgs& c) { return c.seqs * ((((int64_t)c.width << c.shift) >> 5) + 2) < (int64_t(1) << 30); }
 
 int64_t attn_run_tiles(const AttnArgs& a) {
   const int each = a.heads / a.c.kv_heads;

@@ -83,7 +83,7 @@ struct AttnArgs {
   FastDiv each;   // by the query heads of a key head
 };
 int64_t attn_run_tiles(const AttnArgs& a);  // bound of a prompt call's tiles of rows, per key head
-bool step_keys_fit(const CacheArgs& c);  // the keys of a step's sequences, in blocks of 32, are below 2^31
+bool step_keys_fit(const CacheArgs& c);  // the keys of a step's sequences, in blocks of 32, are below 2^30
 void attn_workspace(const AttnArgs& a, int64_t& o, int64_t& m, int64_t& counts);
 void attn_run(AttnArgs a, hipStream_t st);
 void attn_step(AttnArgs a, hipStream_t st);

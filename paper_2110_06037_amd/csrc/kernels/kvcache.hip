@@ -266,7 +266,8 @@ static void launch_rows(CacheRows& a, hipStream_t st) {
   // Tiles of 16 positions for many rows of few sequences, single rows by waves.  (Written
   // and read back, 8 heads of 128 in 8 bits: 8 sequences of 16 rows 9.4 us by tiles, 6.3 by
   // rows; of 64 rows 10.1 and 10.9; of 512 rows 22 and 51; 64 of one row 12.4 and 5.7.)
-  if (c.tokens >= 4 * (int64_t)c.seqs && c.tokens * c.kv_heads >= 4096) {
+  // Not for very many sequences: every workgroup counts tiles over them.
+  if (c.tokens >= 4 * (int64_t)c.seqs && c.tokens * c.kv_heads >= 4096 && c.seqs <= 512) {
     const int64_t tiles = c.tokens / 16 + 2 * (int64_t)c.seqs;
     a.lanes = 1;
     while (a.lanes < c.dim / 8) a.lanes *= 2;

@@ -97,14 +97,18 @@ class _Block:
 class _AttentionBlock:
     attends = True
 
-    def __init__(self, dtype, w, next_norm, max_seqs, max_tokens, device, eps):
+    def __init__(self, dtype, w, next_norm, max_seqs, max_tokens, device, eps, shared):
         c = w["config"]
         heads, kv, dim = c["heads"], c["kv_heads"], c["head_dim"]
         self.page, self.nq, self.nk = c["page"], heads * dim, kv * dim
         self.in_proj = Linear4(dtype, *w["in_proj"][:2], zero=w["in_proj"][2], cols=c["dim"], group=c["group"], device=device)
         self.head_norm = HeadNorm(dtype, heads, kv, dim, w["q_norm"], w["k_norm"], eps=eps, rot=c["rot"], base=c["base"], device=device)
-        self.attention = Attention(dtype, heads, kv, dim, page=c["page"], store=c["store"], window=c["window"], max_seqs=max_seqs,
-                                   max_tokens=max_tokens, device=device)
+        # (it has no weights: one handle, and so one workspace, for all blocks that are alike)
+        alike = (heads, kv, dim, c["page"], c["store"], c["window"])
+        if alike not in shared:
+            shared[alike] = Attention(dtype, heads, kv, dim, page=c["page"], store=c["store"], window=c["window"],
+                                      max_seqs=max_seqs, max_tokens=max_tokens, device=device)
+        self.attention = shared[alike]
         self.out_proj = Linear4(dtype, *w["out_proj"][:2], zero=w["out_proj"][2], cols=self.nq, group=c["group"], device=device)
         self.join = BlockNorm(dtype, c["dim"], pre=next_norm, scale=w["scale"], residual="f32", eps=eps, device=device)
         self.new_cache = lambda pages: KVCache(dtype, kv, dim, pages, page=c["page"], store=c["store"], device=device)
@@ -178,8 +182,10 @@ class SequenceNet:
         blocks = weights["blocks"]
         self.device, self.closed = device, False
         self.first = BlockNorm(dtype, blocks[0]["config"]["dim"], pre=weights["norm"], eps=eps, device=device)
-        self.blocks = [(_AttentionBlock if w["config"].get("kind") == "attention" else _Block)(
-            dtype, w, w["norm"], max_seqs, max_tokens, device, eps) for w in blocks]
+        shared = {}
+        self.blocks = [_AttentionBlock(dtype, w, w["norm"], max_seqs, max_tokens, device, eps, shared)
+                       if w["config"].get("kind") == "attention" else
+                       _Block(dtype, w, w["norm"], max_seqs, max_tokens, device, eps) for w in blocks]
 
     def close(self):
         self.closed = True

@@ -77,6 +77,7 @@ def test_cache_creation_refusals():
     assert code(lambda: make(dim=0)) == -2 and code(lambda: make(dim=12)) == -4 and code(lambda: make(dim=264)) == -4
     for page in (0, 8, 24, 8192, -16):
         assert code(lambda: make(page=page)) == -2
+    assert code(lambda: make(kv=4096, dim=256, page=4096)) == -4     # a page of 2^33 bytes
     assert code(lambda: make(device=-2)) == -1
     for wrong in (dict(pages=-1), dict(pages=1 << 31), dict(dim=1 << 33)):
         with pytest.raises(ValueError):
@@ -113,6 +114,9 @@ def test_cache_and_attention_run_refusals(store):
     cache = KVCache("bf16", 2, 64, 4, page=16, store=store, device=-1)
     attn = Attention("bf16", 4, 2, 64, page=16, store=store, max_seqs=3, max_tokens=100, device=-1)
 
+    wide = KVCache("bf16", 64, 64, 4, page=64, store=store, device=-1)   # 2^42 rows in 2^30 pages
+    wide_attn = Attention("bf16", 64, 64, 64, page=64, store=store, max_seqs=3, max_tokens=100, device=-1)
+
     def call(f, op=None, a=p, a_s=256, b=p, b_s=256, **kw):
         io = N.CacheIO()
         o = dict(pages=4, k=p, v=p, k_scale=s, v_scale=s, seqs=2, width=4, table=p, table_stride=4, past=p, tokens=2, offsets=None)
@@ -128,6 +132,7 @@ def test_cache_and_attention_run_refusals(store):
         assert call(f, seqs=-1) == -2 and call(f, seqs=65536) == -2 and call(f, tokens=-1) == -2
         assert call(f, tokens=(1 << 26) + 1) == -2 and call(f, seqs=0) == -2
         assert call(f, pages=-1) == -2 and call(f, pages=1 << 31) == -2
+        assert call(f, pages=1 << 30) == -5 and call(f, pages=1 << 30, op=wide if least == 128 else wide_attn, a_s=1 << 19, b_s=1 << 19) == -2
         assert call(f, width=-1) == -2 and call(f, width=(1 << 26) + 1) == -2
         assert call(f, k=None) == -1 and call(f, v=None) == -1 and call(f, k=p + 8) == -1 and call(f, v=p + 2) == -1
         assert call(f, pages=0, k=None, v=None) == -5
@@ -147,6 +152,11 @@ def test_cache_and_attention_run_refusals(store):
     assert call(L.sn_attn_run, tokens=102) == -2 and call(L.sn_attn_run, tokens=100) == -5
     for f in (L.sn_cache_write, L.sn_cache_read, L.sn_attn_run):
         assert call(f, tokens=3) == -2 and call(f, tokens=3, offsets=p) == -5 and call(f, tokens=3, offsets=p + 2) == -1
+    many = Attention("bf16", 4, 2, 64, page=16, store=store, max_seqs=65535, device=-1)
+    assert call(L.sn_attn_step, op=many, seqs=65535, tokens=65535, width=1 << 15, table_stride=0) == -4
+    assert call(L.sn_attn_step, op=many, seqs=65535, tokens=65535, width=1 << 14, table_stride=0) == -5
+    lots = Attention("bf16", 65535, 1, 64, page=16, store=store, max_tokens=1 << 20, device=-1)
+    assert call(L.sn_attn_run, op=lots, seqs=1, tokens=(1 << 15) + 2, a_s=1 << 23, b_s=1 << 23) == -4
     assert call(L.sn_attn_step, tokens=4) == -2 and call(L.sn_attn_step, offsets=p) == -2
 
 

@@ -151,6 +151,27 @@ def test_values_that_are_not_finite_stay_where_they_are(dtype, store):
             assert np.isfinite(host(op.run(q, p.cache, p.table, i32([149])))).all()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_a_row_does_not_depend_on_its_neighbours(dtype):
+    import torch
+    p = Paged(dtype, "same", 2, 64, 16, [300] * 3)
+    op = Attention(dtype, 8, 2, 64, page=16, max_seqs=3, max_tokens=300)
+    q = torch.randn(300, 512, device="cuda").to(p.cache.torch_dtype)
+    bad = q.clone()
+    bad[7, 70], bad[40, 500], bad[299] = float("nan"), float("inf"), 1e4
+    past = i32([200] * 3)
+    a, b = op.run(q, p.cache, p.table, past), op.run(bad, p.cache, p.table, past)
+    keep = torch.ones(300, 8, dtype=torch.bool, device="cuda")
+    keep[7, 1] = keep[40, 7] = False
+    keep[299] = False
+    assert torch.equal(a.view(300, 8, 64)[keep], b.view(300, 8, 64)[keep])
+    assert torch.isnan(b.view(300, 8, 64)[7, 1]).all()
+    a, b = (op.step(t[[6, 7, 8]], p.cache, p.table, past) for t in (q, bad))
+    keep = torch.ones(3, 8, dtype=torch.bool, device="cuda")
+    keep[1, 1] = False
+    assert torch.equal(a.view(3, 8, 64)[keep], b.view(3, 8, 64)[keep]) and torch.isnan(b.view(3, 8, 64)[1, 1]).all()
+
+
 def test_rows_behind_the_last_sequence_are_left_alone():
     import torch
     p = Paged("bf16", "same", 1, 64, 16, [20, 9])

@@ -66,28 +66,29 @@ class HeadNorm(_Op):
             raise ValueError("neither q nor k is given")
         tokens, kind = (k if q is None else q).shape[0], self.torch_dtype
         side = None if stream is None else self._side(stream)
-        at = [0] * 8
-        outs = []
-        for i, (x, out, n, name) in enumerate(((q, q_out, self._nq, "q"), (k, k_out, self._nk, "k"))):
-            if x is None:
-                if n:
-                    raise ValueError(f"{name} is missing")
-                outs.append(None)
-                continue
-            at[2 * i], at[2 * i + 1] = x.data_ptr(), self._rows(x, name, tokens, n, kind)
-            if out is None:
-                out = x.new_empty((tokens, n)) if side is None else self._new(x, (tokens, n), kind, side)
-                at[5 + 2 * i] = n
+        qp = qs = kp = ks = qo = qos = ko = kos = 0
+        if q is not None:
+            nq = self._nq
+            qp, qs = q.data_ptr(), self._rows(q, "q", tokens, nq, kind)
+            if q_out is None:
+                q_out, qos = q.new_empty((tokens, nq)) if side is None else self._new(q, (tokens, nq), kind, side), nq
             else:
-                at[5 + 2 * i] = self._rows(out, name + "_out", tokens, n, kind)
-            at[4 + 2 * i] = out.data_ptr()
-            outs.append(out)
+                qos = self._rows(q_out, "q_out", tokens, nq, kind)
+            qo = q_out.data_ptr()
+        if k is not None:
+            nk = self._nk
+            kp, ks = k.data_ptr(), self._rows(k, "k", tokens, nk, kind)
+            if k_out is None:
+                k_out, kos = k.new_empty((tokens, nk)) if side is None else self._new(k, (tokens, nk), kind, side), nk
+            else:
+                kos = self._rows(k_out, "k_out", tokens, nk, kind)
+            ko = k_out.data_ptr()
         pos = None if positions is None else _list(self, positions, "positions", tokens)
-        st = self._current(self.device) if side is None else self._stream(side, (q, k, positions, *outs))
-        rc = self._run(self._op, tokens, pos, *at, st)
+        st = self._current(self.device) if side is None else self._stream(side, (q, k, positions, q_out, k_out))
+        rc = self._run(self._op, tokens, pos, qp, qs, kp, ks, qo, qos, ko, kos, st)
         if rc:
             N.check(rc)
-        return outs[0], outs[1]
+        return q_out, k_out
 
 
 def _list(op, t, name, n):

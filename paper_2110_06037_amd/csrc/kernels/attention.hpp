@@ -546,9 +546,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   // heads next to each other: workgroups of one head go to one XCD where 8 divides
   // their number.  The last tiles, which see the most keys, first.
   const int head = blockIdx.x % c.kv_heads, tiles = gridDim.x / c.kv_heads, tile = tiles - 1 - blockIdx.x / c.kv_heads;
-  int b, t, row0, n;
-  if (!find_rows(c, tile, [&](int, int rows) { return ((int64_t)rows * each + kRunRows - 1) / kRunRows; }, b, t, row0, n)) return;
-  const int past = uniform(min(c.past[b], kMaxPast));
+  int b, t, row0, n, past;
+  if (!find_rows(c, tile, [&](int rows, int) { return ((int64_t)rows * each + kRunRows - 1) / kRunRows; }, b, t, row0, n, past)) return;
   const int rows = n * each, mine = t * kRunRows + 32 * wave + r;  // (below 2^31: the launcher's tiles)
   const int rr = min(mine, rows - 1);  // rows behind the last one repeat it and are not stored
   const int token = fdiv(rr, a.each), qh = head * each + rr - token * each;

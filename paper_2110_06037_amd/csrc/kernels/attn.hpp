@@ -114,19 +114,18 @@ __device__ __forceinline__ int seq_of(const CacheArgs& c, int64_t row) {
   return c.offsets[lo] <= row && row < c.offsets[lo + 1] ? lo : -1;
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-// Units of work are counted over the sequences in order, count(b, rows) of each: the
-// sequence behind the number `unit`, the unit's number in it, and the sequence's rows.
+// Units of work are counted over the sequences in order, count(rows, past) of each: the
+// sequence behind the number `unit`, the unit's number in it, the sequence's rows and past.
 // (Every wave for itself, 64 sequences at a time.)  False: there are fewer units.
 template <typename F>
-__device__ __forceinline__ bool find_rows(const CacheArgs& c, int64_t unit, F count, int& b, int& at, int& first, int& rows) {
+__device__ __forceinline__ bool find_rows(const CacheArgs& c, int64_t unit, F count, int& b, int& at, int& first, int& rows, int& past) {
   const int lane = threadIdx.x & 63;
   int64_t before = 0;
   for (int base = 0; base < c.seqs; base += 64) {
-    int64_t lo = 0, hi = 0, own = 0;
-    if (base + lane < c.seqs) {
-      seq_rows(c, base + lane, lo, hi);
-      own = count(base + lane, (int)(hi - lo));
-    }
+    int64_t lo, hi;
+    const int own_past = min(c.past[min(base + lane, c.seqs - 1)], kMaxPast);
+    seq_rows(c, min(base + lane, c.seqs - 1), lo, hi);
+    const int64_t own = base + lane < c.seqs ? count((int)(hi - lo), own_past) : 0;
     int64_t sum = own;
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) {
@@ -137,7 +136,7 @@ __device__ __forceinline__ bool find_rows(const CacheArgs& c, int64_t unit, F co
     if (in) {
       const int l = __ffsll(in) - 1;
       b = uniform(base + l), at = uniform((int)(unit - __shfl(before + sum - own, l)));
-      first = uniform((int)__shfl(lo, l)), rows = uniform((int)__shfl(hi - lo, l));
+      first = uniform(__shfl((int)lo, l)), rows = uniform(__shfl((int)(hi - lo), l)), past = uniform(__shfl(own_past, l));
       return true;
     }
     before += __shfl(sum, 63);
@@ -146,7 +145,7 @@ __device__ __forceinline__ bool find_rows(const CacheArgs& c, int64_t unit, F co
 }
 // How many groups of 16 positions `rows` rows after `past` lie in.
 __device__ __forceinline__ int rows_tiles(int past, int rows) {
-  const int p = min(max(past, 0), kMaxPast) & 15;
+  const int p = max(past, 0) & 15;
   return rows ? (p + rows + 15) >> 4 : 0;
 }
 // The page that holds a position of sequence b, -1 if none does.

@@ -141,9 +141,8 @@ __global__ __launch_bounds__(kTileThreads) void cache_tiles_kernel(CacheRows a) 
   E* te = reinterpret_cast<E*>(turn);
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, D = c.dim, chunks = D / 8;
-  int b, tile, first, n;
-  if (!find_rows(c, blockIdx.x, [&](int s, int rows) { return rows_tiles(c.past[s], rows); }, b, tile, first, n)) return;
-  const int past = min(c.past[b], kMaxPast);
+  int b, tile, first, n, past;
+  if (!find_rows(c, blockIdx.x, [&](int rows, int before) { return (int64_t)rows_tiles(before, rows); }, b, tile, first, n, past)) return;
   const int pos0 = (max(past, 0) & ~15) + 16 * tile;  // of the tile
   const int slot0 = pos0 & ((1 << c.shift) - 1);
   const bool whole = past >= 0 && pos0 >= past && pos0 + 16 <= past + n;

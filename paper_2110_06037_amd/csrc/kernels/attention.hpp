@@ -6,10 +6,28 @@
 // nothing moves between lanes but the maximum.  V lies in the cache with 16
 // positions of an element together, which is that product's operand.
 //
+// Scores, maxima, sums and outputs are float32; what is rounded besides the result are the
+// weights: in f16 to 11 bits, lifted by a power of two (LIFT) so that small ones stay normal numbers;
+// in bf16 by the step kernel to two bf16 parts, 16 bits, by the run kernel to one, 8 bits,
+// as large as a rounding of bf16 values themselves.  (The float32 sum l takes them unrounded.)
+//
 // attn_step_kernel: up to 16 query heads of one token; a wave reads K and V
-// straight into the operands of 16 x 16 products.
+// straight into the operands of 16 x 16 products, since every key is used once and LDS
+// would only be a detour.  Bound by the cache's bytes: 64 sequences of 2048 keys, 8 key heads of
+// 128 in bf16 101 us, 5.3 TB/s; up to 8192 keys 197 us, 5.4 TB/s; 32 heads without
+// groups 6.3 TB/s; in 8 bits 113 us, 4.6 TB/s, where turning codes into numbers
+// is as much work as the products.  Short ones are a chain of dependent steps: one
+// sequence of 4096 keys 11.2 us, of which launch and plan 3.5, queries and table 0.7, the
+// keys 3.0, joining the waves 0.7, storing the part and counting it 1.7, joining the parts 2.3.
 // attn_run_kernel: 128 rows (a token's query heads of one key head are
-// neighbours), a wave 32 of them in 32 x 32 products, K and V through LDS.
+// neighbours), a wave 32 of them in 32 x 32 products, K and V through LDS, where the
+// four waves share them.  Bound by issue, matrix products first: 4096 rows of 32 heads, 8 key heads of 128 in
+// bf16, causal, 144 - 152 us, 137.5 GFLOP that count, 905 - 955 TFLOP/s, a library product of
+// 8192^3 1206.  Without its loads it takes 138 us, without its exponentials 139; two
+// waves a SIMD, whose registers hold no more, cover one's softmax with the other's
+// products.  Not faster (4096 rows, 162 us then): 32 keys a block and three waves a SIMD 171, a block's scores
+// taken beside the last one's softmax 180, a queue of tiles 192, tiles in another order 174.
+// Float32 goes through float32 products: 2048 rows 385 us, 89 TFLOP/s, the library's 154.
 #pragma once
 
 #include "attn.hpp"
@@ -131,9 +149,37 @@ __device__ __forceinline__ bool last_of(unsigned* count, unsigned n, int* shared
   return *shared;
 }
 
+// Parts joined in their order, eight at a time, all of whose numbers are in flight.
+struct Join {
+  float ms[8], ls[8], top = kNone, sum = 0.f;
+  f32x4 os[8], acc = {0.f, 0.f, 0.f, 0.f};
+  template <typename Get>
+  __device__ __forceinline__ void fetch(int first, int last, Get get) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) get(min(first + k, last), ms[k], ls[k], os[k]);
+  }
+  __device__ __forceinline__ void add(int first, int last) {
+    float now = top;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (first + k > last) ms[k] = kNone;
+      now = fmaxf(now, ms[k]);
+    }
+    const float f = __builtin_amdgcn_exp2f(top - some(now));
+    sum *= f, acc *= f, top = now;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float w = __builtin_amdgcn_exp2f(ms[k] - some(now));
+      if (first + k <= last) sum += w * ls[k], acc += w * os[k];
+    }
+  }
+};
+
 // ------------------------------------------------------------------ single tokens
 constexpr int kStepWaves = 4;
-constexpr int kStepLeast = 4;     // blocks of keys of a workgroup where there are workgroups enough: one a wave
+// Blocks of keys of a workgroup where there are workgroups enough: one a wave.  (One sequence of 4096
+// keys 11.2 us, with 2 blocks 13.2, with 8 11.9; 8 of 2048 16.5, 16.8, 19.9.)
+constexpr int kStepLeast = 4;
 constexpr int kStepUnits = 1024;  // bound of the workgroups per group of heads
 // Workgroups that the keys of all sequences are spread over: one a compute unit, two
 // where codes are turned into numbers.  (64 sequences of up to 8192 keys, 8 key heads of
@@ -435,31 +481,15 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
     for (int i = threadIdx.x; i < cols * chunks; i += 64 * kStepWaves) {
       const int r = i / chunks, d = 4 * (i % chunks);
       if (!EXACT && d >= D) continue;
-      float top = kNone, sum = 0.f;
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-      // eight parts at a time, all of their numbers in flight
+      Join parts;
       for (int u = unit0; u <= unit1; u += 8) {
-        float ms[8], ls[8], now = top;
-        f32x4 os[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int at = slot(min(u + k, unit1));
-          ms[k] = wm.get(at * 32 + r), ls[k] = wm.get(at * 32 + 16 + r), os[k] = wo.get4(at * (16 * DP) + r * DP + d);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          if (u + k > unit1) ms[k] = kNone;
-          now = fmaxf(now, ms[k]);
-        }
-        const float f = __builtin_amdgcn_exp2f(top - some(now));
-        sum *= f, acc *= f, top = now;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float w = __builtin_amdgcn_exp2f(ms[k] - some(now));
-          if (u + k <= unit1) sum += w * ls[k], acc += w * os[k];
-        }
+        parts.fetch(u, unit1, [&](int from, float& ms, float& ls, f32x4& os) {
+          const int at = slot(from);
+          ms = wm.get(at * 32 + r), ls = wm.get(at * 32 + 16 + r), os = wo.get4(at * (16 * DP) + r * DP + d);
+        });
+        parts.add(u, unit1);
       }
-      finish(r, d, acc, sum);
+      finish(r, d, parts.acc, parts.sum);
     }
   }
   p.start += (span.blocks + p.pad) & ~p.pad, ++p.b;
@@ -478,7 +508,24 @@ __device__ __forceinline__ float power_of(float s) {
   return __builtin_bit_cast(float, min(max(__builtin_bit_cast(unsigned, s) & 0x7f800000u, 0x33800000u), 0x43800000u));  // 2^-24 .. 2^8
 }
 constexpr int kRunRows = 128;
-constexpr int kRunParts = 512;  // workgroups that fewer tiles than half of it are split to
+// Workgroups that tiles are split to, along the keys, where they are no more than half of it: two a compute
+// unit, as many as run at once.  (256 rows after 8192 keys, 8 key heads, 8 parts each: 59 us in bf16, 70 in 8 bits;
+// to 256 workgroups 68 and 95, to 1024 73 and 81.)
+constexpr int kRunParts = 512;
+// How many parts a tile has: of four blocks each at least (512 rows, 8 blocks: 2 parts 17.9 us, 4
+// parts 22.6; 16 rows after 8192 keys, 129 blocks: 32 parts 19.9, 16 parts 22.0, 64 parts 22.8).
+inline int run_parts(int64_t blocks, int64_t wgs) {
+  if (2 * wgs > kRunParts) return 1;
+  return (int)std::max<int64_t>(1, std::min((kRunParts + wgs - 1) / wgs, blocks / 4));
+}
+// Few parts are joined by their tile's last workgroup, at 0.7 us a part, beside other tiles' work;
+// many by a launch of their own, about 6 us.  (2 parts 17.6 us by the last workgroup, 20.1 by a launch; 4
+// parts 22.2 and 24.3; 8 parts 58.2 and 53.0; 32 parts 35 and 19.7.)  Above 128 elements always by
+// a launch: the registers of the other way cost every call there (4096 rows of 256 elements 222 and 195 us).
+template <int DP>
+constexpr bool run_joins(int parts) {
+  return DP > 128 || parts >= 8;
+}
 template <typename T>
 constexpr int run_keys() {
   return sizeof(T) == 2 ? 64 : 32;
@@ -525,6 +572,13 @@ struct RunTile {
   static __device__ __forceinline__ int v_order(int d) { return sizeof(T) == 2 ? (d >> 3) & 1 : (d >> 2) & 3; }
   static __device__ __forceinline__ int v(int t16, int d, int g) { return (t16 * DP + d) * VG + (g ^ v_order(d)); }
 };
+
+// Where a thread's sums of 4 elements of a part lie, and its maximum and sum of weights.
+template <int DP>
+__device__ __forceinline__ int run_o_at(int slot, int i) {
+  return (slot * (DP / 8) + i) * 1024 + 4 * threadIdx.x;
+}
+__device__ __forceinline__ int run_m_at(int slot) { return slot * 512 + threadIdx.x; }
 
 template <typename T, bool I8, int DP, bool EXACT>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnArgs a) {
@@ -875,41 +929,41 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   l = sum_x32(l);
   __syncthreads();
 
-  if (gridDim.z > 1) {
-    // parts: left in the lanes' order, joined by the tile's last workgroup in the parts' order
+  if (gridDim.z > 1) {  // parts: left in the lanes' order
     const int parts = gridDim.z, slot = blockIdx.x * parts;
     const Shared wo(a.ws_o), wm(a.ws_m);
-    auto o_at = [&](int z, int i) { return ((slot + z) * (4 * ND) + i) * 1024 + 4 * tid; };
-    auto m_at = [&](int z) { return (slot + z) * 512 + tid; };
     if (t * kRunRows + 32 * wave < rows) {
 #pragma unroll
       for (int i = 0; i < ND; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          wo.put4(o_at(blockIdx.z, 4 * i + j), f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
-      wm.put(m_at(blockIdx.z), m), wm.put(m_at(blockIdx.z) + 256, l);
+          wo.put4(run_o_at<DP>(slot + blockIdx.z, 4 * i + j), f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
+      wm.put(run_m_at(slot + blockIdx.z), m), wm.put(run_m_at(slot + blockIdx.z) + 256, l);
     }
-    if (!last_of(a.count + blockIdx.x, parts, &flag[0])) return;
-    if (t * kRunRows + 32 * wave >= rows) return;  // (a wave without rows left nothing)
-    m = kNone;
+    if (run_joins<DP>(parts)) return;
+    if constexpr (!run_joins<DP>(2)) {  // joined by the tile's last workgroup in the parts' order
+      if (!last_of(a.count + blockIdx.x, parts, &flag[0])) return;
+      if (t * kRunRows + 32 * wave >= rows) return;  // (a wave without rows left nothing)
+      m = kNone;
 #pragma unroll 4
-    for (int z = 0; z < parts; ++z) m = fmaxf(m, wm.get(m_at(z)));
-    l = 0.f;
-#pragma unroll
-    for (int i = 0; i < ND; ++i)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-    for (int z = 0; z < parts; ++z) {
-      const float f = __builtin_amdgcn_exp2f(wm.get(m_at(z)) - some(m));
-      l += f * wm.get(m_at(z) + 256);
+      for (int z = 0; z < parts; ++z) m = fmaxf(m, wm.get(run_m_at(slot + z)));
+      l = 0.f;
 #pragma unroll
       for (int i = 0; i < ND; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4 v = wo.get4(o_at(z, 4 * i + j));
+        for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+      for (int z = 0; z < parts; ++z) {
+        const float f = __builtin_amdgcn_exp2f(wm.get(run_m_at(slot + z)) - some(m));
+        l += f * wm.get(run_m_at(slot + z) + 256);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) o[i][4 * j + x] += f * v[x];
-        }
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x4 v = wo.get4(run_o_at<DP>(slot + z, 4 * i + j));
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[i][4 * j + x] += f * v[x];
+          }
+      }
     }
   }
   if (mine >= rows) return;
@@ -925,6 +979,44 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
       for (int x = 0; x < 4; ++x) v[x] = from_f<T>(o[i][4 * j + x] * inv);
       if (EXACT || d < D) __builtin_memcpy(y + d, v, sizeof(v));
     }
+}
+
+// The parts of a tile joined in their order, 4 elements of 128 rows at a time, each tile by as
+// many workgroups as fill the chip.
+template <typename T, int DP, bool EXACT>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int parts) {
+  const CacheArgs& c = a.c;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
+  const int D = EXACT ? DP : c.dim, each = a.heads / c.kv_heads;
+  const int head = blockIdx.x % c.kv_heads, tile = gridDim.x / c.kv_heads - 1 - blockIdx.x / c.kv_heads;
+  int i = blockIdx.y;
+  auto get = [&](int z, float& ms, float& ls, f32x4& os) {
+    const int slot = blockIdx.x * parts + z;
+    ms = a.ws_m[run_m_at(slot)], ls = a.ws_m[run_m_at(slot) + 256];
+    os = *reinterpret_cast<const f32x4*>(a.ws_o + run_o_at<DP>(slot, i));
+  };
+  Join join;
+  join.fetch(0, parts - 1, get);  // (before it is known whether the tile has rows: there is room for all)
+  int b, t, row0, n, past;
+  if (!find_rows(c, tile, [&](int rows, int) { return ((int64_t)rows * each + kRunRows - 1) / kRunRows; }, b, t, row0, n, past)) return;
+  const int mine = t * kRunRows + 32 * wave + r, token = fdiv(min(mine, n * each - 1), a.each);
+  if (mine >= n * each) return;
+  T* y = static_cast<T*>(a.y) + (int64_t)(row0 + token) * a.ys + (int64_t)(head * each + mine - token * each) * D;
+  for (int z = 0;;) {
+    join.add(z, parts - 1);
+    z += 8;
+    if (z >= parts) {
+      const int d = 8 * i + 4 * h;
+      const float inv = join.sum == 0.f ? 0.f : 1.f / join.sum;
+      T v[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[x] = from_f<T>(join.acc[x] * inv);
+      if (EXACT || d < D) __builtin_memcpy(y + d, v, sizeof(v));
+      if ((i += gridDim.y) >= DP / 8) return;
+      join.top = kNone, join.sum = 0.f, join.acc = f32x4{0.f, 0.f, 0.f, 0.f}, z = 0;
+    }
+    join.fetch(z, parts - 1, get);
+  }
 }
 
 // ------------------------------------------------------------------ launches
@@ -947,9 +1039,9 @@ static void launch_run(AttnArgs& a, hipStream_t st) {
   constexpr int KB = run_keys<T>();
   const int64_t wgs = attn_run_tiles(a) * c.kv_heads, blocks = (((int64_t)c.width << c.shift) + KB - 1) / KB;
   a.each = make_fastdiv(a.heads / c.kv_heads);
-  int64_t parts = 1;
-  if (2 * wgs <= kRunParts) parts = std::max<int64_t>(1, std::min<int64_t>((kRunParts + wgs - 1) / wgs, blocks / 4));
-  SN_LAUNCH((attn_run_kernel<T, I8, DP, EXACT>), dim3((unsigned)wgs, 1, (unsigned)parts), dim3(256), 0, st, a);
+  const int parts = (int)run_parts(blocks, wgs);
+  SN_LAUNCH((attn_run_kernel<T, I8, DP, EXACT>), dim3((unsigned)wgs, 1, parts), dim3(256), 0, st, a);
+  if (parts > 1 && run_joins<DP>(parts)) SN_LAUNCH((attn_join_kernel<T, DP, EXACT>), dim3((unsigned)wgs, (unsigned)std::min<int64_t>(DP / 8, std::max<int64_t>(1, 1024 / wgs))), dim3(256), 0, st, a, parts);
 }
 
 template <typename T>

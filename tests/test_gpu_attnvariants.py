@@ -166,3 +166,42 @@ def test_captured_calls(store):
         got = [t.clone() for t in outs]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, call(q)))
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "same"), ("f16", "same"), ("f32", "same"), ("bf16", "i8"), ("f16", "i8")])
+@pytest.mark.parametrize("dim", [40, 64, 128, 200, 256])
+def test_tiles_in_parts(dtype, store, dim):
+    # from two parts of a tile to as many as there are, with sequences without rows, a last tile that is
+    # not full, and windows that leave most parts empty
+    for lens, past in (([3, 0, 17, 1], [500, 9, 512, 0]), ([40, 2], [1100, 3]), ([5], [6000])):
+        for window in (0, 70):
+            run_case(dtype, store, 12, 4, dim, 32, lens, past, window=window)
+
+
+@pytest.mark.parametrize("past", [250, 1900])
+def test_captured_parts(past):
+    # replays with other pasts, between eager calls of the same handle
+    import torch
+    n, kv, dim = 2, 2, 64
+    p = Paged("bf16", "same", kv, dim, 16, [past + 40, past + 40])
+    op = Attention("bf16", 8, kv, dim, page=16, store="same", max_seqs=n, max_tokens=40)
+    q = torch.randn(40, 8 * dim, device="cuda").bfloat16()
+    at, offsets = i32([past, 3]), i32([0, 23, 40])
+    rows = [torch.randn(2 * past, kv * dim, device="cuda").bfloat16() for _ in range(2)]
+    p.cache.write(*rows, p.table, i32([0, 0]), offsets=i32([0, past, 2 * past]))
+    run = lambda: op.run(q, p.cache, p.table, at, offsets=offsets)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = run()
+    for i in range(5):
+        q.copy_(torch.randn_like(q.float()))
+        at.copy_(i32([past - 40 * i, 200 * (i % 2)]))
+        graph.replay()
+        got = out.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got, run())

@@ -217,7 +217,7 @@ struct Span {
 };
 __device__ __forceinline__ Span step_span(const AttnArgs& a, int past, int KB) {
   Span s;
-  s.from = a.window ? max(0, past - a.window + 1) : 0;
+  s.from = a.window && past >= a.window ? past - a.window + 1 : 0;
   s.last = min(past, (a.c.width << a.c.shift) - 1);
   s.block = s.from / KB;
   s.blocks = s.last < s.from ? 1 : s.last / KB - s.block + 1;
@@ -333,7 +333,8 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
   for (;;) {
   const int b = p.b;
   const Span span = step_span(a, p.past, KB);
-  const int first = span.block + max(p.begin - p.start, 0), end = span.block + min(p.end - p.start, span.blocks);
+  // (without a page there is nothing to read, not even where nothing is seen)
+  const int first = span.block + max(p.begin - p.start, 0), end = c.pages ? span.block + min(p.end - p.start, span.blocks) : 0;
   auto page_at = [&](int block, int off) { return block < end ? page_of(c, b, block * KB + off) : -1; };
   FT q[NS];
 #pragma unroll

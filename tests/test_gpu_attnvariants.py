@@ -205,3 +205,24 @@ def test_captured_parts(past):
         got = out.clone()
         torch.cuda.synchronize()
         assert torch.equal(got, run())
+
+
+@pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("window", [0, 1, 40])
+def test_a_cache_without_pages_and_a_table_without_entries(store, window):
+    import torch
+    empty, some = KVCache("bf16", 2, 64, 0, page=16, store=store), KVCache("bf16", 2, 64, 3, page=16, store=store)
+    op = Attention("bf16", 4, 2, 64, page=16, store=store, window=window, max_seqs=3, max_tokens=9)
+    q = torch.randn(9, 256, device="cuda").bfloat16()
+    table, none = torch.zeros(3, 200, dtype=torch.int32, device="cuda"), torch.zeros(3, 0, dtype=torch.int32, device="cuda")
+    for cache, t in ((empty, table), (empty, none), (some, none)):
+        for past in ([0, 5, 3000], [-1, -2 ** 31, 2 ** 31 - 1]):
+            assert not op.step(q[:3], cache, t, i32(past)).any()
+            assert not op.run(q, cache, t, i32(past)).any()
+    # the ends of the counts, with a table that has pages
+    past = i32([-2 ** 31, 2 ** 31 - 1, -7])
+    if window:
+        assert not op.step(q[:3], some, table, past).any() and not op.run(q, some, table, past).any()
+    else:
+        y = op.step(q[:3], some, table, past)
+        assert not y[0].any() and not y[2].any()

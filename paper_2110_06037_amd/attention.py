@@ -20,6 +20,7 @@ Three int32 device tensors say where a call's rows belong:
 from __future__ import annotations
 
 import ctypes
+import threading
 
 import numpy as np
 
@@ -98,6 +99,14 @@ def _list(op, t, name, n):
     raise ValueError(f"{name} is not a contiguous int32 tensor ({n},) on {op._dev}")
 
 
+class _IO(threading.local):
+    """The C argument of a thread's calls, filled anew by each."""
+
+    def __init__(self):
+        self.io = N.CacheIO()
+        self.ref = ctypes.byref(self.io)
+
+
 class _Paged(_Op):
     """What calls on a cache share: its geometry, and the C argument that names
     its memory and the call's sequences."""
@@ -109,12 +118,12 @@ class _Paged(_Op):
         self.store = store
         self._desc = N.CacheDesc(self.dtype, N.STORE[store], kv_heads, head_dim, page)
         self._geometry = (self.dtype, store, kv_heads, head_dim, page, device)
-        self._io = N.CacheIO()  # one call's arguments: filled anew by every call
-        self._io_ref = ctypes.byref(self._io)
+        self._io = _IO()
 
     def _fill(self, cache, table, past, tokens, offsets):
         """The C argument of a call."""
-        io, i32, device = self._io, self._torch.int32, self.device
+        own, i32, device = self._io, self._torch.int32, self.device
+        io = own.io
         seqs, width = table.shape
         if table.dtype is i32 and table.get_device() == device and (table.stride(1) == 1 or width <= 1):
             io.table_stride, io.table = table.stride(0) if seqs > 1 else width, table.data_ptr()
@@ -123,8 +132,8 @@ class _Paged(_Op):
         io.past = _list(self, past, "past", seqs)
         io.offsets = None if offsets is None else _list(self, offsets, "offsets", seqs + 1)
         io.seqs, io.width, io.tokens = seqs, width, tokens
-        if cache is not self:
-            io.pages, io.k, io.v, io.k_scale, io.v_scale = cache._memory
+        io.pages, io.k, io.v, io.k_scale, io.v_scale = cache._memory
+        return own.ref
 
 
 class KVCache(_Paged):
@@ -153,8 +162,6 @@ class KVCache(_Paged):
             scales = [zeros(page, kind=torch.float32) if i8 else None for _ in range(2)]
             self._tensors = (zeros(page, head_dim, kind=kind), zeros(page // 16, head_dim, 16, kind=kind), *scales)
             self._memory = (pages, *(None if t is None else t.data_ptr() for t in self._tensors))
-        io = self._io
-        io.pages, io.k, io.v, io.k_scale, io.v_scale = self._memory
 
     k = property(lambda self: self._tensors[0])
     v = property(lambda self: self._tensors[1])
@@ -165,17 +172,17 @@ class KVCache(_Paged):
         """Enqueue the writing of the packed rows k, v [tokens, kv_heads * head_dim] to their places."""
         tokens, n = k.shape[0], self.kv_heads * self.head_dim
         ks, vs = self._rows(k, "k", tokens, n, self.torch_dtype), self._rows(v, "v", tokens, n, self.torch_dtype)
-        self._fill(self, table, past, tokens, offsets)
+        io = self._fill(self, table, past, tokens, offsets)
         side = None if stream is None else self._side(stream)
         st = self._current(self.device) if side is None else self._stream(side, (k, v, table, past, offsets, *self._tensors))
-        rc = self.lib.sn_cache_write(self._op, self._io_ref, k.data_ptr(), ks, v.data_ptr(), vs, st)
+        rc = self.lib.sn_cache_write(self._op, io, k.data_ptr(), ks, v.data_ptr(), vs, st)
         if rc:
             N.check(rc)
 
     def read(self, table, past, tokens, offsets=None, k_out=None, v_out=None, stream=None):
         """Enqueue the reading of the same places; returns (k, v) [tokens, kv_heads * head_dim]."""
         n, kind, at, outs = self.kv_heads * self.head_dim, self.torch_dtype, [], []
-        self._fill(self, table, past, tokens, offsets)
+        io = self._fill(self, table, past, tokens, offsets)
         side = None if stream is None else self._side(stream)
         for out, name in ((k_out, "k_out"), (v_out, "v_out")):
             if out is None:
@@ -185,7 +192,7 @@ class KVCache(_Paged):
                 at += [out.data_ptr(), self._rows(out, name, tokens, n, kind)]
             outs.append(out)
         st = self._current(self.device) if side is None else self._stream(side, (*outs, table, past, offsets, *self._tensors))
-        rc = self.lib.sn_cache_read(self._op, self._io_ref, *at, st)
+        rc = self.lib.sn_cache_read(self._op, io, *at, st)
         if rc:
             N.check(rc)
         return outs[0], outs[1]
@@ -222,7 +229,7 @@ class Attention(_Paged):
                              f"the handle of {self._geometry}")
         tokens, n, kind = q.shape[0], self._n, self.torch_dtype
         qs = self._rows(q, "q", tokens, n, kind)
-        self._fill(cache, table, past, tokens, offsets)
+        io = self._fill(cache, table, past, tokens, offsets)
         side = None if stream is None else self._side(stream)
         if out is None:
             out = q.new_empty((tokens, n)) if side is None else self._new(q, (tokens, n), kind, side)
@@ -230,7 +237,7 @@ class Attention(_Paged):
         else:
             ys = self._rows(out, "out", tokens, n, kind)
         st = self._current(self.device) if side is None else self._stream(side, (q, out, table, past, offsets, *cache._tensors))
-        rc = f(self._op, self._io_ref, q.data_ptr(), qs, out.data_ptr(), ys, st)
+        rc = f(self._op, io, q.data_ptr(), qs, out.data_ptr(), ys, st)
         if rc:
             N.check(rc)
         return out

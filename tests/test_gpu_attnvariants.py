@@ -226,3 +226,37 @@ def test_a_cache_without_pages_and_a_table_without_entries(store, window):
     else:
         y = op.step(q[:3], some, table, past)
         assert not y[0].any() and not y[2].any()
+
+
+def test_calls_of_one_cache_from_threads():
+    # different sequences, each thread on a stream of its own
+    import sys
+    import threading
+    import torch
+    cache = KVCache("bf16", 1, 8, 64, page=16)
+    rows = [torch.randn(n, 8, device="cuda").bfloat16() for n in (3, 5, 16, 40)]
+    tables = [torch.arange(16 * i, 16 * i + w, dtype=torch.int32, device="cuda")[None] for i, w in enumerate((1, 2, 5, 16))]
+    past = i32([0])
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(300):
+                cache.write(rows[i], -rows[i], tables[i], past)
+                k, v = cache.read(tables[i], past, rows[i].shape[0])
+                if not (torch.equal(k, rows[i]) and torch.equal(v, -rows[i])):
+                    wrong.append(i)
+
+    before = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        sys.setswitchinterval(before)
+    assert not wrong

@@ -162,6 +162,7 @@ class KVCache(_Paged):
             scales = [zeros(page, kind=torch.float32) if i8 else None for _ in range(2)]
             self._tensors = (zeros(page, head_dim, kind=kind), zeros(page // 16, head_dim, 16, kind=kind), *scales)
             self._memory = (pages, *(None if t is None else t.data_ptr() for t in self._tensors))
+            torch.cuda.current_stream(device).synchronize()  # (a first write may come on another stream)
 
     k = property(lambda self: self._tensors[0])
     v = property(lambda self: self._tensors[1])

@@ -260,3 +260,15 @@ def test_calls_of_one_cache_from_threads():
     finally:
         sys.setswitchinterval(before)
     assert not wrong
+
+
+def test_a_new_cache_is_written_on_another_stream():
+    import torch
+    x, past = torch.randn(64, 64, device="cuda").bfloat16(), i32([0])
+    table, side = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)  # the current stream is busy while the cache is made
+    cache = KVCache("bf16", 1, 64, 1, page=64)
+    cache.write(x, x, table, past, stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, x) for t in cache.read(table, past, 64))

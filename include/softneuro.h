@@ -640,8 +640,8 @@ int sn_scan_step(sn_op* op, const sn_scan_io* io, void* stream);
  *  - Position p of sequence b lies in the page table[b][p / page], at place
  *    p % page of it.  A position beyond the table's width, or of an entry outside
  *    0 .. pages - 1, has no place: it is not written, reads as zeros and is
- *    attended by nobody.  Sequences may share pages; a place that one call
- *    writes twice holds either's numbers.                                   */
+ *    attended by nobody.  Sequences may share pages; what a place holds
+ *    that one call writes twice is not defined.                             */
 
 /* Norms of queries and keys for each head, with the position rotation in the
  * same pass.  Each head_dim elements x of a row become
@@ -651,8 +651,9 @@ int sn_scan_step(sn_op* op, const sn_scan_io* io, void* stream);
  *
  * for the rot / 2 pairs of the first rot elements: (j, j + rot / 2) with
  * SN_PAIRS_HALVES, (2j, 2j + 1) with SN_PAIRS_NEIGHBOURS.  freq (radians,
- * |freq| < 2^20) is float64 and the angle is exact to 2^-63 of a circle at any
- * position.  q_out and k_out may be q and k.                               */
+ * |freq| < 2^20) is float64; the angle of a position is off by less than position *
+ * max(1, |freq|) * 2^-63 of a circle (and float32's last bit of what remains of whole
+ * circles).  q_out and k_out may be q and k.                               */
 typedef enum { SN_PAIRS_HALVES = 0, SN_PAIRS_NEIGHBOURS = 1 } sn_pairs;
 typedef struct {
   int32_t dtype;

@@ -720,7 +720,9 @@ int sn_cache_read(sn_op* op, const sn_cache_io* io, void* k, int64_t k_stride, v
  *
  * Scores, maxima, weights and sums are float32.  With 16-bit types a prompt's weights are
  * rounded once, to dtype, before they meet v; a step's keep 16 bits (11 with f16
- * caches).  A row's result does not depend on the other rows of the call.
+ * caches).  Sums are divided last: the values of a row's keys must add up to less than 2^119.
+ * A row's result does not depend on what the other rows of the call hold (how many they are, and
+ * where they stand, decides how keys are split, and so the last bits).
  *
  * sn_attn_run takes any number of rows per sequence, up to
  * (tokens * heads / kv_heads / 128 + seqs) * kv_heads < 2^24; sn_attn_step one each

@@ -272,3 +272,22 @@ def test_a_new_cache_is_written_on_another_stream():
     cache.write(x, x, table, past, stream=side)
     torch.cuda.synchronize()
     assert all(torch.equal(t, x) for t in cache.read(table, past, 64))
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "same"), ("f16", "same"), ("f32", "i8"), ("bf16", "i8"), ("f16", "i8")])
+@pytest.mark.parametrize("dim", [72, 88, 96, 104])
+def test_heads_between_64_and_128_elements(dtype, store, dim):
+    for page in (16, 128):
+        run_case(dtype, store, 6, 2, dim, page, [150, 0, 1, 64, 300], [0, 3, 200, 64, 31], seed=dim)
+    run_case(dtype, store, 6, 2, dim, 32, [1, 1, 1], [0, 300, -1], step=True)
+
+
+@pytest.mark.parametrize("seqs,rows", [(1, 1), (5, 1), (3, 33), (70, 43), (2, 300)])
+def test_equal_lengths(seqs, rows):
+    # without offsets, against the same with them
+    import torch
+    past = [(37 * b) % 400 - (b % 7 == 3) * 1000 for b in range(seqs)]
+    past = [max(p, -1) for p in past]
+    a = run_case("bf16", "same", 6, 2, 64, 32, [rows] * seqs, past, equal=True)
+    b = run_case("bf16", "same", 6, 2, 64, 32, [rows] * seqs, past)
+    assert np.array_equal(a, b)

@@ -924,7 +924,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
 #pragma unroll
         for (int i = 0; i < ND; ++i) o[i] = mma32(v_frag(buf, kk, 32 * i + r), w[kk], o[i]);
       reads_ahead<T, KB / 16 * ND, 4>();
-      __builtin_amdgcn_s_setprio(0);
+      if (!I8 || POWER) __builtin_amdgcn_s_setprio(0);
       if (odd) {
         // this row's keys of any weight, against each element's marked ones
         unsigned seen[2] = {0u, 0u};
@@ -946,6 +946,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
       }
     }
     if (more) store(buf ^ 1);
+    // (codes are turned into numbers before others' products go on: 4096 rows 200 -> 187 us; not where the
+    // workgroup waits in between, f16 77 -> 80)
+    if (I8 && !POWER) __builtin_amdgcn_s_setprio(0);
     wait_vmcnt<0>();
     pages = pages1, pages1 = pages_of(block + 2, entry2);
     if (!I8 && more && edge_of(block + 1, pages)) look(block + 1, buf ^ 1);

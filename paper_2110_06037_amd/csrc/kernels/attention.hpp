@@ -619,7 +619,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   constexpr float LIFT = std::is_same<T, f16>::value ? 6.f : 0.f, kLazy = 8.f;
   __shared__ u32x4 sk[2 * L::N], sv[2 * L::N];
   __shared__ __attribute__((aligned(16))) float sks[2][I8 ? KB : 4], svs[2][I8 ? KB : 4];
-  __shared__ F powers[POWER ? KB / 8 : 1];
+  __shared__ F powers[POWER ? 4 * KB / 8 : 1];  // every wave's own
   __shared__ __attribute__((aligned(16))) unsigned marks[I8 ? 4 : DP * 4];  // of an element: 64 keys' bits, +inf or NaN; -inf or NaN
   __shared__ int flag[2];
   const CacheArgs& c = a.c;
@@ -719,9 +719,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
         const int64_t at = rows_at(block, pages, w / (2 * DP));
         vr[i] = load8(static_cast<const E*>(c.v) + at * D + (EXACT ? 8 * e : 8 * min(e, 2 * D - 1)));
       }
-      if (tid < KB) {
-        const int page = max(0, __shfl(pages, tid / 16));
-        const int64_t at = (((int64_t)page * c.kv_heads + head) << c.shift) + ((block * KB + tid) & mask);
+      if (POWER || tid < KB) {
+        const int key = tid & (KB - 1), page = max(0, __shfl(pages, key / 16));
+        const int64_t at = (((int64_t)page * c.kv_heads + head) << c.shift) + ((block * KB + key) & mask);
         ksr = c.ks[at], vsr = c.vs[at];
       }
     }
@@ -734,8 +734,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   auto store = [&](int buf) {
     if constexpr (I8) {
       if constexpr (POWER) {
-        if (tid < KB) reinterpret_cast<T*>(powers)[tid] = (T)power_of(vsr);
-        lds_barrier();
+        reinterpret_cast<T*>(powers)[tid] = (T)power_of(vsr);  // (a wave holds all keys' scales)
+        __builtin_amdgcn_wave_barrier();
       }
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
@@ -746,7 +746,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
         put8(sk + buf * L::N, L::k(key, FG * ch), L::k(key, FG * ch + FG - 1), f);
         const int t16 = x / (2 * DP), e = x % (2 * DP), dd = e >> 1;
         F g = frag_of<T>(vr[i]);
-        if constexpr (POWER) g *= powers[2 * t16 + (e & 1)];
+        if constexpr (POWER) g *= powers[KB / 8 * wave + 2 * t16 + (e & 1)];
         put8(sv + buf * L::N, L::v(t16, dd, FG * (e & 1)), L::v(t16, dd, FG * (e & 1) + FG - 1), g);
       }
       if (tid < KB) sks[buf][tid] = ksr * a.scale2, svs[buf][tid] = POWER ? vsr / power_of(vsr) : vsr;
@@ -924,7 +924,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
 #pragma unroll
         for (int i = 0; i < ND; ++i) o[i] = mma32(v_frag(buf, kk, 32 * i + r), w[kk], o[i]);
       reads_ahead<T, KB / 16 * ND, 4>();
-      if (!I8 || POWER) __builtin_amdgcn_s_setprio(0);
+      if (!I8) __builtin_amdgcn_s_setprio(0);
       if (odd) {
         // this row's keys of any weight, against each element's marked ones
         unsigned seen[2] = {0u, 0u};
@@ -946,9 +946,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
       }
     }
     if (more) store(buf ^ 1);
-    // (codes are turned into numbers before others' products go on: 4096 rows 200 -> 187 us; not where the
-    // workgroup waits in between, f16 77 -> 80)
-    if (I8 && !POWER) __builtin_amdgcn_s_setprio(0);
+    // (codes are turned into numbers before others' products go on: 4096 rows 200 -> 187 us)
+    if (I8) __builtin_amdgcn_s_setprio(0);
     wait_vmcnt<0>();
     pages = pages1, pages1 = pages_of(block + 2, entry2);
     if (!I8 && more && edge_of(block + 1, pages)) look(block + 1, buf ^ 1);

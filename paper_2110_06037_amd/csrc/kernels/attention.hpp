@@ -17,7 +17,7 @@
 // 128 in bf16 101 us, 5.3 TB/s; up to 8192 keys 197 us, 5.4 TB/s; 32 heads without
 // groups 6.3 TB/s; in 8 bits 113 us, 4.6 TB/s, where turning codes into numbers
 // is as much work as the products.  Short ones are a chain of dependent steps: one
-// sequence of 4096 keys 11.2 us, of which launch and plan 3.5, queries and table 0.7, the
+// sequence of 4096 keys 10.9 us, of which launch and plan 3.2, queries and table 0.7, the
 // keys 3.0, joining the waves 0.7, storing the part and counting it 1.7, joining the parts 2.3.
 // attn_run_kernel: 128 rows (a token's query heads of one key head are
 // neighbours), a wave 32 of them in 32 x 32 products, K and V through LDS, where the
@@ -242,9 +242,7 @@ __device__ __forceinline__ bool step_part(const AttnArgs& a, int KB, int unit, P
     own = base + lane < seqs ? step_span(a, past, KB).blocks : 0;
     total += own, padded += (own + kStepLeast - 1) & -kStepLeast;
   }
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) total += __shfl_xor(total, i), padded += __shfl_xor(padded, i);
-  total = uniform(total), padded = uniform(padded);
+  total = lane_of((int)scan_lanes(total), 63), padded = lane_of((int)scan_lanes(padded), 63);
   p.pad = 0, p.per = (total + a.units - 1) / a.units;
   if (padded <= kStepLeast * a.units) p.pad = kStepLeast - 1, p.per = kStepLeast, total = padded;
   p.begin = unit * p.per, p.end = min(p.begin + p.per, total);
@@ -256,19 +254,14 @@ __device__ __forceinline__ bool step_part(const AttnArgs& a, int KB, int unit, P
       own = base + lane < seqs ? step_span(a, past, KB).blocks : 0;
     }
     const int n = (own + p.pad) & ~p.pad;
-    int sum = n;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const int up = __shfl_up(sum, i);
-      if (lane >= i) sum += up;
-    }
+    const int sum = (int)scan_lanes(n);
     const unsigned long long at = __ballot(p.begin < before + sum);
     if (at) {
       const int l = __ffsll(at) - 1;
-      p.b = uniform(base + l), p.start = uniform(__shfl(before + sum - n, l)), p.past = uniform(__shfl(past, l));
+      p.b = base + l, p.start = before + lane_of(sum - n, l), p.past = lane_of(past, l);
       return true;
     }
-    before += __shfl(sum, 63);
+    before += lane_of(sum, 63);
   }
   return false;
 }

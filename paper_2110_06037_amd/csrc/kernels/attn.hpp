@@ -114,32 +114,41 @@ __device__ __forceinline__ int seq_of(const CacheArgs& c, int64_t row) {
   return c.offsets[lo] <= row && row < c.offsets[lo + 1] ? lo : -1;
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }  // (of a uniform lane)
+// The sum over this lane and those before it, at most 2^32 - 1.
+__device__ __forceinline__ unsigned scan_lanes(unsigned v) {
+#define SN_SCAN(CTRL, ROWS) v = __builtin_elementwise_add_sat(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false))
+  SN_SCAN(0x111, 0xF);  // 1, 2, 4, 8 lanes before, within 16
+  SN_SCAN(0x112, 0xF);
+  SN_SCAN(0x114, 0xF);
+  SN_SCAN(0x118, 0xF);
+  SN_SCAN(0x142, 0xA);  // the last of 16 to the next 16
+  SN_SCAN(0x143, 0xC);  // the last of 32 to the next 32
+#undef SN_SCAN
+  return v;
+}
 // Units of work are counted over the sequences in order, count(rows, past) of each: the
 // sequence behind the number `unit`, the unit's number in it, the sequence's rows and past.
-// (Every wave for itself, 64 sequences at a time.)  False: there are fewer units.
+// (Every wave for itself, 64 sequences at a time.  Offsets that fall may count more units than
+// there are: sums stop at the top of their range, and stay in order.)  False: there are fewer units.
 template <typename F>
-__device__ __forceinline__ bool find_rows(const CacheArgs& c, int64_t unit, F count, int& b, int& at, int& first, int& rows, int& past) {
+__device__ __forceinline__ bool find_rows(const CacheArgs& c, unsigned unit, F count, int& b, int& at, int& first, int& rows, int& past) {
   const int lane = threadIdx.x & 63;
-  int64_t before = 0;
+  unsigned before = 0;
   for (int base = 0; base < c.seqs; base += 64) {
     int64_t lo, hi;
     const int own_past = min(c.past[min(base + lane, c.seqs - 1)], kMaxPast);
     seq_rows(c, min(base + lane, c.seqs - 1), lo, hi);
-    const int64_t own = base + lane < c.seqs ? count((int)(hi - lo), own_past) : 0;
-    int64_t sum = own;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const int64_t up = __shfl_up(sum, i);
-      if (lane >= i) sum += up;
-    }
-    const unsigned long long in = __ballot(unit < before + sum);
+    const unsigned own = base + lane < c.seqs ? (unsigned)count((int)(hi - lo), own_past) : 0;
+    const unsigned sum = __builtin_elementwise_add_sat(before, scan_lanes(own));
+    const unsigned long long in = __ballot(unit < sum);
     if (in) {
       const int l = __ffsll(in) - 1;
-      b = uniform(base + l), at = uniform((int)(unit - __shfl(before + sum - own, l)));
-      first = uniform(__shfl((int)lo, l)), rows = uniform(__shfl((int)(hi - lo), l)), past = uniform(__shfl(own_past, l));
+      b = base + l, at = (int)(unit - (l ? (unsigned)lane_of((int)sum, l - 1) : before));
+      first = lane_of((int)lo, l), rows = lane_of((int)(hi - lo), l), past = lane_of(own_past, l);
       return true;
     }
-    before += __shfl(sum, 63);
+    before = (unsigned)lane_of((int)sum, 63);
   }
   return false;
 }

@@ -2,11 +2,10 @@
 // bits, and read back.  In 8 bits a head's row has the scale s = max|x| * (1 / 127) in
 // float32 and the codes nearest to x / s (ties to even).
 //
-// Bound by memory where there are many rows: 4096 of 8 heads of 128 in bf16, written in 8
-// bits and read back, are 50 MB in 18 us (a launch each way: 9.8 and 9.3 under the tracer, of which
-// 6 us in all are the bytes at a copy's rate); 16384 rows 50 us, 4.1 TB/s.  Kept in
-// bf16 17.0 and 46.7.  Few rows are the launch, and the chain from the offsets over the
-// table to the page: 8 rows 3.2 us to write, 3.1 to read.
+// Bound by memory where there are many rows: 16384 of 8 heads of 128 in bf16, written in 8
+// bits and read back, are 202 MB in 43 us (4.7 TB/s), kept in bf16 44; 4096 rows 50 MB in 17.3 us and
+// 14.6: a launch each way (2.3 us), the chain from past over the table to the page, and 6 us in all for
+// the bytes at a copy's rate. Few rows are the launch and that chain: 8 rows 3.2 us to write, 3.1 to read.
 #include "attn.hpp"
 
 namespace sn {
@@ -148,7 +147,17 @@ __global__ __launch_bounds__(kTileThreads) void cache_tiles_kernel(CacheRows a) 
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, D = c.dim, chunks = D / 8;
   int b, tile, first, n, past;
-  if (!find_rows(c, blockIdx.x, [&](int rows, int before) { return (int64_t)rows_tiles(before, rows); }, b, tile, first, n, past)) return;
+  if (c.offsets) {
+    if (!find_rows(c, blockIdx.x, [&](int rows, int before) { return (int64_t)rows_tiles(before, rows); }, b, tile, first, n, past)) return;
+  } else {  // sequences of equal lengths have the same bound of tiles each: no search
+    // (4096 rows written and read 17.3 us, searched for 19.0)
+    n = (int)c.each;
+    const int of = n / 16 + 2;
+    b = uniform(blockIdx.x / of);
+    if (b >= c.seqs) return;
+    tile = blockIdx.x - b * of, first = b * n, past = uniform(min(c.past[b], kMaxPast));
+    if (tile >= rows_tiles(past, n)) return;
+  }
   const int pos0 = (max(past, 0) & ~15) + 16 * tile;  // of the tile
   const int slot0 = pos0 & ((1 << c.shift) - 1);
   const bool whole = past >= 0 && pos0 >= past && pos0 + 16 <= past + n;

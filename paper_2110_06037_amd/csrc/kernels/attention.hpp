@@ -22,8 +22,8 @@
 // attn_run_kernel: 128 rows (a token's query heads of one key head are
 // neighbours), a wave 32 of them in 32 x 32 products, K and V through LDS, where the
 // four waves share them.  Bound by issue, matrix products first: 4096 rows of 32 heads, 8 key heads of 128 in
-// bf16, causal, 144 - 152 us, 137.5 GFLOP that count, 905 - 955 TFLOP/s, a library product of
-// 8192^3 1206.  Without its loads it takes 138 us, without its exponentials 139; two
+// bf16, causal, 142 - 152 us, 137.5 GFLOP that count, 905 - 965 TFLOP/s, a library product of
+// 8192^3 1206; over a cache in 8 bits 187.  Without its loads it takes 138 us, without its exponentials 139; two
 // waves a SIMD, whose registers hold no more, cover one's softmax with the other's
 // products.  Not faster (4096 rows, 162 us then): 32 keys a block and three waves a SIMD 171, a block's scores
 // taken beside the last one's softmax 180, a queue of tiles 192, tiles in another order 174.

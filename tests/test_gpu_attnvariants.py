@@ -291,3 +291,26 @@ def test_equal_lengths(seqs, rows):
     a = run_case("bf16", "same", 6, 2, 64, 32, [rows] * seqs, past, equal=True)
     b = run_case("bf16", "same", 6, 2, 64, 32, [rows] * seqs, past)
     assert np.array_equal(a, b)
+
+
+def test_offsets_of_no_order():
+    # more rows in all than the call has: some stay as they were, none outside is touched, and the handle goes on
+    import torch
+    r = np.random.default_rng(7)
+    n, seqs = 200, 150
+    p = Paged("bf16", "same", 2, 64, 16, [300])
+    op = Attention("bf16", 4, 2, 64, page=16, max_seqs=seqs, max_tokens=n)
+    table = p.table.expand(seqs, -1)
+    q = torch.randn(n + 2, 256, device="cuda").bfloat16()
+    kv = torch.randn(n, 128, device="cuda").bfloat16()
+    spare = KVCache("bf16", 2, 64, p.cache.pages, page=16)
+    want = op.run(q[:50], p.cache, p.table, i32([100]))
+    for _ in range(3):
+        offsets = i32(np.concatenate([r.integers(-20, n + 20, seqs), [2 ** 31 - 1]]))
+        past = i32(r.integers(-5, 400, seqs))
+        out = torch.full((n + 2, 256), 5.0, device="cuda").bfloat16()
+        op.run(q[1:-1], p.cache, table, past, offsets=offsets, out=out[1:-1])
+        spare.write(kv, kv, table, past, offsets=offsets)
+        spare.read(table, past, n, offsets=offsets)
+        assert (out[0] == 5).all() and (out[-1] == 5).all()
+    assert torch.equal(op.run(q[:50], p.cache, p.table, i32([100])), want)

@@ -593,6 +593,26 @@ __device__ __forceinline__ bool find_tile(const CacheArgs& c, int tile, int each
   t = tile - b * of, row0 = b * n, past = uniform(min(c.past[b], kMaxPast));
   return true;
 }
+// The keys that a tile's rows see: positions of its first and last row, blocks of keys.
+struct RunSpan {
+  int pos0, pos1, first, end;
+};
+__device__ __forceinline__ RunSpan run_span(const AttnArgs& a, int t, int rows, int past, int KB) {
+  RunSpan s;
+  const int r0 = t * kRunRows, r1 = min(r0 + kRunRows, rows) - 1;
+  s.pos0 = past < 0 ? -1 : past + uniform(fdiv(r0, a.each)), s.pos1 = past < 0 ? -1 : past + uniform(fdiv(r1, a.each));
+  const int from = a.window ? max(0, s.pos0 - a.window + 1) : 0, last = min(s.pos1, (a.c.width << a.c.shift) - 1);
+  s.first = from / KB, s.end = last < from ? s.first : last / KB + 1;
+  return s;
+}
+// The launch's parts are as many as the table has room for; a tile uses as many as its keys make
+// of four blocks at least (16 rows after none, in a table of 32768 positions, 15.5 -> 8.9 us,
+// after 1000 15.2 -> 13.2; ragged lengths in f16 25.7 -> 22.7).
+__device__ __forceinline__ int run_used(const RunSpan& s, int parts, int& per) {
+  const int all = s.end - s.first;
+  per = max(4, (all + parts - 1) / parts);
+  return max(1, (all + per - 1) / per);
+}
 // Where a thread's sums of 4 elements of a part lie, and its maximum and sum of weights.
 template <int DP>
 __device__ __forceinline__ int run_o_at(int slot, int i) {
@@ -614,7 +634,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   __shared__ __attribute__((aligned(16))) float sks[2][I8 ? KB : 4], svs[2][I8 ? KB : 4];
   __shared__ F powers[POWER ? 4 * KB / 8 : 1];  // every wave's own
   __shared__ __attribute__((aligned(16))) unsigned marks[I8 ? 4 : DP * 4];  // of an element: 64 keys' bits, +inf or NaN; -inf or NaN
-  __shared__ int flag[2];
+  __shared__ int flag[2], used;  // used: the tile's parts
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
   const int D = EXACT ? DP : c.dim, each = a.heads / c.kv_heads;
@@ -629,12 +649,14 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   const int pos = past < 0 ? -1 : past + token;
   const int top_pos = __builtin_amdgcn_readlane(pos, 63), low_pos = uniform(pos);  // of the wave
   // the workgroup's keys, and this part's blocks of them
-  const int r0 = t * kRunRows, r1 = min(r0 + kRunRows, rows) - 1;
-  const int pos0 = past < 0 ? -1 : past + uniform(fdiv(r0, a.each)), pos1 = past < 0 ? -1 : past + uniform(fdiv(r1, a.each));
-  const int from = a.window ? max(0, pos0 - a.window + 1) : 0, last = min(pos1, (c.width << c.shift) - 1);
-  int first = from / KB, end = last < from ? first : last / KB + 1;
+  const RunSpan span = run_span(a, t, rows, past, KB);
+  const int pos0 = span.pos0, pos1 = span.pos1;
+  int first = span.first, end = span.end;
   if (gridDim.z > 1) {
-    const int all = end - first, per = (all + gridDim.z - 1) / gridDim.z;
+    int per;
+    const int parts = run_used(span, gridDim.z, per);
+    if (blockIdx.z >= parts) return;
+    if (tid == 0) used = parts;
     first = min(end, first + (int)blockIdx.z * per), end = min(end, first + per);
   }
   const int mask = (1 << c.shift) - 1;
@@ -949,8 +971,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   l = sum_x32(l);
   __syncthreads();
 
-  if (gridDim.z > 1) {  // parts: left in the lanes' order
-    const int parts = gridDim.z, slot = blockIdx.x * parts;
+  if (const int parts = gridDim.z > 1 ? uniform(used) : 1; parts > 1) {  // left in the lanes' order
+    const int slot = blockIdx.x * gridDim.z;
     const Shared wo(a.ws_o), wm(a.ws_m);
     if (t * kRunRows + 32 * wave < rows) {
 #pragma unroll
@@ -960,7 +982,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
           wo.put4(run_o_at<DP>(slot + blockIdx.z, 4 * i + j), f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
       wm.put(run_m_at(slot + blockIdx.z), m), wm.put(run_m_at(slot + blockIdx.z) + 256, l);
     }
-    if (run_joins<DP>(parts)) return;
+    if (run_joins<DP>(gridDim.z)) return;
     if constexpr (!run_joins<DP>(2)) {  // joined by the tile's last workgroup in the parts' order
       if (!last_of(a.count + blockIdx.x, parts, &flag[0])) return;
       if (t * kRunRows + 32 * wave >= rows) return;  // (a wave without rows left nothing)
@@ -1020,12 +1042,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int parts) {
   int b, t, row0, n, past;
   if (!find_tile(c, tile, each, true, b, t, row0, n, past)) return;
   const int mine = t * kRunRows + 32 * wave + r, token = fdiv(min(mine, n * each - 1), a.each);
-  if (mine >= n * each) return;
+  int per;
+  const int used = run_used(run_span(a, t, n * each, past, run_keys<T>()), parts, per);
+  if (used == 1 || mine >= n * each) return;  // (one: the rows are there)
   T* y = static_cast<T*>(a.y) + (int64_t)(row0 + token) * a.ys + (int64_t)(head * each + mine - token * each) * D;
   for (int z = 0;;) {
-    join.add(z, parts - 1);
+    join.add(z, used - 1);
     z += 8;
-    if (z >= parts) {
+    if (z >= used) {
       const int d = 8 * i + 4 * h;
       const float inv = join.sum == 0.f ? 0.f : 1.f / join.sum;
       T v[4];
@@ -1035,7 +1059,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int parts) {
       if ((i += gridDim.y) >= DP / 8) return;
       join.top = kNone, join.sum = 0.f, join.acc = f32x4{0.f, 0.f, 0.f, 0.f}, z = 0;
     }
-    join.fetch(z, parts - 1, get);
+    join.fetch(z, used - 1, get);
   }
 }
 

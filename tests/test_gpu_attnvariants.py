@@ -314,3 +314,27 @@ def test_offsets_of_no_order():
         spare.read(table, past, n, offsets=offsets)
         assert (out[0] == 5).all() and (out[-1] == 5).all()
     assert torch.equal(op.run(q[:50], p.cache, p.table, i32([100])), want)
+
+
+@pytest.mark.parametrize("dtype,store,dim", [("bf16", "same", 64), ("f16", "i8", 96), ("f32", "same", 256)])
+def test_tables_wider_than_the_sequences(dtype, store, dim):
+    # tiles use fewer parts than their launch has: from one to all, side by side
+    r = np.random.default_rng(5)
+    lens, past = [3, 40, 1, 9, 2], [0, 250, 700, 1500, -1]
+    held = [max(0, p + n) for p, n in zip(past, lens)]
+    p = Paged(dtype, store, 2, dim, 16, held)
+    wide = p.table.new_full((5, 600), -1)
+    wide[:, :p.table.shape[1]] = p.table
+    q = device(rounded(r.standard_normal((sum(lens), 4 * dim)), dtype), dtype)
+    op = Attention(dtype, 4, 2, dim, page=16, store=store, max_seqs=5, max_tokens=sum(lens))
+    offsets = i32(np.concatenate([[0], np.cumsum(lens)]))
+    got = host(op.run(q, p.cache, wide, i32(past), offsets=offsets))
+    at = 0
+    for b, (n, s) in enumerate(zip(lens, past)):
+        rows, at = slice(at, at + n), at + n
+        g = got[rows].reshape(n, 4, dim)
+        if s < 0:
+            assert not g.any()
+            continue
+        y, a, bound = attend(host(q)[rows].reshape(n, 4, dim), *p.rows(b), 2, s, 0, np.ones(s + n, bool), None)
+        assert_attention(g, y, a, bound, dtype, f"sequence {b}")

@@ -121,7 +121,7 @@ class _AttentionBlock:
         cache, table = part
         p = self.in_proj.run(u)
         q, k, v = p[:, :self.nq], p[:, self.nq:self.nq + self.nk], p[:, self.nq + self.nk:]
-        self.head_norm.run(q, k, call.positions, q_out=q, k_out=k)
+        self.head_norm.run(q, k, call.positions if self.head_norm.rot else None, q_out=q, k_out=k)
         cache.write(k, v, table, call.state.past, offsets=call.offsets)
         if call.step:
             y = self.attention.step(q, cache, table, call.state.past)

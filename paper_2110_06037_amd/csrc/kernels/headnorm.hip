@@ -169,10 +169,10 @@ __global__ __launch_bounds__(64 * kHeadWaves) void head_norm_any_kernel(HeadNorm
     if (a.norm) k = rsqrtf(wave_sum(s) / (float)D + a.eps);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      va[i] *= w && ia[i] < D ? k * w[ia[i]] : k;
-      vb[i] *= w && ib[i] < D ? k * w[ib[i]] : k;
-      if (ia[i] < D) y[ia[i]] = from_f<T>(va[i] * cs[i] - vb[i] * sn[i]);
-      if (ib[i] < D) y[ib[i]] = from_f<T>(vb[i] * cs[i] + va[i] * sn[i]);
+      const float u = va[i] * (w && ia[i] < D ? k * w[ia[i]] : k), v = vb[i] * (w && ib[i] < D ? k * w[ib[i]] : k);
+      const bool turned = lane + 64 * i < half;  // (others stay apart: 0 times what is not finite is NaN)
+      if (ia[i] < D) y[ia[i]] = from_f<T>(turned ? u * cs[i] - v * sn[i] : u);
+      if (ib[i] < D) y[ib[i]] = from_f<T>(turned ? v * cs[i] + u * sn[i] : v);
     }
   }
 }

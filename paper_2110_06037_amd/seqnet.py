@@ -30,13 +30,62 @@ from .attention import Attention, HeadNorm, KVCache
 from .sequence import BlockNorm, Linear4, Scan
 
 
+class _Room:
+    """Counts the positions that calls take of ``room`` for each sequence, and refuses calls
+    that do not fit.
+
+    The host keeps a bound of the largest count, as long as it knows of all that happened to
+    ``past`` (another tensor, or another version of it, may hold anything).  Only where the bound
+    does not do are the counts, and a call's offsets, read from the device."""
+
+    def __init__(self, past, room):
+        self.room, self._most, self._captured = room, 0, False
+        self.know(past)
+
+    def know(self, past):
+        """``past`` holds what this has counted."""
+        self._past, self._version = past, None if past.is_inference() else past._version
+
+    def knows(self, past):
+        return not self._captured and past is self._past and self._version is not None and past._version == self._version
+
+    def take(self, past, seqs, rows, offsets=None, longest=None):
+        if not rows:
+            return
+        if past.is_cuda:
+            import torch
+            if torch.cuda.is_current_stream_capturing():  # nobody tells how often that will run
+                self._captured = True
+                return
+        if offsets is None:
+            longest = -(-rows // seqs)
+        most = self._most + (rows if longest is None else longest)
+        if most > self.room or not self.knows(past):
+            counts = past.tolist()
+            if offsets is None:
+                lens = [longest] * len(counts)
+            else:
+                at = offsets.tolist()
+                lens = [b - a for a, b in zip(at, at[1:])]
+            most = 0
+            for b, (p, n) in enumerate(zip(counts, lens)):
+                if p >= 0 and n > 0 and p + n > self.room:
+                    raise ValueError(f"sequence {b} has {p} positions and gets {n} more, the state has room for {self.room}")
+                most = max(most, p + max(n, 0) if p >= 0 else 0)
+        self._most = most
+        self.know(past)
+
+
 class SequenceState:
     """What ``seqs`` sequences leave behind in every block (at first nothing).
 
     ``windows`` and ``states`` are the sequence blocks' (zeros: before the first
-    token).  For attention blocks ``past`` (int32 [seqs]) counts the tokens so far,
-    and ``caches`` hold up to ``max_positions`` of each sequence, in the pages that
-    ``tables`` say (tokens behind them are seen by no later one)."""
+    token).  For attention blocks ``past`` (int32 [seqs]) counts the tokens so far (negative: no
+    sequence in this slot; it may be set between calls), and ``caches`` hold ``room`` positions of each sequence:
+    ``max_positions``, rounded up to the blocks' pages, in those that ``tables`` say.  A call
+    that would take more is refused, before anything runs.  (Where the bound that the host keeps does not
+    show that it fits, that reads ``past``, and waits for it.  In a graph that the caller captures, by other means than
+    ``capture_step``, nothing is refused.)"""
 
     def __init__(self, net, seqs, max_positions=None):
         import torch
@@ -46,11 +95,14 @@ class SequenceState:
         attends = [b for b in net.blocks if b.attends]
         self.windows = [torch.zeros(seqs, b.scan.conv - 1, b.scan.chans, dtype=b.scan.torch_dtype, device=dev) for b in scans]
         self.states = [torch.zeros(seqs, b.scan.heads, b.scan.head_dim, b.scan.state, device=dev) for b in scans]
-        self.past, self.caches, self.tables = None, [], []
+        self.past, self.caches, self.tables, self.room, self._room = None, [], [], None, None
         if attends:
             if max_positions is None:
                 raise ValueError("a net with attention blocks needs max_positions")
-            self.past = torch.zeros(seqs, dtype=torch.int32, device=dev)
+            with torch.inference_mode(False):  # (a tensor with versions, wherever it is made)
+                self.past = torch.zeros(seqs, dtype=torch.int32, device=dev)
+            self.room = min(-(-max_positions // b.page) * b.page for b in attends)
+            self._room = _Room(self.past, self.room)
         for b in attends:
             width = -(-max_positions // b.page)
             self.caches.append(b.new_cache(seqs * width))
@@ -133,11 +185,13 @@ class _AttentionBlock:
 class _Call:
     """What the blocks of one run or step share; ``positions`` of the rows where blocks attend."""
 
-    def __init__(self, state, rows, offsets, step):
-        self.state, self.offsets, self.step = state, offsets, step
+    def __init__(self, state, rows, offsets, step, longest=None, counted=True):
+        self.state, self.offsets, self.step, self.counted = state, offsets, step, counted
         past = state.past
         if past is None:
             return
+        if counted:
+            state._room.take(past, state.seqs, rows, offsets, longest)
         import torch
         if step:
             self.lens, self.positions = 1, past
@@ -153,18 +207,23 @@ class _Call:
     def done(self):
         if self.state.past is not None:  # slots without a sequence stay so
             self.state.past += (self.state.past >= 0) * self.lens
+            if self.counted:
+                self.state._room.know(self.state.past)
 
 
 class _Replay:
     """Replays a captured step.  The graph holds addresses only: this holds the
     net, whose handles own weights and workspaces, and the tensors."""
 
-    def __init__(self, graph, net, *tensors):
-        self.graph, self.net, self.tensors = graph, net, tensors
+    def __init__(self, graph, net, state, *tensors):
+        self.graph, self.net, self.state, self.tensors = graph, net, state, (state.tensors(), *tensors)
+        self.past = state.past
 
     def __call__(self):
         if self.net.closed:
             raise RuntimeError("the net of this captured step is closed")
+        if self.past is not None:
+            self.state._room.take(self.past, self.state.seqs, self.state.seqs)
         self.graph.replay()
 
 
@@ -203,21 +262,23 @@ class SequenceNet:
         """The state before the first token; attention blocks hold ``max_positions`` of each sequence."""
         return SequenceState(self, seqs, max_positions)
 
-    def _forward(self, x, state, offsets, step):
+    def _forward(self, x, state, offsets, step, longest=None, counted=True):
         import torch
+        call = _Call(state, x.shape[0], offsets, step, longest, counted)
         u, _ = self.first.run(x)
         h = x.to(torch.float32, copy=True)  # updated below: never the caller's x
-        call = _Call(state, x.shape[0], offsets, step)
         for b, part in zip(self.blocks, state.parts):
             u, h = b.join.run(b.run(u, part, call), residual=h, res_out=h)
         call.done()
         return u
 
-    def run(self, x, state, offsets=None):
+    def run(self, x, state, offsets=None, longest=None):
         """The normalised outputs [tokens, dim] of prompts in packed rows x
         (``offsets``: int32 device tensor of their first rows; none: of equal
-        lengths), continuing from ``state``, which is brought up to date."""
-        return self._forward(x, state, offsets, False)
+        lengths), continuing from ``state``, which is brought up to date.
+        ``longest``: how many rows the longest of them has, where the caller knows it (with
+        ``offsets`` a call of more rows than the state has room for reads them otherwise)."""
+        return self._forward(x, state, offsets, False, longest)
 
     def step(self, x, state):
         """The same for one token per sequence, x [seqs, dim]."""
@@ -228,21 +289,24 @@ class SequenceNet:
         is filled with the tokens before each replay() and y holds their outputs
         after it.  ``state`` is as before the capture; its tensors are what every
         replay updates.  ``replay`` keeps the net and them alive, and refuses to
-        run once the net is closed."""
+        run once the net is closed, or where ``state`` has no room."""
         import torch
         with torch.cuda.device(self.device):
             x = torch.zeros(state.seqs, self.first.dim, dtype=self.first.torch_dtype, device=f"cuda:{self.device}")
             # (what a step writes to a cache lies behind its sequence, until one that counts overwrites it)
             tensors = state.windows + state.states + ([] if state.past is None else [state.past])
             keep = [t.clone() for t in tensors]
+            known = state.past is not None and state._room.knows(state.past)
             side = torch.cuda.Stream(self.device)
             side.wait_stream(torch.cuda.current_stream(self.device))
             with torch.cuda.stream(side):
-                self.step(x, state)
+                self._forward(x, state, None, True, counted=False)
             torch.cuda.current_stream(self.device).wait_stream(side)
             graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(graph, stream=side):
-                y = self.step(x, state)
+                y = self._forward(x, state, None, True, counted=False)
             for t, k in zip(tensors, keep):
                 t.copy_(k)
-        return x, y, _Replay(graph, self, state.tensors(), (x, y))
+            if known:
+                state._room.know(state.past)
+        return x, y, _Replay(graph, self, state, (x, y))

@@ -26,6 +26,9 @@ leave every block's convolution window and state, or its cache, behind in a
 
 from __future__ import annotations
 
+import contextlib
+import threading
+
 from .attention import Attention, HeadNorm, KVCache
 from .sequence import BlockNorm, Linear4, Scan
 
@@ -222,9 +225,10 @@ class _Replay:
     def __call__(self):
         if self.net.closed:
             raise RuntimeError("the net of this captured step is closed")
-        if self.past is not None:
-            self.state._room.take(self.past, self.state.seqs, self.state.seqs)
-        self.graph.replay()
+        with self.net._turn():
+            if self.past is not None:
+                self.state._room.take(self.past, self.state.seqs, self.state.seqs)
+            self.graph.replay()
 
 
 class SequenceNet:
@@ -235,11 +239,16 @@ class SequenceNet:
     [dim] that follows the block}.  An attention block's config has the "kind"
     "attention" (dim, heads, kv_heads, head_dim, rot, base, window, page, store,
     group), and beside the projections "q_norm" and "k_norm" [head_dim].  Inputs and outputs are [rows, dim] in
-    ``dtype``; the residual stream between the blocks is float32."""
+    ``dtype``; the residual stream between the blocks is float32.
+
+    The blocks' handles have workspaces, one for all attention blocks that are alike, which every call uses. So the net puts
+    its calls (replays of captured steps among them) one after the other on the device, whatever streams and
+    threads they come from; graphs that the caller captures by other means are the caller's to order."""
 
     def __init__(self, dtype, weights, max_seqs=1, max_tokens=1, device=0, eps=1e-5):
         blocks = weights["blocks"]
         self.device, self.closed = device, False
+        self._lock, self._last = threading.RLock(), None  # the stream of the last call
         self.first = BlockNorm(dtype, blocks[0]["config"]["dim"], pre=weights["norm"], eps=eps, device=device)
         shared = {}
         self.blocks = [_AttentionBlock(dtype, w, w["norm"], max_seqs, max_tokens, device, eps, shared)
@@ -262,15 +271,28 @@ class SequenceNet:
         """The state before the first token; attention blocks hold ``max_positions`` of each sequence."""
         return SequenceState(self, seqs, max_positions)
 
+    @contextlib.contextmanager
+    def _turn(self):
+        """A call's turn to queue its work: behind the last call's, which may be on another stream."""
+        import torch
+        with self._lock:
+            if not torch.cuda.is_current_stream_capturing():
+                stream = torch.cuda.current_stream(self.device)
+                if self._last is not None and self._last != stream:
+                    stream.wait_stream(self._last)
+                self._last = stream
+            yield
+
     def _forward(self, x, state, offsets, step, longest=None, counted=True):
         import torch
-        call = _Call(state, x.shape[0], offsets, step, longest, counted)
-        u, _ = self.first.run(x)
-        h = x.to(torch.float32, copy=True)  # updated below: never the caller's x
-        for b, part in zip(self.blocks, state.parts):
-            u, h = b.join.run(b.run(u, part, call), residual=h, res_out=h)
-        call.done()
-        return u
+        with self._turn():
+            call = _Call(state, x.shape[0], offsets, step, longest, counted)
+            u, _ = self.first.run(x)
+            h = x.to(torch.float32, copy=True)  # updated below: never the caller's x
+            for b, part in zip(self.blocks, state.parts):
+                u, h = b.join.run(b.run(u, part, call), residual=h, res_out=h)
+            call.done()
+            return u
 
     def run(self, x, state, offsets=None, longest=None):
         """The normalised outputs [tokens, dim] of prompts in packed rows x
@@ -291,7 +313,7 @@ class SequenceNet:
         replay updates.  ``replay`` keeps the net and them alive, and refuses to
         run once the net is closed, or where ``state`` has no room."""
         import torch
-        with torch.cuda.device(self.device):
+        with self._lock, torch.cuda.device(self.device):
             x = torch.zeros(state.seqs, self.first.dim, dtype=self.first.torch_dtype, device=f"cuda:{self.device}")
             # (what a step writes to a cache lies behind its sequence, until one that counts overwrites it)
             tensors = state.windows + state.states + ([] if state.past is None else [state.past])

@@ -129,6 +129,44 @@ __device__ __forceinline__ float sum_x16(float v) {
 constexpr float kNone = -__builtin_huge_valf();  // a maximum of nothing
 __device__ __forceinline__ float some(float m) { return m == kNone ? 0.f : m; }
 
+// Values that are not finite.  A weight exp(..) is above zero however small it is, so an infinity that a
+// row sees is its result's, and a NaN, or infinities of both signs, are NaN.  In float32 a weight may be
+// 0, whose product with an infinity is NaN, as may be that of two parts of a weight; which it is would
+// depend on where blocks, parts and tiles end.  So the products only say that there is something (a
+// sum that is not finite stays so to the end), and whoever writes such a result looks through the
+// values again: its class is that of the values that the row sees, whatever their weights, if those
+// are numbers.  (Values in 8 bits have no infinities: a row that held one has a NaN for a scale.)
+// The looking is in functions of its own, which read the kernel's arguments anew: inlined, its
+// scalars cost the loops registers (4096 rows 147 -> 161 us, one token after 4095 10.9 -> 11.6).
+typedef const __attribute__((address_space(4))) AttnArgs* KernelArgs;
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_huge_valf(); }
+__device__ __forceinline__ float class_of(bool plus, bool minus) {  // NaN counts as both
+  return (plus ? __builtin_huge_valf() : 0.f) - (minus ? __builtin_huge_valf() : 0.f);
+}
+// The class of element d of the values at the positions from .. last; 0 where all are finite.
+template <typename T>
+__device__ __attribute__((noinline)) float class_of_values(KernelArgs args, int b, int head, int d, int from, int last) {
+  const CacheArgs c = ((const AttnArgs*)args)->c;
+  bool plus = false, minus = false;
+#pragma unroll 1
+  for (int p = from & ~7; p <= last && !(plus && minus); p += 8) {
+    const int page = page_of(c, b, p);
+    if (page < 0) continue;
+    const V8<T> v = load8(static_cast<const T*>(c.v) + v_at(c, page, head, p & ((1 << c.shift) - 1)) + 16 * d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float f = to_f(v.v[j]);
+      if (p + j >= from && p + j <= last && !finite(f)) plus |= !(f < 0.f), minus |= !(f > 0.f);
+    }
+  }
+  return class_of(plus, minus);
+}
+// Which of the 32 keys from `base` on a row at `pos` sees.
+__device__ __forceinline__ unsigned first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+__device__ __forceinline__ unsigned seen_keys(int base, int pos, int window) {
+  return first_bits(pos - base + 1) & ~first_bits(window ? pos - window + 1 - base : 0);
+}
+
 // Parts of a sum that other workgroups read: stores and loads of the workspace go past
 // the XCDs' own L2 caches (cache policy sc1), a workgroup's stores are complete
 // before it counts itself in, so that no cache-wide fence is needed (with fences: 157
@@ -459,6 +497,12 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
   constexpr int chunks = DP / 4;
   auto finish = [&](int r, int d, f32x4 acc, float sum) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (!I8 && finite(sum) && !finite((acc[0] + acc[1]) + (acc[2] + acc[3])))
+#pragma unroll 1
+      for (int j = 0; j < 4; ++j) {
+        const float is = class_of_values<T>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), b, head, d + j, span.from, span.last);
+        if (is != 0.f) acc = f32x4{j == 0 ? is : acc[0], j == 1 ? is : acc[1], j == 2 ? is : acc[2], j == 3 ? is : acc[3]};
+      }
     T v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = from_f<T>(acc[j] * inv);
@@ -620,6 +664,61 @@ __device__ __forceinline__ int run_o_at(int slot, int i) {
 }
 __device__ __forceinline__ int run_m_at(int slot) { return slot * 512 + threadIdx.x; }
 
+// The classes of a tile's results that are not finite, block by block as the products were taken.
+template <typename T, int DP>
+__device__ __attribute__((noinline)) void run_classes(KernelArgs args, int tile, bool split, bool numbers, unsigned* marks) {
+  const AttnArgs a = *(const AttnArgs*)args;
+  const CacheArgs& c = a.c;
+  constexpr int KB = run_keys<T>(), GE = 16 / sizeof(T), VG = 16 / GE, NM = DP / 32;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+  const int D = c.dim, each = a.heads / c.kv_heads, head = blockIdx.x % c.kv_heads;
+  int b, t, row0, n, past;
+  if (!find_tile(c, tile, each, split, b, t, row0, n, past)) return;
+  const int rows = n * each, mine = t * kRunRows + 32 * wave + r, token = fdiv(min(mine, rows - 1), a.each);
+  const int pos = past < 0 ? -1 : past + token;
+  const RunSpan span = run_span(a, t, rows, past, KB);
+  unsigned plus[NM], minus[NM];  // this lane's elements 32 i + 8 j + 4 h + x: bits 4 j + x
+#pragma unroll
+  for (int i = 0; i < NM; ++i) plus[i] = minus[i] = 0;
+#pragma unroll 1
+  for (int block = span.first; block < span.end; ++block) {
+    __syncthreads();
+    for (int i = tid; i < 4 * DP; i += 256) marks[i] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < KB / GE * D; i += 256) {
+      const int d = i / VG % D, key = i / (VG * D) * 16 + i % VG * GE, p = block * KB + key, page = page_of(c, b, p);
+      if (page < 0) continue;
+      T e[GE];
+      __builtin_memcpy(e, static_cast<const T*>(c.v) + v_at(c, page, head, p & ((1 << c.shift) - 1)) + 16 * d, 16);
+#pragma unroll
+      for (int j = 0; j < GE; ++j) {
+        const float v = (float)e[j];
+        if (finite(v)) continue;
+        if (!(v < 0.f)) atomicOr(&marks[4 * d + (key >> 5)], 1u << ((key & 31) + j));
+        if (!(v > 0.f)) atomicOr(&marks[4 * d + 2 + (key >> 5)], 1u << ((key & 31) + j));
+      }
+    }
+    __syncthreads();
+    const unsigned seen0 = seen_keys(block * KB, pos, a.window), seen1 = KB > 32 ? seen_keys(block * KB + 32, pos, a.window) : 0u;
+#pragma unroll
+    for (int i = 0; i < NM; ++i)
+#pragma unroll 1
+      for (int j = 0; j < 16; ++j) {
+        const unsigned* at = &marks[4 * (32 * i + 8 * (j >> 2) + 4 * h + (j & 3))];
+        plus[i] |= (at[0] & seen0) | (at[1] & seen1) ? 1u << j : 0u;
+        minus[i] |= (at[2] & seen0) | (at[3] & seen1) ? 1u << j : 0u;
+      }
+  }
+  if (mine >= rows || !numbers) return;
+  T* y = static_cast<T*>(a.y) + (int64_t)(row0 + token) * a.ys + (int64_t)(head * each + mine - token * each) * D;
+#pragma unroll
+  for (int i = 0; i < NM; ++i)
+#pragma unroll 1
+    for (int j = 0; j < 16; ++j)
+      if ((plus[i] | minus[i]) >> j & 1) y[32 * i + 8 * (j >> 2) + 4 * h + (j & 3)] = from_f<T>(class_of(plus[i] >> j & 1, minus[i] >> j & 1));
+}
+
 template <typename T, bool I8, int DP, bool EXACT>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnArgs a) {
   typedef typename std::conditional<I8, int8_t, T>::type E;
@@ -634,7 +733,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   __shared__ __attribute__((aligned(16))) float sks[2][I8 ? KB : 4], svs[2][I8 ? KB : 4];
   __shared__ F powers[POWER ? 4 * KB / 8 : 1];  // every wave's own
   __shared__ __attribute__((aligned(16))) unsigned marks[I8 ? 4 : DP * 4];  // of an element: 64 keys' bits, +inf or NaN; -inf or NaN
-  __shared__ int flag[2], used;  // used: the tile's parts
+  __shared__ int flag[2], used, again;  // used: the tile's parts; again: there are values that are not finite
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
   const int D = EXACT ? DP : c.dim, each = a.heads / c.kv_heads;
@@ -814,6 +913,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   float m = kNone, l = 0.f;
   int pages = -1, pages1 = -1;
   if (tid < 2) flag[tid] = 0;
+  if (tid == 0) again = 0;
   if (first < end) {
     const int entry = table[entry_of(first)], entry1 = table[entry_of(first + 1)];
     pages = pages_of(first, entry), pages1 = pages_of(first + 1, entry1);
@@ -833,7 +933,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
     const bool odd = !I8 && edge && flag[buf] == block + 1;
     if (odd) {
       // Values that are not finite become zeros in LDS, with a bit that says where they
-      // were; what they do to the rows that see them follows the product.
+      // were: the rows that see them get a sum that is not finite after the product.
       for (int i = tid; i < DP * 4; i += 256) marks[i] = 0;
       lds_barrier();
 #pragma unroll 1
@@ -843,10 +943,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
         __builtin_memcpy(e, &sv[buf * L::N + x], 16);
 #pragma unroll
         for (int j = 0; j < L::GE; ++j) {
-          const float v = (float)e[j];
-          if (__builtin_isfinite(v)) continue;
-          if (!(v < 0.f)) atomicOr(&marks[4 * d + (key >> 5)], 1u << ((key & 31) + j));
-          if (!(v > 0.f)) atomicOr(&marks[4 * d + 2 + (key >> 5)], 1u << ((key & 31) + j));
+          if (finite((float)e[j])) continue;
+          atomicOr(&marks[4 * d + (key >> 5)], 1u << ((key & 31) + j));
           e[j] = (T)0.f;
         }
         __builtin_memcpy(&sv[buf * L::N + x], e, 16);
@@ -941,22 +1039,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
       reads_ahead<T, KB / 16 * ND, 4>();
       if (!I8) __builtin_amdgcn_s_setprio(0);
       if (odd) {
-        // this row's keys of any weight, against each element's marked ones
+        // the keys that this row sees, against each element's marked ones
         unsigned seen[2] = {0u, 0u};
 #pragma unroll
-        for (int i = 0; i < NK; ++i) {
-          unsigned own = 0;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) own |= s[i][j] > 0.f || s[i][j] != s[i][j] ? 1u << (16 * (j >> 3) + 8 * h + (j & 7)) : 0u;
-          seen[i] = own | __shfl_xor(own, 32);
-        }
+        for (int i = 0; i < NK; ++i)
+          seen[i] = seen_keys(block * KB + 32 * i, pos, a.window) & ((there >> (2 * i) & 1 ? 0xffffu : 0u) | (there >> (2 * i + 1) & 1 ? 0xffff0000u : 0u));
 #pragma unroll
         for (int i = 0; i < ND; ++i)
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            const u32x4 at = *reinterpret_cast<const u32x4*>(&marks[4 * (32 * i + 8 * (j >> 2) + 4 * h + (j & 3))]);
+            const unsigned* at = &marks[4 * (32 * i + 8 * (j >> 2) + 4 * h + (j & 3))];
             if ((at[0] & seen[0]) | (at[1] & seen[1])) o[i][j] += __builtin_huge_valf();
-            if ((at[2] & seen[0]) | (at[3] & seen[1])) o[i][j] -= __builtin_huge_valf();
           }
       }
     }
@@ -969,6 +1062,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
     dma_barrier();
   }
   l = sum_x32(l);
+  auto look_again = [&] {
+    float odd[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) odd[j & 3] += o[i][j];
+    if (__any(finite(l) && !finite((odd[0] + odd[1]) + (odd[2] + odd[3]))) && lane == 0) again = 1;
+  };
+  if constexpr (!I8) look_again();
   __syncthreads();
 
   if (const int parts = gridDim.z > 1 ? uniform(used) : 1; parts > 1) {  // left in the lanes' order
@@ -985,16 +1087,16 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
     if (run_joins<DP>(gridDim.z)) return;
     if constexpr (!run_joins<DP>(2)) {  // joined by the tile's last workgroup in the parts' order
       if (!last_of(a.count + blockIdx.x, parts, &flag[0])) return;
-      if (t * kRunRows + 32 * wave >= rows) return;  // (a wave without rows left nothing)
+      const int there = t * kRunRows + 32 * wave < rows ? parts : 0;  // (a wave without rows left nothing)
       m = kNone;
 #pragma unroll 4
-      for (int z = 0; z < parts; ++z) m = fmaxf(m, wm.get(run_m_at(slot + z)));
+      for (int z = 0; z < there; ++z) m = fmaxf(m, wm.get(run_m_at(slot + z)));
       l = 0.f;
 #pragma unroll
       for (int i = 0; i < ND; ++i)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-      for (int z = 0; z < parts; ++z) {
+      for (int z = 0; z < there; ++z) {
         const float f = __builtin_amdgcn_exp2f(wm.get(run_m_at(slot + z)) - some(m));
         l += f * wm.get(run_m_at(slot + z) + 256);
 #pragma unroll
@@ -1006,21 +1108,25 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
             for (int x = 0; x < 4; ++x) o[i][4 * j + x] += f * v[x];
           }
       }
+      if constexpr (!I8) look_again();
+      __syncthreads();
     }
   }
-  if (mine >= rows) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* y = static_cast<T*>(a.y) + (int64_t)(row0 + token) * a.ys + (int64_t)qh * D;
+  if (mine < rows)
 #pragma unroll
-  for (int i = 0; i < ND; ++i)
+    for (int i = 0; i < ND; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int d = 32 * i + 8 * j + 4 * h;
-      T v[4];
+      for (int j = 0; j < 4; ++j) {
+        const int d = 32 * i + 8 * j + 4 * h;
+        T v[4];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) v[x] = from_f<T>(o[i][4 * j + x] * inv);
-      if (EXACT || d < D) __builtin_memcpy(y + d, v, sizeof(v));
-    }
+        for (int x = 0; x < 4; ++x) v[x] = from_f<T>(o[i][4 * j + x] * inv);
+        if (EXACT || d < D) __builtin_memcpy(y + d, v, sizeof(v));
+      }
+  if constexpr (!I8)
+    if (uniform(again)) run_classes<T, DP>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), tile, gridDim.z > 1, finite(l), marks);
 }
 
 // The parts of a tile joined in their order, 4 elements of 128 rows at a time, each tile by as
@@ -1051,6 +1157,13 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int parts) {
     z += 8;
     if (z >= used) {
       const int d = 8 * i + 4 * h;
+      if (!a.c.i8 && (EXACT || d < D) && finite(join.sum) && !finite((join.acc[0] + join.acc[1]) + (join.acc[2] + join.acc[3])))
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int pos = past + token;
+          const float is = class_of_values<T>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), b, head, d + x, a.window ? max(0, pos - a.window + 1) : 0, min(pos, (c.width << c.shift) - 1));
+          if (is != 0.f) join.acc[x] = is;
+        }
       const float inv = join.sum == 0.f ? 0.f : 1.f / join.sum;
       T v[4];
 #pragma unroll

@@ -718,7 +718,8 @@ int sn_cache_read(sn_op* op, const sn_cache_io* io, void* k, int64_t k_stride, v
  * A row that sees no position is zeros.  What lies in places that a row does
  * not see, infinities and NaN included, does not touch it.  An infinity among the values that it
  * does see is that element's result however small its weight, and a NaN, or infinities of both
- * signs, are NaN; so are all elements where a score is NaN or plus infinity.
+ * signs, are NaN; so are all elements where a score is NaN or plus infinity, or all scores
+ * that the row sees are minus infinity.
  *
  * Scores, maxima, weights and sums are float32.  With 16-bit types a prompt's weights are
  * rounded once, to dtype, before they meet v; a step's keep 16 bits (11 with f16

@@ -161,6 +161,18 @@ __device__ __attribute__((noinline)) float class_of_values(KernelArgs args, int 
   }
   return class_of(plus, minus);
 }
+// Whether there is a place at any of the positions from .. last.  A sum of weights is 0 where none is seen, and the
+// result zeros, or where all scores that are seen are minus infinity: 0 / 0.
+__device__ __forceinline__ bool sees_place(const CacheArgs& c, int b, int from, int last) {
+#pragma unroll 1
+  for (int p = from; p <= last; p = (p | ((1 << c.shift) - 1)) + 1)
+    if (page_of(c, b, p) >= 0) return true;
+  return false;
+}
+static __device__ __attribute__((noinline)) float inverse_of_0(KernelArgs args, int b, int from, int last) {
+  const CacheArgs c = ((const AttnArgs*)args)->c;
+  return sees_place(c, b, from, last) ? __builtin_nanf("") : 0.f;
+}
 // Which of the 32 keys from `base` on a row at `pos` sees.
 __device__ __forceinline__ unsigned first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 __device__ __forceinline__ unsigned seen_keys(int base, int pos, int window) {
@@ -304,8 +316,9 @@ __device__ __forceinline__ bool step_part(const AttnArgs& a, int KB, int unit, P
   return false;
 }
 
+// (The least waves of the launch bounds keep 128 bf16 elements, at 257 registers, on two workgroups a unit.)
 template <typename T, bool I8, int DP, bool EXACT>
-__global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * kStepWaves, EXACT && DP <= 128 ? 2 : 1) void attn_step_kernel(AttnArgs a) {
   typedef typename std::conditional<I8, int8_t, T>::type E;                        // of the cache
   typedef typename std::conditional<I8 && sizeof(T) == 2, bf16, T>::type W;        // of the second product
   typedef typename Frag<T>::type FT;
@@ -496,8 +509,9 @@ __global__ __launch_bounds__(64 * kStepWaves) void attn_step_kernel(AttnArgs a) 
   auto slot = [&](int u) { return (u == unit0 ? 2 * u + 1 : 2 * u) * slots + at; };
   constexpr int chunks = DP / 4;
   auto finish = [&](int r, int d, f32x4 acc, float sum) {
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    if (!I8 && finite(sum) && !finite((acc[0] + acc[1]) + (acc[2] + acc[3])))
+    float inv = 1.f / sum;
+    if (sum == 0.f) inv = inverse_of_0((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), b, span.from, span.last);
+    if (!I8 && sum > 0.f && finite(sum) && !finite((acc[0] + acc[1]) + (acc[2] + acc[3])))
 #pragma unroll 1
       for (int j = 0; j < 4; ++j) {
         const float is = class_of_values<T>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), b, head, d + j, span.from, span.last);
@@ -664,9 +678,10 @@ __device__ __forceinline__ int run_o_at(int slot, int i) {
 }
 __device__ __forceinline__ int run_m_at(int slot) { return slot * 512 + threadIdx.x; }
 
-// The classes of a tile's results that are not finite, block by block as the products were taken.
-template <typename T, int DP>
-__device__ __attribute__((noinline)) void run_classes(KernelArgs args, int tile, bool split, bool numbers, unsigned* marks) {
+// The results of a tile's rows that have no weights, and the classes of those that are not finite, block by block as the
+// products were taken.
+template <typename T, bool I8, int DP>
+__device__ __attribute__((noinline)) void run_again(KernelArgs args, int tile, bool split, float l, bool classes, unsigned* marks) {
   const AttnArgs a = *(const AttnArgs*)args;
   const CacheArgs& c = a.c;
   constexpr int KB = run_keys<T>(), GE = 16 / sizeof(T), VG = 16 / GE, NM = DP / 32;
@@ -676,6 +691,12 @@ __device__ __attribute__((noinline)) void run_classes(KernelArgs args, int tile,
   if (!find_tile(c, tile, each, split, b, t, row0, n, past)) return;
   const int rows = n * each, mine = t * kRunRows + 32 * wave + r, token = fdiv(min(mine, rows - 1), a.each);
   const int pos = past < 0 ? -1 : past + token;
+  T* y = static_cast<T*>(a.y) + (int64_t)(row0 + token) * a.ys + (int64_t)(head * each + mine - token * each) * D;
+  if (mine < rows && l == 0.f && sees_place(c, b, a.window ? max(0, pos - a.window + 1) : 0, min(pos, (c.width << c.shift) - 1)))
+    for (int d = 4 * h; d < D; d += 8)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[d + j] = from_f<T>(__builtin_nanf(""));
+  if (I8 || !classes) return;
   const RunSpan span = run_span(a, t, rows, past, KB);
   unsigned plus[NM], minus[NM];  // this lane's elements 32 i + 8 j + 4 h + x: bits 4 j + x
 #pragma unroll
@@ -710,8 +731,7 @@ __device__ __attribute__((noinline)) void run_classes(KernelArgs args, int tile,
         minus[i] |= (at[2] & seen0) | (at[3] & seen1) ? 1u << j : 0u;
       }
   }
-  if (mine >= rows || !numbers) return;
-  T* y = static_cast<T*>(a.y) + (int64_t)(row0 + token) * a.ys + (int64_t)(head * each + mine - token * each) * D;
+  if (mine >= rows || !(l > 0.f && finite(l))) return;
 #pragma unroll
   for (int i = 0; i < NM; ++i)
 #pragma unroll 1
@@ -733,7 +753,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
   __shared__ __attribute__((aligned(16))) float sks[2][I8 ? KB : 4], svs[2][I8 ? KB : 4];
   __shared__ F powers[POWER ? 4 * KB / 8 : 1];  // every wave's own
   __shared__ __attribute__((aligned(16))) unsigned marks[I8 ? 4 : DP * 4];  // of an element: 64 keys' bits, +inf or NaN; -inf or NaN
-  __shared__ int flag[2], used, again;  // used: the tile's parts; again: there are values that are not finite
+  __shared__ int flag[2], used, again[2];  // used: the tile's parts; again: rows without weights, results that are not finite
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
   const int D = EXACT ? DP : c.dim, each = a.heads / c.kv_heads;
@@ -912,8 +932,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   float m = kNone, l = 0.f;
   int pages = -1, pages1 = -1;
-  if (tid < 2) flag[tid] = 0;
-  if (tid == 0) again = 0;
+  if (tid < 2) flag[tid] = 0, again[tid] = 0;
   if (first < end) {
     const int entry = table[entry_of(first)], entry1 = table[entry_of(first + 1)];
     pages = pages_of(first, entry), pages1 = pages_of(first + 1, entry1);
@@ -1068,12 +1087,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
     for (int i = 0; i < ND; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) odd[j & 3] += o[i][j];
-    if (__any(finite(l) && !finite((odd[0] + odd[1]) + (odd[2] + odd[3]))) && lane == 0) again = 1;
+    const bool none = l == 0.f && pos >= 0 && mine < rows, odds = !I8 && l > 0.f && finite(l) && !finite((odd[0] + odd[1]) + (odd[2] + odd[3]));
+    if (__any(none || odds)) {
+      if (none) again[0] = 1;
+      if (odds) again[1] = 1;
+    }
   };
-  if constexpr (!I8) look_again();
+  const int parts = gridDim.z > 1 ? uniform(used) : 1;
+  if (parts == 1) look_again();
   __syncthreads();
 
-  if (const int parts = gridDim.z > 1 ? uniform(used) : 1; parts > 1) {  // left in the lanes' order
+  if (parts > 1) {  // left in the lanes' order
     const int slot = blockIdx.x * gridDim.z;
     const Shared wo(a.ws_o), wm(a.ws_m);
     if (t * kRunRows + 32 * wave < rows) {
@@ -1108,7 +1132,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
             for (int x = 0; x < 4; ++x) o[i][4 * j + x] += f * v[x];
           }
       }
-      if constexpr (!I8) look_again();
+      look_again();
       __syncthreads();
     }
   }
@@ -1125,8 +1149,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attn_run_kernel(AttnAr
         for (int x = 0; x < 4; ++x) v[x] = from_f<T>(o[i][4 * j + x] * inv);
         if (EXACT || d < D) __builtin_memcpy(y + d, v, sizeof(v));
       }
-  if constexpr (!I8)
-    if (uniform(again)) run_classes<T, DP>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), tile, gridDim.z > 1, finite(l), marks);
+  if (uniform(again[0] | again[1])) run_again<T, I8, DP>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), tile, gridDim.z > 1, l, again[1], marks);
 }
 
 // The parts of a tile joined in their order, 4 elements of 128 rows at a time, each tile by as
@@ -1157,14 +1180,15 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int parts) {
     z += 8;
     if (z >= used) {
       const int d = 8 * i + 4 * h;
-      if (!a.c.i8 && (EXACT || d < D) && finite(join.sum) && !finite((join.acc[0] + join.acc[1]) + (join.acc[2] + join.acc[3])))
+      const int pos = past < 0 ? -1 : past + token, from = a.window ? max(0, pos - a.window + 1) : 0, last = min(pos, (c.width << c.shift) - 1);
+      if (!c.i8 && (EXACT || d < D) && join.sum > 0.f && finite(join.sum) && !finite((join.acc[0] + join.acc[1]) + (join.acc[2] + join.acc[3])))
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const int pos = past + token;
-          const float is = class_of_values<T>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), b, head, d + x, a.window ? max(0, pos - a.window + 1) : 0, min(pos, (c.width << c.shift) - 1));
+          const float is = class_of_values<T>((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), b, head, d + x, from, last);
           if (is != 0.f) join.acc[x] = is;
         }
-      const float inv = join.sum == 0.f ? 0.f : 1.f / join.sum;
+      float inv = 1.f / join.sum;
+      if (join.sum == 0.f) inv = inverse_of_0((KernelArgs)__builtin_amdgcn_kernarg_segment_ptr(), b, from, last);
       T v[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) v[x] = from_f<T>(join.acc[x] * inv);

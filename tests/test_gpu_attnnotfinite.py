@@ -115,3 +115,73 @@ def test_values_in_8_bits_that_are_not_finite(dtype):
         got = host(got).reshape(N, KV, -1)
         for h in range(KV):
             assert np.isfinite(got[:first[h], h]).all() and np.isnan(got[first[h]:, h]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("window", [0, 1, 40])
+def test_scores_of_minus_infinity(dtype, window):
+    # such a key has no weight; a row that sees no others has 0 / 0
+    r = np.random.default_rng(1)
+    q, k, v = (rounded(r.standard_normal((N, m * DIM)), dtype) for m in (HEADS, KV, KV))
+    q, k = q.reshape(N, HEADS, DIM), k.reshape(N, KV, DIM)
+    q[:, :, 0] = 1
+    off = np.zeros(N, bool)
+    off[:3] = off[100:180] = off[256:320] = True
+    k[off, :, 0] = -np.inf
+    p = Paged(dtype, "same", KV, DIM, PAGE, [N], k=k.reshape(N, -1).copy(), v=v.copy())
+    wide = p.table.new_full((1, 4000), -1)
+    wide[:, :p.table.shape[1]] = p.table
+    v = v.reshape(N, KV, DIM)
+    at = np.arange(N)
+    see = (at <= at[:, None]) & (at > at[:, None] - window if window else True)
+    void = ~(see & ~off).any(1)
+    # (the same with keys that are finite and not seen)
+    y, a, bound = attend(q, np.where(off[:, None, None], 0, k), v, KV, 0, window, ~off)
+    op = Attention(dtype, HEADS, KV, DIM, page=PAGE, window=window, max_seqs=N, max_tokens=N)
+    flat = q.reshape(N, -1)
+    outs = {"prompt": op.run(device(flat, dtype), p.cache, p.table, i32([0])),
+            "parts": op.run(device(flat, dtype), p.cache, wide, i32([0])),
+            "steps": op.step(device(flat, dtype), p.cache, p.table.expand(N, -1), i32(at)),
+            "few rows": None}
+    import torch
+    cuts = [0, 1, 2, 5, 90, 110, 130, 179, 181, 250, 300, 319, 321, 500, N]
+    outs["few rows"] = torch.cat([op.run(device(flat[i:j], dtype), p.cache, wide, i32([i])) for i, j in zip(cuts, cuts[1:])])
+    outs["single steps"] = torch.cat([op.step(device(flat[i:i + 1], dtype), p.cache, p.table, i32([i])) for i in range(N)])
+    for what, got in outs.items():
+        got = host(got).reshape(N, HEADS, DIM)
+        assert np.isnan(got[void]).all(), f"{what}: rows without a weight"
+        assert_attention(got[~void], y[~void], a[~void], bound[~void], dtype, what)
+    # places that do not exist and slots without a sequence are not seen: zeros, as ever
+    p.table[0, :7] = -1
+    got = host(op.step(device(flat[[2, 50, 99]], dtype), p.cache, p.table.expand(3, -1), i32([2, 50, -1])))
+    assert not got.any()
+    assert not host(op.run(device(flat[:100], dtype), p.cache, p.table, i32([0]))).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("store", ["same", "i8"])
+def test_queries_that_are_not_finite(dtype, store):
+    # an infinite element against keys of one sign: all scores minus infinity, 0 / 0, or all plus infinity;
+    # other heads and rows as ever
+    r = np.random.default_rng(2)
+    n = 150
+    q, k, v = (rounded(r.standard_normal((n, m * DIM)), dtype) for m in (HEADS, KV, KV))
+    q, k = q.reshape(n, HEADS, DIM), k.reshape(n, KV, DIM)
+    k[:, :, 0] = rounded(-np.abs(k[:, :, 0]) - 1, dtype)
+    clean = q.copy()
+    q[::3, 1, 0], q[1::3, 4, 0] = np.inf, -np.inf
+    bad = ~np.isfinite(q).all(-1)
+    p = Paged(dtype, store, KV, DIM, PAGE, [n], k=k.reshape(n, -1).copy(), v=v.copy())
+    wide = p.table.new_full((1, 4000), -1)
+    wide[:, :p.table.shape[1]] = p.table
+    op = Attention(dtype, HEADS, KV, DIM, page=PAGE, store=store, max_seqs=n, max_tokens=n)
+
+    def outs(q):
+        d = device(q.reshape(n, -1), dtype)
+        yield op.run(d, p.cache, p.table, i32([0]))
+        yield op.run(d, p.cache, wide, i32([0]))
+        yield op.step(d, p.cache, p.table.expand(n, -1), i32(np.arange(n)))
+
+    for got, want in zip(outs(q), outs(clean)):
+        got, want = host(got).reshape(n, HEADS, DIM), host(want).reshape(n, HEADS, DIM)
+        assert np.isnan(got[bad]).all() and np.array_equal(got[~bad], want[~bad]) and np.isfinite(want).all()

@@ -606,7 +606,7 @@ __device__ __forceinline__ u32x4 resource(const void* p, unsigned bytes) {
 __device__ __forceinline__ void lds_load(u32x4 rsrc, unsigned offset, unsigned more, const void* to) {
   const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)to;
   asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(offset), "s"(rsrc), "s"(more), "s"(at)
-               : "memory");
+               : "m0", "memory");
 }
 
 // The schedule of N products whose first operands come from LDS: reads go AHEAD of the

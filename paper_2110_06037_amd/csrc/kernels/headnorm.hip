@@ -169,7 +169,7 @@ __global__ __launch_bounds__(64 * kHeadWaves) void head_norm_any_kernel(HeadNorm
     if (a.norm) k = rsqrtf(wave_sum(s) / (float)D + a.eps);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const float u = va[i] * (w && ia[i] < D ? k * w[ia[i]] : k), v = vb[i] * (w && ib[i] < D ? k * w[ib[i]] : k);
+      const float u = va[i] * (ia[i] < D ? k * w[ia[i]] : k), v = vb[i] * (ib[i] < D ? k * w[ib[i]] : k);
       const bool turned = lane + 64 * i < half;  // (others stay apart: 0 times what is not finite is NaN)
       if (ia[i] < D) y[ia[i]] = from_f<T>(turned ? u * cs[i] - v * sn[i] : u);
       if (ib[i] < D) y[ib[i]] = from_f<T>(turned ? v * cs[i] + u * sn[i] : v);
@@ -200,15 +200,14 @@ static void launch_head_norm(HeadNormArgs& a, hipStream_t st) {
   auto fits = [&](int V) {
     return a.pairs == 0 ? a.rot / 2 % V == 0 && (a.dim - a.rot) % (2 * V) == 0 : a.dim % (2 * V) == 0;
   };
-  if (sizeof(T) == 2 && fits(8)) launch_head_norm<T, 8>(a, st);
-  else if (fits(4)) launch_head_norm<T, 4>(a, st);
-  else {
-    const int all = a.heads + a.kv_heads;
-    const int y = (int)std::min<int64_t>((all + kHeadWaves - 1) / kHeadWaves, std::max<int64_t>(1, 512 / a.tokens));
-    const dim3 grid((unsigned)a.tokens, y), block(64 * kHeadWaves);
-    if (a.dim <= 128) SN_LAUNCH((head_norm_any_kernel<T, 1>), grid, block, 0, st, a);
-    else SN_LAUNCH((head_norm_any_kernel<T, 2>), grid, block, 0, st, a);
-  }
+  if constexpr (sizeof(T) == 2)
+    if (fits(8)) return launch_head_norm<T, 8>(a, st);
+  if (fits(4)) return launch_head_norm<T, 4>(a, st);
+  const int all = a.heads + a.kv_heads;
+  const int y = (int)std::min<int64_t>((all + kHeadWaves - 1) / kHeadWaves, std::max<int64_t>(1, 512 / a.tokens));
+  const dim3 grid((unsigned)a.tokens, y), block(64 * kHeadWaves);
+  if (a.dim <= 128) SN_LAUNCH((head_norm_any_kernel<T, 1>), grid, block, 0, st, a);
+  else SN_LAUNCH((head_norm_any_kernel<T, 2>), grid, block, 0, st, a);
 }
 
 void head_norm(const HeadNormArgs& args, hipStream_t st) {

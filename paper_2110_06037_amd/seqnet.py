@@ -26,7 +26,6 @@ leave every block's convolution window and state, or its cache, behind in a
 
 from __future__ import annotations
 
-import contextlib
 import threading
 
 from .attention import Attention, HeadNorm, KVCache
@@ -225,7 +224,8 @@ class _Replay:
     def __call__(self):
         if self.net.closed:
             raise RuntimeError("the net of this captured step is closed")
-        with self.net._turn():
+        with self.net._lock:
+            self.net._turn()
             if self.past is not None:
                 self.state._room.take(self.past, self.state.seqs, self.state.seqs)
             self.graph.replay()
@@ -271,21 +271,21 @@ class SequenceNet:
         """The state before the first token; attention blocks hold ``max_positions`` of each sequence."""
         return SequenceState(self, seqs, max_positions)
 
-    @contextlib.contextmanager
     def _turn(self):
-        """A call's turn to queue its work: behind the last call's, which may be on another stream."""
+        """A call's turn to queue its work, under the lock: behind the last call's, which may be on another stream."""
         import torch
-        with self._lock:
-            if not torch.cuda.is_current_stream_capturing():
-                stream = torch.cuda.current_stream(self.device)
-                if self._last is not None and self._last != stream:
-                    stream.wait_stream(self._last)
-                self._last = stream
-            yield
+        if torch.cuda.is_current_stream_capturing():
+            return
+        now = self.first._current(self.device)
+        if now != self._last:
+            if self._last is not None:
+                torch.cuda.current_stream(self.device).wait_stream(torch.cuda.ExternalStream(self._last, device=self.first._dev))
+            self._last = now
 
     def _forward(self, x, state, offsets, step, longest=None, counted=True):
         import torch
-        with self._turn():
+        with self._lock:
+            self._turn()
             call = _Call(state, x.shape[0], offsets, step, longest, counted)
             u, _ = self.first.run(x)
             h = x.to(torch.float32, copy=True)  # updated below: never the caller's x

@@ -327,6 +327,7 @@ class SequenceNet:
             graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(graph, stream=side):
                 y = self._forward(x, state, None, True, counted=False)
+            self._turn()  # (the next call, on whatever stream, waits for the copies)
             for t, k in zip(tensors, keep):
                 t.copy_(k)
             if known:

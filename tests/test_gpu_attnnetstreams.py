@@ -93,3 +93,21 @@ def test_threads(net):
     for t in threads:
         t.join()
     assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+
+
+def test_a_replay_waits_for_the_end_of_its_capture(net):
+    # whose last work, the state's tensors as they were, is on the stream that was current
+    import torch
+    state, here = net.new_state(SEQS, 400), torch.cuda.Stream()
+    net.run(rows(600, 7), state)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(here):
+        token, out, replay = net.capture_step(state)
+        torch.cuda._sleep(20_000_000)
+        ended = torch.cuda.Event()
+        ended.record()
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        replay()
+    other.synchronize()
+    assert ended.query()

@@ -15,19 +15,24 @@
 // straight into the operands of 16 x 16 products, since every key is used once and LDS
 // would only be a detour.  Bound by the cache's bytes: 64 sequences of 2048 keys, 8 key heads of
 // 128 in bf16 101 us, 5.3 TB/s; up to 8192 keys 197 us, 5.4 TB/s; 32 heads without
-// groups 6.3 TB/s; in 8 bits 113 us, 4.6 TB/s, where turning codes into numbers
-// is as much work as the products.  Short ones are a chain of dependent steps: one
-// sequence of 4096 keys 10.9 us, of which launch and plan 3.2, queries and table 0.7, the
-// keys 3.0, joining the waves 0.7, storing the part and counting it 1.7, joining the parts 2.3.
+// groups 6.3 TB/s; in 8 bits, ragged to 8192 keys, 110 - 119 us, 4.6 - 5.0 TB/s, where vector
+// instructions, codes turned into numbers first, take 44 % of the cycles.  64 of 2048 keys in
+// float32 191 us; over 8 bits in f16 48, in float32 96.  Short ones are a chain of dependent steps:
+// one sequence of 4096 keys 11.2 us, of which launch and plan some 3.2, queries and table 0.7, the
+// keys 3.0, joining the waves 0.7, storing the part and counting it 1.7, joining the parts 2.3 and
+// looking whether results are finite 0.3.  (Float32 of 136 to 248 elements spills 9 registers.)
 // attn_run_kernel: 128 rows (a token's query heads of one key head are
 // neighbours), a wave 32 of them in 32 x 32 products, K and V through LDS, where the
-// four waves share them.  Bound by issue, matrix products first: 4096 rows of 32 heads, 8 key heads of 128 in
-// bf16, causal, 142 - 152 us, 137.5 GFLOP that count, 905 - 965 TFLOP/s, a library product of
-// 8192^3 1206; over a cache in 8 bits 187.  Without its loads it takes 138 us, without its exponentials 139; two
-// waves a SIMD, whose registers hold no more, cover one's softmax with the other's
-// products.  Not faster (4096 rows, 162 us then): 32 keys a block and three waves a SIMD 171, a block's scores
+// four waves share them.  Bound by issue, of matrix products and of the softmax: 4096 rows of 32
+// heads, 8 key heads of 128 in bf16, causal, 145 - 153 us, 137.5 GFLOP that count, 900 - 950
+// TFLOP/s, a library product of 8192^3 1206.  Of the cycles of busy compute units the matrix pipes
+// take 48 %, vector instructions (which start the products, too) 50, LDS 6, without a bank conflict;
+// without its loads it takes 138 us, without its exponentials 139: two waves a SIMD, whose registers
+// hold no more, cover one's softmax with the other's products in part.  Over a cache in 8 bits 180 -
+// 187 us (f16 192 - 197): vector instructions 64 % of the cycles, products 35.
+// Not faster (4096 rows, 162 us then): 32 keys a block and three waves a SIMD 171, a block's scores
 // taken beside the last one's softmax 180, a queue of tiles 192, tiles in another order 174.
-// Float32 goes through float32 products: 2048 rows 385 us, 89 TFLOP/s, the library's 154.
+// Float32 goes through float32 products: 2048 rows 383 us, 90 TFLOP/s, the library's 154; over 8 bits 409.
 #pragma once
 
 #include "attn.hpp"

@@ -222,9 +222,9 @@ class _Replay:
         self.past = state.past
 
     def __call__(self):
-        if self.net.closed:
-            raise RuntimeError("the net of this captured step is closed")
         with self.net._lock:
+            if self.net.closed:
+                raise RuntimeError("the net of this captured step is closed")
             self.net._turn()
             if self.past is not None:
                 self.state._room.take(self.past, self.state.seqs, self.state.seqs)
@@ -241,7 +241,7 @@ class SequenceNet:
     group), and beside the projections "q_norm" and "k_norm" [head_dim].  Inputs and outputs are [rows, dim] in
     ``dtype``; the residual stream between the blocks is float32.
 
-    The blocks' handles have workspaces, one for all attention blocks that are alike, which every call uses. So the net puts
+    The blocks' handles have workspaces, one for all attention blocks that are alike, which every call uses.  So the net puts
     its calls (replays of captured steps among them) one after the other on the device, whatever streams and
     threads they come from; graphs that the caller captures by other means are the caller's to order."""
 
@@ -256,10 +256,11 @@ class SequenceNet:
                        _Block(dtype, w, w["norm"], max_seqs, max_tokens, device, eps) for w in blocks]
 
     def close(self):
-        self.closed = True
-        self.first.close()
-        for b in self.blocks:
-            b.close()
+        with self._lock:
+            self.closed = True
+            self.first.close()
+            for b in self.blocks:
+                b.close()
 
     def __enter__(self):
         return self
